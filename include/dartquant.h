@@ -324,6 +324,71 @@ double dq_calib_mma_flops(dq_calib_t* h);
  * path with d >= 256 only; call it after at least one step.  Changes no state of the calibration. */
 dq_status dq_calib_time_product(dq_calib_t* h, int32_t nterms, int32_t reps, float* h_ms);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Microscaled operators (no counterpart in the paper, which quantises to integers: the forward pass of a model whose
+ * activations a calibrated rotation has made quantisable, in the formats the B200's tensor cores multiply).
+ *
+ * Formats: OCP microscaling, blocks of 32 values along a row.  A block has one power-of-two scale, the E8M0 byte
+ * max(floor(log2 max|x|) - EMAX + 127, 0), and 32 elements round-to-nearest-even(x / scale), saturated:
+ *   DQ_MXFP4: E2M1 (EMAX 2, values 0, .5, 1, 1.5, 2, 3, 4, 6), two to a byte, the even one in the low half
+ *   DQ_MXFP8: E4M3 (EMAX 8, largest 448), one to a byte
+ * A block with a NaN or an infinity gets the NaN scale 0xFF and reads back as NaN, all 32 of it; so does every output
+ * of a product that it enters.  A block of zeros has scale byte 0.  A last block that is not full is quantised as if
+ * the missing values were zeros.
+ * Codes: [rows][dq_mx_row_bytes]; rows are padded with zero codes to a multiple of 128 values.  32-byte aligned.
+ * Scales: dq_mx_scale_bytes bytes, tiles of 128 rows x 4 blocks in the order the tensor cores read them: the scale of
+ *   (row, block) is byte ((row / 128) * ceil(k / 128) + block / 4) * 512 + row % 32 * 16 + row / 32 % 4 * 4 + block % 4.
+ *   Bytes of rows past the last one are not defined and not used.  16-byte aligned.
+ * Matrices of values (X, Y, sums, values) are row-major with a row stride of at least their width, of DQ_FP32, DQ_BF16
+ *   or DQ_FP16; 16-byte aligned rows are read and written fastest, no alignment beyond the type's is needed.
+ * Calls are asynchronous on the given stream, allocate nothing, keep nothing and can be captured in a graph.  A call with
+ *   no rows does nothing.  Limits: k <= 2^24, rows < 2^31 - 256.
+ * Errors: INVALID_ARG (null, sizes, enums, a pointer that its type's alignment rules out), UNSUPPORTED (alignment of codes
+ *   and scales, limits, a device that is not sm_100), CUDA. */
+enum { DQ_FP16 = 2 };                   /* third value of the microscaled operators' *_dtype arguments */
+enum { DQ_MXFP4 = 0, DQ_MXFP8 = 1 };
+
+/* Bytes of a row of codes, of the scales of a matrix, and of dq_mx_linear's workspace; -1 for arguments out of range. */
+int64_t dq_mx_row_bytes(int32_t fmt, int64_t k);
+int64_t dq_mx_scale_bytes(int64_t rows, int64_t k);
+int64_t dq_mx_linear_workspace(int32_t a_fmt, int64_t m, int64_t k);
+
+/* Codes and scales of X [rows][ldx].  d_values (nullable, [rows][ldv] of X's type) receives the values that the codes
+ * stand for; it may be X itself (with ldv == ldx), for evaluating a quantised model on unquantised products. */
+dq_status dq_mx_quantize(const void* d_X, int32_t x_dtype, int64_t rows, int64_t k, int64_t ldx, int32_t fmt, void* d_codes,
+                         void* d_scales, void* d_values, int64_t ldv, void* cuda_stream);
+
+/* The values that codes and scales stand for, Y [rows][ldy] (rounded once where y_dtype cannot hold them). */
+dq_status dq_mx_dequantize(int32_t fmt, const void* d_codes, const void* d_scales, int64_t rows, int64_t k, void* d_Y,
+                           int32_t y_dtype, int64_t ldy, void* cuda_stream);
+
+/* Root-mean-square norm with the residual's addition and a quantised output:
+ *   h = x + residual (fp32),  y = h / sqrt(mean_j h_j^2 + eps) gamma,  codes and scales of y
+ * X, residual, sum and values have type `dtype`.  d_residual (nullable: h = x).  d_gamma (nullable: ones, as where gamma
+ * was folded into the weights before a rotation): [k] of gamma_dtype, DQ_FP32 or `dtype`.  d_sum (nullable) receives
+ * h rounded once, what the next layer adds to; it may be X or residual itself (equal row strides).  y is computed from
+ * the unrounded h.  d_values (nullable) as in dq_mx_quantize.  k <= 32768. */
+dq_status dq_rmsnorm_quantize(const void* d_X, const void* d_residual, int32_t dtype, int64_t rows, int64_t k, int64_t ldx,
+                              int64_t ldr, const void* d_gamma, int32_t gamma_dtype, float eps, int32_t fmt, void* d_codes,
+                              void* d_scales, void* d_sum, int64_t lds, void* d_values, int64_t ldv, void* cuda_stream);
+
+/* Y[i][j] = sum_k A[i][k] W[j][k] for m rows of quantised activations (DQ_MXFP4 or DQ_MXFP8) and n rows of DQ_MXFP4
+ * weights, on the block-scaled tensor-core products with fp32 accumulation, rounded once to y_dtype.  Results do not depend
+ * on the run.  Y must not overlap the operands. */
+dq_status dq_mx_matmul(int32_t a_fmt, const void* d_a_codes, const void* d_a_scales, int64_t m, const void* d_w_codes,
+                       const void* d_w_scales, int64_t n, int64_t k, void* d_Y, int32_t y_dtype, int64_t ldy,
+                       void* cuda_stream);
+
+/* The same from activations X [m][ldx] that the call quantises to a_fmt first (exactly as dq_mx_quantize).
+ * d_workspace: dq_mx_linear_workspace bytes, 32-byte aligned; calls that overlap on the GPU need one each. */
+dq_status dq_mx_linear(const void* d_X, int32_t x_dtype, int64_t m, int64_t k, int64_t ldx, int32_t a_fmt,
+                       const void* d_w_codes, const void* d_w_scales, int64_t n, void* d_Y, int32_t y_dtype, int64_t ldy,
+                       void* d_workspace, void* cuda_stream);
+
+/* Synchronises the stream; returns and clears the current device's status word of the microscaled operators:
+ * DQ_OK, or DQ_ERR_TIMEOUT once a bounded wait inside a product gave up (its output is then not valid). */
+dq_status dq_mx_status(void* cuda_stream);
+
 const char* dq_status_string(dq_status s);
 void dq_calib_destroy(dq_calib_t* h);
 

@@ -17,7 +17,8 @@ DQ_ERR_SINGULAR, DQ_ERR_NONFINITE, DQ_ERR_TIMEOUT, DQ_ERR_NOT_CONVERGED = 5, 6, 
 DQ_QR_HOUSEHOLDER, DQ_QR_ITERATIVE = 0, 1
 DQ_ORTH_QR, DQ_ORTH_CAYLEY = 0, 1
 DQ_OBJ_WHIP, DQ_OBJ_VARIANCE, DQ_OBJ_KURTOSIS, DQ_OBJ_QUANT = 0, 1, 2, 3
-DQ_FP32, DQ_BF16 = 0, 1
+DQ_FP32, DQ_BF16, DQ_FP16 = 0, 1, 2
+DQ_MXFP4, DQ_MXFP8 = 0, 1
 DQ_PATH_FP32, DQ_PATH_BF16_TC = 0, 1
 DQ_MEAN_TOKENS, DQ_SUM_TOKENS = 0, 1
 DQ_SGD, DQ_SGD_MOMENTUM, DQ_ADAM = 0, 1, 2
@@ -32,6 +33,8 @@ EXPORTED_SYMBOLS = (
     "dq_calib_destroy", "dq_version", "dq_rotate_apply_static", "dq_calib_set_qr_method", "dq_calib_set_optimizer", "dq_gather_tokens", "dq_eval_rotation",
     "dq_calib_set_orth_method", "dq_calib_set_objective", "dq_calib_run_epochs", "dq_calib_mma_flops", "dq_calib_set_keep_gradient",
     "dq_calib_set_backward_precision", "dq_calib_selftest_bounded_wait", "dq_calib_time_product",
+    "dq_mx_row_bytes", "dq_mx_scale_bytes", "dq_mx_linear_workspace", "dq_mx_quantize", "dq_mx_dequantize", "dq_rmsnorm_quantize",
+    "dq_mx_matmul", "dq_mx_linear", "dq_mx_status",
 )
 
 
@@ -95,6 +98,19 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.dq_calib_time_product.restype = i32
     lib.dq_calib_set_backward_precision.argtypes = [vp, i32]
     lib.dq_calib_set_backward_precision.restype = i32
+    for name, args in (("dq_mx_quantize", [vp, i32, i64, i64, i64, i32, vp, vp, vp, i64, vp]),
+                       ("dq_mx_dequantize", [i32, vp, vp, i64, i64, vp, i32, i64, vp]),
+                       ("dq_rmsnorm_quantize", [vp, vp, i32, i64, i64, i64, i64, vp, i32, C.c_float, i32, vp, vp, vp, i64, vp, i64,
+                                                vp]),
+                       ("dq_mx_matmul", [i32, vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, vp]),
+                       ("dq_mx_linear", [vp, i32, i64, i64, i64, i32, vp, vp, i64, vp, i32, i64, vp, vp]),
+                       ("dq_mx_status", [vp])):
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = i32
+    for name, args in (("dq_mx_row_bytes", [i32, i64]), ("dq_mx_scale_bytes", [i64, i64]),
+                       ("dq_mx_linear_workspace", [i32, i64, i64])):
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = i64
     lib.dq_calib_launch_count.argtypes = [vp]
     lib.dq_calib_mma_flops.argtypes = [vp]
     lib.dq_calib_mma_flops.restype = C.c_double
@@ -318,6 +334,147 @@ def dq_eval_rotation(X, R, tau: float, bits: int, stream=None):
            "dq_eval_rotation")
     res = out.cpu()
     return int(round(float(res[0]))), float(res[1])
+
+
+# ---------------------------------------------------------------------------
+# Microscaled operators.  Their wrappers check what the C entry cannot see (devices, types, sizes of buffers); a
+# wrong tensor raises ValueError, a refusal of the library DartQuantError.
+# ---------------------------------------------------------------------------
+_DTYPES = None
+
+
+def _mx_call(name: str, stream, first, *args):
+    """lib.name(*args, stream) on the current device, where `first` must lie."""
+    import torch
+    index = first.get_device()
+    if index != torch.cuda.current_device():
+        raise ValueError("%s: the tensors have to be on the current CUDA device" % name)
+    s = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    status = getattr(_lib or load_library(), name)(*args, s)
+    if status != DQ_OK:
+        raise DartQuantError(status, name)
+
+
+def _mx_values(t, name: str, rows=None, k=None, like=None):
+    """(address, type, row stride) of a matrix of values: CUDA, 2-D, unit stride along a row."""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: DQ_FP32, torch.bfloat16: DQ_BF16, torch.float16: DQ_FP16}
+    dtype = _DTYPES.get(t.dtype)
+    shape = t.shape
+    if dtype is None or len(shape) != 2 or not t.is_cuda:
+        raise ValueError("%s: a 2-D CUDA tensor of float32, bfloat16 or float16 is needed" % name)
+    if (rows is not None and shape[0] != rows) or (k is not None and shape[1] != k):
+        raise ValueError("%s: shape %s, and [%s, %s] is needed" % (name, tuple(shape), rows, k))
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError("%s: type or device differs from the input's" % name)
+    ld, step = t.stride()
+    if (step != 1 and shape[1] > 1) or (ld < shape[1] and shape[0] > 1):
+        raise ValueError("%s: rows have to be contiguous and must not overlap" % name)
+    return t.data_ptr(), dtype, max(ld, shape[1])
+
+
+def _mx_bytes(t, name: str, least: int, like):
+    """Address of a contiguous buffer of at least `least` bytes, on the device of `like`."""
+    if not t.is_contiguous() or t.device != like.device or t.numel() * t.element_size() < least:
+        raise ValueError("%s: a contiguous buffer of at least %d bytes on the inputs' device is needed" % (name, least))
+    return t.data_ptr()
+
+
+def dq_mx_row_bytes(fmt: int, k: int) -> int:
+    return int(load_library().dq_mx_row_bytes(fmt, k))
+
+
+def dq_mx_scale_bytes(rows: int, k: int) -> int:
+    return int(load_library().dq_mx_scale_bytes(rows, k))
+
+
+def dq_mx_linear_workspace(a_fmt: int, m: int, k: int) -> int:
+    return int(load_library().dq_mx_linear_workspace(a_fmt, m, k))
+
+
+def _mx_held(fmt: int, rows: int, k: int):
+    """Bytes of the codes and of the scales of a [rows, k] matrix."""
+    if fmt != DQ_MXFP4 and fmt != DQ_MXFP8:
+        raise ValueError("format %r: DQ_MXFP4 or DQ_MXFP8 is needed" % (fmt,))
+    tiles = (k + 127) // 128
+    return rows * tiles * (64 if fmt == DQ_MXFP4 else 128), (rows + 127) // 128 * tiles * 512
+
+
+def dq_mx_empty(rows: int, k: int, fmt: int, device="cuda"):
+    """(codes, scales): buffers for a [rows, k] matrix, torch.uint8."""
+    import torch
+    codes, scales = _mx_held(fmt, rows, k)
+    return (torch.empty((rows, codes // rows if rows else 0), dtype=torch.uint8, device=device),
+            torch.empty(scales, dtype=torch.uint8, device=device))
+
+
+def dq_mx_quantize(X, fmt: int, codes, scales, values=None, stream=None):
+    """Codes and scales of X ([rows, k]; float32, bfloat16 or float16).  values (same type and shape; may be X): what
+    the codes stand for."""
+    x, dtype, ldx = _mx_values(X, "X")
+    rows, k = X.shape
+    n_codes, n_scales = _mx_held(fmt, rows, k)
+    v, _, ldv = _mx_values(values, "values", rows, k, X) if values is not None else (0, 0, 0)
+    _mx_call("dq_mx_quantize", stream, X, x, dtype, rows, k, ldx, fmt, _mx_bytes(codes, "codes", n_codes, X),
+             _mx_bytes(scales, "scales", n_scales, X), v, ldv)
+
+
+def dq_mx_dequantize(codes, scales, fmt: int, Y, stream=None):
+    """Y ([rows, k]) = the values that codes and scales stand for."""
+    y, dtype, ldy = _mx_values(Y, "Y")
+    rows, k = Y.shape
+    n_codes, n_scales = _mx_held(fmt, rows, k)
+    _mx_call("dq_mx_dequantize", stream, Y, fmt, _mx_bytes(codes, "codes", n_codes, Y), _mx_bytes(scales, "scales", n_scales, Y),
+             rows, k, y, dtype, ldy)
+
+
+def dq_rmsnorm_quantize(X, gamma, eps: float, fmt: int, codes, scales, residual=None, sum_out=None, values=None, stream=None):
+    """h = X + residual; codes and scales of h / sqrt(mean(h^2) + eps) * gamma.  gamma: [k] of X's type or float32, or None.
+    sum_out (may be X or residual) receives h, values the quantised output's values; all [rows, k] of X's type."""
+    x, dtype, ldx = _mx_values(X, "X")
+    rows, k = X.shape
+    n_codes, n_scales = _mx_held(fmt, rows, k)
+    r, _, ldr = _mx_values(residual, "residual", rows, k, X) if residual is not None else (0, 0, 0)
+    h, _, lds = _mx_values(sum_out, "sum_out", rows, k, X) if sum_out is not None else (0, 0, 0)
+    v, _, ldv = _mx_values(values, "values", rows, k, X) if values is not None else (0, 0, 0)
+    g, g_dtype = 0, dtype
+    if gamma is not None:
+        g_dtype = _DTYPES.get(gamma.dtype)
+        if gamma.shape != (k,) or (g_dtype != dtype and g_dtype != DQ_FP32) or gamma.device != X.device or not gamma.is_contiguous():
+            raise ValueError("gamma: a contiguous [%d] tensor of X's type or float32 on X's device is needed" % k)
+        g = gamma.data_ptr()
+    _mx_call("dq_rmsnorm_quantize", stream, X, x, r, dtype, rows, k, ldx, ldr, g, g_dtype, eps, fmt,
+             _mx_bytes(codes, "codes", n_codes, X), _mx_bytes(scales, "scales", n_scales, X), h, lds, v, ldv)
+
+
+def dq_mx_matmul(a_codes, a_scales, a_fmt: int, w_codes, w_scales, k: int, Y, stream=None):
+    """Y ([m, n]) = A W^T for m rows of activations (DQ_MXFP4 or DQ_MXFP8) and n rows of DQ_MXFP4 weights, k values each."""
+    y, dtype, ldy = _mx_values(Y, "Y")
+    m, n = Y.shape
+    a_n, a_s = _mx_held(a_fmt, m, k)
+    w_n, w_s = _mx_held(DQ_MXFP4, n, k)
+    _mx_call("dq_mx_matmul", stream, Y, a_fmt, _mx_bytes(a_codes, "a_codes", a_n, Y), _mx_bytes(a_scales, "a_scales", a_s, Y), m,
+             _mx_bytes(w_codes, "w_codes", w_n, Y), _mx_bytes(w_scales, "w_scales", w_s, Y), n, k, y, dtype, ldy)
+
+
+def dq_mx_linear(X, a_fmt: int, w_codes, w_scales, Y, workspace, stream=None):
+    """Y ([m, n]) = quantised(X) W^T for activations X ([m, k]) and n rows of DQ_MXFP4 weights.  workspace: a buffer of
+    dq_mx_linear_workspace(a_fmt, m, k) bytes."""
+    x, x_dtype, ldx = _mx_values(X, "X")
+    m, k = X.shape
+    y, y_dtype, ldy = _mx_values(Y, "Y", m)
+    n = Y.shape[1]
+    w_n, w_s = _mx_held(DQ_MXFP4, n, k)
+    a_n, a_s = _mx_held(a_fmt, m, k)
+    _mx_call("dq_mx_linear", stream, X, x, x_dtype, m, k, ldx, a_fmt, _mx_bytes(w_codes, "w_codes", w_n, X),
+             _mx_bytes(w_scales, "w_scales", w_s, X), n, y, y_dtype, ldy, _mx_bytes(workspace, "workspace", a_n + a_s, X))
+
+
+def dq_mx_status(stream=None) -> int:
+    """Synchronises the stream; the microscaled operators' status on the current device, which is cleared."""
+    return int(load_library().dq_mx_status(_stream_ptr(stream)))
 
 
 def dq_version() -> str:

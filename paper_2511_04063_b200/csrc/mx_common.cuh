@@ -1,0 +1,227 @@
+// Shared device code of the microscaled operators (mx_quant.cu, mx_matmul.cu): the block format, its conversions and
+// the addresses of its scales.
+//
+// A row of k values is cut into blocks of 32.  A block is held as one power of two, the E8M0 byte
+//     s = max(exponent field of max|x| - EMAX, 0)            (value 2^(s - 127); 0xFF is NaN)
+// and 32 elements q = RNE(x 2^(127 - s)), saturated, of type E2M1 (EMAX 2, largest 6) or E4M3 (EMAX 8, largest 448).
+// The exponent field of a float is floor(log2) + 127 for every normal number and 0 below, so the shared exponent is
+// floor(log2 max|x|) - EMAX, clamped at 2^-127, without a logarithm.  A block that holds a NaN or an infinity has
+// an exponent field of 255: its scale becomes NaN and with it every value of the block.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace dq {
+namespace mx {
+
+constexpr int BLOCK = 32;          // values that share a scale
+constexpr int KTILE = 128;         // values of a scale tile (4 blocks); rows of codes are padded to it
+constexpr int ROW_TILE = 128;      // rows of a scale tile
+constexpr int TILE_BYTES = 512;    // 128 rows x 4 scales
+
+inline __host__ __device__ int64_t k_tiles(int64_t k) { return (k + KTILE - 1) / KTILE; }
+inline __host__ __device__ int64_t row_bytes(int fmt, int64_t k) { return k_tiles(k) * (fmt == DQ_MXFP4 ? 64 : 128); }
+inline int64_t scale_bytes(int64_t rows, int64_t k) { return (rows + ROW_TILE - 1) / ROW_TILE * k_tiles(k) * TILE_BYTES; }
+
+// Byte of the scale of (row, block): tiles of 128 rows x 4 blocks, [row tile][k tile][row % 32][row / 32 % 4][block % 4].
+// This is the order in which the block-scaled MMA wants the scales in tensor memory: 32 lanes x 4 columns of 4 bytes.
+__device__ __forceinline__ int64_t scale_offset(int64_t row, int64_t block, int64_t ktiles) {
+  return ((row >> 7) * ktiles + (block >> 2)) * TILE_BYTES + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
+}
+
+template <typename T> struct Vec8;   // eight consecutive values
+template <> struct Vec8<float> {
+  static __device__ __forceinline__ void load(const float* p, float (&v)[8]) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+  static __device__ __forceinline__ void store(float* p, const float (&v)[8]) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+};
+template <> struct Vec8<__nv_bfloat16> {
+  static __device__ __forceinline__ void load(const __nv_bfloat16* p, float (&v)[8]) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  }
+  static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&v)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <> struct Vec8<__half> {
+  static __device__ __forceinline__ void load(const __half* p, float (&v)[8]) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      v[2 * i] = f.x; v[2 * i + 1] = f.y;
+    }
+  }
+  static __device__ __forceinline__ void store(__half* p, const float (&v)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+// Eight values starting at column c of a row of k: 16-byte accesses where `vec` says that every row starts on a
+// 16-byte boundary and all eight exist, else one by one; what lies outside the row reads as zero.
+template <typename T>
+__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t k, bool vec, float (&v)[8]) {
+  if (vec && c + 8 <= k) { Vec8<T>::load(row + c, v); return; }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (c + i < k) ? to_f32(row[c + i]) : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* row, int64_t c, int64_t k, bool vec, const float (&v)[8]) {
+  if (vec && c + 8 <= k) { Vec8<T>::store(row + c, v); return; }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) if (c + i < k) row[c + i] = from_f32<T>(v[i]);
+}
+
+// Largest magnitude of eight values as a bit pattern: magnitudes order like their bits, NaN above infinity above all.
+__device__ __forceinline__ uint32_t amax8_bits(const float (&v)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  return m;
+}
+// The four lanes that hold a block agree on its largest magnitude.
+__device__ __forceinline__ uint32_t block_max(uint32_t m) {
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  return max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t scale_code(uint32_t amax_bits) {
+  constexpr int EMAX = (FMT == DQ_MXFP4) ? 2 : 8;
+  const int e = (int)(amax_bits >> 23);
+  return e == 255 ? 255u : (uint32_t)max(e - EMAX, 0);
+}
+// 2^(127 - s): what the values are multiplied with (0 for a NaN block, whose elements are held as zeros).
+__device__ __forceinline__ float inverse_scale(uint32_t s) { return s == 255u ? 0.f : __uint_as_float((254u - s) << 23); }
+// 2^(s - 127)
+__device__ __forceinline__ float scale_value(uint32_t s) {
+  return __uint_as_float(s == 0u ? 0x00400000u : (s == 255u ? 0x7fffffffu : s << 23));
+}
+
+// Eight elements: E2M1 packed into 4 bytes (element 0 in the lowest bits), E4M3 into 8.  The conversions of a pair put
+// their first operand into the upper half.  Rounding is to nearest even, saturating.
+template <int FMT> struct Codes8;
+template <> struct Codes8<DQ_MXFP4> {
+  uint32_t w;
+  __device__ __forceinline__ void encode(const float (&v)[8], float inv) {
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+        "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
+        : "=r"(w)
+        : "f"(v[0] * inv), "f"(v[1] * inv), "f"(v[2] * inv), "f"(v[3] * inv), "f"(v[4] * inv), "f"(v[5] * inv),
+          "f"(v[6] * inv), "f"(v[7] * inv));
+  }
+  __device__ __forceinline__ void clear() { w = 0u; }
+  __device__ __forceinline__ void decode(float s, float (&v)[8]) const {
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+      v[2 * i] = f.x * s; v[2 * i + 1] = f.y * s;
+    }
+  }
+  static constexpr int BYTES = 4;
+  __device__ __forceinline__ void store(uint8_t* p) const { *reinterpret_cast<uint32_t*>(p) = w; }
+  __device__ __forceinline__ void load(const uint8_t* p) { w = __ldg(reinterpret_cast<const uint32_t*>(p)); }
+};
+template <> struct Codes8<DQ_MXFP8> {
+  uint32_t w[2];
+  __device__ __forceinline__ void encode(const float (&v)[8], float inv) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      asm("{\n\t.reg .b16 a, b;\n\t"
+          "cvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\n\t"
+          "cvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\n\t"
+          "mov.b32 %0, {a, b};\n\t}"
+          : "=r"(w[i]) : "f"(v[4 * i] * inv), "f"(v[4 * i + 1] * inv), "f"(v[4 * i + 2] * inv), "f"(v[4 * i + 3] * inv));
+  }
+  __device__ __forceinline__ void clear() { w[0] = w[1] = 0u; }
+  __device__ __forceinline__ void decode(float s, float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint32_t h0, h1;
+      asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\t"
+          "cvt.rn.f16x2.e4m3x2 %0, a;\n\t"
+          "cvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+          : "=r"(h0), "=r"(h1) : "r"(w[i]));
+      const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0));
+      const float2 f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+      v[4 * i] = f0.x * s; v[4 * i + 1] = f0.y * s; v[4 * i + 2] = f1.x * s; v[4 * i + 3] = f1.y * s;
+    }
+  }
+  static constexpr int BYTES = 8;
+  __device__ __forceinline__ void store(uint8_t* p) const { *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]); }
+  __device__ __forceinline__ void load(const uint8_t* p) {
+    const uint2 a = __ldg(reinterpret_cast<const uint2*>(p));
+    w[0] = a.x; w[1] = a.y;
+  }
+};
+// Codes and scale of a block from the eight values this lane holds of it; all 32 lanes call it.
+template <int FMT>
+__device__ __forceinline__ uint32_t encode_block(const float (&v)[8], Codes8<FMT>& codes) {
+  const uint32_t s = scale_code<FMT>(block_max(amax8_bits(v)));
+  codes.encode(v, inverse_scale(s));
+  if (s == 255u) codes.clear();      // (infinity * 0 is NaN, which the conversion would turn into a number)
+  return s;
+}
+
+// What an entry point knows of the current device; 0 where it is none that the kernels were built for.
+struct Device {
+  int sms = 0;
+  int* d_status = nullptr;   // the operators' status word (dq_mx_status)
+};
+dq_status current_device(Device& out);
+
+// dq_mx_quantize's work, used by dq_mx_linear too
+dq_status quantize(cudaStream_t stream, const void* X, int x_dtype, int64_t rows, int64_t k, int64_t ldx, int fmt,
+                   uint8_t* codes, uint8_t* scales, void* values, int64_t ldv);
+dq_status dequantize(cudaStream_t stream, int fmt, const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t k,
+                     void* Y, int y_dtype, int64_t ldy);
+dq_status rmsnorm_quantize(cudaStream_t stream, const void* X, int dtype, int64_t rows, int64_t k, int64_t ldx,
+                           const void* residual, int64_t ldr, const void* gamma, int gamma_dtype, float eps, int fmt,
+                           uint8_t* codes, uint8_t* scales, void* sum, int64_t lds, void* values, int64_t ldv);
+dq_status matmul(cudaStream_t stream, int a_fmt, const uint8_t* a_codes, const uint8_t* a_scales, int64_t m,
+                 const uint8_t* w_codes, const uint8_t* w_scales, int64_t n, int64_t k, void* Y, int y_dtype, int64_t ldy);
+dq_status linear(cudaStream_t stream, const void* X, int x_dtype, int64_t m, int64_t k, int64_t ldx, int a_fmt,
+                 const uint8_t* w_codes, const uint8_t* w_scales, int64_t n, void* Y, int y_dtype, int64_t ldy,
+                 uint8_t* workspace);
+
+}  // namespace mx
+}  // namespace dq

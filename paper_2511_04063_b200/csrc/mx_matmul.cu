@@ -1,0 +1,368 @@
+// Product of microscaled operands (dq_mx_matmul, dq_mx_linear):  Y[m][n] = sum_k A[m][k] W[n][k].
+//
+// The tensor cores take the elements and the block scales as they are held: D[n][m] (weight rows are the MMA's M, tokens
+// its N) accumulates  2^(sW + sA - 254) q_W q_A  in fp32 tensor memory; nothing is dequantised.  4-bit activations use
+// kind::mxf4 (64 values per MMA step), 8-bit ones kind::mxf8f6f4 (32 per step), for which the copy engine spreads the
+// weights' 4-bit codes to one 16-byte slot per 16 values while it brings them into shared memory.
+#include "mx_common.cuh"
+#include "tc_host.cuh"
+
+namespace dq {
+namespace mx {
+namespace {
+
+using namespace tc;
+using tc2::cluster_ctarank;
+using tc2::cluster_sync_all;
+
+struct Params {
+  void* y; int64_t ldy; int y_dtype;
+  int64_t m, n;            // tokens, weight rows
+  int n_blocks, m_blocks;  // tiles
+  int stages;              // pipeline steps of the whole reduction
+  int splits;              // CTAs of a cluster that share a tile's reduction
+  int dependent;           // the activations come from the kernel before this one, which may still be running
+  int* d_status;
+};
+
+// A pipeline step: 128 bytes of every row, as the MMAs read them: 256 4-bit values, or 128 8-bit ones.
+template <bool A8> struct Step {
+  static constexpr int KT = A8 ? 1 : 2;                    // scale tiles along k
+  static constexpr int MMAS = 4;                           // MMA steps of 32 bytes
+};
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+               ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+// Scales: 32 rows of 16 bytes, copied to the same 4 columns of all four 32-lane quarters of tensor memory.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t smem_addr) {
+  return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+}
+template <int GROUP>
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
+  if (GROUP == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+template <int GROUP, bool A8>
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
+                                           uint32_t accumulate) {
+#define DQ_MX_MMA(G, KIND)                                                                                     \
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                               \
+               "tcgen05.mma.cta_group::" #G ".kind::" KIND ".block_scale.block32 [%0], %1, %2, %3, [%4], [%5], p;\n\t}" \
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory")
+  if (GROUP == 1) { if (A8) DQ_MX_MMA(1, "mxf8f6f4"); else DQ_MX_MMA(1, "mxf4"); }
+  else { if (A8) DQ_MX_MMA(2, "mxf8f6f4"); else DQ_MX_MMA(2, "mxf4"); }
+#undef DQ_MX_MMA
+}
+// Instruction descriptor of the block-scaled kinds: M = weight rows (E2M1), N = tokens (E2M1 or E4M3), E8M0 scales.
+template <bool A8>
+__host__ __device__ constexpr uint32_t scaled_idesc(int m, int n) {
+  const uint32_t w_format = A8 ? 5u : 1u, a_format = A8 ? 0u : 1u;
+  return (w_format << 7) | (a_format << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 4) << 24);
+}
+// Which byte of a 32-bit scale column MMA step `s` of a pipeline step reads (both operands alike): mxf4 two blocks of a
+// column's four per step, mxf8f6f4 one.
+template <bool A8>
+__device__ __forceinline__ uint32_t scale_select(int s) {
+  const uint32_t id = A8 ? (uint32_t)s : 2u * (uint32_t)(s & 1);
+  return (id << 29) | (id << 4);
+}
+
+__device__ __forceinline__ void store_value(const Params& p, int64_t at, float v) {
+  if (p.y_dtype == DQ_BF16) reinterpret_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
+  else if (p.y_dtype == DQ_FP16) reinterpret_cast<__half*>(p.y)[at] = __float2half_rn(v);
+  else reinterpret_cast<float*>(p.y)[at] = v;
+}
+__device__ __forceinline__ void store_four(const Params& p, int64_t at, const float4& v) {
+  if (p.y_dtype == DQ_FP32) { *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + at) = v; return; }
+  uint2 w;
+  if (p.y_dtype == DQ_BF16) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+    w = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+  } else {
+    const __half2 a = __floats2half2_rn(v.x, v.y), b = __floats2half2_rn(v.z, v.w);
+    w = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+  }
+  *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.y) + at) = w;
+}
+
+// ------------------------------------------------------------------------------------------------ one tile per cluster
+// Few tokens: a tile of 128 weight rows x BN tokens, its reduction shared by the CTAs of a cluster.  What bounds it is
+// bringing the weights in; `splits` is chosen so that every SM brings some.  The CTAs leave their fp32 partial sums in
+// shared memory and each adds up a part of the columns over the cluster, in the order of the ranks: the result does not
+// depend on which CTA ends first.
+template <int BN, bool A8>
+struct ClusterSmem {
+  static constexpr int W_BYTES = 128 * 128;
+  static constexpr int W_LOADED = A8 ? W_BYTES / 2 : W_BYTES;   // (codes that are spread count as they lie in memory)
+  static constexpr int X_BYTES = BN * 128;
+  static constexpr int X_SCALE_TILES = BN > 128 ? 2 : 1;
+  static constexpr int SF_BYTES = Step<A8>::KT * TILE_BYTES * (1 + X_SCALE_TILES);
+  static constexpr int STAGE_BYTES = (W_BYTES + X_BYTES + SF_BYTES + 1023) / 1024 * 1024;
+  static constexpr int PARTIAL_BYTES = BN * 128 * 4;
+  static constexpr int STAGES = BN <= 32 ? 5 : (BN <= 128 ? 6 : 4);
+  static constexpr int TOTAL = STAGES * STAGE_BYTES + 1024 + 256;
+  static_assert(PARTIAL_BYTES <= STAGES * STAGE_BYTES, "the partial sums reuse the stages");
+  static constexpr int SCALE_COLS = 4 * Step<A8>::KT * (1 + X_SCALE_TILES);
+  static constexpr int NEED = BN + 2 * SCALE_COLS;
+  static constexpr int TMEM = NEED <= 64 ? 64 : (NEED <= 128 ? 128 : (NEED <= 256 ? 256 : 512));
+};
+
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, uint32_t rank) {
+  uint32_t remote;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
+  return v;
+}
+
+template <int BN, bool A8>
+__global__ void __launch_bounds__(192)
+cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws,
+               const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_xs, const Params p) {
+  using L = ClusterSmem<BN, A8>;
+  constexpr int STAGES = L::STAGES, KT = Step<A8>::KT;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t bars = base + STAGES * L::STAGE_BYTES;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 8u * (STAGES + s); };
+  const uint32_t done = bars + 8u * (2 * STAGES), tmem_slot = done + 8u;
+  uint8_t* smem = smem_raw + (base - smem_u32(smem_raw));
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = p.splits > 1 ? (int)cluster_ctarank() : 0;
+  const int tile = blockIdx.x / p.splits;
+  const int nb = tile % p.n_blocks, mb = tile / p.n_blocks;
+  const int k0 = (int)((int64_t)rank * p.stages / p.splits), kn = (int)((int64_t)(rank + 1) * p.stages / p.splits) - k0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    mbar_init(done, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_tensormap(&map_w); prefetch_tensormap(&map_ws); prefetch_tensormap(&map_x); prefetch_tensormap(&map_xs);
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, L::TMEM);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem + (tmem_slot - base));
+
+  if (warp == 0) {
+    if (lane == 0) {
+      auto weights = [&](int i) {
+        const int s = i % STAGES;
+        const uint32_t at = base + s * L::STAGE_BYTES;
+        mbar_expect_tx(full(s), L::W_LOADED + L::X_BYTES + L::SF_BYTES);
+        tma_load_2d(at, &map_w, full(s), (k0 + i) * (A8 ? 128 : 128), nb * 128);
+        tma_load_3d(at + L::W_BYTES + L::X_BYTES, &map_ws, full(s), 0, (k0 + i) * KT, nb);
+      };
+      auto tokens = [&](int i) {
+        const int s = i % STAGES;
+        const uint32_t at = base + s * L::STAGE_BYTES;
+        tma_load_2d(at + L::W_BYTES, &map_x, full(s), (k0 + i) * 128, mb * BN);
+        tma_load_3d(at + L::W_BYTES + L::X_BYTES + KT * TILE_BYTES, &map_xs, full(s), 0, (k0 + i) * KT, mb * BN / 128);
+      };
+      // The weights do not depend on the kernel before this one: the first stages' are on their way before its end.
+      const int ahead = kn < STAGES ? kn : STAGES;
+      for (int i = 0; i < ahead; ++i) weights(i);
+      if (p.dependent) asm volatile("griddepcontrol.wait;" ::: "memory");
+      for (int i = 0; i < ahead; ++i) tokens(i);
+      for (int i = ahead; i < kn; ++i) {
+        if (!mbar_wait(empty(i % STAGES), (uint32_t)(i / STAGES - 1) & 1u, p.d_status)) break;
+        weights(i);
+        tokens(i);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t IDESC = scaled_idesc<A8>(128, BN);
+      for (int i = 0; i < kn; ++i) {
+        const int s = i % STAGES;
+        const uint32_t at = base + s * L::STAGE_BYTES;
+        // the scales' columns of two steps ago are free once the MMAs that read them have completed
+        if (i >= 2 && !mbar_wait(empty((i - 2) % STAGES), (uint32_t)((i - 2) / STAGES) & 1u, p.d_status)) break;
+        if (!mbar_wait(full(s), (uint32_t)(i / STAGES) & 1u, p.d_status)) break;
+        tc_fence_after();
+        const uint32_t sw = tmem + BN + (i & 1) * L::SCALE_COLS, sx = sw + 4 * KT;
+        const uint32_t sf = at + L::W_BYTES + L::X_BYTES;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          copy_scales<1>(sw + 4 * t, scale_desc(sf + t * TILE_BYTES));
+#pragma unroll
+          for (int r = 0; r < L::X_SCALE_TILES; ++r)
+            copy_scales<1>(sx + (t * L::X_SCALE_TILES + r) * 4, scale_desc(sf + (KT * (1 + r) + t) * TILE_BYTES));
+        }
+        const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(at + L::W_BYTES);
+#pragma unroll
+        for (int m = 0; m < Step<A8>::MMAS; ++m) {
+          const int t = A8 ? 0 : m >> 1;
+          mma_scaled<1, A8>(tmem, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * t,
+                            sx + t * L::X_SCALE_TILES * 4, (i | m) ? 1u : 0u);
+        }
+        umma_commit(empty(s));
+      }
+      umma_commit(done);
+    }
+    __syncwarp();
+  } else {
+    const int q = warp & 3;
+    mbar_wait(done, 0, p.d_status);
+    tc_fence_after();
+    // every MMA has completed, so the stages are free: partial sums as [token][128 weight rows]
+    float* part = reinterpret_cast<float*>(smem);
+    for (int c = 0; c < BN; c += 16) {
+      uint32_t v[16];
+      asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                   : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+                     "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                   : "r"(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c) : "memory");
+      tmem_ld_wait();
+#pragma unroll
+      for (int e = 0; e < 16; ++e) part[(c + e) * 128 + q * 32 + lane] = __uint_as_float(v[e]);
+    }
+    tc_fence_before();
+  }
+  if (p.splits > 1) cluster_sync_all(); else __syncthreads();
+
+  // Y[token][4 weight rows] by all threads; the columns are dealt over the cluster
+  const int64_t left = p.m - (int64_t)mb * BN;
+  const int cols = left < BN ? (int)left : BN;
+  const int c0 = rank * cols / p.splits, c1 = (rank + 1) * cols / p.splits;
+  const int64_t n0 = (int64_t)nb * 128;
+  const int esize = p.y_dtype == DQ_FP32 ? 4 : 2;
+  const bool vec = (((uintptr_t)p.y | (uintptr_t)(p.ldy * esize)) & (uintptr_t)(4 * esize - 1)) == 0;
+  for (int i = (int)threadIdx.x + c0 * 32; i < c1 * 32; i += blockDim.x) {
+    const int c = i >> 5, n4 = (i & 31) * 4;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int r = 0; r < p.splits; ++r) {
+      const uint32_t at = base + (uint32_t)(c * 128 + n4) * 4u;
+      float4 v;
+      if (p.splits > 1) v = ld_cluster_f4(at, (uint32_t)r);
+      else v = *reinterpret_cast<const float4*>(smem + (at - base));
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    const int64_t n = n0 + n4, at = ((int64_t)mb * BN + c) * p.ldy + n;
+    if (vec && n + 4 <= p.n) store_four(p, at, s);
+    else {
+      const float e[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) if (n + j < p.n) store_value(p, at + j, e[j]);
+    }
+  }
+  tc_fence_before();
+  if (p.splits > 1) cluster_sync_all(); else __syncthreads();   // the peers have read this CTA's sums
+  if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, L::TMEM); }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+// Codes as rows of bytes; `spread`: 4-bit codes that arrive as 16 values per 16-byte slot (coordinates in values).
+dq_status codes_map(CUtensorMap* m, const uint8_t* codes, int fmt, int64_t rows, int64_t k, int box_rows, bool spread) {
+  tch::EncodeFn fn = tch::get_encode_fn();
+  if (!fn) return DQ_ERR_CUDA;
+  const cuuint64_t bytes = (cuuint64_t)row_bytes(fmt, k);
+  cuuint64_t dims[2] = {spread ? (cuuint64_t)(k_tiles(k) * KTILE) : bytes, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {bytes};
+  cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  cuuint32_t ones[2] = {1, 1};
+  const CUresult r = fn(m, spread ? CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)codes, dims,
+                        strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? DQ_OK : DQ_ERR_CUDA;
+}
+// Scale tiles [row tile][k tile][512 bytes]; a box past the last k tile reads zeros, which scale zeros.
+dq_status scales_map(CUtensorMap* m, const uint8_t* scales, int64_t rows, int64_t k, int kt, int row_tiles) {
+  tch::EncodeFn fn = tch::get_encode_fn();
+  if (!fn) return DQ_ERR_CUDA;
+  cuuint64_t dims[3] = {TILE_BYTES / 4, (cuuint64_t)k_tiles(k), (cuuint64_t)((rows + ROW_TILE - 1) / ROW_TILE)};
+  cuuint64_t strides[2] = {TILE_BYTES, (cuuint64_t)(k_tiles(k) * TILE_BYTES)};
+  cuuint32_t box[3] = {TILE_BYTES / 4, (cuuint32_t)kt, (cuuint32_t)row_tiles};
+  cuuint32_t ones[3] = {1, 1, 1};
+  const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, (void*)scales, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? DQ_OK : DQ_ERR_CUDA;
+}
+
+struct Operands {
+  int a_fmt;
+  const uint8_t *a_codes, *a_scales, *w_codes, *w_scales;
+  int64_t m, n, k;
+  void* y; int y_dtype; int64_t ldy;
+  bool dependent;
+};
+
+template <int BN, bool A8>
+dq_status launch_cluster(cudaStream_t stream, const Device& dev, const Operands& o) {
+  using L = ClusterSmem<BN, A8>;
+  constexpr int KT = Step<A8>::KT;
+  CUtensorMap w, ws, x, xs;
+  DQ_CHECK(codes_map(&w, o.w_codes, DQ_MXFP4, o.n, o.k, 128, A8));
+  DQ_CHECK(codes_map(&x, o.a_codes, o.a_fmt, o.m, o.k, BN, false));
+  DQ_CHECK(scales_map(&ws, o.w_scales, o.n, o.k, KT, 1));
+  DQ_CHECK(scales_map(&xs, o.a_scales, o.m, o.k, KT, L::X_SCALE_TILES));
+  Params p{};
+  p.y = o.y; p.ldy = o.ldy; p.y_dtype = o.y_dtype; p.m = o.m; p.n = o.n;
+  p.n_blocks = (int)((o.n + 127) / 128); p.m_blocks = (int)((o.m + BN - 1) / BN);
+  p.stages = (int)((k_tiles(o.k) + KT - 1) / KT);
+  p.dependent = o.dependent; p.d_status = dev.d_status;
+  const int64_t tiles = (int64_t)p.n_blocks * p.m_blocks;
+  p.splits = 1;
+  while (p.splits < 8 && tiles * p.splits * 2 <= dev.sms && p.splits * 2 <= p.stages) p.splits *= 2;
+  if (tiles * p.splits > 0x7fffffff) return DQ_ERR_UNSUPPORTED;
+  static SmemOptIn attr;
+  auto kern = cluster_kernel<BN, A8>;
+  DQ_CHECK(opt_in_dynamic_smem(kern, L::TOTAL, attr));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * p.splits)); cfg.blockDim = dim3(192);
+  cfg.dynamicSmemBytes = L::TOTAL; cfg.stream = stream;
+  cudaLaunchAttribute at[2];
+  int n_at = 0;
+  if (p.splits > 1) {
+    at[n_at].id = cudaLaunchAttributeClusterDimension;
+    at[n_at].val.clusterDim.x = (unsigned)p.splits; at[n_at].val.clusterDim.y = 1; at[n_at].val.clusterDim.z = 1;
+    ++n_at;
+  }
+  if (o.dependent) {
+    at[n_at].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n_at].val.programmaticStreamSerializationAllowed = 1;
+    ++n_at;
+  }
+  cfg.attrs = at; cfg.numAttrs = n_at;
+  return cudaLaunchKernelEx(&cfg, kern, w, ws, x, xs, p) == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
+}
+
+template <bool A8>
+dq_status product(cudaStream_t stream, const Device& dev, const Operands& o) {
+  if (o.m <= 16) return launch_cluster<16, A8>(stream, dev, o);
+  if (o.m <= 32) return launch_cluster<32, A8>(stream, dev, o);
+  if (o.m <= 64) return launch_cluster<64, A8>(stream, dev, o);
+  return launch_cluster<128, A8>(stream, dev, o);
+}
+
+dq_status run(cudaStream_t stream, const Operands& o) {
+  Device dev;
+  DQ_CHECK(current_device(dev));
+  if ((((uintptr_t)o.w_codes | (uintptr_t)o.a_codes) & 31) || (((uintptr_t)o.w_scales | (uintptr_t)o.a_scales) & 15))
+    return DQ_ERR_UNSUPPORTED;     // the copy engine's alignment
+  return o.a_fmt == DQ_MXFP4 ? product<false>(stream, dev, o) : product<true>(stream, dev, o);
+}
+
+}  // namespace
+
+dq_status matmul(cudaStream_t stream, int a_fmt, const uint8_t* a_codes, const uint8_t* a_scales, int64_t m,
+                 const uint8_t* w_codes, const uint8_t* w_scales, int64_t n, int64_t k, void* Y, int y_dtype, int64_t ldy) {
+  return run(stream, Operands{a_fmt, a_codes, a_scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy, false});
+}
+
+dq_status linear(cudaStream_t stream, const void* X, int x_dtype, int64_t m, int64_t k, int64_t ldx, int a_fmt,
+                 const uint8_t* w_codes, const uint8_t* w_scales, int64_t n, void* Y, int y_dtype, int64_t ldy,
+                 uint8_t* workspace) {
+  uint8_t* scales = workspace + m * row_bytes(a_fmt, k);
+  DQ_CHECK(quantize(stream, X, x_dtype, m, k, ldx, a_fmt, workspace, scales, nullptr, 0));
+  return run(stream, Operands{a_fmt, workspace, scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy, false});
+}
+
+}  // namespace mx
+}  // namespace dq
