@@ -109,6 +109,12 @@ struct ClusterSmem {
   static constexpr int TMEM = NEED <= 64 ? 64 : (NEED <= 128 ? 128 : (NEED <= 256 ? 256 : 512));
 };
 
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+                 "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+               : "r"(taddr) : "memory");
+}
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, uint32_t rank) {
   uint32_t remote;
   float4 v;
@@ -155,7 +161,7 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         const int s = i % STAGES;
         const uint32_t at = base + s * L::STAGE_BYTES;
         mbar_expect_tx(full(s), L::W_LOADED + L::X_BYTES + L::SF_BYTES);
-        tma_load_2d(at, &map_w, full(s), (k0 + i) * (A8 ? 128 : 128), nb * 128);
+        tma_load_2d(at, &map_w, full(s), (k0 + i) * 128, nb * 128);
         tma_load_3d(at + L::W_BYTES + L::X_BYTES, &map_ws, full(s), 0, (k0 + i) * KT, nb);
       };
       auto tokens = [&](int i) {
@@ -215,10 +221,7 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     float* part = reinterpret_cast<float*>(smem);
     for (int c = 0; c < BN; c += 16) {
       uint32_t v[16];
-      asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                   : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
-                     "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-                   : "r"(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c) : "memory");
+      tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c, v);
       tmem_ld_wait();
 #pragma unroll
       for (int e = 0; e < 16; ++e) part[(c + e) * 128 + q * 32 + lane] = __uint_as_float(v[e]);
@@ -255,6 +258,172 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   tc_fence_before();
   if (p.splits > 1) cluster_sync_all(); else __syncthreads();   // the peers have read this CTA's sums
   if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, L::TMEM); }
+}
+
+// ------------------------------------------------------------------------------------------------ persistent pairs
+// Many tokens: CTA pairs walk over tiles of 256 weight rows x 256 tokens with cta_group::2, each CTA staging half of both
+// operands (64 bytes of shared memory per SM and cycle at the 4-bit rate, where one CTA alone would need 96 for a tile of
+// 128 x 256).  The two accumulators of a pair's tiles share tensor memory with the scales (2 x 256 columns do not fit beside
+// 2 x 24): the second starts 208 columns after the first.  The epilogue of a tile therefore drains the 48 shared columns
+// first, and the next tile's MMAs start once those are free.
+template <bool A8>
+struct PairSmem {
+  static constexpr int KT = Step<A8>::KT;
+  static constexpr int W_BYTES = 128 * 128;
+  static constexpr int W_LOADED = A8 ? W_BYTES / 2 : W_BYTES;
+  static constexpr int X_BYTES = 128 * 128;
+  static constexpr int SF_BYTES = KT * TILE_BYTES * 3;     // its 128 weight rows', all 256 tokens'
+  static constexpr int STAGE_BYTES = (W_BYTES + X_BYTES + SF_BYTES + 1023) / 1024 * 1024;
+  static constexpr int STAGES = 6;
+  static constexpr int TOTAL = STAGES * STAGE_BYTES + 1024 + 256;
+  static constexpr int SCALE_COLS = 12 * KT;
+};
+constexpr int ACC_STRIDE = 208, SHARED_CHUNKS = 3;         // columns; chunks of 16 columns both accumulators cover
+constexpr int PAIR_SCALES = ACC_STRIDE + 256;              // first column of the scales
+constexpr int PAIR_GROUP = 8;                              // weight tiles that consecutive tiles go over before the next tokens
+
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+               ::"r"(dst), "l"((uint64_t)map), "r"(bar & tc2::PEER_MASK), "r"(c0), "r"(c1) : "memory");
+}
+
+template <bool A8>
+__global__ void __launch_bounds__(192, 1)
+pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws,
+            const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_xs, const Params p) {
+  using L = PairSmem<A8>;
+  constexpr int STAGES = L::STAGES, KT = L::KT;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t bars = base + STAGES * L::STAGE_BYTES;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 8u * (STAGES + s); };
+  auto ready = [&](int a) { return bars + 8u * (2 * STAGES + a); };          // accumulator a is complete
+  const uint32_t drained = bars + 8u * (2 * STAGES + 2);                     // the columns it shares are read
+  const uint32_t tmem_slot = drained + 8u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const bool leader = rank == 0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    mbar_init(ready(0), 1); mbar_init(ready(1), 1);
+    mbar_init(drained, 8);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_tensormap(&map_w); prefetch_tensormap(&map_ws); prefetch_tensormap(&map_x); prefetch_tensormap(&map_xs);
+  }
+  if (warp == 1) tc2::tmem_alloc_pair(tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem_raw + (tmem_slot - smem_u32(smem_raw)));
+
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int tiles = p.n_blocks * p.m_blocks;
+  auto tile_of = [&](int u, int& nb, int& mb) {
+    const int group = u / (PAIR_GROUP * p.m_blocks), r = u % (PAIR_GROUP * p.m_blocks);
+    const int left = p.n_blocks - group * PAIR_GROUP, wide = left < PAIR_GROUP ? left : PAIR_GROUP;
+    nb = group * PAIR_GROUP + r % wide;
+    mb = r / wide;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      if (p.dependent) asm volatile("griddepcontrol.wait;" ::: "memory");
+      int it = 0;
+      bool ok = true;
+      for (int u = pair; u < tiles && ok; u += pairs) {
+        int nb, mb;
+        tile_of(u, nb, mb);
+        for (int k = 0; k < p.stages; ++k, ++it) {
+          const int s = it % STAGES;
+          if (it >= STAGES && !mbar_wait(empty(s), (uint32_t)(it / STAGES - 1) & 1u, p.d_status)) { ok = false; break; }
+          const uint32_t at = base + s * L::STAGE_BYTES, sf = at + L::W_BYTES + L::X_BYTES;
+          if (leader) mbar_expect_tx(full(s), 2 * (L::W_LOADED + L::X_BYTES + L::SF_BYTES));
+          tma_load_2d_pair(at, &map_w, full(s), k * 128, nb * 256 + (int)rank * 128);
+          tma_load_2d_pair(at + L::W_BYTES, &map_x, full(s), k * 128, mb * 256 + (int)rank * 128);
+          tc2::tma_load_3d_pair(sf, &map_ws, full(s), 0, k * KT, nb * 2 + (int)rank);
+          tc2::tma_load_3d_pair(sf + KT * TILE_BYTES, &map_xs, full(s), 0, k * KT, mb * 2);
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (leader && lane == 0) {
+      constexpr uint32_t IDESC = scaled_idesc<A8>(256, 256);
+      int it = 0, t = 0;
+      bool ok = true;
+      for (int u = pair; u < tiles && ok; u += pairs, ++t) {
+        const uint32_t acc = tmem + (uint32_t)((t & 1) * ACC_STRIDE);
+        if (t >= 1) {
+          if (!mbar_wait(drained, (uint32_t)(t - 1) & 1u, p.d_status)) break;
+          tc_fence_after();
+        }
+        for (int k = 0; k < p.stages; ++k, ++it) {
+          const int s = it % STAGES;
+          const uint32_t at = base + s * L::STAGE_BYTES, sf = at + L::W_BYTES + L::X_BYTES;
+          // the scales' columns of two steps ago are free once the MMAs that read them have completed
+          if (it >= 2 && !mbar_wait(empty((it - 2) % STAGES), (uint32_t)((it - 2) / STAGES) & 1u, p.d_status)) { ok = false; break; }
+          if (!mbar_wait(full(s), (uint32_t)(it / STAGES) & 1u, p.d_status)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t sw = tmem + PAIR_SCALES + (uint32_t)((it & 1) * L::SCALE_COLS), sx = sw + 4 * KT;
+#pragma unroll
+          for (int j = 0; j < KT; ++j) {
+            copy_scales<2>(sw + 4 * j, scale_desc(sf + j * TILE_BYTES));
+            copy_scales<2>(sx + 8 * j, scale_desc(sf + (KT + j) * TILE_BYTES));
+            copy_scales<2>(sx + 8 * j + 4, scale_desc(sf + (2 * KT + j) * TILE_BYTES));
+          }
+          const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(at + L::W_BYTES);
+#pragma unroll
+          for (int m = 0; m < Step<A8>::MMAS; ++m) {
+            const int j = A8 ? 0 : m >> 1;
+            mma_scaled<2, A8>(acc, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * j, sx + 8 * j, (k | m) ? 1u : 0u);
+          }
+          tc2::umma_commit_pair(empty(s));
+        }
+        if (ok) tc2::umma_commit_pair(ready(t & 1));
+      }
+    }
+    __syncwarp();
+  } else {
+    const int q = warp & 3;
+    int t = 0;
+    for (int u = pair; u < tiles; u += pairs, ++t) {
+      int nb, mb;
+      tile_of(u, nb, mb);
+      const int a = t & 1;
+      if (!mbar_wait(ready(a), (uint32_t)(t >> 1) & 1u, p.d_status)) break;
+      tc_fence_after();
+      const int64_t n = (int64_t)nb * 256 + rank * 128 + q * 32 + lane;
+      const int64_t m0 = (int64_t)mb * 256;
+      const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * ACC_STRIDE);
+      // accumulator 0 ends with the shared columns, accumulator 1 begins with them
+      const int first = a == 0 ? 16 - SHARED_CHUNKS : 0;
+#pragma unroll 1
+      for (int i = 0; i < 16; ++i) {
+        const int c = ((first + i) & 15) * 16;
+        uint32_t v[16];
+        tmem_ld16(acc + (uint32_t)c, v);
+        tmem_ld_wait();
+        if (i == SHARED_CHUNKS - 1) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) tc2::mbar_arrive_leader(drained);
+        }
+        const int64_t left = p.m - m0 - c;
+        if (n < p.n) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (e < left) store_value(p, (m0 + c + e) * p.ldy + n, __uint_as_float(v[e]));
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  if (warp == 1) { tc_fence_after(); tc2::tmem_dealloc_pair(tmem, 512); }
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -334,11 +503,43 @@ dq_status launch_cluster(cudaStream_t stream, const Device& dev, const Operands&
 }
 
 template <bool A8>
+dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o) {
+  using L = PairSmem<A8>;
+  CUtensorMap w, ws, x, xs;
+  DQ_CHECK(codes_map(&w, o.w_codes, DQ_MXFP4, o.n, o.k, 128, A8));
+  DQ_CHECK(codes_map(&x, o.a_codes, o.a_fmt, o.m, o.k, 128, false));
+  DQ_CHECK(scales_map(&ws, o.w_scales, o.n, o.k, L::KT, 1));
+  DQ_CHECK(scales_map(&xs, o.a_scales, o.m, o.k, L::KT, 2));
+  Params p{};
+  p.y = o.y; p.ldy = o.ldy; p.y_dtype = o.y_dtype; p.m = o.m; p.n = o.n;
+  p.n_blocks = (int)((o.n + 255) / 256); p.m_blocks = (int)((o.m + 255) / 256);
+  p.stages = (int)((k_tiles(o.k) + L::KT - 1) / L::KT);
+  p.splits = 1; p.dependent = o.dependent; p.d_status = dev.d_status;
+  const int64_t tiles = (int64_t)p.n_blocks * p.m_blocks;
+  if (tiles * PAIR_GROUP > 0x7fffffff) return DQ_ERR_UNSUPPORTED;
+  const int pairs = tiles < dev.sms / 2 ? (int)tiles : dev.sms / 2;
+  static SmemOptIn attr;
+  auto kern = pair_kernel<A8>;
+  DQ_CHECK(opt_in_dynamic_smem(kern, L::TOTAL, attr));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * pairs)); cfg.blockDim = dim3(192);
+  cfg.dynamicSmemBytes = L::TOTAL; cfg.stream = stream;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = o.dependent ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, w, ws, x, xs, p) == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
+}
+
+template <bool A8>
 dq_status product(cudaStream_t stream, const Device& dev, const Operands& o) {
   if (o.m <= 16) return launch_cluster<16, A8>(stream, dev, o);
   if (o.m <= 32) return launch_cluster<32, A8>(stream, dev, o);
   if (o.m <= 64) return launch_cluster<64, A8>(stream, dev, o);
-  return launch_cluster<128, A8>(stream, dev, o);
+  if (o.m <= 192) return launch_cluster<128, A8>(stream, dev, o);
+  return launch_pair<A8>(stream, dev, o);
 }
 
 dq_status run(cudaStream_t stream, const Operands& o) {
