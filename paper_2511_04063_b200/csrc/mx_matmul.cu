@@ -17,6 +17,7 @@ using tc2::cluster_sync_all;
 
 struct Params {
   void* y; int64_t ldy; int y_dtype;
+  int y_vec;               // Y's rows start on 16-byte boundaries
   int64_t m, n;            // tokens, weight rows
   int n_blocks, m_blocks;  // tiles
   int stages;              // pipeline steps of the whole reduction
@@ -25,12 +26,24 @@ struct Params {
   int* d_status;
 };
 
+// The scales of a pipeline step lie in one of four slots of tensor memory.  They are copied there a step ahead of the MMAs that
+// read them, so that the copy runs beside the MMAs of the step before (one step's copies and MMAs in order: 1.8 times the time
+// of a 16384 x 8192 x 8192 product); a slot is free once the MMAs of four steps before have completed.
+constexpr int SCALE_SLOTS = 4;
+
 // A pipeline step: 128 bytes of every row, as the MMAs read them: 256 4-bit values, or 128 8-bit ones.
 template <bool A8> struct Step {
   static constexpr int KT = A8 ? 1 : 2;                    // scale tiles along k
   static constexpr int MMAS = 4;                           // MMA steps of 32 bytes
 };
 
+// One lane of a converged warp, always the same.  The instructions of the copy engine and the tensor cores take uniform
+// registers; behind `lane == 0` the compiler has to assume a divergent warp and each of them costs the issuer 60 cycles.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
+}
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(c0), "r"(c1) : "memory");
@@ -105,7 +118,7 @@ struct ClusterSmem {
   static constexpr int TOTAL = STAGES * STAGE_BYTES + 1024 + 256;
   static_assert(PARTIAL_BYTES <= STAGES * STAGE_BYTES, "the partial sums reuse the stages");
   static constexpr int SCALE_COLS = 4 * Step<A8>::KT * (1 + X_SCALE_TILES);
-  static constexpr int NEED = BN + 2 * SCALE_COLS;
+  static constexpr int NEED = BN + SCALE_SLOTS * SCALE_COLS;
   static constexpr int TMEM = NEED <= 64 ? 64 : (NEED <= 128 ? 128 : (NEED <= 256 ? 256 : 512));
 };
 
@@ -183,17 +196,15 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0) {
+    {
       constexpr uint32_t IDESC = scaled_idesc<A8>(128, BN);
-      for (int i = 0; i < kn; ++i) {
-        const int s = i % STAGES;
-        const uint32_t at = base + s * L::STAGE_BYTES;
-        // the scales' columns of two steps ago are free once the MMAs that read them have completed
-        if (i >= 2 && !mbar_wait(empty((i - 2) % STAGES), (uint32_t)((i - 2) / STAGES) & 1u, p.d_status)) break;
-        if (!mbar_wait(full(s), (uint32_t)(i / STAGES) & 1u, p.d_status)) break;
+      auto slot = [&](int i) { return tmem + BN + (uint32_t)(i % SCALE_SLOTS) * L::SCALE_COLS; };
+      auto scales = [&](int i) {
+        if (i >= SCALE_SLOTS && !mbar_wait(empty((i - SCALE_SLOTS) % STAGES), (uint32_t)((i - SCALE_SLOTS) / STAGES) & 1u, p.d_status))
+          return false;
         tc_fence_after();
-        const uint32_t sw = tmem + BN + (i & 1) * L::SCALE_COLS, sx = sw + 4 * KT;
-        const uint32_t sf = at + L::W_BYTES + L::X_BYTES;
+        if (elect_one()) {
+        const uint32_t sw = slot(i), sx = sw + 4 * KT, sf = base + (i % STAGES) * L::STAGE_BYTES + L::W_BYTES + L::X_BYTES;
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
           copy_scales<1>(sw + 4 * t, scale_desc(sf + t * TILE_BYTES));
@@ -201,6 +212,22 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
           for (int r = 0; r < L::X_SCALE_TILES; ++r)
             copy_scales<1>(sx + (t * L::X_SCALE_TILES + r) * 4, scale_desc(sf + (KT * (1 + r) + t) * TILE_BYTES));
         }
+        }
+        __syncwarp();
+        return true;
+      };
+      int copied = 0;                                        // steps whose scales are on their way
+      for (int i = 0; i < kn; ++i) {
+        if (copied == i) {
+          if (!mbar_wait(full(i % STAGES), (uint32_t)(i / STAGES) & 1u, p.d_status) || !scales(i)) break;
+          ++copied;
+        }
+        if (copied < kn && mbar_try_wait(full(copied % STAGES), (uint32_t)(copied / STAGES) & 1u)) {
+          if (!scales(copied)) break;
+          ++copied;
+        }
+        if (elect_one()) {
+        const uint32_t sw = slot(i), sx = sw + 4 * KT, at = base + (i % STAGES) * L::STAGE_BYTES;
         const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(at + L::W_BYTES);
 #pragma unroll
         for (int m = 0; m < Step<A8>::MMAS; ++m) {
@@ -208,9 +235,11 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
           mma_scaled<1, A8>(tmem, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * t,
                             sx + t * L::X_SCALE_TILES * 4, (i | m) ? 1u : 0u);
         }
-        umma_commit(empty(s));
+        umma_commit(empty(i % STAGES));
+        }
+        __syncwarp();
       }
-      umma_commit(done);
+      if (elect_one()) umma_commit(done);
     }
     __syncwarp();
   } else {
@@ -263,9 +292,9 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
 // ------------------------------------------------------------------------------------------------ persistent pairs
 // Many tokens: CTA pairs walk over tiles of 256 weight rows x 256 tokens with cta_group::2, each CTA staging half of both
 // operands (64 bytes of shared memory per SM and cycle at the 4-bit rate, where one CTA alone would need 96 for a tile of
-// 128 x 256).  The two accumulators of a pair's tiles share tensor memory with the scales (2 x 256 columns do not fit beside
-// 2 x 24): the second starts 208 columns after the first.  The epilogue of a tile therefore drains the 48 shared columns
-// first, and the next tile's MMAs start once those are free.
+// 128 x 256).  Two accumulators of 256 columns do not fit beside four slots of 24 (8 bits: 12) columns of scales: the second
+// accumulator starts 160 (208) columns after the first.  The epilogue of a tile takes the 96 (48) shared columns into
+// registers first, and the next tile's MMAs start once those are free.
 template <bool A8>
 struct PairSmem {
   static constexpr int KT = Step<A8>::KT;
@@ -275,11 +304,13 @@ struct PairSmem {
   static constexpr int SF_BYTES = KT * TILE_BYTES * 3;     // its 128 weight rows', all 256 tokens'
   static constexpr int STAGE_BYTES = (W_BYTES + X_BYTES + SF_BYTES + 1023) / 1024 * 1024;
   static constexpr int STAGES = 6;
-  static constexpr int TOTAL = STAGES * STAGE_BYTES + 1024 + 256;
   static constexpr int SCALE_COLS = 12 * KT;
+  static constexpr int SCALES = 512 - SCALE_SLOTS * SCALE_COLS;   // first column of the scales
+  static constexpr int ACC_STRIDE = SCALES - 256;                 // column where the second accumulator starts
+  static constexpr int SHARED = (256 - ACC_STRIDE + 31) / 32 * 32;   // columns both accumulators cover, to a multiple of 32
+  static constexpr int EPI_BYTES = 4 * 16 * 32 * 4;               // 16 tokens x 32 weight rows of the largest type a warp
+  static constexpr int TOTAL = STAGES * STAGE_BYTES + EPI_BYTES + 1024 + 256;
 };
-constexpr int ACC_STRIDE = 208, SHARED_CHUNKS = 3;         // columns; chunks of 16 columns both accumulators cover
-constexpr int PAIR_SCALES = ACC_STRIDE + 256;              // first column of the scales
 constexpr int PAIR_GROUP = 8;                              // weight tiles that consecutive tiles go over before the next tokens
 
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
@@ -287,7 +318,34 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
                ::"r"(dst), "l"((uint64_t)map), "r"(bar & tc2::PEER_MASK), "r"(c0), "r"(c1) : "memory");
 }
 
-template <bool A8>
+// 16 columns (tokens from m0 on) of a warp's 32 lanes (weight rows from n0 on) to Y: through shared memory, so that 16-byte
+// pieces of a token's row leave; one by one where Y's rows are not aligned or the tile reaches over an edge.
+template <typename T>
+__device__ __forceinline__ void store_columns(const Params& p, const uint32_t (&v)[16], uint8_t* stage, int lane, int64_t n0, int64_t m0) {
+  constexpr int PER = 16 / sizeof(T), LANES = 32 / PER, ROWS = 32 / LANES;   // values a piece, lanes a token, tokens a pass
+  T* y = reinterpret_cast<T*>(p.y);
+  if (p.y_vec && n0 + 32 <= p.n && m0 + 16 <= p.m) {
+    T* s = reinterpret_cast<T*>(stage);
+    __syncwarp();                                            // the pieces of the call before have been read
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e * 32 + lane] = from_f32<T>(__uint_as_float(v[e]));
+    __syncwarp();
+#pragma unroll
+    for (int r = 0; r < 16; r += ROWS) {
+      const int e = r + lane / LANES, c = lane % LANES * PER;
+      if (ROWS <= 16 || e < 16) *reinterpret_cast<uint4*>(y + (m0 + e) * p.ldy + n0 + c) = *reinterpret_cast<const uint4*>(s + e * 32 + c);
+    }
+    return;
+  }
+  const int64_t n = n0 + lane, left = p.m - m0;
+  if (n < p.n) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (e < left) y[(m0 + e) * p.ldy + n] = from_f32<T>(__uint_as_float(v[e]));
+  }
+}
+
+template <bool A8, typename T>
 __global__ void __launch_bounds__(192, 1)
 pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws,
             const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_xs, const Params p) {
@@ -295,7 +353,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
   constexpr int STAGES = L::STAGES, KT = L::KT;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t bars = base + STAGES * L::STAGE_BYTES;
+  const uint32_t epi = base + STAGES * L::STAGE_BYTES, bars = epi + L::EPI_BYTES;
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 8u * (STAGES + s); };
   auto ready = [&](int a) { return bars + 8u * (2 * STAGES + a); };          // accumulator a is complete
@@ -350,44 +408,72 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (leader && lane == 0) {
+    if (leader) {
       constexpr uint32_t IDESC = scaled_idesc<A8>(256, 256);
-      int it = 0, t = 0;
-      bool ok = true;
-      for (int u = pair; u < tiles && ok; u += pairs, ++t) {
-        const uint32_t acc = tmem + (uint32_t)((t & 1) * ACC_STRIDE);
-        if (t >= 1) {
+      const int mine = pair < tiles ? (tiles - pair + pairs - 1) / pairs : 0;
+      const int64_t steps = (int64_t)mine * p.stages;
+      // Ring positions: `next` is the step whose scales are copied next, `now` the one whose MMAs are issued next, `old` the one
+      // SCALE_SLOTS before `next`, whose MMAs have to have completed.
+      struct Ring {
+        int stage = 0, slot = 0;
+        uint32_t phase = 0;
+        __device__ __forceinline__ void step() {
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          slot = (slot + 1) % SCALE_SLOTS;
+        }
+      } next, now, old;
+      int64_t copied = 0;                                    // steps whose scales are on their way
+      auto scales = [&]() {
+        if (copied >= SCALE_SLOTS) {
+          if (!mbar_wait(empty(old.stage), old.phase, p.d_status)) return false;
+          old.step();
+        }
+        tc_fence_after();
+        if (elect_one()) {
+        const uint32_t sw = tmem + L::SCALES + (uint32_t)next.slot * L::SCALE_COLS, sx = sw + 4 * KT;
+        const uint32_t sf = base + (uint32_t)next.stage * L::STAGE_BYTES + L::W_BYTES + L::X_BYTES;
+#pragma unroll
+        for (int j = 0; j < KT; ++j) {
+          copy_scales<2>(sw + 4 * j, scale_desc(sf + j * TILE_BYTES));
+          copy_scales<2>(sx + 8 * j, scale_desc(sf + (KT + j) * TILE_BYTES));
+          copy_scales<2>(sx + 8 * j + 4, scale_desc(sf + (2 * KT + j) * TILE_BYTES));
+        }
+        }
+        __syncwarp();
+        next.step();
+        ++copied;
+        return true;
+      };
+      int k = 0, t = 0;                                      // step of the tile, tile
+      for (int64_t i = 0; i < steps; ++i) {
+        if (copied == i && (!mbar_wait(full(next.stage), next.phase, p.d_status) || !scales())) break;
+        if (copied < steps && mbar_try_wait(full(next.stage), next.phase) && !scales()) break;
+        if (k == 0 && t >= 1) {
           if (!mbar_wait(drained, (uint32_t)(t - 1) & 1u, p.d_status)) break;
           tc_fence_after();
         }
-        for (int k = 0; k < p.stages; ++k, ++it) {
-          const int s = it % STAGES;
-          const uint32_t at = base + s * L::STAGE_BYTES, sf = at + L::W_BYTES + L::X_BYTES;
-          // the scales' columns of two steps ago are free once the MMAs that read them have completed
-          if (it >= 2 && !mbar_wait(empty((it - 2) % STAGES), (uint32_t)((it - 2) / STAGES) & 1u, p.d_status)) { ok = false; break; }
-          if (!mbar_wait(full(s), (uint32_t)(it / STAGES) & 1u, p.d_status)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t sw = tmem + PAIR_SCALES + (uint32_t)((it & 1) * L::SCALE_COLS), sx = sw + 4 * KT;
+        const uint32_t acc = tmem + (uint32_t)((t & 1) * L::ACC_STRIDE);
+        if (elect_one()) {
+        const uint32_t sw = tmem + L::SCALES + (uint32_t)now.slot * L::SCALE_COLS, sx = sw + 4 * KT;
+        const uint32_t at = base + (uint32_t)now.stage * L::STAGE_BYTES;
+        const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(at + L::W_BYTES);
 #pragma unroll
-          for (int j = 0; j < KT; ++j) {
-            copy_scales<2>(sw + 4 * j, scale_desc(sf + j * TILE_BYTES));
-            copy_scales<2>(sx + 8 * j, scale_desc(sf + (KT + j) * TILE_BYTES));
-            copy_scales<2>(sx + 8 * j + 4, scale_desc(sf + (2 * KT + j) * TILE_BYTES));
-          }
-          const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(at + L::W_BYTES);
-#pragma unroll
-          for (int m = 0; m < Step<A8>::MMAS; ++m) {
-            const int j = A8 ? 0 : m >> 1;
-            mma_scaled<2, A8>(acc, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * j, sx + 8 * j, (k | m) ? 1u : 0u);
-          }
-          tc2::umma_commit_pair(empty(s));
+        for (int m = 0; m < Step<A8>::MMAS; ++m) {
+          const int j = A8 ? 0 : m >> 1;
+          mma_scaled<2, A8>(acc, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * j, sx + 8 * j, (k | m) ? 1u : 0u);
         }
-        if (ok) tc2::umma_commit_pair(ready(t & 1));
+        tc2::umma_commit_pair(empty(now.stage));
+        if (k + 1 == p.stages) tc2::umma_commit_pair(ready(t & 1));
+        }
+        __syncwarp();
+        now.step();
+        if (++k == p.stages) { k = 0; ++t; }
       }
     }
     __syncwarp();
   } else {
     const int q = warp & 3;
+    uint8_t* stage = smem_raw + (epi - smem_u32(smem_raw)) + q * (L::EPI_BYTES / 4);
     int t = 0;
     for (int u = pair; u < tiles; u += pairs, ++t) {
       int nb, mb;
@@ -395,28 +481,31 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
       const int a = t & 1;
       if (!mbar_wait(ready(a), (uint32_t)(t >> 1) & 1u, p.d_status)) break;
       tc_fence_after();
-      const int64_t n = (int64_t)nb * 256 + rank * 128 + q * 32 + lane;
-      const int64_t m0 = (int64_t)mb * 256;
-      const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * ACC_STRIDE);
+      const int64_t n0 = (int64_t)nb * 256 + rank * 128 + q * 32, m0 = (int64_t)mb * 256;
+      const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * L::ACC_STRIDE);
       // accumulator 0 ends with the shared columns, accumulator 1 begins with them
-      const int first = a == 0 ? 16 - SHARED_CHUNKS : 0;
-#pragma unroll 1
-      for (int i = 0; i < 16; ++i) {
-        const int c = ((first + i) & 15) * 16;
-        uint32_t v[16];
-        tmem_ld16(acc + (uint32_t)c, v);
-        tmem_ld_wait();
-        if (i == SHARED_CHUNKS - 1) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) tc2::mbar_arrive_leader(drained);
-        }
-        const int64_t left = p.m - m0 - c;
-        if (n < p.n) {
+      constexpr int SHARED = L::SHARED;
+      const int c0 = a == 0 ? 256 - SHARED : 0;
+      {
+        uint32_t v[SHARED / 16][16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (e < left) store_value(p, (m0 + c + e) * p.ldy + n, __uint_as_float(v[e]));
-        }
+        for (int i = 0; i < SHARED / 16; ++i) tmem_ld16(acc + (uint32_t)(c0 + 16 * i), v[i]);
+        tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc2::mbar_arrive_leader(drained);
+#pragma unroll
+        for (int i = 0; i < SHARED / 16; ++i) store_columns<T>(p, v[i], stage, lane, n0, m0 + c0 + 16 * i);
+      }
+      const int c1 = a == 0 ? 0 : SHARED;
+#pragma unroll 1
+      for (int i = 0; i < (256 - SHARED) / 32; ++i) {
+        uint32_t v[2][16];
+        tmem_ld16(acc + (uint32_t)(c1 + 32 * i), v[0]);
+        tmem_ld16(acc + (uint32_t)(c1 + 32 * i + 16), v[1]);
+        tmem_ld_wait();
+        store_columns<T>(p, v[0], stage, lane, n0, m0 + c1 + 32 * i);
+        store_columns<T>(p, v[1], stage, lane, n0, m0 + c1 + 32 * i + 16);
       }
     }
   }
@@ -502,7 +591,7 @@ dq_status launch_cluster(cudaStream_t stream, const Device& dev, const Operands&
   return cudaLaunchKernelEx(&cfg, kern, w, ws, x, xs, p) == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
 }
 
-template <bool A8>
+template <bool A8, typename T>
 dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o) {
   using L = PairSmem<A8>;
   CUtensorMap w, ws, x, xs;
@@ -515,11 +604,12 @@ dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o)
   p.n_blocks = (int)((o.n + 255) / 256); p.m_blocks = (int)((o.m + 255) / 256);
   p.stages = (int)((k_tiles(o.k) + L::KT - 1) / L::KT);
   p.splits = 1; p.dependent = o.dependent; p.d_status = dev.d_status;
+  p.y_vec = (((uintptr_t)o.y | (uintptr_t)(o.ldy * (int64_t)sizeof(T))) & 15) == 0;
   const int64_t tiles = (int64_t)p.n_blocks * p.m_blocks;
   if (tiles * PAIR_GROUP > 0x7fffffff) return DQ_ERR_UNSUPPORTED;
   const int pairs = tiles < dev.sms / 2 ? (int)tiles : dev.sms / 2;
   static SmemOptIn attr;
-  auto kern = pair_kernel<A8>;
+  auto kern = pair_kernel<A8, T>;
   DQ_CHECK(opt_in_dynamic_smem(kern, L::TOTAL, attr));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * pairs)); cfg.blockDim = dim3(192);
@@ -539,7 +629,9 @@ dq_status product(cudaStream_t stream, const Device& dev, const Operands& o) {
   if (o.m <= 32) return launch_cluster<32, A8>(stream, dev, o);
   if (o.m <= 64) return launch_cluster<64, A8>(stream, dev, o);
   if (o.m <= 192) return launch_cluster<128, A8>(stream, dev, o);
-  return launch_pair<A8>(stream, dev, o);
+  if (o.y_dtype == DQ_BF16) return launch_pair<A8, __nv_bfloat16>(stream, dev, o);
+  if (o.y_dtype == DQ_FP16) return launch_pair<A8, __half>(stream, dev, o);
+  return launch_pair<A8, float>(stream, dev, o);
 }
 
 dq_status run(cudaStream_t stream, const Operands& o) {
