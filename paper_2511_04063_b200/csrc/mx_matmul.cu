@@ -26,9 +26,8 @@ struct Params {
   int* d_status;
 };
 
-// The scales of a pipeline step lie in one of four slots of tensor memory.  They are copied there a step ahead of the MMAs that
-// read them, so that the copy runs beside the MMAs of the step before (one step's copies and MMAs in order: 1.8 times the time
-// of a 16384 x 8192 x 8192 product); a slot is free once the MMAs of four steps before have completed.
+// The scales of a pipeline step lie in one of four slots of tensor memory; a slot is free once the MMAs of four steps before have
+// completed (with two slots the issuer waits for MMAs that have hardly begun).
 constexpr int SCALE_SLOTS = 4;
 
 // A pipeline step: 128 bytes of every row, as the MMAs read them: 256 4-bit values, or 128 8-bit ones.
@@ -110,14 +109,14 @@ struct ClusterSmem {
   static constexpr int W_BYTES = 128 * 128;
   static constexpr int W_LOADED = A8 ? W_BYTES / 2 : W_BYTES;   // (codes that are spread count as they lie in memory)
   static constexpr int X_BYTES = BN * 128;
-  static constexpr int X_SCALE_TILES = BN > 128 ? 2 : 1;
-  static constexpr int SF_BYTES = Step<A8>::KT * TILE_BYTES * (1 + X_SCALE_TILES);
+  static_assert(BN <= 128, "one tile of token scales");
+  static constexpr int SF_BYTES = Step<A8>::KT * TILE_BYTES * 2;
   static constexpr int STAGE_BYTES = (W_BYTES + X_BYTES + SF_BYTES + 1023) / 1024 * 1024;
   static constexpr int PARTIAL_BYTES = BN * 128 * 4;
-  static constexpr int STAGES = BN <= 32 ? 5 : (BN <= 128 ? 6 : 4);
+  static constexpr int STAGES = BN <= 32 ? 5 : 6;
   static constexpr int TOTAL = STAGES * STAGE_BYTES + 1024 + 256;
   static_assert(PARTIAL_BYTES <= STAGES * STAGE_BYTES, "the partial sums reuse the stages");
-  static constexpr int SCALE_COLS = 4 * Step<A8>::KT * (1 + X_SCALE_TILES);
+  static constexpr int SCALE_COLS = 4 * Step<A8>::KT * 2;
   static constexpr int NEED = BN + SCALE_SLOTS * SCALE_COLS;
   static constexpr int TMEM = NEED <= 64 ? 64 : (NEED <= 128 ? 128 : (NEED <= 256 ? 256 : 512));
 };
@@ -169,7 +168,7 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem + (tmem_slot - base));
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (elect_one()) {
       auto weights = [&](int i) {
         const int s = i % STAGES;
         const uint32_t at = base + s * L::STAGE_BYTES;
@@ -198,44 +197,27 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   } else if (warp == 1) {
     {
       constexpr uint32_t IDESC = scaled_idesc<A8>(128, BN);
-      auto slot = [&](int i) { return tmem + BN + (uint32_t)(i % SCALE_SLOTS) * L::SCALE_COLS; };
-      auto scales = [&](int i) {
+      for (int i = 0; i < kn; ++i) {
+        const int st = i % STAGES;
+        if (!mbar_wait(full(st), (uint32_t)(i / STAGES) & 1u, p.d_status)) break;
         if (i >= SCALE_SLOTS && !mbar_wait(empty((i - SCALE_SLOTS) % STAGES), (uint32_t)((i - SCALE_SLOTS) / STAGES) & 1u, p.d_status))
-          return false;
+          break;
         tc_fence_after();
         if (elect_one()) {
-        const uint32_t sw = slot(i), sx = sw + 4 * KT, sf = base + (i % STAGES) * L::STAGE_BYTES + L::W_BYTES + L::X_BYTES;
+          const uint32_t sw = tmem + BN + (uint32_t)(i % SCALE_SLOTS) * L::SCALE_COLS, sx = sw + 4 * KT;
+          const uint32_t at = base + st * L::STAGE_BYTES, sf = at + L::W_BYTES + L::X_BYTES;
 #pragma unroll
-        for (int t = 0; t < KT; ++t) {
-          copy_scales<1>(sw + 4 * t, scale_desc(sf + t * TILE_BYTES));
+          for (int t = 0; t < KT; ++t) {
+            copy_scales<1>(sw + 4 * t, scale_desc(sf + t * TILE_BYTES));
+            copy_scales<1>(sx + 4 * t, scale_desc(sf + (KT + t) * TILE_BYTES));
+          }
+          const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(at + L::W_BYTES);
 #pragma unroll
-          for (int r = 0; r < L::X_SCALE_TILES; ++r)
-            copy_scales<1>(sx + (t * L::X_SCALE_TILES + r) * 4, scale_desc(sf + (KT * (1 + r) + t) * TILE_BYTES));
-        }
-        }
-        __syncwarp();
-        return true;
-      };
-      int copied = 0;                                        // steps whose scales are on their way
-      for (int i = 0; i < kn; ++i) {
-        if (copied == i) {
-          if (!mbar_wait(full(i % STAGES), (uint32_t)(i / STAGES) & 1u, p.d_status) || !scales(i)) break;
-          ++copied;
-        }
-        if (copied < kn && mbar_try_wait(full(copied % STAGES), (uint32_t)(copied / STAGES) & 1u)) {
-          if (!scales(copied)) break;
-          ++copied;
-        }
-        if (elect_one()) {
-        const uint32_t sw = slot(i), sx = sw + 4 * KT, at = base + (i % STAGES) * L::STAGE_BYTES;
-        const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(at + L::W_BYTES);
-#pragma unroll
-        for (int m = 0; m < Step<A8>::MMAS; ++m) {
-          const int t = A8 ? 0 : m >> 1;
-          mma_scaled<1, A8>(tmem, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * t,
-                            sx + t * L::X_SCALE_TILES * 4, (i | m) ? 1u : 0u);
-        }
-        umma_commit(empty(i % STAGES));
+          for (int m = 0; m < Step<A8>::MMAS; ++m) {
+            const int t = A8 ? 0 : m >> 1;
+            mma_scaled<1, A8>(tmem, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * t, sx + 4 * t, (i | m) ? 1u : 0u);
+          }
+          umma_commit(empty(st));
         }
         __syncwarp();
       }
@@ -387,7 +369,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
   };
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (elect_one()) {
       if (p.dependent) asm volatile("griddepcontrol.wait;" ::: "memory");
       int it = 0;
       bool ok = true;
@@ -412,8 +394,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
       constexpr uint32_t IDESC = scaled_idesc<A8>(256, 256);
       const int mine = pair < tiles ? (tiles - pair + pairs - 1) / pairs : 0;
       const int64_t steps = (int64_t)mine * p.stages;
-      // Ring positions: `next` is the step whose scales are copied next, `now` the one whose MMAs are issued next, `old` the one
-      // SCALE_SLOTS before `next`, whose MMAs have to have completed.
+      // ring positions of this step, and of the one SCALE_SLOTS before it, whose MMAs have to have completed
       struct Ring {
         int stage = 0, slot = 0;
         uint32_t phase = 0;
@@ -421,49 +402,37 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
           slot = (slot + 1) % SCALE_SLOTS;
         }
-      } next, now, old;
-      int64_t copied = 0;                                    // steps whose scales are on their way
-      auto scales = [&]() {
-        if (copied >= SCALE_SLOTS) {
-          if (!mbar_wait(empty(old.stage), old.phase, p.d_status)) return false;
-          old.step();
-        }
-        tc_fence_after();
-        if (elect_one()) {
-        const uint32_t sw = tmem + L::SCALES + (uint32_t)next.slot * L::SCALE_COLS, sx = sw + 4 * KT;
-        const uint32_t sf = base + (uint32_t)next.stage * L::STAGE_BYTES + L::W_BYTES + L::X_BYTES;
-#pragma unroll
-        for (int j = 0; j < KT; ++j) {
-          copy_scales<2>(sw + 4 * j, scale_desc(sf + j * TILE_BYTES));
-          copy_scales<2>(sx + 8 * j, scale_desc(sf + (KT + j) * TILE_BYTES));
-          copy_scales<2>(sx + 8 * j + 4, scale_desc(sf + (2 * KT + j) * TILE_BYTES));
-        }
-        }
-        __syncwarp();
-        next.step();
-        ++copied;
-        return true;
-      };
+      } now, old;
       int k = 0, t = 0;                                      // step of the tile, tile
       for (int64_t i = 0; i < steps; ++i) {
-        if (copied == i && (!mbar_wait(full(next.stage), next.phase, p.d_status) || !scales())) break;
-        if (copied < steps && mbar_try_wait(full(next.stage), next.phase) && !scales()) break;
+        if (!mbar_wait(full(now.stage), now.phase, p.d_status)) break;
+        if (i >= SCALE_SLOTS) {
+          if (!mbar_wait(empty(old.stage), old.phase, p.d_status)) break;
+          old.step();
+        }
         if (k == 0 && t >= 1) {
           if (!mbar_wait(drained, (uint32_t)(t - 1) & 1u, p.d_status)) break;
           tc_fence_after();
         }
-        const uint32_t acc = tmem + (uint32_t)((t & 1) * L::ACC_STRIDE);
+        tc_fence_after();
         if (elect_one()) {
-        const uint32_t sw = tmem + L::SCALES + (uint32_t)now.slot * L::SCALE_COLS, sx = sw + 4 * KT;
-        const uint32_t at = base + (uint32_t)now.stage * L::STAGE_BYTES;
-        const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(at + L::W_BYTES);
+          const uint32_t acc = tmem + (uint32_t)((t & 1) * L::ACC_STRIDE);
+          const uint32_t sw = tmem + L::SCALES + (uint32_t)now.slot * L::SCALE_COLS, sx = sw + 4 * KT;
+          const uint32_t at = base + (uint32_t)now.stage * L::STAGE_BYTES, sf = at + L::W_BYTES + L::X_BYTES;
 #pragma unroll
-        for (int m = 0; m < Step<A8>::MMAS; ++m) {
-          const int j = A8 ? 0 : m >> 1;
-          mma_scaled<2, A8>(acc, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * j, sx + 8 * j, (k | m) ? 1u : 0u);
-        }
-        tc2::umma_commit_pair(empty(now.stage));
-        if (k + 1 == p.stages) tc2::umma_commit_pair(ready(t & 1));
+          for (int j = 0; j < KT; ++j) {
+            copy_scales<2>(sw + 4 * j, scale_desc(sf + j * TILE_BYTES));
+            copy_scales<2>(sx + 8 * j, scale_desc(sf + (KT + j) * TILE_BYTES));
+            copy_scales<2>(sx + 8 * j + 4, scale_desc(sf + (2 * KT + j) * TILE_BYTES));
+          }
+          const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(at + L::W_BYTES);
+#pragma unroll
+          for (int m = 0; m < Step<A8>::MMAS; ++m) {
+            const int j = A8 ? 0 : m >> 1;
+            mma_scaled<2, A8>(acc, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * j, sx + 8 * j, (k | m) ? 1u : 0u);
+          }
+          tc2::umma_commit_pair(empty(now.stage));
+          if (k + 1 == p.stages) tc2::umma_commit_pair(ready(t & 1));
         }
         __syncwarp();
         now.step();
@@ -559,7 +528,7 @@ dq_status launch_cluster(cudaStream_t stream, const Device& dev, const Operands&
   DQ_CHECK(codes_map(&w, o.w_codes, DQ_MXFP4, o.n, o.k, 128, A8));
   DQ_CHECK(codes_map(&x, o.a_codes, o.a_fmt, o.m, o.k, BN, false));
   DQ_CHECK(scales_map(&ws, o.w_scales, o.n, o.k, KT, 1));
-  DQ_CHECK(scales_map(&xs, o.a_scales, o.m, o.k, KT, L::X_SCALE_TILES));
+  DQ_CHECK(scales_map(&xs, o.a_scales, o.m, o.k, KT, 1));
   Params p{};
   p.y = o.y; p.ldy = o.ldy; p.y_dtype = o.y_dtype; p.m = o.m; p.n = o.n;
   p.n_blocks = (int)((o.n + 127) / 128); p.m_blocks = (int)((o.m + BN - 1) / BN);
