@@ -290,7 +290,7 @@ struct PairSmem {
   static constexpr int SCALES = 512 - SCALE_SLOTS * SCALE_COLS;   // first column of the scales
   static constexpr int ACC_STRIDE = SCALES - 256;                 // column where the second accumulator starts
   static constexpr int SHARED = (256 - ACC_STRIDE + 31) / 32 * 32;   // columns both accumulators cover, to a multiple of 32
-  static constexpr int EPI_BYTES = 4 * 16 * 32 * 4;               // 16 tokens x 32 weight rows of the largest type a warp
+  static constexpr int EPI_BYTES = 8 * 1024;                      // of the eight epilogue warps
   static constexpr int TOTAL = STAGES * STAGE_BYTES + EPI_BYTES + 1024 + 256;
 };
 constexpr int PAIR_GROUP = 8;                              // weight tiles that consecutive tiles go over before the next tokens
@@ -300,35 +300,41 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
                ::"r"(dst), "l"((uint64_t)map), "r"(bar & tc2::PEER_MASK), "r"(c0), "r"(c1) : "memory");
 }
 
-// 16 columns (tokens from m0 on) of a warp's 32 lanes (weight rows from n0 on) to Y: through shared memory, so that 16-byte
-// pieces of a token's row leave; one by one where Y's rows are not aligned or the tile reaches over an edge.
+// 32 columns (tokens from m0 on) of a warp's 32 lanes (weight rows from n0 on) to Y: through 1 KB of shared memory, so that
+// 16-byte pieces of a token's row leave; one by one where Y's rows are not aligned or the tile reaches over an edge.
 template <typename T>
-__device__ __forceinline__ void store_columns(const Params& p, const uint32_t (&v)[16], uint8_t* stage, int lane, int64_t n0, int64_t m0) {
-  constexpr int PER = 16 / sizeof(T), LANES = 32 / PER, ROWS = 32 / LANES;   // values a piece, lanes a token, tokens a pass
+__device__ __forceinline__ void store_columns(const Params& p, const uint32_t (&v)[32], uint8_t* stage, int lane, int64_t n0, int64_t m0) {
+  constexpr int PER = 16 / sizeof(T), LANES = 32 / PER, ROWS = 32 / LANES;   // values a piece, lanes a token, tokens a store
+  constexpr int PASS = 32 / sizeof(T);                                       // tokens the buffer holds
   T* y = reinterpret_cast<T*>(p.y);
-  if (p.y_vec && n0 + 32 <= p.n && m0 + 16 <= p.m) {
+  if (p.y_vec && n0 + 32 <= p.n && m0 + 32 <= p.m) {
     T* s = reinterpret_cast<T*>(stage);
-    __syncwarp();                                            // the pieces of the call before have been read
+    T* to = y + (m0 + lane / LANES) * p.ldy + n0 + lane % LANES * PER;
+    const T* from = s + lane / LANES * 32 + lane % LANES * PER;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e * 32 + lane] = from_f32<T>(__uint_as_float(v[e]));
-    __syncwarp();
+    for (int e0 = 0; e0 < 32; e0 += PASS) {
+      __syncwarp();                                          // the pieces of the pass before have been read
 #pragma unroll
-    for (int r = 0; r < 16; r += ROWS) {
-      const int e = r + lane / LANES, c = lane % LANES * PER;
-      if (ROWS <= 16 || e < 16) *reinterpret_cast<uint4*>(y + (m0 + e) * p.ldy + n0 + c) = *reinterpret_cast<const uint4*>(s + e * 32 + c);
+      for (int e = 0; e < PASS; ++e) s[e * 32 + lane] = from_f32<T>(__uint_as_float(v[e0 + e]));
+      __syncwarp();
+#pragma unroll
+      for (int r = 0; r < PASS; r += ROWS)
+        *reinterpret_cast<uint4*>(to + (int64_t)(e0 + r) * p.ldy) = *reinterpret_cast<const uint4*>(from + r * 32);
     }
     return;
   }
   const int64_t n = n0 + lane, left = p.m - m0;
   if (n < p.n) {
+    T* to = y + m0 * p.ldy + n;
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (e < left) y[(m0 + e) * p.ldy + n] = from_f32<T>(__uint_as_float(v[e]));
+    for (int e = 0; e < 32; ++e, to += p.ldy)
+      if (e < left) *to = from_f32<T>(__uint_as_float(v[e]));
   }
 }
 
+constexpr int PAIR_THREADS = 320;                          // producer, issuer, eight epilogue warps
 template <bool A8, typename T>
-__global__ void __launch_bounds__(192, 1)
+__global__ void __launch_bounds__(PAIR_THREADS, 1)
 pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws,
             const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_xs, const Params p) {
   using L = PairSmem<A8>;
@@ -348,7 +354,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     mbar_init(ready(0), 1); mbar_init(ready(1), 1);
-    mbar_init(drained, 8);
+    mbar_init(drained, 16);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_tensormap(&map_w); prefetch_tensormap(&map_ws); prefetch_tensormap(&map_x); prefetch_tensormap(&map_xs);
   }
@@ -441,8 +447,11 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
     }
     __syncwarp();
   } else {
-    const int q = warp & 3;
-    uint8_t* stage = smem_raw + (epi - smem_u32(smem_raw)) + q * (L::EPI_BYTES / 4);
+    // Two warps for each quarter of the tensor-memory lanes; they take turns at the tile's eight pieces of 32 columns,
+    // those that both accumulators cover first (accumulator 0 ends with them, accumulator 1 begins with them).
+    constexpr int SHARED = L::SHARED / 32;
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    uint8_t* stage = smem_raw + (epi - smem_u32(smem_raw)) + (warp - 2) * 1024;
     int t = 0;
     for (int u = pair; u < tiles; u += pairs, ++t) {
       int nb, mb;
@@ -452,30 +461,24 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
       tc_fence_after();
       const int64_t n0 = (int64_t)nb * 256 + rank * 128 + q * 32, m0 = (int64_t)mb * 256;
       const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * L::ACC_STRIDE);
-      // accumulator 0 ends with the shared columns, accumulator 1 begins with them
-      constexpr int SHARED = L::SHARED;
-      const int c0 = a == 0 ? 256 - SHARED : 0;
-      {
-        uint32_t v[SHARED / 16][16];
-#pragma unroll
-        for (int i = 0; i < SHARED / 16; ++i) tmem_ld16(acc + (uint32_t)(c0 + 16 * i), v[i]);
-        tmem_ld_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) tc2::mbar_arrive_leader(drained);
-#pragma unroll
-        for (int i = 0; i < SHARED / 16; ++i) store_columns<T>(p, v[i], stage, lane, n0, m0 + c0 + 16 * i);
-      }
-      const int c1 = a == 0 ? 0 : SHARED;
-#pragma unroll 1
-      for (int i = 0; i < (256 - SHARED) / 32; ++i) {
-        uint32_t v[2][16];
-        tmem_ld16(acc + (uint32_t)(c1 + 32 * i), v[0]);
-        tmem_ld16(acc + (uint32_t)(c1 + 32 * i + 16), v[1]);
-        tmem_ld_wait();
-        store_columns<T>(p, v[0], stage, lane, n0, m0 + c1 + 32 * i);
-        store_columns<T>(p, v[1], stage, lane, n0, m0 + c1 + 32 * i + 16);
-      }
+      const int first = a == 0 ? 8 - SHARED : 0;
+      auto column = [&](int i) { return ((first + i) & 7) * 32; };
+      uint32_t v[2][32];
+      tmem_ld32(acc + (uint32_t)column(half), v[0]);
+      tmem_ld32(acc + (uint32_t)column(half + 2), v[1]);
+      tmem_ld_wait();
+      static_assert(SHARED <= 4, "the first two pieces of both warps cover the shared columns");
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc2::mbar_arrive_leader(drained);
+      store_columns<T>(p, v[0], stage, lane, n0, m0 + column(half));
+      tmem_ld32(acc + (uint32_t)column(half + 4), v[0]);     // (on its way during the next stores)
+      store_columns<T>(p, v[1], stage, lane, n0, m0 + column(half + 2));
+      tmem_ld_wait();
+      tmem_ld32(acc + (uint32_t)column(half + 6), v[1]);
+      store_columns<T>(p, v[0], stage, lane, n0, m0 + column(half + 4));
+      tmem_ld_wait();
+      store_columns<T>(p, v[1], stage, lane, n0, m0 + column(half + 6));
     }
   }
   tc_fence_before();
@@ -581,7 +584,7 @@ dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o)
   auto kern = pair_kernel<A8, T>;
   DQ_CHECK(opt_in_dynamic_smem(kern, L::TOTAL, attr));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(2 * pairs)); cfg.blockDim = dim3(192);
+  cfg.gridDim = dim3((unsigned)(2 * pairs)); cfg.blockDim = dim3(PAIR_THREADS);
   cfg.dynamicSmemBytes = L::TOTAL; cfg.stream = stream;
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeClusterDimension;
