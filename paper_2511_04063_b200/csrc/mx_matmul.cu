@@ -285,12 +285,12 @@ struct PairSmem {
   static constexpr int X_BYTES = 128 * 128;
   static constexpr int SF_BYTES = KT * TILE_BYTES * 3;     // its 128 weight rows', all 256 tokens'
   static constexpr int STAGE_BYTES = (W_BYTES + X_BYTES + SF_BYTES + 1023) / 1024 * 1024;
-  static constexpr int STAGES = 6;
+  static constexpr int STAGES = 5;
   static constexpr int SCALE_COLS = 12 * KT;
   static constexpr int SCALES = 512 - SCALE_SLOTS * SCALE_COLS;   // first column of the scales
   static constexpr int ACC_STRIDE = SCALES - 256;                 // column where the second accumulator starts
   static constexpr int SHARED = (256 - ACC_STRIDE + 31) / 32 * 32;   // columns both accumulators cover, to a multiple of 32
-  static constexpr int EPI_BYTES = 8 * 1024;                      // of the eight epilogue warps
+  static constexpr int EPI_BYTES = 4 * 8192;                      // two buffers for each group of epilogue warps
   static constexpr int TOTAL = STAGES * STAGE_BYTES + EPI_BYTES + 1024 + 256;
 };
 constexpr int PAIR_GROUP = 8;                              // weight tiles that consecutive tiles go over before the next tokens
@@ -300,43 +300,56 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
                ::"r"(dst), "l"((uint64_t)map), "r"(bar & tc2::PEER_MASK), "r"(c0), "r"(c1) : "memory");
 }
 
-// 32 columns (tokens from m0 on) of a warp's 32 lanes (weight rows from n0 on) to Y: through 1 KB of shared memory, so that
-// 16-byte pieces of a token's row leave; one by one where Y's rows are not aligned or the tile reaches over an edge.
+// The pieces of 32 columns (tokens from m0 on) x 128 lanes (weight rows) that a group of four epilogue warps takes to Y.  Where
+// Y's rows are aligned they leave through shared memory as rows of 128 values, written by the copy engine, which also clips
+// them at Y's edges: whole 256-byte rows, where the warps' own stores would write 64 bytes of a row at a time (MEASURED).
+// Each group has two buffers of 8 KB, a piece of a 4-byte type goes in two parts.
+constexpr int PIECE_BYTES = 8192;
 template <typename T>
-__device__ __forceinline__ void store_columns(const Params& p, const uint32_t (&v)[32], uint8_t* stage, int lane, int64_t n0, int64_t m0) {
-  constexpr int PER = 16 / sizeof(T), LANES = 32 / PER, ROWS = 32 / LANES;   // values a piece, lanes a token, tokens a store
-  constexpr int PASS = 32 / sizeof(T);                                       // tokens the buffer holds
-  T* y = reinterpret_cast<T*>(p.y);
-  if (p.y_vec && n0 + 32 <= p.n && m0 + 32 <= p.m) {
-    T* s = reinterpret_cast<T*>(stage);
-    T* to = y + (m0 + lane / LANES) * p.ldy + n0 + lane % LANES * PER;
-    const T* from = s + lane / LANES * 32 + lane % LANES * PER;
+struct Output {
+  static constexpr int PASS = PIECE_BYTES / 128 / sizeof(T);   // tokens of a buffer
+  const CUtensorMap* map;
+  uint8_t* buffers;
+  int group, q, lane, turn = 0;
+  __device__ __forceinline__ void piece(const Params& p, const uint32_t (&v)[32], int64_t n0, int64_t m0) {
+    if (p.y_vec) {
+      const bool one = q == 2 && lane == 0;                     // (the group's first warp)
 #pragma unroll
-    for (int e0 = 0; e0 < 32; e0 += PASS) {
-      __syncwarp();                                          // the pieces of the pass before have been read
+      for (int e0 = 0; e0 < 32; e0 += PASS, turn ^= 1) {
+        T* s = reinterpret_cast<T*>(buffers + turn * PIECE_BYTES);
+        if (one) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");   // the buffer's last piece has been read
+        asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
 #pragma unroll
-      for (int e = 0; e < PASS; ++e) s[e * 32 + lane] = from_f32<T>(__uint_as_float(v[e0 + e]));
-      __syncwarp();
-#pragma unroll
-      for (int r = 0; r < PASS; r += ROWS)
-        *reinterpret_cast<uint4*>(to + (int64_t)(e0 + r) * p.ldy) = *reinterpret_cast<const uint4*>(from + r * 32);
+        for (int e = 0; e < PASS; ++e) s[e * 128 + q * 32 + lane] = from_f32<T>(__uint_as_float(v[e0 + e]));
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
+        if (one) {
+          asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                       ::"l"((uint64_t)map), "r"(smem_u32(s)), "r"((int)n0), "r"((int)(m0 + e0)) : "memory");
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+      }
+      return;
     }
-    return;
-  }
-  const int64_t n = n0 + lane, left = p.m - m0;
-  if (n < p.n) {
-    T* to = y + m0 * p.ldy + n;
+    const int64_t n = n0 + q * 32 + lane, left = p.m - m0;
+    if (n < p.n) {
+      T* to = reinterpret_cast<T*>(p.y) + m0 * p.ldy + n;
 #pragma unroll
-    for (int e = 0; e < 32; ++e, to += p.ldy)
-      if (e < left) *to = from_f32<T>(__uint_as_float(v[e]));
+      for (int e = 0; e < 32; ++e, to += p.ldy)
+        if (e < left) *to = from_f32<T>(__uint_as_float(v[e]));
+    }
   }
-}
+  __device__ __forceinline__ void finish(const Params& p) const {   // before the shared memory goes away
+    if (p.y_vec && q == 2 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+};
 
 constexpr int PAIR_THREADS = 320;                          // producer, issuer, eight epilogue warps
 template <bool A8, typename T>
 __global__ void __launch_bounds__(PAIR_THREADS, 1)
 pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws,
-            const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_xs, const Params p) {
+            const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_xs,
+            const __grid_constant__ CUtensorMap map_y, const Params p) {
   using L = PairSmem<A8>;
   constexpr int STAGES = L::STAGES, KT = L::KT;
   extern __shared__ uint8_t smem_raw[];
@@ -451,7 +464,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
     // those that both accumulators cover first (accumulator 0 ends with them, accumulator 1 begins with them).
     constexpr int SHARED = L::SHARED / 32;
     const int q = warp & 3, half = (warp - 2) >> 2;
-    uint8_t* stage = smem_raw + (epi - smem_u32(smem_raw)) + (warp - 2) * 1024;
+    Output<T> out{&map_y, smem_raw + (epi - smem_u32(smem_raw)) + half * 2 * PIECE_BYTES, half, q, lane};
     int t = 0;
     for (int u = pair; u < tiles; u += pairs, ++t) {
       int nb, mb;
@@ -459,7 +472,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
       const int a = t & 1;
       if (!mbar_wait(ready(a), (uint32_t)(t >> 1) & 1u, p.d_status)) break;
       tc_fence_after();
-      const int64_t n0 = (int64_t)nb * 256 + rank * 128 + q * 32, m0 = (int64_t)mb * 256;
+      const int64_t n0 = (int64_t)nb * 256 + rank * 128, m0 = (int64_t)mb * 256;
       const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * L::ACC_STRIDE);
       const int first = a == 0 ? 8 - SHARED : 0;
       auto column = [&](int i) { return ((first + i) & 7) * 32; };
@@ -471,15 +484,16 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
       tc_fence_before();
       __syncwarp();
       if (lane == 0) tc2::mbar_arrive_leader(drained);
-      store_columns<T>(p, v[0], stage, lane, n0, m0 + column(half));
+      out.piece(p, v[0], n0, m0 + column(half));
       tmem_ld32(acc + (uint32_t)column(half + 4), v[0]);     // (on its way during the next stores)
-      store_columns<T>(p, v[1], stage, lane, n0, m0 + column(half + 2));
+      out.piece(p, v[1], n0, m0 + column(half + 2));
       tmem_ld_wait();
       tmem_ld32(acc + (uint32_t)column(half + 6), v[1]);
-      store_columns<T>(p, v[0], stage, lane, n0, m0 + column(half + 4));
+      out.piece(p, v[0], n0, m0 + column(half + 4));
       tmem_ld_wait();
-      store_columns<T>(p, v[1], stage, lane, n0, m0 + column(half + 6));
+      out.piece(p, v[1], n0, m0 + column(half + 6));
     }
+    out.finish(p);
   }
   tc_fence_before();
   __syncthreads();
@@ -512,6 +526,21 @@ dq_status scales_map(CUtensorMap* m, const uint8_t* scales, int64_t rows, int64_
   cuuint32_t ones[3] = {1, 1, 1};
   const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, (void*)scales, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                         CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? DQ_OK : DQ_ERR_CUDA;
+}
+
+// Y as boxes of 128 weight rows x `tokens`; only where its rows are 16-byte aligned.
+dq_status output_map(CUtensorMap* m, void* y, int dtype, int64_t rows, int64_t n, int64_t ldy, int tokens) {
+  tch::EncodeFn fn = tch::get_encode_fn();
+  if (!fn) return DQ_ERR_CUDA;
+  const CUtensorMapDataType type = dtype == DQ_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == DQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  cuuint64_t dims[2] = {(cuuint64_t)n, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)ldy * (dtype == DQ_FP32 ? 4 : 2)};
+  cuuint32_t box[2] = {128, (cuuint32_t)tokens};
+  cuuint32_t ones[2] = {1, 1};
+  const CUresult r = fn(m, type, 2, y, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                        CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? DQ_OK : DQ_ERR_CUDA;
 }
 
@@ -566,7 +595,7 @@ dq_status launch_cluster(cudaStream_t stream, const Device& dev, const Operands&
 template <bool A8, typename T>
 dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o) {
   using L = PairSmem<A8>;
-  CUtensorMap w, ws, x, xs;
+  CUtensorMap w, ws, x, xs, y = {};
   DQ_CHECK(codes_map(&w, o.w_codes, DQ_MXFP4, o.n, o.k, 128, A8));
   DQ_CHECK(codes_map(&x, o.a_codes, o.a_fmt, o.m, o.k, 128, false));
   DQ_CHECK(scales_map(&ws, o.w_scales, o.n, o.k, L::KT, 1));
@@ -577,6 +606,7 @@ dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o)
   p.stages = (int)((k_tiles(o.k) + L::KT - 1) / L::KT);
   p.splits = 1; p.dependent = o.dependent; p.d_status = dev.d_status;
   p.y_vec = (((uintptr_t)o.y | (uintptr_t)(o.ldy * (int64_t)sizeof(T))) & 15) == 0;
+  if (p.y_vec) DQ_CHECK(output_map(&y, o.y, o.y_dtype, o.m, o.n, o.ldy, Output<T>::PASS));
   const int64_t tiles = (int64_t)p.n_blocks * p.m_blocks;
   if (tiles * PAIR_GROUP > 0x7fffffff) return DQ_ERR_UNSUPPORTED;
   const int pairs = tiles < dev.sms / 2 ? (int)tiles : dev.sms / 2;
@@ -592,7 +622,7 @@ dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o)
   at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at; cfg.numAttrs = o.dependent ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, w, ws, x, xs, p) == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, kern, w, ws, x, xs, y, p) == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
 }
 
 template <bool A8>
