@@ -202,6 +202,31 @@ __device__ __forceinline__ uint32_t encode_block(const float (&v)[8], Codes8<FMT
   return s;
 }
 
+// Programmatic dependent launch, used by every kernel here: a kernel may be scheduled while the one before it still runs, does
+// what touches no memory, and waits for that kernel's end (and for all before it) with `wait_for_previous` before it reads or
+// writes anything.  Only then does it allow its own successor to be scheduled, so that whatever a successor reads before its
+// own wait can only have been written by the kernel directly before it.
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+struct LaunchConfig {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[2];
+  LaunchConfig(cudaStream_t stream, int64_t ctas, int threads, int smem = 0, int cluster = 1) {
+    cfg.gridDim = dim3((unsigned)ctas); cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem; cfg.stream = stream;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
+  }
+};
+template <typename... P, typename... A>
+inline dq_status launch(const LaunchConfig& c, void (*kern)(P...), A&&... args) {
+  return cudaLaunchKernelEx(&c.cfg, kern, static_cast<P>(args)...) == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
+}
+
 // What an entry point knows of the current device; 0 where it is none that the kernels were built for.
 struct Device {
   int sms = 0;

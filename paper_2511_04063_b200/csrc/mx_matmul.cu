@@ -22,7 +22,8 @@ struct Params {
   int n_blocks, m_blocks;  // tiles
   int stages;              // pipeline steps of the whole reduction
   int splits;              // CTAs of a cluster that share a tile's reduction
-  int dependent;           // the activations come from the kernel before this one, which may still be running
+  int weights_first;       // the kernel before this one writes no weights: the first may be read before its end
+  const void* x; int64_t ldx; int64_t k; int x_vec;   // FUSED: activations
   int* d_status;
 };
 
@@ -104,22 +105,31 @@ __device__ __forceinline__ void store_four(const Params& p, int64_t at, const fl
 // bringing the weights in; `splits` is chosen so that every SM brings some.  The CTAs leave their fp32 partial sums in
 // shared memory and each adds up a part of the columns over the cluster, in the order of the ranks: the result does not
 // depend on which CTA ends first.
-template <int BN, bool A8>
+//
+// FUSED (dq_mx_linear): the tokens come as T and every CTA quantises the part of them that it multiplies, which stays in shared
+// memory for its whole reduction, while the first weights are on their way.
+template <int BN, bool A8, bool FUSED>
 struct ClusterSmem {
+  static constexpr int KT = Step<A8>::KT;
   static constexpr int W_BYTES = 128 * 128;
   static constexpr int W_LOADED = A8 ? W_BYTES / 2 : W_BYTES;   // (codes that are spread count as they lie in memory)
   static constexpr int X_BYTES = BN * 128;
   static_assert(BN <= 128, "one tile of token scales");
-  static constexpr int SF_BYTES = Step<A8>::KT * TILE_BYTES * 2;
-  static constexpr int STAGE_BYTES = (W_BYTES + X_BYTES + SF_BYTES + 1023) / 1024 * 1024;
+  static constexpr int SF_BYTES = KT * TILE_BYTES;              // of one operand
+  static constexpr int RING_X = FUSED ? 0 : X_BYTES + SF_BYTES;
+  static constexpr int STAGE_BYTES = (W_BYTES + SF_BYTES + RING_X + 1023) / 1024 * 1024;
+  static constexpr int STAGE_LOADED = W_LOADED + SF_BYTES + RING_X;
   static constexpr int PARTIAL_BYTES = BN * 128 * 4;
   static constexpr int STAGES = BN <= 32 ? 5 : 6;
-  static constexpr int TOTAL = STAGES * STAGE_BYTES + 1024 + 256;
   static_assert(PARTIAL_BYTES <= STAGES * STAGE_BYTES, "the partial sums reuse the stages");
-  static constexpr int SCALE_COLS = 4 * Step<A8>::KT * 2;
+  static constexpr int FIXED = STAGES * STAGE_BYTES + 1024 + 256;
+  static constexpr int RESIDENT = FUSED ? X_BYTES + SF_BYTES : 0;   // and for each step of a CTA's reduction
+  static constexpr int SCALE_COLS = 4 * KT * 2;
   static constexpr int NEED = BN + SCALE_SLOTS * SCALE_COLS;
   static constexpr int TMEM = NEED <= 64 ? 64 : (NEED <= 128 ? 128 : (NEED <= 256 ? 256 : 512));
+  static constexpr int THREADS = FUSED ? 320 : 192;
 };
+constexpr int MAX_SMEM = 232448;
 
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -135,18 +145,57 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, uint32_t rank) {
   return v;
 }
 
-template <int BN, bool A8>
-__global__ void __launch_bounds__(192)
+// Rows [0, m) x values [c0, c0 + 8 groups) of X as a CTA's resident operand: codes of step i at codes + i X_BYTES in the K-major
+// 128-byte-swizzled order of the MMA's operands, its scale tiles at scales + i SF_BYTES.
+template <int BN, bool A8, typename T>
+__device__ __forceinline__ void quantize_resident(const Params& p, uint8_t* codes, uint8_t* scales, int64_t c0, int groups, int t, int threads) {
+  using L = ClusterSmem<BN, A8, true>;
+  constexpr int FMT = A8 ? DQ_MXFP8 : DQ_MXFP4, BYTES = Codes8<FMT>::BYTES, PER_STEP = 128 / BYTES;
+  const T* X = reinterpret_cast<const T*>(p.x);
+  const int total = (int)p.m * groups;                       // a multiple of 16: the lanes of a block stay together
+  constexpr int AT_ONCE = 4;
+  for (int i0 = t; i0 < (total + 31) / 32 * 32; i0 += AT_ONCE * threads) {
+    float v[AT_ONCE][8];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u * threads;
+      if (i < total) load8(X + (int64_t)(i / groups) * p.ldx, c0 + (int64_t)(i % groups) * 8, p.k, p.x_vec, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u * threads;
+      if (i - (t & 31) >= total) break;                      // (whole warps)
+      if (i >= total) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
+      }
+      Codes8<FMT> q;
+      const uint32_t s = encode_block<FMT>(v[u], q);
+      if (i < total) {
+        const int row = i / groups, g = i % groups, step = g / PER_STEP, byte = g % PER_STEP * BYTES;
+        q.store(codes + step * L::X_BYTES + row * 128 + ((((byte >> 4) ^ row) & 7) << 4) + (byte & 15));
+        if ((i & 3) == 0) {
+          const int block = g / 4;
+          scales[block / 4 * TILE_BYTES + (row & 31) * 16 + (row >> 5) * 4 + (block & 3)] = (uint8_t)s;
+        }
+      }
+    }
+  }
+}
+
+template <int BN, bool A8, bool FUSED, typename T>
+__global__ void __launch_bounds__(ClusterSmem<BN, A8, FUSED>::THREADS)
 cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws,
                const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_xs, const Params p) {
-  using L = ClusterSmem<BN, A8>;
-  constexpr int STAGES = L::STAGES, KT = Step<A8>::KT;
+  using L = ClusterSmem<BN, A8, FUSED>;
+  constexpr int STAGES = L::STAGES, KT = L::KT;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t bars = base + STAGES * L::STAGE_BYTES;
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 8u * (STAGES + s); };
-  const uint32_t done = bars + 8u * (2 * STAGES), tmem_slot = done + 8u;
+  const uint32_t done = bars + 8u * (2 * STAGES), held = done + 8u, tmem_slot = held + 8u;
+  const uint32_t res = (bars + 256u + 1023u) & ~1023u;       // FUSED: the resident tokens, then their scales
   uint8_t* smem = smem_raw + (base - smem_u32(smem_raw));
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -154,12 +203,15 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   const int tile = blockIdx.x / p.splits;
   const int nb = tile % p.n_blocks, mb = tile / p.n_blocks;
   const int k0 = (int)((int64_t)rank * p.stages / p.splits), kn = (int)((int64_t)(rank + 1) * p.stages / p.splits) - k0;
+  const uint32_t res_sf = res + (uint32_t)kn * L::X_BYTES;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     mbar_init(done, 1);
+    mbar_init(held, 8);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    prefetch_tensormap(&map_w); prefetch_tensormap(&map_ws); prefetch_tensormap(&map_x); prefetch_tensormap(&map_xs);
+    prefetch_tensormap(&map_w); prefetch_tensormap(&map_ws);
+    if (!FUSED) { prefetch_tensormap(&map_x); prefetch_tensormap(&map_xs); }
   }
   if (warp == 1) tmem_alloc(tmem_slot, L::TMEM);
   tc_fence_before();
@@ -172,20 +224,22 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
       auto weights = [&](int i) {
         const int s = i % STAGES;
         const uint32_t at = base + s * L::STAGE_BYTES;
-        mbar_expect_tx(full(s), L::W_LOADED + L::X_BYTES + L::SF_BYTES);
+        mbar_expect_tx(full(s), L::STAGE_LOADED);
         tma_load_2d(at, &map_w, full(s), (k0 + i) * 128, nb * 128);
-        tma_load_3d(at + L::W_BYTES + L::X_BYTES, &map_ws, full(s), 0, (k0 + i) * KT, nb);
+        tma_load_3d(at + L::W_BYTES, &map_ws, full(s), 0, (k0 + i) * KT, nb);
       };
       auto tokens = [&](int i) {
         const int s = i % STAGES;
-        const uint32_t at = base + s * L::STAGE_BYTES;
-        tma_load_2d(at + L::W_BYTES, &map_x, full(s), (k0 + i) * 128, mb * BN);
-        tma_load_3d(at + L::W_BYTES + L::X_BYTES + KT * TILE_BYTES, &map_xs, full(s), 0, (k0 + i) * KT, mb * BN / 128);
+        const uint32_t at = base + s * L::STAGE_BYTES + L::W_BYTES + L::SF_BYTES;
+        if (FUSED) return;
+        tma_load_2d(at, &map_x, full(s), (k0 + i) * 128, mb * BN);
+        tma_load_3d(at + L::X_BYTES, &map_xs, full(s), 0, (k0 + i) * KT, mb * BN / 128);
       };
-      // The weights do not depend on the kernel before this one: the first stages' are on their way before its end.
       const int ahead = kn < STAGES ? kn : STAGES;
+      if (!p.weights_first) wait_for_previous();
       for (int i = 0; i < ahead; ++i) weights(i);
-      if (p.dependent) asm volatile("griddepcontrol.wait;" ::: "memory");
+      if (p.weights_first) wait_for_previous();
+      allow_next();
       for (int i = 0; i < ahead; ++i) tokens(i);
       for (int i = ahead; i < kn; ++i) {
         if (!mbar_wait(empty(i % STAGES), (uint32_t)(i / STAGES - 1) & 1u, p.d_status)) break;
@@ -195,49 +249,61 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     }
     __syncwarp();
   } else if (warp == 1) {
-    {
-      constexpr uint32_t IDESC = scaled_idesc<A8>(128, BN);
-      for (int i = 0; i < kn; ++i) {
-        const int st = i % STAGES;
-        if (!mbar_wait(full(st), (uint32_t)(i / STAGES) & 1u, p.d_status)) break;
-        if (i >= SCALE_SLOTS && !mbar_wait(empty((i - SCALE_SLOTS) % STAGES), (uint32_t)((i - SCALE_SLOTS) / STAGES) & 1u, p.d_status))
-          break;
-        tc_fence_after();
-        if (elect_one()) {
-          const uint32_t sw = tmem + BN + (uint32_t)(i % SCALE_SLOTS) * L::SCALE_COLS, sx = sw + 4 * KT;
-          const uint32_t at = base + st * L::STAGE_BYTES, sf = at + L::W_BYTES + L::X_BYTES;
+    constexpr uint32_t IDESC = scaled_idesc<A8>(128, BN);
+    bool ok = !FUSED || mbar_wait(held, 0, p.d_status);
+    for (int i = 0; i < kn && ok; ++i) {
+      const int st = i % STAGES;
+      if (!mbar_wait(full(st), (uint32_t)(i / STAGES) & 1u, p.d_status)) break;
+      if (i >= SCALE_SLOTS && !mbar_wait(empty((i - SCALE_SLOTS) % STAGES), (uint32_t)((i - SCALE_SLOTS) / STAGES) & 1u, p.d_status))
+        break;
+      tc_fence_after();
+      if (elect_one()) {
+        const uint32_t sw = tmem + BN + (uint32_t)(i % SCALE_SLOTS) * L::SCALE_COLS, sx = sw + 4 * KT;
+        const uint32_t at = base + st * L::STAGE_BYTES;
+        const uint32_t x = FUSED ? res + i * L::X_BYTES : at + L::W_BYTES + L::SF_BYTES;
+        const uint32_t xs = FUSED ? res_sf + i * L::SF_BYTES : x + L::X_BYTES;
 #pragma unroll
-          for (int t = 0; t < KT; ++t) {
-            copy_scales<1>(sw + 4 * t, scale_desc(sf + t * TILE_BYTES));
-            copy_scales<1>(sx + 4 * t, scale_desc(sf + (KT + t) * TILE_BYTES));
-          }
-          const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(at + L::W_BYTES);
-#pragma unroll
-          for (int m = 0; m < Step<A8>::MMAS; ++m) {
-            const int t = A8 ? 0 : m >> 1;
-            mma_scaled<1, A8>(tmem, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * t, sx + 4 * t, (i | m) ? 1u : 0u);
-          }
-          umma_commit(empty(st));
+        for (int t = 0; t < KT; ++t) {
+          copy_scales<1>(sw + 4 * t, scale_desc(at + L::W_BYTES + t * TILE_BYTES));
+          copy_scales<1>(sx + 4 * t, scale_desc(xs + t * TILE_BYTES));
         }
-        __syncwarp();
+        const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(x);
+#pragma unroll
+        for (int m = 0; m < Step<A8>::MMAS; ++m) {
+          const int t = A8 ? 0 : m >> 1;
+          mma_scaled<1, A8>(tmem, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * t, sx + 4 * t, (i | m) ? 1u : 0u);
+        }
+        umma_commit(empty(st));
       }
-      if (elect_one()) umma_commit(done);
+      __syncwarp();
     }
+    if (elect_one()) umma_commit(done);
     __syncwarp();
   } else {
-    const int q = warp & 3;
-    mbar_wait(done, 0, p.d_status);
-    tc_fence_after();
-    // every MMA has completed, so the stages are free: partial sums as [token][128 weight rows]
-    float* part = reinterpret_cast<float*>(smem);
-    for (int c = 0; c < BN; c += 16) {
-      uint32_t v[16];
-      tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c, v);
-      tmem_ld_wait();
-#pragma unroll
-      for (int e = 0; e < 16; ++e) part[(c + e) * 128 + q * 32 + lane] = __uint_as_float(v[e]);
+    if (FUSED) {
+      wait_for_previous();
+      const int64_t values = A8 ? 128 : 256;                 // of a step
+      quantize_resident<BN, A8, T>(p, smem + (res - base), smem + (res_sf - base), k0 * values, kn * (int)(values / 8),
+                                   (int)threadIdx.x - 64, L::THREADS - 64);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(held);
     }
-    tc_fence_before();
+    if (warp < 6) {
+      const int q = warp & 3;
+      mbar_wait(done, 0, p.d_status);
+      tc_fence_after();
+      // every MMA has completed, so the stages are free: partial sums as [token][128 weight rows]
+      float* part = reinterpret_cast<float*>(smem);
+      for (int c = 0; c < BN; c += 16) {
+        uint32_t v[16];
+        tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) part[(c + e) * 128 + q * 32 + lane] = __uint_as_float(v[e]);
+      }
+      tc_fence_before();
+    }
   }
   if (p.splits > 1) cluster_sync_all(); else __syncthreads();
 
@@ -389,7 +455,8 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
 
   if (warp == 0) {
     if (elect_one()) {
-      if (p.dependent) asm volatile("griddepcontrol.wait;" ::: "memory");
+      wait_for_previous();
+      allow_next();
       int it = 0;
       bool ok = true;
       for (int u = pair; u < tiles && ok; u += pairs) {
@@ -549,47 +616,40 @@ struct Operands {
   const uint8_t *a_codes, *a_scales, *w_codes, *w_scales;
   int64_t m, n, k;
   void* y; int y_dtype; int64_t ldy;
-  bool dependent;
+  bool weights_first = false;
+  const void* x = nullptr; int64_t ldx = 0; int x_vec = 0;   // unquantised activations
 };
 
-template <int BN, bool A8>
-dq_status launch_cluster(cudaStream_t stream, const Device& dev, const Operands& o) {
-  using L = ClusterSmem<BN, A8>;
-  constexpr int KT = Step<A8>::KT;
-  CUtensorMap w, ws, x, xs;
-  DQ_CHECK(codes_map(&w, o.w_codes, DQ_MXFP4, o.n, o.k, 128, A8));
-  DQ_CHECK(codes_map(&x, o.a_codes, o.a_fmt, o.m, o.k, BN, false));
-  DQ_CHECK(scales_map(&ws, o.w_scales, o.n, o.k, KT, 1));
-  DQ_CHECK(scales_map(&xs, o.a_scales, o.m, o.k, KT, 1));
+Params params(const Device& dev, const Operands& o, int rows, int tokens, int kt) {
   Params p{};
-  p.y = o.y; p.ldy = o.ldy; p.y_dtype = o.y_dtype; p.m = o.m; p.n = o.n;
-  p.n_blocks = (int)((o.n + 127) / 128); p.m_blocks = (int)((o.m + BN - 1) / BN);
-  p.stages = (int)((k_tiles(o.k) + KT - 1) / KT);
-  p.dependent = o.dependent; p.d_status = dev.d_status;
+  p.y = o.y; p.ldy = o.ldy; p.y_dtype = o.y_dtype; p.m = o.m; p.n = o.n; p.k = o.k;
+  p.n_blocks = (int)((o.n + rows - 1) / rows); p.m_blocks = (int)((o.m + tokens - 1) / tokens);
+  p.stages = (int)((k_tiles(o.k) + kt - 1) / kt);
+  p.splits = 1; p.weights_first = o.weights_first; p.d_status = dev.d_status;
+  p.x = o.x; p.ldx = o.ldx; p.x_vec = o.x_vec;
+  return p;
+}
+
+template <int BN, bool A8, bool FUSED, typename T>
+dq_status launch_cluster(cudaStream_t stream, const Device& dev, const Operands& o) {
+  using L = ClusterSmem<BN, A8, FUSED>;
+  CUtensorMap w, ws, x = {}, xs = {};
+  Params p = params(dev, o, 128, BN, L::KT);
   const int64_t tiles = (int64_t)p.n_blocks * p.m_blocks;
   p.splits = 1;
-  while (p.splits < 8 && tiles * p.splits * 2 <= dev.sms && p.splits * 2 <= p.stages) p.splits *= 2;
-  if (tiles * p.splits > 0x7fffffff) return DQ_ERR_UNSUPPORTED;
+  auto smem = [&]() { return L::FIXED + (FUSED ? 1024 + (p.stages + p.splits - 1) / p.splits * L::RESIDENT : 0); };
+  while (p.splits < 8 && p.splits * 2 <= p.stages && (tiles * p.splits * 2 <= dev.sms || smem() > MAX_SMEM)) p.splits *= 2;
+  if (tiles * p.splits > 0x7fffffff || smem() > MAX_SMEM) return DQ_ERR_UNSUPPORTED;
+  DQ_CHECK(codes_map(&w, o.w_codes, DQ_MXFP4, o.n, o.k, 128, A8));
+  DQ_CHECK(scales_map(&ws, o.w_scales, o.n, o.k, L::KT, 1));
+  if (!FUSED) {
+    DQ_CHECK(codes_map(&x, o.a_codes, o.a_fmt, o.m, o.k, BN, false));
+    DQ_CHECK(scales_map(&xs, o.a_scales, o.m, o.k, L::KT, 1));
+  }
   static SmemOptIn attr;
-  auto kern = cluster_kernel<BN, A8>;
-  DQ_CHECK(opt_in_dynamic_smem(kern, L::TOTAL, attr));
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * p.splits)); cfg.blockDim = dim3(192);
-  cfg.dynamicSmemBytes = L::TOTAL; cfg.stream = stream;
-  cudaLaunchAttribute at[2];
-  int n_at = 0;
-  if (p.splits > 1) {
-    at[n_at].id = cudaLaunchAttributeClusterDimension;
-    at[n_at].val.clusterDim.x = (unsigned)p.splits; at[n_at].val.clusterDim.y = 1; at[n_at].val.clusterDim.z = 1;
-    ++n_at;
-  }
-  if (o.dependent) {
-    at[n_at].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[n_at].val.programmaticStreamSerializationAllowed = 1;
-    ++n_at;
-  }
-  cfg.attrs = at; cfg.numAttrs = n_at;
-  return cudaLaunchKernelEx(&cfg, kern, w, ws, x, xs, p) == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
+  auto kern = cluster_kernel<BN, A8, FUSED, T>;
+  DQ_CHECK(opt_in_dynamic_smem(kern, FUSED ? MAX_SMEM : L::FIXED, attr));
+  return launch(LaunchConfig(stream, tiles * p.splits, L::THREADS, smem(), p.splits), kern, w, ws, x, xs, p);
 }
 
 template <bool A8, typename T>
@@ -600,11 +660,7 @@ dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o)
   DQ_CHECK(codes_map(&x, o.a_codes, o.a_fmt, o.m, o.k, 128, false));
   DQ_CHECK(scales_map(&ws, o.w_scales, o.n, o.k, L::KT, 1));
   DQ_CHECK(scales_map(&xs, o.a_scales, o.m, o.k, L::KT, 2));
-  Params p{};
-  p.y = o.y; p.ldy = o.ldy; p.y_dtype = o.y_dtype; p.m = o.m; p.n = o.n;
-  p.n_blocks = (int)((o.n + 255) / 256); p.m_blocks = (int)((o.m + 255) / 256);
-  p.stages = (int)((k_tiles(o.k) + L::KT - 1) / L::KT);
-  p.splits = 1; p.dependent = o.dependent; p.d_status = dev.d_status;
+  Params p = params(dev, o, 256, 256, L::KT);
   p.y_vec = (((uintptr_t)o.y | (uintptr_t)(o.ldy * (int64_t)sizeof(T))) & 15) == 0;
   if (p.y_vec) DQ_CHECK(output_map(&y, o.y, o.y_dtype, o.m, o.n, o.ldy, Output<T>::PASS));
   const int64_t tiles = (int64_t)p.n_blocks * p.m_blocks;
@@ -613,50 +669,55 @@ dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o)
   static SmemOptIn attr;
   auto kern = pair_kernel<A8, T>;
   DQ_CHECK(opt_in_dynamic_smem(kern, L::TOTAL, attr));
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(2 * pairs)); cfg.blockDim = dim3(PAIR_THREADS);
-  cfg.dynamicSmemBytes = L::TOTAL; cfg.stream = stream;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at; cfg.numAttrs = o.dependent ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, w, ws, x, xs, y, p) == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
+  return launch(LaunchConfig(stream, 2 * pairs, PAIR_THREADS, L::TOTAL, 2), kern, w, ws, x, xs, y, p);
 }
 
 template <bool A8>
 dq_status product(cudaStream_t stream, const Device& dev, const Operands& o) {
-  if (o.m <= 16) return launch_cluster<16, A8>(stream, dev, o);
-  if (o.m <= 32) return launch_cluster<32, A8>(stream, dev, o);
-  if (o.m <= 64) return launch_cluster<64, A8>(stream, dev, o);
-  if (o.m <= 192) return launch_cluster<128, A8>(stream, dev, o);
+  if (o.m <= 16) return launch_cluster<16, A8, false, float>(stream, dev, o);
+  if (o.m <= 32) return launch_cluster<32, A8, false, float>(stream, dev, o);
+  if (o.m <= 64) return launch_cluster<64, A8, false, float>(stream, dev, o);
+  if (o.m <= 192) return launch_cluster<128, A8, false, float>(stream, dev, o);
   if (o.y_dtype == DQ_BF16) return launch_pair<A8, __nv_bfloat16>(stream, dev, o);
   if (o.y_dtype == DQ_FP16) return launch_pair<A8, __half>(stream, dev, o);
   return launch_pair<A8, float>(stream, dev, o);
 }
 
-dq_status run(cudaStream_t stream, const Operands& o) {
-  Device dev;
-  DQ_CHECK(current_device(dev));
-  if ((((uintptr_t)o.w_codes | (uintptr_t)o.a_codes) & 31) || (((uintptr_t)o.w_scales | (uintptr_t)o.a_scales) & 15))
-    return DQ_ERR_UNSUPPORTED;     // the copy engine's alignment
+dq_status run(cudaStream_t stream, const Device& dev, const Operands& o) {
   return o.a_fmt == DQ_MXFP4 ? product<false>(stream, dev, o) : product<true>(stream, dev, o);
+}
+template <bool A8>
+dq_status fused(cudaStream_t stream, const Device& dev, const Operands& o, int x_dtype) {
+  if (x_dtype == DQ_BF16) return launch_cluster<16, A8, true, __nv_bfloat16>(stream, dev, o);
+  if (x_dtype == DQ_FP16) return launch_cluster<16, A8, true, __half>(stream, dev, o);
+  return launch_cluster<16, A8, true, float>(stream, dev, o);
 }
 
 }  // namespace
 
 dq_status matmul(cudaStream_t stream, int a_fmt, const uint8_t* a_codes, const uint8_t* a_scales, int64_t m,
                  const uint8_t* w_codes, const uint8_t* w_scales, int64_t n, int64_t k, void* Y, int y_dtype, int64_t ldy) {
-  return run(stream, Operands{a_fmt, a_codes, a_scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy, false});
+  Device dev;
+  DQ_CHECK(current_device(dev));
+  return run(stream, dev, Operands{a_fmt, a_codes, a_scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy});
 }
 
 dq_status linear(cudaStream_t stream, const void* X, int x_dtype, int64_t m, int64_t k, int64_t ldx, int a_fmt,
                  const uint8_t* w_codes, const uint8_t* w_scales, int64_t n, void* Y, int y_dtype, int64_t ldy,
                  uint8_t* workspace) {
+  Device dev;
+  DQ_CHECK(current_device(dev));
   uint8_t* scales = workspace + m * row_bytes(a_fmt, k);
+  Operands o{a_fmt, workspace, scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy};
+  if (m <= 16) {
+    o.x = X; o.ldx = ldx;
+    o.x_vec = ((uintptr_t)X & 15) == 0 && ldx * (x_dtype == DQ_FP32 ? 4 : 2) % 16 == 0;
+    const dq_status st = a_fmt == DQ_MXFP4 ? fused<false>(stream, dev, o, x_dtype) : fused<true>(stream, dev, o, x_dtype);
+    if (st != DQ_ERR_UNSUPPORTED) return st;                 // (too long a reduction for its tokens to stay in shared memory)
+  }
   DQ_CHECK(quantize(stream, X, x_dtype, m, k, ldx, a_fmt, workspace, scales, nullptr, 0));
-  return run(stream, Operands{a_fmt, workspace, scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy, false});
+  o.weights_first = true;
+  return run(stream, dev, o);
 }
 
 }  // namespace mx

@@ -47,6 +47,8 @@ template <typename T, int FMT>
 __global__ void __launch_bounds__(256) quantize_kernel(const T* X, int64_t rows, int64_t k, int64_t ldx, int row_groups,
                                                        int64_t col_chunks, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                                                        T* values, int64_t ldv, int x_vec, int v_vec) {
+  wait_for_previous();
+  allow_next();
   const int lane = threadIdx.x & 31;
   const int64_t w = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   const int64_t ktiles = k_tiles(k);
@@ -92,6 +94,8 @@ __global__ void __launch_bounds__(256) quantize_kernel(const T* X, int64_t rows,
 template <typename T, int FMT>
 __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                          int64_t rows, int64_t k, T* __restrict__ Y, int64_t ldy, int vec) {
+  wait_for_previous();
+  allow_next();
   const int64_t groups = (k + 7) / 8;
   const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   const int64_t r = at / groups, c = at % groups * 8;
@@ -111,6 +115,8 @@ __global__ void rmsnorm_kernel(const T* X, int64_t rows, int64_t k, int64_t ldx,
                                const G* __restrict__ gamma, float eps, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                                T* sum, int64_t lds, T* values, int64_t ldv, int threads_per_row, int vec, int g_vec) {
   __shared__ float part[32];
+  wait_for_previous();
+  allow_next();
   const int row_in_cta = threadIdx.x / threads_per_row, t = threadIdx.x % threads_per_row;
   const int lane = threadIdx.x & 31, warps = threads_per_row >> 5, warp0 = row_in_cta * warps;
   const int64_t r = (int64_t)blockIdx.x * (blockDim.x / threads_per_row) + row_in_cta;
@@ -197,7 +203,6 @@ dq_status by_format(int fmt, F f) {
   if (fmt == DQ_MXFP8) return f(Fmt<DQ_MXFP8>{});
   return DQ_ERR_INVALID_ARG;
 }
-inline dq_status launched() { return cudaGetLastError() == cudaSuccess ? DQ_OK : DQ_ERR_CUDA; }
 
 }  // namespace
 
@@ -213,10 +218,8 @@ dq_status quantize(cudaStream_t stream, const void* X, int x_dtype, int64_t rows
       const int threads = 256;
       const int64_t ctas = (warps + threads / 32 - 1) / (threads / 32);
       if (ctas > 0x7fffffff) return DQ_ERR_UNSUPPORTED;
-      quantize_kernel<T, FMT><<<(unsigned)ctas, threads, 0, stream>>>(
-          (const T*)X, rows, k, ldx, groups, chunks, codes, scales, (T*)values, ldv, rows_aligned(X, ldx, x_dtype),
-          rows_aligned(values, ldv, x_dtype));
-      return launched();
+      return launch(LaunchConfig(stream, ctas, threads), quantize_kernel<T, FMT>, (const T*)X, rows, k, ldx, groups, chunks, codes,
+                    scales, (T*)values, ldv, rows_aligned(X, ldx, x_dtype), rows_aligned(values, ldv, x_dtype));
     });
   });
 }
@@ -229,8 +232,8 @@ dq_status dequantize(cudaStream_t stream, int fmt, const uint8_t* codes, const u
       constexpr int FMT = decltype(f)::value;
       const int64_t ctas = (rows * ((k + 7) / 8) + 255) / 256;
       if (ctas > 0x7fffffff) return DQ_ERR_UNSUPPORTED;
-      dequantize_kernel<T, FMT><<<(unsigned)ctas, 256, 0, stream>>>(codes, scales, rows, k, (T*)Y, ldy, rows_aligned(Y, ldy, y_dtype));
-      return launched();
+      return launch(LaunchConfig(stream, ctas, 256), dequantize_kernel<T, FMT>, codes, scales, rows, k, (T*)Y, ldy,
+                    rows_aligned(Y, ldy, y_dtype));
     });
   });
 }
@@ -252,18 +255,16 @@ dq_status rmsnorm_quantize(cudaStream_t stream, const void* X, int dtype, int64_
     using T = decltype(t);
     return by_format(fmt, [&](auto f) {
       constexpr int FMT = decltype(f)::value;
-      auto launch = [&](auto g, auto kern) {
+      auto run = [&](auto g, auto kern) {
         using G = decltype(g);
-        kern<<<(unsigned)ctas, per_row * rows_per_cta, 0, stream>>>((const T*)X, rows, k, ldx, (const T*)residual, ldr,
-                                                                    (const G*)gamma, eps, codes, scales, (T*)sum, lds,
-                                                                    (T*)values, ldv, per_row, vec, g_vec);
-        return launched();
+        return launch(LaunchConfig(stream, ctas, per_row * rows_per_cta), kern, (const T*)X, rows, k, ldx, (const T*)residual, ldr,
+                      (const G*)gamma, eps, codes, scales, (T*)sum, lds, (T*)values, ldv, per_row, vec, g_vec);
       };
       auto with_gamma = [&](auto g) {
         using G = decltype(g);
-        if (V == 1) return launch(g, rmsnorm_kernel<T, G, FMT, 1>);
-        if (V == 2) return launch(g, rmsnorm_kernel<T, G, FMT, 2>);
-        return launch(g, rmsnorm_kernel<T, G, FMT, 4>);
+        if (V == 1) return run(g, rmsnorm_kernel<T, G, FMT, 1>);
+        if (V == 2) return run(g, rmsnorm_kernel<T, G, FMT, 2>);
+        return run(g, rmsnorm_kernel<T, G, FMT, 4>);
       };
       if (gamma && gamma_dtype == DQ_FP32) return with_gamma(float{});
       return with_gamma(T{});
