@@ -23,7 +23,7 @@ struct Params {
   int stages;              // pipeline steps of the whole reduction
   int splits;              // CTAs of a cluster that share a tile's reduction
   int weights_first;       // the kernel before this one writes no weights: the first may be read before its end
-  const void* x; int64_t ldx; int64_t k; int x_vec;   // FUSED: activations
+  const void* x; int64_t ldx; int64_t k; int x_vec;   // FUSED: activations; every row in whole 16-byte pieces
   int* d_status;
 };
 
@@ -148,29 +148,32 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, uint32_t rank) {
 // Rows [0, m) x values [c0, c0 + 8 groups) of X as a CTA's resident operand: codes of step i at codes + i X_BYTES in the K-major
 // 128-byte-swizzled order of the MMA's operands, its scale tiles at scales + i SF_BYTES.
 template <int BN, bool A8, typename T>
-__device__ __forceinline__ void quantize_resident(const Params& p, uint8_t* codes, uint8_t* scales, int64_t c0, int groups, int t, int threads) {
+__device__ __forceinline__ void quantize_resident(const Params& p, uint8_t* codes, uint8_t* scales, int c0, int groups, int t, int threads) {
   using L = ClusterSmem<BN, A8, true>;
   constexpr int FMT = A8 ? DQ_MXFP8 : DQ_MXFP4, BYTES = Codes8<FMT>::BYTES, PER_STEP = 128 / BYTES;
   const T* X = reinterpret_cast<const T*>(p.x);
   const int total = (int)p.m * groups;                       // a multiple of 16: the lanes of a block stay together
   constexpr int AT_ONCE = 4;
   for (int i0 = t; i0 < (total + 31) / 32 * 32; i0 += AT_ONCE * threads) {
-    float v[AT_ONCE][8];
+    Vec8<T> v[AT_ONCE];
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
       const int i = i0 + u * threads;
-      if (i < total) load8(X + (int64_t)(i / groups) * p.ldx, c0 + (int64_t)(i % groups) * 8, p.k, p.x_vec, v[u]);
+      v[u].clear();
+      if (i < total) {
+        const T* row = X + (int64_t)(i / groups) * p.ldx;
+        const int c = c0 + i % groups * 8;
+        if (!p.x_vec) load_each(v[u], row, c, (int)p.k);
+        else if (c < p.k) v[u].load(row + c);
+      }
     }
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
       const int i = i0 + u * threads;
       if (i - (t & 31) >= total) break;                      // (whole warps)
-      if (i >= total) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
-      }
+      const uint32_t s = scale_code<FMT>(block_exponent(v[u].exponent()));
       Codes8<FMT> q;
-      const uint32_t s = encode_block<FMT>(v[u], q);
+      q.encode(v[u], s);
       if (i < total) {
         const int row = i / groups, g = i % groups, step = g / PER_STEP, byte = g % PER_STEP * BYTES;
         q.store(codes + step * L::X_BYTES + row * 128 + ((((byte >> 4) ^ row) & 7) << 4) + (byte & 15));
@@ -282,8 +285,8 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   } else {
     if (FUSED) {
       wait_for_previous();
-      const int64_t values = A8 ? 128 : 256;                 // of a step
-      quantize_resident<BN, A8, T>(p, smem + (res - base), smem + (res_sf - base), k0 * values, kn * (int)(values / 8),
+      const int values = A8 ? 128 : 256;                     // of a step
+      quantize_resident<BN, A8, T>(p, smem + (res - base), smem + (res_sf - base), k0 * values, kn * (values / 8),
                                    (int)threadIdx.x - 64, L::THREADS - 64);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
@@ -711,7 +714,7 @@ dq_status linear(cudaStream_t stream, const void* X, int x_dtype, int64_t m, int
   Operands o{a_fmt, workspace, scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy};
   if (m <= 16) {
     o.x = X; o.ldx = ldx;
-    o.x_vec = ((uintptr_t)X & 15) == 0 && ldx * (x_dtype == DQ_FP32 ? 4 : 2) % 16 == 0;
+    o.x_vec = whole_pieces(X, ldx, k, x_dtype);
     const dq_status st = a_fmt == DQ_MXFP4 ? fused<false>(stream, dev, o, x_dtype) : fused<true>(stream, dev, o, x_dtype);
     if (st != DQ_ERR_UNSUPPORTED) return st;                 // (too long a reduction for its tokens to stay in shared memory)
   }

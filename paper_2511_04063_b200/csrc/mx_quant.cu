@@ -1,6 +1,8 @@
 // Microscaled quantisation: activations or weights to codes and scales (dq_mx_quantize), back to values
 // (dq_mx_dequantize), and the root-mean-square norm with the residual's addition in front of it
 // (dq_rmsnorm_quantize).  All three are bound by HBM: one read and one write of everything.
+#include <type_traits>
+
 #include "mx_common.cuh"
 
 namespace dq {
@@ -32,54 +34,89 @@ dq_status current_device(Device& out) {
 
 namespace {
 
-inline int type_bytes(int dtype) { return dtype == DQ_FP32 ? 4 : 2; }
-// Whether every row of a matrix starts on a 16-byte boundary.
-inline bool rows_aligned(const void* p, int64_t ld, int dtype) {
-  return ((uintptr_t)p & 15) == 0 && (ld * type_bytes(dtype)) % 16 == 0;
-}
-
-// One warp: rows {i, i + 32, i + 64, i + 96} of a row tile x 256 columns, 8 values of each row per lane.  The four rows
-// are the ones whose scales are neighbours, so a k tile's 16 scale bytes leave in one piece, and their four independent
-// 16-byte loads per lane are what keeps HBM busy.  Every lane has read its values before it writes any, and reads no
-// other lane's: the values may go back to where X lies.
-constexpr int Q_COLS = 256;
-template <typename T, int FMT>
-__global__ void __launch_bounds__(256) quantize_kernel(const T* X, int64_t rows, int64_t k, int64_t ldx, int row_groups,
-                                                       int64_t col_chunks, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                                                       T* values, int64_t ldv, int x_vec, int v_vec) {
-  wait_for_previous();
-  allow_next();
-  const int lane = threadIdx.x & 31;
-  const int64_t w = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  const int64_t ktiles = k_tiles(k);
-  const int64_t chunk = w % col_chunks, g = w / col_chunks;
-  const int64_t i = g % row_groups, tile = g / row_groups;
-  if (tile * ROW_TILE >= rows) return;                        // (whole warps)
-  const int64_t c = chunk * Q_COLS + lane * 8;
-  const bool in = c < ktiles * KTILE;
-  float v[4][8];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int64_t r = tile * ROW_TILE + 32 * j + i;
-    if (r < rows) load8(X + r * ldx, c, k, x_vec, v[j]);
-    else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[j][e] = 0.f;
+// A warp takes 256 columns of a row at a time, eight consecutive ones a lane, four lanes a block of 32.  WHOLE: rows come in
+// 16-byte pieces, eight values are one or two loads, and a lane's eight columns exist all or not at all.  Otherwise the warp
+// reads and writes 32 neighbouring values at a time and turns them in shared memory (1 KB a warp and row): one by one
+// from each lane's own eight columns every load would touch 32 different sectors (MEASURED).
+constexpr int PIECE = 256;
+template <typename T, bool WHOLE>
+struct Piece {
+  static __device__ __forceinline__ void load(Vec8<T>& v, const T* row, int c0, int k, int lane, T*) {
+    if (WHOLE) {
+      v.clear();
+      if (c0 + lane * 8 < k) v.load(row + c0 + lane * 8);
     }
   }
+  static __device__ __forceinline__ void store(const Vec8<T>& v, T* row, int c0, int k, int lane, T*) {
+    if (c0 + lane * 8 < k) v.store(row + c0 + lane * 8);
+  }
+};
+template <typename T>
+struct Piece<T, false> {
+  static __device__ __forceinline__ void load(Vec8<T>& v, const T* row, int c0, int k, int lane, T* turn) {
+    T x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = c0 + i * 32 + lane < k ? row[c0 + i * 32 + lane] : from_f32<T>(0.f);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) turn[i * 32 + lane] = x[i];
+    __syncwarp();
+    v.load(turn + lane * 8);
+  }
+  static __device__ __forceinline__ void store(const Vec8<T>& v, T* row, int c0, int k, int lane, T* turn) {
+    __syncwarp();
+    v.store(turn + lane * 8);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c0 + i * 32 + lane < k) row[c0 + i * 32 + lane] = turn[i * 32 + lane];
+  }
+};
+
+// One warp: rows {i, i + 32, i + 64, i + 96} of a row tile x 256 columns.  The four rows are the ones whose scales are
+// neighbours, so a k tile's 16 scale bytes leave in one piece, and their four independent loads per lane are what keeps HBM
+// busy.  Every lane has read its values before it writes any, and reads no other lane's (!WHOLE: its warp has, and no other
+// warp's): the values may go back to where X lies.  A CTA's eight warps lie side by side, 2^wide of them along the columns.
+constexpr int Q_WARPS = 8;
+template <typename T, int FMT, bool WHOLE>
+__global__ void __launch_bounds__(32 * Q_WARPS)
+quantize_kernel(const T* X, int64_t rows, int k, int64_t ldx, int wide, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                T* values, int64_t ldv) {
+  __shared__ __align__(16) T turn[WHOLE ? 1 : Q_WARPS][WHOLE ? 8 : PIECE];
+  wait_for_previous();
+  allow_next();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int ktiles = (k + KTILE - 1) / KTILE;
+  const int c0 = (((int)blockIdx.y << wide) + (warp & ((1 << wide) - 1))) * PIECE, c = c0 + lane * 8;
+  const int64_t g = (int64_t)blockIdx.x * (Q_WARPS >> wide) + (warp >> wide);
+  const int64_t tile = rows < 32 ? 0 : g >> 5;
+  const int64_t i = rows < 32 ? g : g & 31, r0 = tile * ROW_TILE + i;
+  if (c0 >= ktiles * KTILE || r0 >= rows) return;             // (whole warps)
+  const bool in = c < ktiles * KTILE;
+  T* stage = turn[WHOLE ? 0 : warp];
+  Vec8<T> v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (r0 + 32 * j < rows) Piece<T, WHOLE>::load(v[j], X + (r0 + 32 * j) * ldx, c0, k, lane, stage);
+    else v[j].clear();
+  }
+  const uint32_t e01 = block_exponent(v[0].exponent() | v[1].exponent() << 16);
+  const uint32_t e23 = block_exponent(v[2].exponent() | v[3].exponent() << 16);
+  const uint32_t e[4] = {e01 & 0xffffu, e01 >> 16, e23 & 0xffffu, e23 >> 16};
+  const int64_t pitch = row_bytes(FMT, k);
+  uint8_t* to = codes + r0 * pitch + c / 8 * Codes8<FMT>::BYTES;
   uint32_t mine = 0;                                          // scale of row (lane % 4) of the four
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const int64_t r = tile * ROW_TILE + 32 * j + i;
-    Codes8<FMT> q;
-    const uint32_t s = encode_block<FMT>(v[j], q);
+    const uint32_t s = scale_code<FMT>(e[j]);
     if ((lane & 3) == j) mine = s;
-    if (r < rows && in) {
-      q.store(codes + r * row_bytes(FMT, k) + c / 8 * Codes8<FMT>::BYTES);
+    if (r0 + 32 * j < rows) {
+      Codes8<FMT> q;
+      q.encode(v[j], s);
+      if (in) q.store(to + 32 * j * pitch);
       if (values) {
-        float y[8];
-        q.decode(scale_value(s), y);
-        store8(values + r * ldv, c, k, v_vec, y);
+        q.decode(s, v[j]);
+        Piece<T, WHOLE>::store(v[j], values + (r0 + 32 * j) * ldv, c0, k, lane, stage);
       }
     }
   }
@@ -91,101 +128,123 @@ __global__ void __launch_bounds__(256) quantize_kernel(const T* X, int64_t rows,
     *reinterpret_cast<uint32_t*>(scales + (tile * ktiles + c / KTILE) * TILE_BYTES + i * 16 + (lane & 3) * 4) = mine;
 }
 
-template <typename T, int FMT>
-__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                         int64_t rows, int64_t k, T* __restrict__ Y, int64_t ldy, int vec) {
+// A warp per 256 columns of a row.
+template <typename T, int FMT, bool WHOLE>
+__global__ void __launch_bounds__(32 * Q_WARPS)
+dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int k, int wide, T* __restrict__ Y,
+                  int64_t ldy) {
+  __shared__ __align__(16) T turn[WHOLE ? 1 : Q_WARPS][WHOLE ? 8 : PIECE];
   wait_for_previous();
   allow_next();
-  const int64_t groups = (k + 7) / 8;
-  const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const int64_t r = at / groups, c = at % groups * 8;
-  if (r >= rows) return;
-  Codes8<FMT> q;
-  q.load(codes + r * row_bytes(FMT, k) + c / 8 * Codes8<FMT>::BYTES);
-  float v[8];
-  q.decode(scale_value(scales[scale_offset(r, c / BLOCK, k_tiles(k))]), v);
-  store8(Y + r * ldy, c, k, vec, v);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c0 = (((int)blockIdx.y << wide) + (warp & ((1 << wide) - 1))) * PIECE, c = c0 + lane * 8;
+  const int64_t r = (int64_t)blockIdx.x * (Q_WARPS >> wide) + (warp >> wide);
+  if (c0 >= k || r >= rows) return;                           // (whole warps)
+  Vec8<T> v;
+  v.clear();
+  if (c < k) {
+    Codes8<FMT> q;
+    q.load(codes + r * row_bytes(FMT, k) + c / 8 * Codes8<FMT>::BYTES);
+    q.decode(scales[scale_offset(r, c / BLOCK, k_tiles(k))], v);
+  }
+  Piece<T, WHOLE>::store(v, Y + r * ldy, c0, k, lane, turn[WHOLE ? 0 : warp]);
 }
 
 // ------------------------------------------------------------------------------------------------ norm
-// A row belongs to a group of `threads_per_row` threads (whole warps); V vectors of 8 values a thread stay in registers
-// between the sum of squares and the scaling, so x and the residual are read once.
-template <typename T, typename G, int FMT, int V>
-__global__ void rmsnorm_kernel(const T* X, int64_t rows, int64_t k, int64_t ldx, const T* residual, int64_t ldr,
-                               const G* __restrict__ gamma, float eps, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                               T* sum, int64_t lds, T* values, int64_t ldv, int threads_per_row, int vec, int g_vec) {
+// A row belongs to `warps` warps, each with V pieces of 256 columns that stay in registers between the sum of squares and the
+// scaling, so x and the residual are read once.  One warp a row: eight rows a CTA, no barrier; else one row a CTA.
+template <typename T, typename G, int FMT, int V, bool WHOLE>
+__global__ void __launch_bounds__(V == 1 ? 1024 : 512)
+rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, int64_t ldr, const G* gamma, float eps,
+                               uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, T* sum, int64_t lds, T* values, int64_t ldv,
+                               int warps) {
+  extern __shared__ __align__(16) uint8_t turn[];             // !WHOLE: 1 KB a warp
   __shared__ float part[32];
   wait_for_previous();
   allow_next();
-  const int row_in_cta = threadIdx.x / threads_per_row, t = threadIdx.x % threads_per_row;
-  const int lane = threadIdx.x & 31, warps = threads_per_row >> 5, warp0 = row_in_cta * warps;
-  const int64_t r = (int64_t)blockIdx.x * (blockDim.x / threads_per_row) + row_in_cta;
-  const bool live = r < rows;
-  float h[V][8];
-  float ss = 0.f;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int64_t r = warps == 1 ? (int64_t)blockIdx.x * (blockDim.x >> 5) + w : blockIdx.x;
+  if (r >= rows) return;                                      // (whole warps; with more than one a row, whole CTAs)
+  const int first = warps == 1 ? 0 : w;
+  T* stage = reinterpret_cast<T*>(turn + (WHOLE ? 0 : w * 1024));
+  G* g_stage = reinterpret_cast<G*>(stage);
+  auto column = [&](int u) { return (u * warps + first) * PIECE; };
+  float2 h[V][4];
+  float2 ss = make_float2(0.f, 0.f);
+  {
+    Vec8<T> x[V];
 #pragma unroll
-  for (int u = 0; u < V; ++u) {
-    const int64_t c = ((int64_t)u * threads_per_row + t) * 8;
-    if (live) load8(X + r * ldx, c, k, vec, h[u]);
-    else {
+    for (int u = 0; u < V; ++u) Piece<T, WHOLE>::load(x[u], X + r * ldx, column(u), k, lane, stage);
+    if (residual) {
+      Vec8<T> b[V];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[u][e] = 0.f;
-    }
-    if (residual && live) {
-      float b[8];
-      load8(residual + r * ldr, c, k, vec, b);
+      for (int u = 0; u < V; ++u) Piece<T, WHOLE>::load(b[u], residual + r * ldr, column(u), k, lane, stage);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[u][e] += b[e];
-    }
-  }
+      for (int u = 0; u < V; ++u)
 #pragma unroll
-  for (int u = 0; u < V; ++u) {
-    const int64_t c = ((int64_t)u * threads_per_row + t) * 8;
-    if (sum && live) store8(sum + r * lds, c, k, vec, h[u]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ss += h[u][e] * h[u][e];
-  }
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-  if (warps > 1) {
-    if (lane == 0) part[warp0 + (t >> 5)] = ss;
-    __syncthreads();
-    ss = 0.f;
-    for (int i = 0; i < warps; ++i) ss += part[warp0 + i];
-  }
-  const float rstd = rsqrtf(ss / (float)k + eps);
-  const int64_t ktiles = k_tiles(k);
-#pragma unroll
-  for (int u = 0; u < V; ++u) {
-    const int64_t c = ((int64_t)u * threads_per_row + t) * 8;
-    float y[8];
-    if (gamma) {
-      load8(gamma, c, k, g_vec, y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = h[u][e] * rstd * y[e];
+        for (int i = 0; i < 4; ++i) h[u][i] = add2(x[u].pair(i), b[u].pair(i));
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = h[u][e] * rstd;
-    }
-    if (c >= k) {      // padding: not a value, whatever the row's statistics are
+      for (int u = 0; u < V; ++u)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = 0.f;
+        for (int i = 0; i < 4; ++i) h[u][i] = x[u].pair(i);
     }
+  }
+#pragma unroll
+  for (int u = 0; u < V; ++u) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ss = add2(ss, mul2(h[u][i], h[u][i]));
+    if (sum) {
+      Vec8<T> s;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s.set_pair(i, h[u][i]);
+      Piece<T, WHOLE>::store(s, sum + r * lds, column(u), k, lane, stage);
+    }
+  }
+  float all = ss.x + ss.y;
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+  if (warps > 1) {
+    if (lane == 0) part[w] = all;
+    __syncthreads();
+    all = lane < warps ? part[lane] : 0.f;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+  }
+  const float rstd = rsqrtf(all / (float)k + eps);
+  const int ktiles = (k + KTILE - 1) / KTILE;
+  uint8_t* to = codes + r * row_bytes(FMT, k);
+#pragma unroll
+  for (int u = 0; u < V; ++u) {
+    const int c0 = column(u), c = c0 + lane * 8;
+    if (c0 >= ktiles * KTILE) break;                          // (whole warps)
+    Vec8<float> y;
+    Vec8<G> g;
+    if (gamma) Piece<G, WHOLE>::load(g, gamma, c0, k, lane, g_stage);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = mul2(h[u][i], make_float2(rstd, rstd));
+      y.set_pair(i, gamma ? mul2(f, g.pair(i)) : f);
+    }
+    if (c >= k) y.clear();       // padding: not a value, whatever the row's statistics are
+    else if (!WHOLE && c + 8 > k) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (c + e >= k) y.v[e] = 0.f;
+    }
+    uint32_t s = scale_code<FMT>(block_exponent(y.exponent()));
     Codes8<FMT> q;
-    uint32_t s = encode_block<FMT>(y, q);
-    if (live && c < ktiles * KTILE) {
-      q.store(codes + r * row_bytes(FMT, k) + c / 8 * Codes8<FMT>::BYTES);
-      if (values) {
-        float d[8];
-        q.decode(scale_value(s), d);
-        store8(values + r * ldv, c, k, vec, d);
-      }
+    q.encode(y, s);
+    const bool in = c < ktiles * KTILE;
+    if (in) q.store(to + c / 8 * Codes8<FMT>::BYTES);
+    if (values) {
+      Vec8<T> d;
+      q.decode(s, d);
+      Piece<T, WHOLE>::store(d, values + r * ldv, c0, k, lane, stage);
     }
     s <<= 8 * ((lane >> 2) & 3);
     s |= __shfl_xor_sync(0xffffffffu, s, 4);
     s |= __shfl_xor_sync(0xffffffffu, s, 8);
-    if (live && c < ktiles * KTILE && (lane & 15) == 0)
-      *reinterpret_cast<uint32_t*>(scales + scale_offset(r, c / BLOCK, ktiles)) = s;
+    if (in && (lane & 15) == 0) *reinterpret_cast<uint32_t*>(scales + scale_offset(r, c / BLOCK, ktiles)) = s;
   }
 }
 
@@ -206,34 +265,50 @@ dq_status by_format(int fmt, F f) {
 
 }  // namespace
 
+namespace {
+// Warps of a CTA that lie along the columns: as many as there are pieces, up to all (as a power of two).
+inline int columns_wide(int64_t pieces) { return pieces >= 8 ? 3 : pieces >= 4 ? 2 : pieces >= 2 ? 1 : 0; }
+inline dq_status grid(LaunchConfig& c, int64_t pieces, int64_t row_groups, int wide) {
+  const int64_t x = (row_groups + (Q_WARPS >> wide) - 1) / (Q_WARPS >> wide), y = (pieces + (1 << wide) - 1) >> wide;
+  if (x > 0x7fffffff || y > 65535) return DQ_ERR_UNSUPPORTED;
+  c.cfg.gridDim = dim3((unsigned)x, (unsigned)y);
+  return DQ_OK;
+}
+template <typename F>
+dq_status by_flag(bool flag, F f) { return flag ? f(std::true_type{}) : f(std::false_type{}); }
+}  // namespace
+
 dq_status quantize(cudaStream_t stream, const void* X, int x_dtype, int64_t rows, int64_t k, int64_t ldx, int fmt,
                    uint8_t* codes, uint8_t* scales, void* values, int64_t ldv) {
+  const bool whole = whole_pieces(X, ldx, k, x_dtype) && (!values || whole_pieces(values, ldv, k, x_dtype));
+  const int64_t pieces = (k_tiles(k) * KTILE + PIECE - 1) / PIECE;
+  const int64_t groups = rows < 32 ? rows : (rows + ROW_TILE - 1) / ROW_TILE * 32;
+  const int wide = columns_wide(pieces);
+  LaunchConfig c(stream, 1, 32 * Q_WARPS);
+  DQ_CHECK(grid(c, pieces, groups, wide));
   return by_type(x_dtype, [&](auto t) {
     using T = decltype(t);
     return by_format(fmt, [&](auto f) {
-      constexpr int FMT = decltype(f)::value;
-      const int64_t chunks = (k_tiles(k) * KTILE + Q_COLS - 1) / Q_COLS;
-      const int groups = (int)(rows < 32 ? rows : 32);
-      const int64_t warps = (rows + ROW_TILE - 1) / ROW_TILE * groups * chunks;
-      const int threads = 256;
-      const int64_t ctas = (warps + threads / 32 - 1) / (threads / 32);
-      if (ctas > 0x7fffffff) return DQ_ERR_UNSUPPORTED;
-      return launch(LaunchConfig(stream, ctas, threads), quantize_kernel<T, FMT>, (const T*)X, rows, k, ldx, groups, chunks, codes,
-                    scales, (T*)values, ldv, rows_aligned(X, ldx, x_dtype), rows_aligned(values, ldv, x_dtype));
+      return by_flag(whole, [&](auto v) {
+        return launch(c, quantize_kernel<T, decltype(f)::value, decltype(v)::value>, (const T*)X, rows, (int)k, ldx, wide, codes,
+                      scales, (T*)values, ldv);
+      });
     });
   });
 }
 
 dq_status dequantize(cudaStream_t stream, int fmt, const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t k,
                      void* Y, int y_dtype, int64_t ldy) {
+  const int64_t pieces = (k + PIECE - 1) / PIECE;
+  const int wide = columns_wide(pieces);
+  LaunchConfig c(stream, 1, 32 * Q_WARPS);
+  DQ_CHECK(grid(c, pieces, rows, wide));
   return by_type(y_dtype, [&](auto t) {
     using T = decltype(t);
     return by_format(fmt, [&](auto f) {
-      constexpr int FMT = decltype(f)::value;
-      const int64_t ctas = (rows * ((k + 7) / 8) + 255) / 256;
-      if (ctas > 0x7fffffff) return DQ_ERR_UNSUPPORTED;
-      return launch(LaunchConfig(stream, ctas, 256), dequantize_kernel<T, FMT>, codes, scales, rows, k, (T*)Y, ldy,
-                    rows_aligned(Y, ldy, y_dtype));
+      return by_flag(whole_pieces(Y, ldy, k, y_dtype), [&](auto v) {
+        return launch(c, dequantize_kernel<T, decltype(f)::value, decltype(v)::value>, codes, scales, rows, (int)k, wide, (T*)Y, ldy);
+      });
     });
   });
 }
@@ -241,33 +316,40 @@ dq_status dequantize(cudaStream_t stream, int fmt, const uint8_t* codes, const u
 dq_status rmsnorm_quantize(cudaStream_t stream, const void* X, int dtype, int64_t rows, int64_t k, int64_t ldx,
                            const void* residual, int64_t ldr, const void* gamma, int gamma_dtype, float eps, int fmt,
                            uint8_t* codes, uint8_t* scales, void* sum, int64_t lds, void* values, int64_t ldv) {
-  const bool vec = rows_aligned(X, ldx, dtype) && (!residual || rows_aligned(residual, ldr, dtype)) &&
-                   (!sum || rows_aligned(sum, lds, dtype)) && (!values || rows_aligned(values, ldv, dtype));
-  const bool g_vec = ((uintptr_t)gamma & 15) == 0;
-  const int64_t groups = k_tiles(k) * (KTILE / 8);
-  if (groups > 4 * 1024) return DQ_ERR_UNSUPPORTED;           // 32768 columns: a row has to stay in one CTA's registers
-  const int V = groups <= 1024 ? (groups <= 64 ? 1 : 2) : 4;
-  const int per_row = (int)((groups + 32 * V - 1) / (32 * V)) * 32;
-  const int rows_per_cta = per_row >= 128 ? 1 : 128 / per_row;
-  const int64_t ctas = (rows + rows_per_cta - 1) / rows_per_cta;
-  if (ctas > 0x7fffffff) return DQ_ERR_UNSUPPORTED;
+  const bool whole = whole_pieces(X, ldx, k, dtype) && (!residual || whole_pieces(residual, ldr, k, dtype)) &&
+                     (!sum || whole_pieces(sum, lds, k, dtype)) && (!values || whole_pieces(values, ldv, k, dtype)) &&
+                     (!gamma || whole_pieces(gamma, 0, k, gamma_dtype));
+  const int pieces = (int)((k_tiles(k) * KTILE + PIECE - 1) / PIECE);
+  if (pieces > 4 * 32) return DQ_ERR_UNSUPPORTED;             // 32768 columns: a row has to stay in one CTA's registers
+  Device dev;
+  DQ_CHECK(current_device(dev));
+  // Few rows: as many warps a row as there are pieces; else four pieces a warp (eight where 16 warps would not be enough).
+  const int V = pieces == 1 || (rows <= 2 * dev.sms && pieces <= 32) ? 1 : pieces == 2 ? 2 : pieces <= 64 ? 4 : 8;
+  const int warps = (pieces + V - 1) / V;
+  const int threads = warps == 1 ? 256 : warps * 32;
+  const int64_t ctas = warps == 1 ? (rows + 7) / 8 : rows;
+  LaunchConfig c(stream, ctas, threads, whole ? 0 : threads * 32);
   return by_type(dtype, [&](auto t) {
     using T = decltype(t);
     return by_format(fmt, [&](auto f) {
       constexpr int FMT = decltype(f)::value;
-      auto run = [&](auto g, auto kern) {
-        using G = decltype(g);
-        return launch(LaunchConfig(stream, ctas, per_row * rows_per_cta), kern, (const T*)X, rows, k, ldx, (const T*)residual, ldr,
-                      (const G*)gamma, eps, codes, scales, (T*)sum, lds, (T*)values, ldv, per_row, vec, g_vec);
-      };
-      auto with_gamma = [&](auto g) {
-        using G = decltype(g);
-        if (V == 1) return run(g, rmsnorm_kernel<T, G, FMT, 1>);
-        if (V == 2) return run(g, rmsnorm_kernel<T, G, FMT, 2>);
-        return run(g, rmsnorm_kernel<T, G, FMT, 4>);
-      };
-      if (gamma && gamma_dtype == DQ_FP32) return with_gamma(float{});
-      return with_gamma(T{});
+      return by_flag(whole, [&](auto wh) {
+        constexpr bool WHOLE = decltype(wh)::value;
+        auto run = [&](auto g, auto kern) {
+          using G = decltype(g);
+          return launch(c, kern, (const T*)X, rows, (int)k, ldx, (const T*)residual, ldr, (const G*)gamma, eps, codes, scales,
+                        (T*)sum, lds, (T*)values, ldv, warps);
+        };
+        auto with_gamma = [&](auto g) {
+          using G = decltype(g);
+          if (V == 1) return run(g, rmsnorm_kernel<T, G, FMT, 1, WHOLE>);
+          if (V == 2) return run(g, rmsnorm_kernel<T, G, FMT, 2, WHOLE>);
+          if (V == 4) return run(g, rmsnorm_kernel<T, G, FMT, 4, WHOLE>);
+          return run(g, rmsnorm_kernel<T, G, FMT, 8, WHOLE>);
+        };
+        if (gamma && gamma_dtype == DQ_FP32) return with_gamma(float{});
+        return with_gamma(T{});
+      });
     });
   });
 }
