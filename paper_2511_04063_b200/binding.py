@@ -340,44 +340,58 @@ def dq_eval_rotation(X, R, tau: float, bits: int, stream=None):
 # Microscaled operators.  Their wrappers check what the C entry cannot see (devices, types, sizes of buffers); a
 # wrong tensor raises ValueError, a refusal of the library DartQuantError.
 # ---------------------------------------------------------------------------
-_DTYPES = None
+_MX_TYPES = {}                       # torch type -> DQ_*, filled by the first call
+_mx_device = _mx_raw_stream = None   # torch's own lookups of the current device and stream
 
 
-def _mx_call(name: str, stream, first, *args):
-    """lib.name(*args, stream) on the current device, where `first` must lie."""
+def _mx_load():
+    """The library; on the first call also what the wrappers need of torch."""
+    global _mx_device, _mx_raw_stream
     import torch
-    index = first.get_device()
-    if index != torch.cuda.current_device():
+    _MX_TYPES.update({torch.float32: DQ_FP32, torch.bfloat16: DQ_BF16, torch.float16: DQ_FP16})
+    torch.cuda.current_device()
+    _mx_device, _mx_raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    return load_library()
+
+
+def _mx_call(fn, name: str, index: int, stream, *args):
+    """fn(*args, stream) on the current device, which has to be `index`, the tensors'."""
+    if index != _mx_device():
         raise ValueError("%s: the tensors have to be on the current CUDA device" % name)
-    s = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
-    status = getattr(_lib or load_library(), name)(*args, s)
+    status = fn(*args, _mx_raw_stream(index) if stream is None else stream.cuda_stream)
     if status != DQ_OK:
         raise DartQuantError(status, name)
 
 
-def _mx_values(t, name: str, rows=None, k=None, like=None):
-    """(address, type, row stride) of a matrix of values: CUDA, 2-D, unit stride along a row."""
-    global _DTYPES
-    if _DTYPES is None:
-        import torch
-        _DTYPES = {torch.float32: DQ_FP32, torch.bfloat16: DQ_BF16, torch.float16: DQ_FP16}
-    dtype = _DTYPES.get(t.dtype)
+def _mx_matrix(t, name: str):
+    """(address, type, row stride, rows, width, device) of a matrix of values with contiguous rows."""
     shape = t.shape
-    if dtype is None or len(shape) != 2 or not t.is_cuda:
+    dtype = _MX_TYPES.get(t.dtype)
+    index = t.get_device()
+    if dtype is None or index < 0 or len(shape) != 2:
         raise ValueError("%s: a 2-D CUDA tensor of float32, bfloat16 or float16 is needed" % name)
-    if (rows is not None and shape[0] != rows) or (k is not None and shape[1] != k):
-        raise ValueError("%s: shape %s, and [%s, %s] is needed" % (name, tuple(shape), rows, k))
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        raise ValueError("%s: type or device differs from the input's" % name)
+    rows, k = shape
     ld, step = t.stride()
-    if (step != 1 and shape[1] > 1) or (ld < shape[1] and shape[0] > 1):
-        raise ValueError("%s: rows have to be contiguous and must not overlap" % name)
-    return t.data_ptr(), dtype, max(ld, shape[1])
+    if step != 1 or ld < k:
+        if (step != 1 and k > 1) or (ld < k and rows > 1):
+            raise ValueError("%s: rows have to be contiguous and must not overlap" % name)
+        ld = k
+    return t.data_ptr(), dtype, ld, rows, k, index
 
 
-def _mx_bytes(t, name: str, least: int, like):
-    """Address of a contiguous buffer of at least `least` bytes, on the device of `like`."""
-    if not t.is_contiguous() or t.device != like.device or t.numel() * t.element_size() < least:
+def _mx_like(t, name: str, x):
+    """(address, row stride) of a matrix that has to be of the shape, type and device of x (its _mx_matrix); None: (0, 0)."""
+    if t is None:
+        return 0, 0
+    ptr, dtype, ld, rows, k, index = _mx_matrix(t, name)
+    if dtype != x[1] or rows != x[3] or k != x[4] or index != x[5]:
+        raise ValueError("%s: shape, type or device differs from the input's" % name)
+    return ptr, ld
+
+
+def _mx_bytes(t, name: str, least: int, index: int):
+    """Address of a contiguous buffer of at least `least` bytes on device `index`."""
+    if t.nbytes < least or t.get_device() != index or not t.is_contiguous():
         raise ValueError("%s: a contiguous buffer of at least %d bytes on the inputs' device is needed" % (name, least))
     return t.data_ptr()
 
@@ -413,63 +427,66 @@ def dq_mx_empty(rows: int, k: int, fmt: int, device="cuda"):
 def dq_mx_quantize(X, fmt: int, codes, scales, values=None, stream=None):
     """Codes and scales of X ([rows, k]; float32, bfloat16 or float16).  values (same type and shape; may be X): what
     the codes stand for."""
-    x, dtype, ldx = _mx_values(X, "X")
-    rows, k = X.shape
+    lib = _lib if _mx_device else _mx_load()
+    x = ptr, dtype, ld, rows, k, index = _mx_matrix(X, "X")
     n_codes, n_scales = _mx_held(fmt, rows, k)
-    v, _, ldv = _mx_values(values, "values", rows, k, X) if values is not None else (0, 0, 0)
-    _mx_call("dq_mx_quantize", stream, X, x, dtype, rows, k, ldx, fmt, _mx_bytes(codes, "codes", n_codes, X),
-             _mx_bytes(scales, "scales", n_scales, X), v, ldv)
+    v, ldv = _mx_like(values, "values", x)
+    _mx_call(lib.dq_mx_quantize, "dq_mx_quantize", index, stream, ptr, dtype, rows, k, ld, fmt,
+             _mx_bytes(codes, "codes", n_codes, index), _mx_bytes(scales, "scales", n_scales, index), v, ldv)
 
 
 def dq_mx_dequantize(codes, scales, fmt: int, Y, stream=None):
     """Y ([rows, k]) = the values that codes and scales stand for."""
-    y, dtype, ldy = _mx_values(Y, "Y")
-    rows, k = Y.shape
+    lib = _lib if _mx_device else _mx_load()
+    ptr, dtype, ld, rows, k, index = _mx_matrix(Y, "Y")
     n_codes, n_scales = _mx_held(fmt, rows, k)
-    _mx_call("dq_mx_dequantize", stream, Y, fmt, _mx_bytes(codes, "codes", n_codes, Y), _mx_bytes(scales, "scales", n_scales, Y),
-             rows, k, y, dtype, ldy)
+    _mx_call(lib.dq_mx_dequantize, "dq_mx_dequantize", index, stream, fmt, _mx_bytes(codes, "codes", n_codes, index),
+             _mx_bytes(scales, "scales", n_scales, index), rows, k, ptr, dtype, ld)
 
 
 def dq_rmsnorm_quantize(X, gamma, eps: float, fmt: int, codes, scales, residual=None, sum_out=None, values=None, stream=None):
     """h = X + residual; codes and scales of h / sqrt(mean(h^2) + eps) * gamma.  gamma: [k] of X's type or float32, or None.
     sum_out (may be X or residual) receives h, values the quantised output's values; all [rows, k] of X's type."""
-    x, dtype, ldx = _mx_values(X, "X")
-    rows, k = X.shape
+    lib = _lib if _mx_device else _mx_load()
+    x = ptr, dtype, ld, rows, k, index = _mx_matrix(X, "X")
     n_codes, n_scales = _mx_held(fmt, rows, k)
-    r, _, ldr = _mx_values(residual, "residual", rows, k, X) if residual is not None else (0, 0, 0)
-    h, _, lds = _mx_values(sum_out, "sum_out", rows, k, X) if sum_out is not None else (0, 0, 0)
-    v, _, ldv = _mx_values(values, "values", rows, k, X) if values is not None else (0, 0, 0)
+    r, ldr = _mx_like(residual, "residual", x)
+    h, lds = _mx_like(sum_out, "sum_out", x)
+    v, ldv = _mx_like(values, "values", x)
     g, g_dtype = 0, dtype
     if gamma is not None:
-        g_dtype = _DTYPES.get(gamma.dtype)
-        if gamma.shape != (k,) or (g_dtype != dtype and g_dtype != DQ_FP32) or gamma.device != X.device or not gamma.is_contiguous():
-            raise ValueError("gamma: a contiguous [%d] tensor of X's type or float32 on X's device is needed" % k)
-        g = gamma.data_ptr()
-    _mx_call("dq_rmsnorm_quantize", stream, X, x, r, dtype, rows, k, ldx, ldr, g, g_dtype, eps, fmt,
-             _mx_bytes(codes, "codes", n_codes, X), _mx_bytes(scales, "scales", n_scales, X), h, lds, v, ldv)
+        g_dtype = _MX_TYPES.get(gamma.dtype)
+        if gamma.shape != (k,) or (g_dtype != dtype and g_dtype != DQ_FP32):
+            raise ValueError("gamma: a [%d] tensor of X's type or float32 is needed" % k)
+        g = _mx_bytes(gamma, "gamma", 0, index)
+    _mx_call(lib.dq_rmsnorm_quantize, "dq_rmsnorm_quantize", index, stream, ptr, r, dtype, rows, k, ld, ldr, g, g_dtype, eps, fmt,
+             _mx_bytes(codes, "codes", n_codes, index), _mx_bytes(scales, "scales", n_scales, index), h, lds, v, ldv)
 
 
 def dq_mx_matmul(a_codes, a_scales, a_fmt: int, w_codes, w_scales, k: int, Y, stream=None):
     """Y ([m, n]) = A W^T for m rows of activations (DQ_MXFP4 or DQ_MXFP8) and n rows of DQ_MXFP4 weights, k values each."""
-    y, dtype, ldy = _mx_values(Y, "Y")
-    m, n = Y.shape
+    lib = _lib if _mx_device else _mx_load()
+    ptr, dtype, ld, m, n, index = _mx_matrix(Y, "Y")
     a_n, a_s = _mx_held(a_fmt, m, k)
     w_n, w_s = _mx_held(DQ_MXFP4, n, k)
-    _mx_call("dq_mx_matmul", stream, Y, a_fmt, _mx_bytes(a_codes, "a_codes", a_n, Y), _mx_bytes(a_scales, "a_scales", a_s, Y), m,
-             _mx_bytes(w_codes, "w_codes", w_n, Y), _mx_bytes(w_scales, "w_scales", w_s, Y), n, k, y, dtype, ldy)
+    _mx_call(lib.dq_mx_matmul, "dq_mx_matmul", index, stream, a_fmt, _mx_bytes(a_codes, "a_codes", a_n, index),
+             _mx_bytes(a_scales, "a_scales", a_s, index), m, _mx_bytes(w_codes, "w_codes", w_n, index),
+             _mx_bytes(w_scales, "w_scales", w_s, index), n, k, ptr, dtype, ld)
 
 
 def dq_mx_linear(X, a_fmt: int, w_codes, w_scales, Y, workspace, stream=None):
     """Y ([m, n]) = quantised(X) W^T for activations X ([m, k]) and n rows of DQ_MXFP4 weights.  workspace: a buffer of
     dq_mx_linear_workspace(a_fmt, m, k) bytes."""
-    x, x_dtype, ldx = _mx_values(X, "X")
-    m, k = X.shape
-    y, y_dtype, ldy = _mx_values(Y, "Y", m)
-    n = Y.shape[1]
+    lib = _lib if _mx_device else _mx_load()
+    x, x_dtype, ldx, m, k, index = _mx_matrix(X, "X")
+    y, y_dtype, ldy, rows, n, y_index = _mx_matrix(Y, "Y")
+    if rows != m or y_index != index:
+        raise ValueError("Y: %d rows on X's device are needed" % m)
     w_n, w_s = _mx_held(DQ_MXFP4, n, k)
     a_n, a_s = _mx_held(a_fmt, m, k)
-    _mx_call("dq_mx_linear", stream, X, x, x_dtype, m, k, ldx, a_fmt, _mx_bytes(w_codes, "w_codes", w_n, X),
-             _mx_bytes(w_scales, "w_scales", w_s, X), n, y, y_dtype, ldy, _mx_bytes(workspace, "workspace", a_n + a_s, X))
+    _mx_call(lib.dq_mx_linear, "dq_mx_linear", index, stream, x, x_dtype, m, k, ldx, a_fmt,
+             _mx_bytes(w_codes, "w_codes", w_n, index), _mx_bytes(w_scales, "w_scales", w_s, index), n, y, y_dtype, ldy,
+             _mx_bytes(workspace, "workspace", a_n + a_s, index))
 
 
 def dq_mx_status(stream=None) -> int:
