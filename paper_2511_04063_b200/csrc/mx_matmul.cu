@@ -27,11 +27,9 @@ struct Params {
   int* d_status;
 };
 
-// The scales of a pipeline step lie in one of four slots of tensor memory; a slot is free once the MMAs of four steps before have
-// completed (with two slots the issuer waits for MMAs that have hardly begun).
-constexpr int SCALE_SLOTS = 4;
-
-// A pipeline step: 128 bytes of every row, as the MMAs read them: 256 4-bit values, or 128 8-bit ones.
+// A pipeline step: 128 bytes of every row, as the MMAs read them: 256 4-bit values, or 128 8-bit ones.  Every stage of shared
+// memory has its own columns of tensor memory for the scales of the step that it holds: whoever fills the stage has waited
+// for the MMAs that read both, so the issuer needs no wait of its own before it copies new scales there.
 template <bool A8> struct Step {
   static constexpr int KT = A8 ? 1 : 2;                    // scale tiles along k
   static constexpr int MMAS = 4;                           // MMA steps of 32 bytes
@@ -47,6 +45,13 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+// Whether a phase has completed, without waiting (the lanes of a warp agree on the answer).
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return __all_sync(0xffffffffu, ok != 0);
 }
 // Scales: 32 rows of 16 bytes, copied to the same 4 columns of all four 32-lane quarters of tensor memory.
 __device__ __forceinline__ uint64_t scale_desc(uint32_t smem_addr) {
@@ -125,7 +130,7 @@ struct ClusterSmem {
   static constexpr int FIXED = STAGES * STAGE_BYTES + 1024 + 256;
   static constexpr int RESIDENT = FUSED ? X_BYTES + SF_BYTES : 0;   // and for each step of a CTA's reduction
   static constexpr int SCALE_COLS = 4 * KT * 2;
-  static constexpr int NEED = BN + SCALE_SLOTS * SCALE_COLS;
+  static constexpr int NEED = BN + STAGES * SCALE_COLS;
   static constexpr int TMEM = NEED <= 64 ? 64 : (NEED <= 128 ? 128 : (NEED <= 256 ? 256 : 512));
   static constexpr int THREADS = FUSED ? 320 : 192;
 };
@@ -253,24 +258,37 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     __syncwarp();
   } else if (warp == 1) {
     constexpr uint32_t IDESC = scaled_idesc<A8>(128, BN);
+    // The scales of a step are copied ahead of the MMAs of the step before it where that step has arrived: its copies then run
+    // beside those MMAs (for few tokens the MMAs of a step take less time than the copies it waits for).
     bool ok = !FUSED || mbar_wait(held, 0, p.d_status);
-    for (int i = 0; i < kn && ok; ++i) {
-      const int st = i % STAGES;
-      if (!mbar_wait(full(st), (uint32_t)(i / STAGES) & 1u, p.d_status)) break;
-      if (i >= SCALE_SLOTS && !mbar_wait(empty((i - SCALE_SLOTS) % STAGES), (uint32_t)((i - SCALE_SLOTS) / STAGES) & 1u, p.d_status))
-        break;
+    auto copy = [&](int i) {
       tc_fence_after();
       if (elect_one()) {
-        const uint32_t sw = tmem + BN + (uint32_t)(i % SCALE_SLOTS) * L::SCALE_COLS, sx = sw + 4 * KT;
-        const uint32_t at = base + st * L::STAGE_BYTES;
-        const uint32_t x = FUSED ? res + i * L::X_BYTES : at + L::W_BYTES + L::SF_BYTES;
-        const uint32_t xs = FUSED ? res_sf + i * L::SF_BYTES : x + L::X_BYTES;
+        const int st = i % STAGES;
+        const uint32_t sw = tmem + BN + (uint32_t)st * L::SCALE_COLS, sx = sw + 4 * KT;
+        const uint32_t ws = base + st * L::STAGE_BYTES + L::W_BYTES;
+        const uint32_t xs = FUSED ? res_sf + i * L::SF_BYTES : ws + L::SF_BYTES + L::X_BYTES;
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
-          copy_scales<1>(sw + 4 * t, scale_desc(at + L::W_BYTES + t * TILE_BYTES));
+          copy_scales<1>(sw + 4 * t, scale_desc(ws + t * TILE_BYTES));
           copy_scales<1>(sx + 4 * t, scale_desc(xs + t * TILE_BYTES));
         }
-        const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(x);
+      }
+      __syncwarp();
+    };
+    int copied = 0;
+    for (int i = 0; i < kn && ok; ++i) {
+      if (copied == i) {
+        if (!mbar_wait(full(i % STAGES), (uint32_t)(i / STAGES) & 1u, p.d_status)) break;
+        copy(copied++);
+      }
+      if (copied < kn && mbar_test(full(copied % STAGES), (uint32_t)(copied / STAGES) & 1u)) copy(copied++);
+      if (elect_one()) {
+        const int st = i % STAGES;
+        const uint32_t sw = tmem + BN + (uint32_t)st * L::SCALE_COLS, sx = sw + 4 * KT;
+        const uint32_t at = base + st * L::STAGE_BYTES;
+        const uint64_t a = make_kmajor_sw128_desc(at);
+        const uint64_t b = make_kmajor_sw128_desc(FUSED ? res + i * L::X_BYTES : at + L::W_BYTES + L::SF_BYTES);
 #pragma unroll
         for (int m = 0; m < Step<A8>::MMAS; ++m) {
           const int t = A8 ? 0 : m >> 1;
@@ -343,8 +361,8 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
 // ------------------------------------------------------------------------------------------------ persistent pairs
 // Many tokens: CTA pairs walk over tiles of 256 weight rows x 256 tokens with cta_group::2, each CTA staging half of both
 // operands (64 bytes of shared memory per SM and cycle at the 4-bit rate, where one CTA alone would need 96 for a tile of
-// 128 x 256).  Two accumulators of 256 columns do not fit beside four slots of 24 (8 bits: 12) columns of scales: the second
-// accumulator starts 160 (208) columns after the first.  The epilogue of a tile takes the 96 (48) shared columns into
+// 128 x 256).  Two accumulators of 256 columns do not fit beside five stages' 24 (8 bits: 12) columns of scales: the second
+// accumulator starts 136 (196) columns after the first.  The epilogue of a tile takes the columns that both cover into
 // registers first, and the next tile's MMAs start once those are free.
 template <bool A8>
 struct PairSmem {
@@ -356,7 +374,7 @@ struct PairSmem {
   static constexpr int STAGE_BYTES = (W_BYTES + X_BYTES + SF_BYTES + 1023) / 1024 * 1024;
   static constexpr int STAGES = 5;
   static constexpr int SCALE_COLS = 12 * KT;
-  static constexpr int SCALES = 512 - SCALE_SLOTS * SCALE_COLS;   // first column of the scales
+  static constexpr int SCALES = 512 - STAGES * SCALE_COLS;        // first column of the scales
   static constexpr int ACC_STRIDE = SCALES - 256;                 // column where the second accumulator starts
   static constexpr int SHARED = (256 - ACC_STRIDE + 31) / 32 * 32;   // columns both accumulators cover, to a multiple of 32
   static constexpr int EPI_BYTES = 4 * 8192;                      // two buffers for each group of epilogue warps
@@ -483,22 +501,11 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
       constexpr uint32_t IDESC = scaled_idesc<A8>(256, 256);
       const int mine = pair < tiles ? (tiles - pair + pairs - 1) / pairs : 0;
       const int64_t steps = (int64_t)mine * p.stages;
-      // ring positions of this step, and of the one SCALE_SLOTS before it, whose MMAs have to have completed
-      struct Ring {
-        int stage = 0, slot = 0;
-        uint32_t phase = 0;
-        __device__ __forceinline__ void step() {
-          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-          slot = (slot + 1) % SCALE_SLOTS;
-        }
-      } now, old;
+      int stage = 0;
+      uint32_t phase = 0;
       int k = 0, t = 0;                                      // step of the tile, tile
       for (int64_t i = 0; i < steps; ++i) {
-        if (!mbar_wait(full(now.stage), now.phase, p.d_status)) break;
-        if (i >= SCALE_SLOTS) {
-          if (!mbar_wait(empty(old.stage), old.phase, p.d_status)) break;
-          old.step();
-        }
+        if (!mbar_wait(full(stage), phase, p.d_status)) break;
         if (k == 0 && t >= 1) {
           if (!mbar_wait(drained, (uint32_t)(t - 1) & 1u, p.d_status)) break;
           tc_fence_after();
@@ -506,8 +513,8 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
         tc_fence_after();
         if (elect_one()) {
           const uint32_t acc = tmem + (uint32_t)((t & 1) * L::ACC_STRIDE);
-          const uint32_t sw = tmem + L::SCALES + (uint32_t)now.slot * L::SCALE_COLS, sx = sw + 4 * KT;
-          const uint32_t at = base + (uint32_t)now.stage * L::STAGE_BYTES, sf = at + L::W_BYTES + L::X_BYTES;
+          const uint32_t sw = tmem + L::SCALES + (uint32_t)stage * L::SCALE_COLS, sx = sw + 4 * KT;
+          const uint32_t at = base + (uint32_t)stage * L::STAGE_BYTES, sf = at + L::W_BYTES + L::X_BYTES;
 #pragma unroll
           for (int j = 0; j < KT; ++j) {
             copy_scales<2>(sw + 4 * j, scale_desc(sf + j * TILE_BYTES));
@@ -520,11 +527,11 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
             const int j = A8 ? 0 : m >> 1;
             mma_scaled<2, A8>(acc, a + 2 * m, b + 2 * m, IDESC | scale_select<A8>(m), sw + 4 * j, sx + 8 * j, (k | m) ? 1u : 0u);
           }
-          tc2::umma_commit_pair(empty(now.stage));
+          tc2::umma_commit_pair(empty(stage));
           if (k + 1 == p.stages) tc2::umma_commit_pair(ready(t & 1));
         }
         __syncwarp();
-        now.step();
+        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         if (++k == p.stages) { k = 0; ++t; }
       }
     }
