@@ -301,7 +301,7 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     if (elect_one()) umma_commit(done);
     __syncwarp();
   } else {
-    if (FUSED) {
+    if constexpr (FUSED) {
       wait_for_previous();
       const int values = A8 ? 128 : 256;                     // of a step
       quantize_resident<BN, A8, T>(p, smem + (res - base), smem + (res_sf - base), k0 * values, kn * (values / 8),
@@ -335,23 +335,40 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   const int64_t n0 = (int64_t)nb * 128;
   const int esize = p.y_dtype == DQ_FP32 ? 4 : 2;
   const bool vec = (((uintptr_t)p.y | (uintptr_t)(p.ldy * esize)) & (uintptr_t)(4 * esize - 1)) == 0;
-  for (int i = (int)threadIdx.x + c0 * 32; i < c1 * 32; i += blockDim.x) {
-    const int c = i >> 5, n4 = (i & 31) * 4;
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int r = 0; r < p.splits; ++r) {
-      const uint32_t at = base + (uint32_t)(c * 128 + n4) * 4u;
-      float4 v;
-      if (p.splits > 1) v = ld_cluster_f4(at, (uint32_t)r);
-      else v = *reinterpret_cast<const float4*>(smem + (at - base));
-      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-    }
-    const int64_t n = n0 + n4, at = ((int64_t)mb * BN + c) * p.ldy + n;
-    if (vec && n + 4 <= p.n) store_four(p, at, s);
-    else {
-      const float e[4] = {s.x, s.y, s.z, s.w};
+  auto store = [&](int i, const float4& s) {                 // piece i of [token][32 pieces of four weight rows]
+    const int c = i >> 5;
+    const int64_t n = n0 + (i & 31) * 4, at = ((int64_t)mb * BN + c) * p.ldy + n;
+    if (vec && n + 4 <= p.n) { store_four(p, at, s); return; }
+    const float e[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) if (n + j < p.n) store_value(p, at + j, e[j]);
+    for (int j = 0; j < 4; ++j) if (n + j < p.n) store_value(p, at + j, e[j]);
+  };
+  if (p.splits == 1) {
+    for (int i = threadIdx.x; i < cols * 32; i += blockDim.x) store(i, reinterpret_cast<const float4*>(smem)[i]);
+  } else {
+  // all loads of two pieces at once: one at a time they cost the cluster's latency each
+  constexpr int AT_ONCE = 2, MOST = 8;
+  for (int i0 = (int)threadIdx.x + c0 * 32; i0 < c1 * 32; i0 += AT_ONCE * blockDim.x) {
+    float4 v[AT_ONCE][MOST];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u * (int)blockDim.x;
+      const uint32_t at = base + (uint32_t)i * 16u;          // [token][32 pieces]
+#pragma unroll
+      for (int r = 0; r < MOST; ++r)
+        if (r < p.splits && i < c1 * 32) v[u][r] = ld_cluster_f4(at, (uint32_t)r);
     }
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u * (int)blockDim.x;
+      if (i >= c1 * 32) break;
+      float4 s = v[u][0];
+#pragma unroll
+      for (int r = 1; r < MOST; ++r)
+        if (r < p.splits) { s.x += v[u][r].x; s.y += v[u][r].y; s.z += v[u][r].z; s.w += v[u][r].w; }
+      store(i, s);
+    }
+  }
   }
   tc_fence_before();
   if (p.splits > 1) cluster_sync_all(); else __syncthreads();   // the peers have read this CTA's sums
@@ -646,9 +663,14 @@ dq_status launch_cluster(cudaStream_t stream, const Device& dev, const Operands&
   CUtensorMap w, ws, x = {}, xs = {};
   Params p = params(dev, o, 128, BN, L::KT);
   const int64_t tiles = (int64_t)p.n_blocks * p.m_blocks;
-  p.splits = 1;
+  // The reduction is split until every SM has a CTA; for few tokens until it has two, whose latencies hide each other's, as long
+  // as each keeps eight steps (16 x 8192 x 8192: 9.8 us with two CTAs of 8 steps an SM against 11.1 with one of 16; one token,
+  // 4096 x 4096: 5.4 with one CTA of 4 steps against 5.8 with two of 2).
+  const int64_t room = BN <= 32 ? 2 * dev.sms : dev.sms;
   auto smem = [&]() { return L::FIXED + (FUSED ? 1024 + (p.stages + p.splits - 1) / p.splits * L::RESIDENT : 0); };
-  while (p.splits < 8 && p.splits * 2 <= p.stages && (tiles * p.splits * 2 <= dev.sms || smem() > MAX_SMEM)) p.splits *= 2;
+  while (p.splits < 8 && p.splits * 2 <= p.stages &&
+         (tiles * p.splits * 2 <= (p.stages >= p.splits * 16 ? room : dev.sms) || smem() > MAX_SMEM))
+    p.splits *= 2;
   if (tiles * p.splits > 0x7fffffff || smem() > MAX_SMEM) return DQ_ERR_UNSUPPORTED;
   DQ_CHECK(codes_map(&w, o.w_codes, DQ_MXFP4, o.n, o.k, 128, A8));
   DQ_CHECK(scales_map(&ws, o.w_scales, o.n, o.k, L::KT, 1));
@@ -682,12 +704,30 @@ dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o)
   return launch(LaunchConfig(stream, 2 * pairs, PAIR_THREADS, L::TOTAL, 2), kern, w, ws, x, xs, y, p);
 }
 
+// Which kernel.  Up to 32 tokens a cluster's tile always: weights are what counts, and two CTAs an SM bring them.  Above, pairs
+// unless their one tile after another is longer than a cluster's share of the reduction.  Measured (5 to 50 us, k 512 to 8192,
+// n 1000 to 11008, 80 to 1536 tokens): a pair's step takes 0.28 us, a cluster CTA's 0.38, and its epilogue over the cluster
+// as long as five of the pair's steps; with more CTAs than SMs the clusters lose everywhere.
+// (256 x 8192 x 1000, 8 bits: clusters 16.0, pairs 22.2 us; 256 x 8192 x 11008: clusters 52.1, pairs 26.5.)
+bool cluster_is_faster(const Device& dev, const Operands& o, int tokens, int kt) {
+  if (o.m <= 32) return true;
+  const int64_t steps = (k_tiles(o.k) + kt - 1) / kt;
+  const int64_t tiles = (o.n + 127) / 128 * ((o.m + tokens - 1) / tokens), pair_tiles = (o.n + 255) / 256 * ((o.m + 255) / 256);
+  if (tiles > dev.sms) return false;
+  int64_t splits = 1;
+  while (splits < 8 && splits * 2 <= steps && tiles * splits * 2 <= dev.sms) splits *= 2;
+  const int64_t pairs = dev.sms / 2, waves = (pair_tiles + pairs - 1) / pairs;
+  return 4 * ((steps + splits - 1) / splits) + 15 < 3 * waves * steps;
+}
+
 template <bool A8>
 dq_status product(cudaStream_t stream, const Device& dev, const Operands& o) {
-  if (o.m <= 16) return launch_cluster<16, A8, false, float>(stream, dev, o);
-  if (o.m <= 32) return launch_cluster<32, A8, false, float>(stream, dev, o);
-  if (o.m <= 64) return launch_cluster<64, A8, false, float>(stream, dev, o);
-  if (o.m <= 192) return launch_cluster<128, A8, false, float>(stream, dev, o);
+  if (cluster_is_faster(dev, o, o.m <= 64 ? 64 : 128, Step<A8>::KT)) {
+    if (o.m <= 16) return launch_cluster<16, A8, false, float>(stream, dev, o);
+    if (o.m <= 32) return launch_cluster<32, A8, false, float>(stream, dev, o);
+    if (o.m <= 64) return launch_cluster<64, A8, false, float>(stream, dev, o);
+    return launch_cluster<128, A8, false, float>(stream, dev, o);
+  }
   if (o.y_dtype == DQ_BF16) return launch_pair<A8, __nv_bfloat16>(stream, dev, o);
   if (o.y_dtype == DQ_FP16) return launch_pair<A8, __half>(stream, dev, o);
   return launch_pair<A8, float>(stream, dev, o);
@@ -719,7 +759,9 @@ dq_status linear(cudaStream_t stream, const void* X, int x_dtype, int64_t m, int
   DQ_CHECK(current_device(dev));
   uint8_t* scales = workspace + m * row_bytes(a_fmt, k);
   Operands o{a_fmt, workspace, scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy};
-  if (m <= 16) {
+  // Few tokens are quantised by the product's own CTAs, each the part that it multiplies; from five on the CTAs' repeated work costs
+  // more than a launch (4096 x 4096: 1 token 5.4 us against 6.9 in two launches, 4 tokens 6.2 against 6.9, 16 tokens 8.7 against 7.0).
+  if (m <= 4) {
     o.x = X; o.ldx = ldx;
     o.x_vec = whole_pieces(X, ldx, k, x_dtype);
     const dq_status st = a_fmt == DQ_MXFP4 ? fused<false>(stream, dev, o, x_dtype) : fused<true>(stream, dev, o, x_dtype);
