@@ -224,6 +224,7 @@ __device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.laun
 struct LaunchConfig {
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[2];
+  LaunchConfig(const LaunchConfig&) = delete;                 // (cfg points into it)
   LaunchConfig(cudaStream_t stream, int64_t ctas, int threads, int smem = 0, int cluster = 1) {
     cfg.gridDim = dim3((unsigned)ctas); cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = (size_t)smem; cfg.stream = stream;
@@ -246,7 +247,7 @@ inline bool whole_pieces(const void* p, int64_t ld, int64_t k, int dtype) {
 
 // What an entry point knows of the current device; 0 where it is none that the kernels were built for.
 struct Device {
-  int sms = 0;
+  int index = 0, sms = 0;
   int* d_status = nullptr;   // the operators' status word (dq_mx_status)
 };
 dq_status current_device(Device& out);

@@ -657,31 +657,57 @@ Params params(const Device& dev, const Operands& o, int rows, int tokens, int kt
   return p;
 }
 
+template <int BN, bool A8, bool FUSED>
+int cluster_smem(int stages, int splits) {
+  using L = ClusterSmem<BN, A8, FUSED>;
+  return L::FIXED + (FUSED ? 1024 + (stages + splits - 1) / splits * L::RESIDENT : 0);
+}
+
+// Into how many CTAs the reduction of each of `tiles` tiles is split: as many as run at once, until every SM has one; for few
+// tokens until it has two, whose latencies hide each other's, as long as each keeps eight steps (16 x 8192 x 8192: 9.8 us with
+// two CTAs of 8 steps an SM against 11.1 with one of 16; one token, 4096 x 4096: 5.4 with one CTA of 4 steps against 5.8 with two
+// of 2).  Clusters have to find their SMs together: of 8 CTAs with an SM each, 15 run at once, not 18.  FUSED: at least as
+// many as make the tokens fit.
+template <int BN, bool A8, bool FUSED, typename T>
+dq_status choose_splits(const Device& dev, int64_t tiles, int stages, int& splits) {
+  using L = ClusterSmem<BN, A8, FUSED>;
+  static SmemOptIn attr;
+  static int known[64][9] = {};                              // clusters with an SM a CTA at once, by device and size; asked once
+  constexpr int ALONE = L::FIXED > MAX_SMEM / 2 + 1024 ? L::FIXED : MAX_SMEM / 2 + 1024;   // shared memory that leaves no room for two
+  auto kern = cluster_kernel<BN, A8, FUSED, T>;
+  DQ_CHECK(opt_in_dynamic_smem(kern, FUSED ? MAX_SMEM : ALONE, attr));
+  splits = 1;
+  for (int s = 2; s <= 8 && s <= stages; s *= 2) {
+    int& most = known[dev.index][s];
+    if (most == 0) {
+      LaunchConfig c(nullptr, s, L::THREADS, ALONE, s);
+      int n = 0;
+      DQ_CHECK_CUDA(cudaOccupancyMaxActiveClusters(&n, kern, &c.cfg));
+      most = n > 0 ? n : -1;
+    }
+    const int smem = cluster_smem<BN, A8, FUSED>(stages, s);
+    const bool two = BN <= 32 && smem <= MAX_SMEM / 2 - 1024 && stages >= s * 8;
+    if (cluster_smem<BN, A8, FUSED>(stages, splits) > MAX_SMEM || tiles <= (two ? 2 : 1) * most) splits = s;
+  }
+  return DQ_OK;
+}
+
 template <int BN, bool A8, bool FUSED, typename T>
 dq_status launch_cluster(cudaStream_t stream, const Device& dev, const Operands& o) {
   using L = ClusterSmem<BN, A8, FUSED>;
   CUtensorMap w, ws, x = {}, xs = {};
   Params p = params(dev, o, 128, BN, L::KT);
   const int64_t tiles = (int64_t)p.n_blocks * p.m_blocks;
-  // The reduction is split until every SM has a CTA; for few tokens until it has two, whose latencies hide each other's, as long
-  // as each keeps eight steps (16 x 8192 x 8192: 9.8 us with two CTAs of 8 steps an SM against 11.1 with one of 16; one token,
-  // 4096 x 4096: 5.4 with one CTA of 4 steps against 5.8 with two of 2).
-  const int64_t room = BN <= 32 ? 2 * dev.sms : dev.sms;
-  auto smem = [&]() { return L::FIXED + (FUSED ? 1024 + (p.stages + p.splits - 1) / p.splits * L::RESIDENT : 0); };
-  while (p.splits < 8 && p.splits * 2 <= p.stages &&
-         (tiles * p.splits * 2 <= (p.stages >= p.splits * 16 ? room : dev.sms) || smem() > MAX_SMEM))
-    p.splits *= 2;
-  if (tiles * p.splits > 0x7fffffff || smem() > MAX_SMEM) return DQ_ERR_UNSUPPORTED;
+  DQ_CHECK((choose_splits<BN, A8, FUSED, T>(dev, tiles, p.stages, p.splits)));
+  const int smem = cluster_smem<BN, A8, FUSED>(p.stages, p.splits);
+  if (tiles * p.splits > 0x7fffffff || smem > MAX_SMEM) return DQ_ERR_UNSUPPORTED;
   DQ_CHECK(codes_map(&w, o.w_codes, DQ_MXFP4, o.n, o.k, 128, A8));
   DQ_CHECK(scales_map(&ws, o.w_scales, o.n, o.k, L::KT, 1));
   if (!FUSED) {
     DQ_CHECK(codes_map(&x, o.a_codes, o.a_fmt, o.m, o.k, BN, false));
     DQ_CHECK(scales_map(&xs, o.a_scales, o.m, o.k, L::KT, 1));
   }
-  static SmemOptIn attr;
-  auto kern = cluster_kernel<BN, A8, FUSED, T>;
-  DQ_CHECK(opt_in_dynamic_smem(kern, FUSED ? MAX_SMEM : L::FIXED, attr));
-  return launch(LaunchConfig(stream, tiles * p.splits, L::THREADS, smem(), p.splits), kern, w, ws, x, xs, p);
+  return launch(LaunchConfig(stream, tiles * p.splits, L::THREADS, smem, p.splits), cluster_kernel<BN, A8, FUSED, T>, w, ws, x, xs, p);
 }
 
 template <bool A8, typename T>
@@ -704,25 +730,30 @@ dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o)
   return launch(LaunchConfig(stream, 2 * pairs, PAIR_THREADS, L::TOTAL, 2), kern, w, ws, x, xs, y, p);
 }
 
-// Which kernel.  Up to 32 tokens a cluster's tile always: weights are what counts, and two CTAs an SM bring them.  Above, pairs
-// unless their one tile after another is longer than a cluster's share of the reduction.  Measured (5 to 50 us, k 512 to 8192,
-// n 1000 to 11008, 80 to 1536 tokens): a pair's step takes 0.28 us, a cluster CTA's 0.38, and its epilogue over the cluster
-// as long as five of the pair's steps; with more CTAs than SMs the clusters lose everywhere.
+// Which kernel.  Up to 64 tokens a cluster's tile: weights are what counts, and a pair's tile would be three quarters empty.
+// Above, pairs unless their one tile after another is longer than a cluster's share of the reduction.  Measured (4 to 50 us,
+// k 256 to 8192, n 512 to 13824, 80 to 1536 tokens): a pair's step takes 0.28 us, a cluster CTA's 0.38, and its epilogue over the
+// cluster as long as five of the pair's steps; with more tiles than SMs the clusters lose everywhere.
 // (256 x 8192 x 1000, 8 bits: clusters 16.0, pairs 22.2 us; 256 x 8192 x 11008: clusters 52.1, pairs 26.5.)
-bool cluster_is_faster(const Device& dev, const Operands& o, int tokens, int kt) {
-  if (o.m <= 32) return true;
-  const int64_t steps = (k_tiles(o.k) + kt - 1) / kt;
-  const int64_t tiles = (o.n + 127) / 128 * ((o.m + tokens - 1) / tokens), pair_tiles = (o.n + 255) / 256 * ((o.m + 255) / 256);
-  if (tiles > dev.sms) return false;
-  int64_t splits = 1;
-  while (splits < 8 && splits * 2 <= steps && tiles * splits * 2 <= dev.sms) splits *= 2;
+template <bool A8>
+dq_status cluster_is_faster(const Device& dev, const Operands& o, bool& yes) {
+  constexpr int KT = Step<A8>::KT;
+  const int64_t steps = (k_tiles(o.k) + KT - 1) / KT;
+  const int64_t tiles = (o.n + 127) / 128 * ((o.m + 127) / 128), pair_tiles = (o.n + 255) / 256 * ((o.m + 255) / 256);
   const int64_t pairs = dev.sms / 2, waves = (pair_tiles + pairs - 1) / pairs;
-  return 4 * ((steps + splits - 1) / splits) + 15 < 3 * waves * steps;
+  int splits = 1;
+  yes = o.m <= 64;
+  if (yes || tiles > dev.sms) return DQ_OK;
+  DQ_CHECK((choose_splits<128, A8, false, float>(dev, tiles, (int)steps, splits)));
+  yes = 4 * ((steps + splits - 1) / splits) + 15 < 3 * waves * steps;
+  return DQ_OK;
 }
 
 template <bool A8>
 dq_status product(cudaStream_t stream, const Device& dev, const Operands& o) {
-  if (cluster_is_faster(dev, o, o.m <= 64 ? 64 : 128, Step<A8>::KT)) {
+  bool cluster = false;
+  DQ_CHECK(cluster_is_faster<A8>(dev, o, cluster));
+  if (cluster) {
     if (o.m <= 16) return launch_cluster<16, A8, false, float>(stream, dev, o);
     if (o.m <= 32) return launch_cluster<32, A8, false, float>(stream, dev, o);
     if (o.m <= 64) return launch_cluster<64, A8, false, float>(stream, dev, o);

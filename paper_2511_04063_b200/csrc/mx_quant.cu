@@ -25,6 +25,7 @@ dq_status current_device(Device& out) {
     DQ_CHECK_CUDA(cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev));
     DQ_CHECK_CUDA(cudaGetSymbolAddress(&p, g_mx_status));
     d.d_status = (int*)p;
+    d.index = dev;
     known[dev] = d;
     done[dev] = true;
   }
