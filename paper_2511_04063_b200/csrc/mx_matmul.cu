@@ -493,22 +493,34 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
 
   if (warp == 0) {
     if (elect_one()) {
-      wait_for_previous();
+      auto weights = [&](int s, int k, int nb) {
+        const uint32_t at = base + s * L::STAGE_BYTES;
+        if (leader) mbar_expect_tx(full(s), 2 * (L::W_LOADED + L::X_BYTES + L::SF_BYTES));
+        tma_load_2d_pair(at, &map_w, full(s), k * 128, nb * 256 + (int)rank * 128);
+        tc2::tma_load_3d_pair(at + L::W_BYTES + L::X_BYTES, &map_ws, full(s), 0, k * KT, nb * 2 + (int)rank);
+      };
+      auto tokens = [&](int s, int k, int mb) {
+        const uint32_t at = base + s * L::STAGE_BYTES + L::W_BYTES;
+        tma_load_2d_pair(at, &map_x, full(s), k * 128, mb * 256 + (int)rank * 128);
+        tc2::tma_load_3d_pair(at + L::X_BYTES + KT * TILE_BYTES, &map_xs, full(s), 0, k * KT, mb * 2);
+      };
+      const int ahead = p.stages < STAGES ? p.stages : STAGES;   // steps of the first tile that need no free stage
+      int nb, mb;
+      tile_of(pair, nb, mb);
+      if (!p.weights_first) wait_for_previous();
+      for (int k = 0; k < ahead; ++k) weights(k, k, nb);
+      if (p.weights_first) wait_for_previous();
       allow_next();
-      int it = 0;
+      for (int k = 0; k < ahead; ++k) tokens(k, k, mb);
+      int s = ahead % STAGES, round = ahead / STAGES;            // stage, and how often it was used
       bool ok = true;
-      for (int u = pair; u < tiles && ok; u += pairs) {
-        int nb, mb;
+      for (int u = pair, k = ahead; u < tiles && ok; u += pairs, k = 0) {
         tile_of(u, nb, mb);
-        for (int k = 0; k < p.stages; ++k, ++it) {
-          const int s = it % STAGES;
-          if (it >= STAGES && !mbar_wait(empty(s), (uint32_t)(it / STAGES - 1) & 1u, p.d_status)) { ok = false; break; }
-          const uint32_t at = base + s * L::STAGE_BYTES, sf = at + L::W_BYTES + L::X_BYTES;
-          if (leader) mbar_expect_tx(full(s), 2 * (L::W_LOADED + L::X_BYTES + L::SF_BYTES));
-          tma_load_2d_pair(at, &map_w, full(s), k * 128, nb * 256 + (int)rank * 128);
-          tma_load_2d_pair(at + L::W_BYTES, &map_x, full(s), k * 128, mb * 256 + (int)rank * 128);
-          tc2::tma_load_3d_pair(sf, &map_ws, full(s), 0, k * KT, nb * 2 + (int)rank);
-          tc2::tma_load_3d_pair(sf + KT * TILE_BYTES, &map_xs, full(s), 0, k * KT, mb * 2);
+        for (; k < p.stages; ++k) {
+          if (round > 0 && !mbar_wait(empty(s), (uint32_t)(round - 1) & 1u, p.d_status)) { ok = false; break; }
+          weights(s, k, nb);
+          tokens(s, k, mb);
+          if (++s == STAGES) { s = 0; ++round; }
         }
       }
     }

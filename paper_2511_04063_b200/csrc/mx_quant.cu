@@ -42,27 +42,31 @@ namespace {
 constexpr int PIECE = 256;
 template <typename T, bool WHOLE>
 struct Piece {
-  static __device__ __forceinline__ void load(Vec8<T>& v, const T* row, int c0, int k, int lane, T*) {
-    if (WHOLE) {
-      v.clear();
-      if (c0 + lane * 8 < k) v.load(row + c0 + lane * 8);
-    }
+  using Raw = Vec8<T>;                       // what a lane fetches
+  static __device__ __forceinline__ void fetch(Raw& x, const T* row, int c0, int k, int lane) {
+    x.clear();
+    if (c0 + lane * 8 < k) x.load(row + c0 + lane * 8);
   }
+  static __device__ __forceinline__ const Vec8<T>& turned(const Raw& x, int, T*) { return x; }
   static __device__ __forceinline__ void store(const Vec8<T>& v, T* row, int c0, int k, int lane, T*) {
     if (c0 + lane * 8 < k) v.store(row + c0 + lane * 8);
   }
 };
 template <typename T>
 struct Piece<T, false> {
-  static __device__ __forceinline__ void load(Vec8<T>& v, const T* row, int c0, int k, int lane, T* turn) {
-    T x[8];
+  struct Raw { T x[8]; };                    // every 32nd value
+  static __device__ __forceinline__ void fetch(Raw& x, const T* row, int c0, int k, int lane) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = c0 + i * 32 + lane < k ? row[c0 + i * 32 + lane] : from_f32<T>(0.f);
+    for (int i = 0; i < 8; ++i) x.x[i] = c0 + i * 32 + lane < k ? row[c0 + i * 32 + lane] : from_f32<T>(0.f);
+  }
+  static __device__ __forceinline__ Vec8<T> turned(const Raw& x, int lane, T* turn) {
+    Vec8<T> v;
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn[i * 32 + lane] = x[i];
+    for (int i = 0; i < 8; ++i) turn[i * 32 + lane] = x.x[i];
     __syncwarp();
     v.load(turn + lane * 8);
+    return v;
   }
   static __device__ __forceinline__ void store(const Vec8<T>& v, T* row, int c0, int k, int lane, T* turn) {
     __syncwarp();
@@ -96,10 +100,16 @@ quantize_kernel(const T* X, int64_t rows, int k, int64_t ldx, int wide, uint8_t*
   const bool in = c < ktiles * KTILE;
   T* stage = turn[WHOLE ? 0 : warp];
   Vec8<T> v[4];
+  {
+    typename Piece<T, WHOLE>::Raw x[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if (r0 + 32 * j < rows) Piece<T, WHOLE>::load(v[j], X + (r0 + 32 * j) * ldx, c0, k, lane, stage);
-    else v[j].clear();
+    for (int j = 0; j < 4; ++j)
+      if (r0 + 32 * j < rows) Piece<T, WHOLE>::fetch(x[j], X + (r0 + 32 * j) * ldx, c0, k, lane);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (r0 + 32 * j < rows) v[j] = Piece<T, WHOLE>::turned(x[j], lane, stage);
+      else v[j].clear();
+    }
   }
   const uint32_t e01 = block_exponent(v[0].exponent() | v[1].exponent() << 16);
   const uint32_t e23 = block_exponent(v[2].exponent() | v[3].exponent() << 16);
@@ -173,22 +183,26 @@ rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, 
   float2 h[V][4];
   float2 ss = make_float2(0.f, 0.f);
   {
-    Vec8<T> x[V];
+    typename Piece<T, WHOLE>::Raw x[V], b[V];
 #pragma unroll
-    for (int u = 0; u < V; ++u) Piece<T, WHOLE>::load(x[u], X + r * ldx, column(u), k, lane, stage);
+    for (int u = 0; u < V; ++u) Piece<T, WHOLE>::fetch(x[u], X + r * ldx, column(u), k, lane);
     if (residual) {
-      Vec8<T> b[V];
 #pragma unroll
-      for (int u = 0; u < V; ++u) Piece<T, WHOLE>::load(b[u], residual + r * ldr, column(u), k, lane, stage);
+      for (int u = 0; u < V; ++u) Piece<T, WHOLE>::fetch(b[u], residual + r * ldr, column(u), k, lane);
+    }
 #pragma unroll
-      for (int u = 0; u < V; ++u)
+    for (int u = 0; u < V; ++u) {
+      const Vec8<T> v = Piece<T, WHOLE>::turned(x[u], lane, stage);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[u][i] = add2(x[u].pair(i), b[u].pair(i));
-    } else {
+      for (int i = 0; i < 4; ++i) h[u][i] = v.pair(i);
+    }
+    if (residual) {
 #pragma unroll
-      for (int u = 0; u < V; ++u)
+      for (int u = 0; u < V; ++u) {
+        const Vec8<T> v = Piece<T, WHOLE>::turned(b[u], lane, stage);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[u][i] = x[u].pair(i);
+        for (int i = 0; i < 4; ++i) h[u][i] = add2(h[u][i], v.pair(i));
+      }
     }
   }
 #pragma unroll
@@ -221,7 +235,11 @@ rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, 
     if (c0 >= ktiles * KTILE) break;                          // (whole warps)
     Vec8<float> y;
     Vec8<G> g;
-    if (gamma) Piece<G, WHOLE>::load(g, gamma, c0, k, lane, g_stage);
+    if (gamma) {
+      typename Piece<G, WHOLE>::Raw x;
+      Piece<G, WHOLE>::fetch(x, gamma, c0, k, lane);
+      g = Piece<G, WHOLE>::turned(x, lane, g_stage);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float2 f = mul2(h[u][i], make_float2(rstd, rstd));
@@ -324,8 +342,12 @@ dq_status rmsnorm_quantize(cudaStream_t stream, const void* X, int dtype, int64_
   if (pieces > 4 * 32) return DQ_ERR_UNSUPPORTED;             // 32768 columns: a row has to stay in one CTA's registers
   Device dev;
   DQ_CHECK(current_device(dev));
-  // Few rows: as many warps a row as there are pieces; else four pieces a warp (eight where 16 warps would not be enough).
-  const int V = pieces == 1 || (rows <= 2 * dev.sms && pieces <= 32) ? 1 : pieces == 2 ? 2 : pieces <= 64 ? 4 : 8;
+  // Pieces a warp: one where there are few rows (latency), else four, or two where four would leave too few warps to keep HBM
+  // busy or the rows are not in whole pieces (4096 x 1024: 9.4 us with two, 11.4 with four; 16384 x 8192: 185 with four,
+  // 207 with two; 5000 x 5111: 62 with two, 73 with four); eight where a CTA of 16 warps would not hold the row.
+  const bool few = rows <= 4 * dev.sms || (pieces <= 4 && rows <= 64 * dev.sms);
+  const int V = pieces == 1 || (rows <= 2 * dev.sms && pieces <= 32) ? 1
+                : pieces == 2 || (pieces <= 32 && (few || !whole)) ? 2 : pieces <= 64 ? 4 : 8;
   const int warps = (pieces + V - 1) / V;
   const int threads = warps == 1 ? 256 : warps * 32;
   const int64_t ctas = warps == 1 ? (rows + 7) / 8 : rows;
