@@ -379,14 +379,14 @@ def _mx_matrix(t, name: str):
     return t.data_ptr(), dtype, ld, rows, k, index
 
 
-def _mx_like(t, name: str, x):
-    """(address, row stride) of a matrix that has to be of the shape, type and device of x (its _mx_matrix); None: (0, 0)."""
+def _mx_like(t, name: str, X, index: int):
+    """(address, row stride) of a matrix that has to be of the shape, type and device (`index`) of X; None: (0, 0)."""
     if t is None:
         return 0, 0
-    ptr, dtype, ld, rows, k, index = _mx_matrix(t, name)
-    if dtype != x[1] or rows != x[3] or k != x[4] or index != x[5]:
+    if t.shape != X.shape or t.dtype != X.dtype or t.get_device() != index:
         raise ValueError("%s: shape, type or device differs from the input's" % name)
-    return ptr, ld
+    ld, step = t.stride()
+    return (t.data_ptr(), ld) if step == 1 and ld >= t.shape[1] else _mx_matrix(t, name)[0::2][:2]
 
 
 def _mx_bytes(t, name: str, least: int, index: int):
@@ -428,9 +428,9 @@ def dq_mx_quantize(X, fmt: int, codes, scales, values=None, stream=None):
     """Codes and scales of X ([rows, k]; float32, bfloat16 or float16).  values (same type and shape; may be X): what
     the codes stand for."""
     lib = _lib if _mx_device else _mx_load()
-    x = ptr, dtype, ld, rows, k, index = _mx_matrix(X, "X")
+    ptr, dtype, ld, rows, k, index = _mx_matrix(X, "X")
     n_codes, n_scales = _mx_held(fmt, rows, k)
-    v, ldv = _mx_like(values, "values", x)
+    v, ldv = _mx_like(values, "values", X, index)
     _mx_call(lib.dq_mx_quantize, "dq_mx_quantize", index, stream, ptr, dtype, rows, k, ld, fmt,
              _mx_bytes(codes, "codes", n_codes, index), _mx_bytes(scales, "scales", n_scales, index), v, ldv)
 
@@ -448,11 +448,11 @@ def dq_rmsnorm_quantize(X, gamma, eps: float, fmt: int, codes, scales, residual=
     """h = X + residual; codes and scales of h / sqrt(mean(h^2) + eps) * gamma.  gamma: [k] of X's type or float32, or None.
     sum_out (may be X or residual) receives h, values the quantised output's values; all [rows, k] of X's type."""
     lib = _lib if _mx_device else _mx_load()
-    x = ptr, dtype, ld, rows, k, index = _mx_matrix(X, "X")
+    ptr, dtype, ld, rows, k, index = _mx_matrix(X, "X")
     n_codes, n_scales = _mx_held(fmt, rows, k)
-    r, ldr = _mx_like(residual, "residual", x)
-    h, lds = _mx_like(sum_out, "sum_out", x)
-    v, ldv = _mx_like(values, "values", x)
+    r, ldr = _mx_like(residual, "residual", X, index)
+    h, lds = _mx_like(sum_out, "sum_out", X, index)
+    v, ldv = _mx_like(values, "values", X, index)
     g, g_dtype = 0, dtype
     if gamma is not None:
         g_dtype = _MX_TYPES.get(gamma.dtype)

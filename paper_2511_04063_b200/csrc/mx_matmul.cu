@@ -53,6 +53,13 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return __all_sync(0xffffffffu, ok != 0);
 }
+// After a wait that ran out: the last loads into the stages (`fills` of them were issued in all) have to land before the shared
+// memory may go to another CTA.
+template <int STAGES, typename Full>
+__device__ __forceinline__ void await_loads(int64_t fills, Full full, int* d_status) {
+  for (int64_t i = fills > STAGES ? fills - STAGES : 0; i < fills; ++i)
+    mbar_wait(full((int)(i % STAGES)), (uint32_t)(i / STAGES) & 1u, d_status);
+}
 // Scales: 32 rows of 16 bytes, copied to the same 4 columns of all four 32-lane quarters of tensor memory.
 __device__ __forceinline__ uint64_t scale_desc(uint32_t smem_addr) {
   return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
@@ -250,7 +257,7 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
       allow_next();
       for (int i = 0; i < ahead; ++i) tokens(i);
       for (int i = ahead; i < kn; ++i) {
-        if (!mbar_wait(empty(i % STAGES), (uint32_t)(i / STAGES - 1) & 1u, p.d_status)) break;
+        if (!mbar_wait(empty(i % STAGES), (uint32_t)(i / STAGES - 1) & 1u, p.d_status)) { await_loads<STAGES>(i, full, p.d_status); break; }
         weights(i);
         tokens(i);
       }
@@ -523,6 +530,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
           if (++s == STAGES) { s = 0; ++round; }
         }
       }
+      if (!ok && leader) await_loads<STAGES>((int64_t)round * STAGES + s, full, p.d_status);   // (both CTAs' loads end there)
     }
     __syncwarp();
   } else if (warp == 1) {

@@ -197,6 +197,17 @@ def test_rmsnorm_in_place_and_bare():
         assert torch.equal(a if target == "x" else b, (x.float() + r.float()).to(torch.bfloat16))
 
 
+@pytest.mark.parametrize("rows,k", [(2000, 700), (10000, 512), (1500, 4096), (700, 4099)])
+def test_rmsnorm_many_rows(rows, k):
+    """The variants for many rows: several pieces a warp, several rows a CTA, rows that are not in whole pieces."""
+    x, r = draw(rows, k, torch.bfloat16, 1), draw(rows, k, torch.bfloat16, 2)
+    gamma = (1 + 0.1 * draw(1, k, torch.float32, 3)[0]).to(torch.bfloat16)
+    codes, scales = dq.dq_mx_empty(rows, k, dq.DQ_MXFP8)
+    h, values = torch.empty_like(x), torch.empty_like(x)
+    dq.dq_rmsnorm_quantize(x, gamma, 1e-5, dq.DQ_MXFP8, codes, scales, residual=r, sum_out=h, values=values)
+    check_norm(x, r, gamma, 1e-5, dq.DQ_MXFP8, codes, scales, h, values)
+
+
 def test_rmsnorm_rows_are_independent():
     """A row with a NaN, one with an infinity and one of zeros beside ordinary ones."""
     x = draw(8, 256, torch.float32, 4)
@@ -231,7 +242,8 @@ def check_product(y, a, w, k):
 
 
 SHAPES = [(1, 1, 1), (1, 128, 32), (3, 5, 31), (16, 128, 128), (17, 130, 129), (7, 300, 1000), (32, 64, 257), (33, 257, 384),
-          (64, 1, 2048), (65, 384, 300), (128, 256, 512), (129, 200, 640), (200, 1000, 100), (256, 512, 1152), (300, 333, 777)]
+          (64, 1, 2048), (65, 384, 300), (128, 256, 512), (129, 200, 640), (200, 1000, 100), (256, 512, 1152), (300, 333, 777),
+          (300, 1, 256), (257, 8, 31), (70, 129, 4096)]
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -290,6 +302,18 @@ def test_matmul_keeps_rows_apart(fmt, m):
     keep = [i for i in range(n) if i != 7]
     if m > 1:
         check_product(y[:m - 1, keep], a[:m - 1], w[keep], k)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("m,n,k", [(3, 256, 33000), (64, 40000, 160), (130, 20000, 384), (1200, 4100, 96)])
+def test_matmul_many_steps_and_many_tiles(fmt, m, n, k):
+    """More pipeline steps than stages by far; more tiles than SMs; the token tile's and the weight tile's last rows."""
+    a_codes, a_scales, a = quantized(draw(m, k, torch.float32, 1), fmt)
+    w_codes, w_scales, w = quantized(draw(n, k, torch.float32, 2), dq.DQ_MXFP4)
+    y = torch.full((m, n), float("nan"), dtype=torch.float32, device="cuda")
+    dq.dq_mx_matmul(a_codes, a_scales, fmt, w_codes, w_scales, k, y)
+    finished()
+    check_product(y, a, w, k)
 
 
 @pytest.mark.parametrize("fmt", FMTS)
