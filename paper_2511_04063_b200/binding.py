@@ -337,63 +337,26 @@ def dq_eval_rotation(X, R, tau: float, bits: int, stream=None):
 
 
 # ---------------------------------------------------------------------------
-# Microscaled operators.  Their wrappers check what the C entry cannot see (devices, types, sizes of buffers); a
-# wrong tensor raises ValueError, a refusal of the library DartQuantError.
+# Microscaled operators.  Their arguments are checked and passed on by the compiled module _calls (csrc/py_calls.cpp): a
+# ctypes call with checks in Python takes longer than the smaller kernels.  A wrong tensor raises ValueError, a refusal of
+# the library DartQuantError.
 # ---------------------------------------------------------------------------
-_MX_TYPES = {}                       # torch type -> DQ_*, filled by the first call
-_mx_device = _mx_raw_stream = None   # torch's own lookups of the current device and stream
+_calls = None
 
 
-def _mx_load():
-    """The library; on the first call also what the wrappers need of torch."""
-    global _mx_device, _mx_raw_stream
-    import torch
-    _MX_TYPES.update({torch.float32: DQ_FP32, torch.bfloat16: DQ_BF16, torch.float16: DQ_FP16})
-    torch.cuda.current_device()
-    _mx_device, _mx_raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
-    return load_library()
-
-
-def _mx_call(fn, name: str, index: int, stream, *args):
-    """fn(*args, stream) on the current device, which has to be `index`, the tensors'."""
-    if index != _mx_device():
-        raise ValueError("%s: the tensors have to be on the current CUDA device" % name)
-    status = fn(*args, _mx_raw_stream(index) if stream is None else stream.cuda_stream)
-    if status != DQ_OK:
-        raise DartQuantError(status, name)
-
-
-def _mx_matrix(t, name: str):
-    """(address, type, row stride, rows, width, device) of a matrix of values with contiguous rows."""
-    shape = t.shape
-    dtype = _MX_TYPES.get(t.dtype)
-    index = t.get_device()
-    if dtype is None or index < 0 or len(shape) != 2:
-        raise ValueError("%s: a 2-D CUDA tensor of float32, bfloat16 or float16 is needed" % name)
-    rows, k = shape
-    ld, step = t.stride()
-    if step != 1 or ld < k:
-        if (step != 1 and k > 1) or (ld < k and rows > 1):
-            raise ValueError("%s: rows have to be contiguous and must not overlap" % name)
-        ld = k
-    return t.data_ptr(), dtype, ld, rows, k, index
-
-
-def _mx_like(t, name: str, X, index: int):
-    """(address, row stride) of a matrix that has to be of the shape, type and device (`index`) of X; None: (0, 0)."""
-    if t is None:
-        return 0, 0
-    if t.shape != X.shape or t.dtype != X.dtype or t.get_device() != index:
-        raise ValueError("%s: shape, type or device differs from the input's" % name)
-    ld, step = t.stride()
-    return (t.data_ptr(), ld) if step == 1 and ld >= t.shape[1] else _mx_matrix(t, name)[0::2][:2]
-
-
-def _mx_bytes(t, name: str, least: int, index: int):
-    """Address of a contiguous buffer of at least `least` bytes on device `index`."""
-    if t.nbytes < least or t.get_device() != index or not t.is_contiguous():
-        raise ValueError("%s: a contiguous buffer of at least %d bytes on the inputs' device is needed" % (name, least))
-    return t.data_ptr()
+def _mx():
+    """The compiled calls, bound to the library."""
+    global _calls
+    if _calls is None:
+        import torch
+        lib = load_library()
+        from . import _calls as calls
+        torch.cuda.current_device()
+        calls.bind(tuple(C.cast(getattr(lib, n), C.c_void_p).value for n in
+                         ("dq_mx_quantize", "dq_mx_dequantize", "dq_rmsnorm_quantize", "dq_mx_matmul", "dq_mx_linear")),
+                   (torch.float32, torch.bfloat16, torch.float16), torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        _calls = calls
+    return _calls
 
 
 def dq_mx_row_bytes(fmt: int, k: int) -> int:
@@ -408,85 +371,51 @@ def dq_mx_linear_workspace(a_fmt: int, m: int, k: int) -> int:
     return int(load_library().dq_mx_linear_workspace(a_fmt, m, k))
 
 
-def _mx_held(fmt: int, rows: int, k: int):
-    """Bytes of the codes and of the scales of a [rows, k] matrix."""
-    if fmt != DQ_MXFP4 and fmt != DQ_MXFP8:
-        raise ValueError("format %r: DQ_MXFP4 or DQ_MXFP8 is needed" % (fmt,))
-    tiles = (k + 127) // 128
-    return rows * tiles * (64 if fmt == DQ_MXFP4 else 128), (rows + 127) // 128 * tiles * 512
-
-
 def dq_mx_empty(rows: int, k: int, fmt: int, device="cuda"):
     """(codes, scales): buffers for a [rows, k] matrix, torch.uint8."""
     import torch
-    codes, scales = _mx_held(fmt, rows, k)
-    return (torch.empty((rows, codes // rows if rows else 0), dtype=torch.uint8, device=device),
-            torch.empty(scales, dtype=torch.uint8, device=device))
+    if fmt != DQ_MXFP4 and fmt != DQ_MXFP8:
+        raise ValueError("format %r: DQ_MXFP4 or DQ_MXFP8 is needed" % (fmt,))
+    return (torch.empty((rows, dq_mx_row_bytes(fmt, k)), dtype=torch.uint8, device=device),
+            torch.empty(dq_mx_scale_bytes(rows, k), dtype=torch.uint8, device=device))
 
 
 def dq_mx_quantize(X, fmt: int, codes, scales, values=None, stream=None):
     """Codes and scales of X ([rows, k]; float32, bfloat16 or float16).  values (same type and shape; may be X): what
     the codes stand for."""
-    lib = _lib if _mx_device else _mx_load()
-    ptr, dtype, ld, rows, k, index = _mx_matrix(X, "X")
-    n_codes, n_scales = _mx_held(fmt, rows, k)
-    v, ldv = _mx_like(values, "values", X, index)
-    _mx_call(lib.dq_mx_quantize, "dq_mx_quantize", index, stream, ptr, dtype, rows, k, ld, fmt,
-             _mx_bytes(codes, "codes", n_codes, index), _mx_bytes(scales, "scales", n_scales, index), v, ldv)
+    status = (_calls or _mx()).quantize(X, fmt, codes, scales, values, stream)
+    if status != DQ_OK:
+        raise DartQuantError(status, "dq_mx_quantize")
 
 
 def dq_mx_dequantize(codes, scales, fmt: int, Y, stream=None):
     """Y ([rows, k]) = the values that codes and scales stand for."""
-    lib = _lib if _mx_device else _mx_load()
-    ptr, dtype, ld, rows, k, index = _mx_matrix(Y, "Y")
-    n_codes, n_scales = _mx_held(fmt, rows, k)
-    _mx_call(lib.dq_mx_dequantize, "dq_mx_dequantize", index, stream, fmt, _mx_bytes(codes, "codes", n_codes, index),
-             _mx_bytes(scales, "scales", n_scales, index), rows, k, ptr, dtype, ld)
+    status = (_calls or _mx()).dequantize(codes, scales, fmt, Y, stream)
+    if status != DQ_OK:
+        raise DartQuantError(status, "dq_mx_dequantize")
 
 
 def dq_rmsnorm_quantize(X, gamma, eps: float, fmt: int, codes, scales, residual=None, sum_out=None, values=None, stream=None):
     """h = X + residual; codes and scales of h / sqrt(mean(h^2) + eps) * gamma.  gamma: [k] of X's type or float32, or None.
     sum_out (may be X or residual) receives h, values the quantised output's values; all [rows, k] of X's type."""
-    lib = _lib if _mx_device else _mx_load()
-    ptr, dtype, ld, rows, k, index = _mx_matrix(X, "X")
-    n_codes, n_scales = _mx_held(fmt, rows, k)
-    r, ldr = _mx_like(residual, "residual", X, index)
-    h, lds = _mx_like(sum_out, "sum_out", X, index)
-    v, ldv = _mx_like(values, "values", X, index)
-    g, g_dtype = 0, dtype
-    if gamma is not None:
-        g_dtype = _MX_TYPES.get(gamma.dtype)
-        if gamma.shape != (k,) or (g_dtype != dtype and g_dtype != DQ_FP32):
-            raise ValueError("gamma: a [%d] tensor of X's type or float32 is needed" % k)
-        g = _mx_bytes(gamma, "gamma", 0, index)
-    _mx_call(lib.dq_rmsnorm_quantize, "dq_rmsnorm_quantize", index, stream, ptr, r, dtype, rows, k, ld, ldr, g, g_dtype, eps, fmt,
-             _mx_bytes(codes, "codes", n_codes, index), _mx_bytes(scales, "scales", n_scales, index), h, lds, v, ldv)
+    status = (_calls or _mx()).rmsnorm_quantize(X, gamma, eps, fmt, codes, scales, residual, sum_out, values, stream)
+    if status != DQ_OK:
+        raise DartQuantError(status, "dq_rmsnorm_quantize")
 
 
 def dq_mx_matmul(a_codes, a_scales, a_fmt: int, w_codes, w_scales, k: int, Y, stream=None):
     """Y ([m, n]) = A W^T for m rows of activations (DQ_MXFP4 or DQ_MXFP8) and n rows of DQ_MXFP4 weights, k values each."""
-    lib = _lib if _mx_device else _mx_load()
-    ptr, dtype, ld, m, n, index = _mx_matrix(Y, "Y")
-    a_n, a_s = _mx_held(a_fmt, m, k)
-    w_n, w_s = _mx_held(DQ_MXFP4, n, k)
-    _mx_call(lib.dq_mx_matmul, "dq_mx_matmul", index, stream, a_fmt, _mx_bytes(a_codes, "a_codes", a_n, index),
-             _mx_bytes(a_scales, "a_scales", a_s, index), m, _mx_bytes(w_codes, "w_codes", w_n, index),
-             _mx_bytes(w_scales, "w_scales", w_s, index), n, k, ptr, dtype, ld)
+    status = (_calls or _mx()).matmul(a_codes, a_scales, a_fmt, w_codes, w_scales, k, Y, stream)
+    if status != DQ_OK:
+        raise DartQuantError(status, "dq_mx_matmul")
 
 
 def dq_mx_linear(X, a_fmt: int, w_codes, w_scales, Y, workspace, stream=None):
     """Y ([m, n]) = quantised(X) W^T for activations X ([m, k]) and n rows of DQ_MXFP4 weights.  workspace: a buffer of
     dq_mx_linear_workspace(a_fmt, m, k) bytes."""
-    lib = _lib if _mx_device else _mx_load()
-    x, x_dtype, ldx, m, k, index = _mx_matrix(X, "X")
-    y, y_dtype, ldy, rows, n, y_index = _mx_matrix(Y, "Y")
-    if rows != m or y_index != index:
-        raise ValueError("Y: %d rows on X's device are needed" % m)
-    w_n, w_s = _mx_held(DQ_MXFP4, n, k)
-    a_n, a_s = _mx_held(a_fmt, m, k)
-    _mx_call(lib.dq_mx_linear, "dq_mx_linear", index, stream, x, x_dtype, m, k, ldx, a_fmt,
-             _mx_bytes(w_codes, "w_codes", w_n, index), _mx_bytes(w_scales, "w_scales", w_s, index), n, y, y_dtype, ldy,
-             _mx_bytes(workspace, "workspace", a_n + a_s, index))
+    status = (_calls or _mx()).linear(X, a_fmt, w_codes, w_scales, Y, workspace, stream)
+    if status != DQ_OK:
+        raise DartQuantError(status, "dq_mx_linear")
 
 
 def dq_mx_status(stream=None) -> int:

@@ -1,15 +1,17 @@
-"""Builds libdartquant.so (sm_100a only) in-tree with nvcc."""
+"""Builds libdartquant.so (sm_100a only, nvcc) and _calls.so (its Python calls, the host compiler) in-tree."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libdartquant.so")
+CALLS = os.path.join(HERE, "_calls.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.cu", "gemm_ffma.cu", "qr_forward.cu", "qr_backward.cu", "tc_path.cu", "qr_tc.cu", "qr_panel_tc.cu", "qr128.cu", "token_sampling.cu", "eval_metrics.cu", "cayley_tc.cu", "objectives.cu", "qr128_inc.cu", "qr128_tc5.cu", "mx_quant.cu", "mx_matmul.cu", "mx_api.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -24,9 +26,9 @@ def _nvcc() -> str:
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not (os.path.exists(LIB) and os.path.exists(CALLS)):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(INCLUDE, "dartquant.h")]
     return any(os.path.getmtime(p) > t for p in deps)
 
@@ -53,6 +55,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
                        capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stderr)
+    r = subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"],
+                        "-I", INCLUDE, os.path.join(CSRC, "py_calls.cpp"), "-o", CALLS], capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("host compiler failed for py_calls.cpp:\n" + r.stderr)
     return LIB
 
 

@@ -51,3 +51,27 @@ def test_refusals_come_before_any_cuda_call(lib):
     assert li(p, 1, 4, 64, 64, 0, p, p, 64, p, 1, 64, None, None) == bad
     assert li(p, 1, 4, 64, 64, 0, p, p, 64, p, 1, 64, p + 16, None) == big
     assert li(p, 1, 4, 64, 60, 0, p, p, 64, p, 1, 64, p, None) == bad
+
+
+def test_compiled_calls_check_their_arguments(lib):
+    """The Python calls' checks, with the lookups of device and stream replaced: no CUDA tensor, nothing is launched."""
+    import ctypes as C
+
+    import torch
+
+    from paper_2511_04063_b200 import _calls
+    names = ("dq_mx_quantize", "dq_mx_dequantize", "dq_rmsnorm_quantize", "dq_mx_matmul", "dq_mx_linear")
+    entries = tuple(C.cast(getattr(lib, n), C.c_void_p).value for n in names)
+    types = (torch.float32, torch.bfloat16, torch.float16)
+    with pytest.raises(TypeError):
+        _calls.bind(entries[:4], types, lambda: 0, lambda index: 0)
+    _calls.bind(entries, types, lambda: 0, lambda index: 0)
+    x, held = torch.zeros(4, 64), torch.zeros(4096, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="CUDA"):
+        _calls.quantize(x, 0, held, held, None, None)
+    with pytest.raises(ValueError, match="CUDA"):
+        _calls.matmul(held, held, 0, held, held, 64, x, None)
+    with pytest.raises(TypeError):
+        _calls.linear(x)
+    with pytest.raises(AttributeError):
+        _calls.rmsnorm_quantize(None, None, 1e-5, 0, held, held, None, None, None, None)
