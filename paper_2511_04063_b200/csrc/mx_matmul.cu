@@ -378,7 +378,14 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   }
   }
   tc_fence_before();
-  if (p.splits > 1) cluster_sync_all(); else __syncthreads();   // the peers have read this CTA's sums
+  if (p.splits > 1) {
+    // the peers have read this CTA's sums; nothing else is handed over (a release would wait for the stores to Y)
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  } else {
+    __syncthreads();
+  }
   if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, L::TMEM); }
 }
 
