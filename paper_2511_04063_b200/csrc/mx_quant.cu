@@ -82,32 +82,33 @@ struct Piece<T, false> {
 // neighbours, so a k tile's 16 scale bytes leave in one piece, and their four independent loads per lane are what keeps HBM
 // busy.  Every lane has read its values before it writes any, and reads no other lane's (!WHOLE: its warp has, and no other
 // warp's): the values may go back to where X lies.  A CTA's eight warps lie side by side, 2^wide of them along the columns.
+// NARROW: rows of at most 128 columns, the other half warp takes the next four rows.
 constexpr int Q_WARPS = 8;
-template <typename T, int FMT, bool WHOLE>
+template <typename T, int FMT, bool WHOLE, bool NARROW>
 __global__ void __launch_bounds__(32 * Q_WARPS)
 quantize_kernel(const T* X, int64_t rows, int k, int64_t ldx, int wide, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                 T* values, int64_t ldv) {
   __shared__ __align__(16) T turn[WHOLE ? 1 : Q_WARPS][WHOLE ? 8 : PIECE];
   wait_for_previous();
   allow_next();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, half = NARROW ? lane >> 4 : 0, place = NARROW ? lane & 15 : lane;
   const int ktiles = (k + KTILE - 1) / KTILE;
-  const int c0 = (((int)blockIdx.y << wide) + (warp & ((1 << wide) - 1))) * PIECE, c = c0 + lane * 8;
-  const int64_t g = (int64_t)blockIdx.x * (Q_WARPS >> wide) + (warp >> wide);
+  const int c0 = NARROW ? 0 : (((int)blockIdx.y << wide) + (warp & ((1 << wide) - 1))) * PIECE, c = c0 + place * 8;
+  const int64_t g = NARROW ? ((int64_t)blockIdx.x * Q_WARPS + warp) * 2 + half : (int64_t)blockIdx.x * (Q_WARPS >> wide) + (warp >> wide);
   const int64_t tile = rows < 32 ? 0 : g >> 5;
   const int64_t i = rows < 32 ? g : g & 31, r0 = tile * ROW_TILE + i;
-  if (c0 >= ktiles * KTILE || r0 >= rows) return;             // (whole warps)
-  const bool in = c < ktiles * KTILE;
+  if (c0 >= ktiles * KTILE || __all_sync(0xffffffffu, r0 >= rows)) return;   // (whole warps)
+  const bool in = c < ktiles * KTILE && r0 < rows;
   T* stage = turn[WHOLE ? 0 : warp];
   Vec8<T> v[4];
   {
     typename Piece<T, WHOLE>::Raw x[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (r0 + 32 * j < rows) Piece<T, WHOLE>::fetch(x[j], X + (r0 + 32 * j) * ldx, c0, k, lane);
+      if (r0 + 32 * j < rows) Piece<T, WHOLE>::fetch(x[j], X + (r0 + 32 * j) * ldx, c0, k, place);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (r0 + 32 * j < rows) v[j] = Piece<T, WHOLE>::turned(x[j], lane, stage);
+      if (r0 + 32 * j < rows) v[j] = Piece<T, WHOLE>::turned(x[j], place, stage);
       else v[j].clear();
     }
   }
@@ -127,7 +128,7 @@ quantize_kernel(const T* X, int64_t rows, int k, int64_t ldx, int wide, uint8_t*
       if (in) q.store(to + 32 * j * pitch);
       if (values) {
         q.decode(s, v[j]);
-        Piece<T, WHOLE>::store(v[j], values + (r0 + 32 * j) * ldv, c0, k, lane, stage);
+        Piece<T, WHOLE>::store(v[j], values + (r0 + 32 * j) * ldv, c0, k, place, stage);
       }
     }
   }
@@ -164,7 +165,8 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
 // ------------------------------------------------------------------------------------------------ norm
 // A row belongs to `warps` warps, each with V pieces of 256 columns that stay in registers between the sum of squares and the
 // scaling, so x and the residual are read once.  One warp a row: eight rows a CTA, no barrier; else one row a CTA.
-template <typename T, typename G, int FMT, int V, bool WHOLE>
+// NARROW (V = 1): rows of at most 128 columns, half a warp each.
+template <typename T, typename G, int FMT, int V, bool WHOLE, bool NARROW>
 __global__ void __launch_bounds__(V == 1 ? 1024 : 512)
 rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, int64_t ldr, const G* gamma, float eps,
                                uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, T* sum, int64_t lds, T* values, int64_t ldv,
@@ -173,9 +175,13 @@ rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, 
   __shared__ float part[32];
   wait_for_previous();
   allow_next();
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int64_t r = warps == 1 ? (int64_t)blockIdx.x * (blockDim.x >> 5) + w : blockIdx.x;
-  if (r >= rows) return;                                      // (whole warps; with more than one a row, whole CTAs)
+  static_assert(!NARROW || (WHOLE && V == 1), "narrow rows come in whole pieces");
+  const int w = threadIdx.x >> 5, lane = NARROW ? threadIdx.x & 15 : threadIdx.x & 31;
+  int64_t r = warps == 1 ? (int64_t)blockIdx.x * (blockDim.x >> 5) + w : blockIdx.x;
+  if (NARROW) r = r * 2 + (threadIdx.x >> 4 & 1);
+  if (__all_sync(0xffffffffu, r >= rows)) return;             // (whole warps; with more than one a row, whole CTAs)
+  const bool live = !NARROW || r < rows;                      // (the half of a last warp that has no row repeats the last one)
+  if (NARROW && !live) r = rows - 1;
   const int first = warps == 1 ? 0 : w;
   T* stage = reinterpret_cast<T*>(turn + (WHOLE ? 0 : w * 1024));
   G* g_stage = reinterpret_cast<G*>(stage);
@@ -209,7 +215,7 @@ rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, 
   for (int u = 0; u < V; ++u) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) ss = add2(ss, mul2(h[u][i], h[u][i]));
-    if (sum) {
+    if (sum && live) {
       Vec8<T> s;
 #pragma unroll
       for (int i = 0; i < 4; ++i) s.set_pair(i, h[u][i]);
@@ -218,7 +224,7 @@ rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, 
   }
   float all = ss.x + ss.y;
 #pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+  for (int o = NARROW ? 8 : 16; o >= 1; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
   if (warps > 1) {
     if (lane == 0) part[w] = all;
     __syncthreads();
@@ -253,9 +259,9 @@ rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, 
     uint32_t s = scale_code<FMT>(block_exponent(y.exponent()));
     Codes8<FMT> q;
     q.encode(y, s);
-    const bool in = c < ktiles * KTILE;
+    const bool in = c < ktiles * KTILE && live;
     if (in) q.store(to + c / 8 * Codes8<FMT>::BYTES);
-    if (values) {
+    if (values && live) {
       Vec8<T> d;
       q.decode(s, d);
       Piece<T, WHOLE>::store(d, values + r * ldv, c0, k, lane, stage);
@@ -303,15 +309,17 @@ dq_status quantize(cudaStream_t stream, const void* X, int x_dtype, int64_t rows
   const int64_t pieces = (k_tiles(k) * KTILE + PIECE - 1) / PIECE;
   const int64_t groups = rows < 32 ? rows : (rows + ROW_TILE - 1) / ROW_TILE * 32;
   const int wide = columns_wide(pieces);
+  const bool narrow = whole && k <= KTILE;
   LaunchConfig c(stream, 1, 32 * Q_WARPS);
-  DQ_CHECK(grid(c, pieces, groups, wide));
+  DQ_CHECK(grid(c, pieces, narrow ? (groups + 1) / 2 : groups, wide));
   return by_type(x_dtype, [&](auto t) {
     using T = decltype(t);
     return by_format(fmt, [&](auto f) {
-      return by_flag(whole, [&](auto v) {
-        return launch(c, quantize_kernel<T, decltype(f)::value, decltype(v)::value>, (const T*)X, rows, (int)k, ldx, wide, codes,
-                      scales, (T*)values, ldv);
-      });
+      constexpr int FMT = decltype(f)::value;
+      auto run = [&](auto kern) { return launch(c, kern, (const T*)X, rows, (int)k, ldx, wide, codes, scales, (T*)values, ldv); };
+      if (narrow) return run(quantize_kernel<T, FMT, true, true>);
+      if (whole) return run(quantize_kernel<T, FMT, true, false>);
+      return run(quantize_kernel<T, FMT, false, false>);
     });
   });
 }
@@ -350,7 +358,8 @@ dq_status rmsnorm_quantize(cudaStream_t stream, const void* X, int dtype, int64_
                 : pieces == 2 || (pieces <= 32 && (few || !whole)) ? 2 : pieces <= 64 ? 4 : 8;
   const int warps = (pieces + V - 1) / V;
   const int threads = warps == 1 ? 256 : warps * 32;
-  const int64_t ctas = warps == 1 ? (rows + 7) / 8 : rows;
+  const bool narrow = whole && k <= KTILE;
+  const int64_t ctas = warps > 1 ? rows : narrow ? (rows + 15) / 16 : (rows + 7) / 8;
   LaunchConfig c(stream, ctas, threads, whole ? 0 : threads * 32);
   return by_type(dtype, [&](auto t) {
     using T = decltype(t);
@@ -365,10 +374,13 @@ dq_status rmsnorm_quantize(cudaStream_t stream, const void* X, int dtype, int64_
         };
         auto with_gamma = [&](auto g) {
           using G = decltype(g);
-          if (V == 1) return run(g, rmsnorm_kernel<T, G, FMT, 1, WHOLE>);
-          if (V == 2) return run(g, rmsnorm_kernel<T, G, FMT, 2, WHOLE>);
-          if (V == 4) return run(g, rmsnorm_kernel<T, G, FMT, 4, WHOLE>);
-          return run(g, rmsnorm_kernel<T, G, FMT, 8, WHOLE>);
+          if constexpr (WHOLE) {
+            if (narrow) return run(g, rmsnorm_kernel<T, G, FMT, 1, true, true>);
+          }
+          if (V == 1) return run(g, rmsnorm_kernel<T, G, FMT, 1, WHOLE, false>);
+          if (V == 2) return run(g, rmsnorm_kernel<T, G, FMT, 2, WHOLE, false>);
+          if (V == 4) return run(g, rmsnorm_kernel<T, G, FMT, 4, WHOLE, false>);
+          return run(g, rmsnorm_kernel<T, G, FMT, 8, WHOLE, false>);
         };
         if (gamma && gamma_dtype == DQ_FP32) return with_gamma(float{});
         return with_gamma(T{});
