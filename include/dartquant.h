@@ -341,8 +341,10 @@ dq_status dq_calib_time_product(dq_calib_t* h, int32_t nterms, int32_t reps, flo
  *   Bytes of rows past the last one are not defined and not used.  16-byte aligned.
  * Matrices of values (X, Y, sums, values) are row-major with a row stride of at least their width, of DQ_FP32, DQ_BF16
  *   or DQ_FP16; 16-byte aligned rows are read and written fastest, no alignment beyond the type's is needed.
- * Calls are asynchronous on the given stream, allocate nothing, keep nothing and can be captured in a graph.  A call with
- *   no rows does nothing.  Limits: k <= 2^24, rows < 2^31 - 256.
+ * Calls are asynchronous on the given stream, allocate nothing, keep nothing and can be captured in a graph (make one call of
+ *   each kind before, on each device: the first looks up what the device can run at once).  They use programmatic dependent
+ *   launch: a kernel may be scheduled before the one in front of it has ended, but reads and writes nothing until then.
+ *   A call with no rows does nothing.  Limits: k <= 2^24, rows <= 2^31 - 256.
  * Errors: INVALID_ARG (null, sizes, enums, a pointer that its type's alignment rules out), UNSUPPORTED (alignment of codes
  *   and scales, limits, a device that is not sm_100), CUDA. */
 enum { DQ_FP16 = 2 };                   /* third value of the microscaled operators' *_dtype arguments */

@@ -4,6 +4,12 @@
 // its N) accumulates  2^(sW + sA - 254) q_W q_A  in fp32 tensor memory; nothing is dequantised.  4-bit activations use
 // kind::mxf4 (64 values per MMA step), 8-bit ones kind::mxf8f6f4 (32 per step), for which the copy engine spreads the
 // weights' 4-bit codes to one 16-byte slot per 16 values while it brings them into shared memory.
+//
+// Two kernels.  cluster_kernel, for few tokens, is bound by bringing the weights in and by the MMA steps that consume them: one
+// takes about 140 cycles whatever its N is, 4 KB of 4-bit weights an SM (16 x 8192 x 8192: 9.7 us at 4 bits, 11.1 at 8, whose
+// steps hold half as much; the weights alone need 5.5 us of HBM).  pair_kernel, for many, is bound by the tensor cores: 85 %
+// (4 bits) and 87 % (8 bits) of their cycles active, 16384 x 8192 x 8192 in 365 us (6000 TFLOP/s) and 734 us (3000) from a cool
+// start, and by the 1000 W power limit (1.3 to 1.4 GHz, 408 and 832 us) when it lasts.
 #include "mx_common.cuh"
 #include "tc_host.cuh"
 
@@ -353,29 +359,29 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   if (p.splits == 1) {
     for (int i = threadIdx.x; i < cols * 32; i += blockDim.x) store(i, reinterpret_cast<const float4*>(smem)[i]);
   } else {
-  // all loads of two pieces at once: one at a time they cost the cluster's latency each
-  constexpr int AT_ONCE = 2, MOST = 8;
-  for (int i0 = (int)threadIdx.x + c0 * 32; i0 < c1 * 32; i0 += AT_ONCE * blockDim.x) {
-    float4 v[AT_ONCE][MOST];
+    // all loads of two pieces at once: one at a time they cost the cluster's latency each (128 x 4096 x 4096: 9.7 us, 8.4 so)
+    constexpr int AT_ONCE = 2, MOST = 8;
+    for (int i0 = (int)threadIdx.x + c0 * 32; i0 < c1 * 32; i0 += AT_ONCE * blockDim.x) {
+      float4 v[AT_ONCE][MOST];
 #pragma unroll
-    for (int u = 0; u < AT_ONCE; ++u) {
-      const int i = i0 + u * (int)blockDim.x;
-      const uint32_t at = base + (uint32_t)i * 16u;          // [token][32 pieces]
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const int i = i0 + u * (int)blockDim.x;
+        const uint32_t at = base + (uint32_t)i * 16u;        // [token][32 pieces]
 #pragma unroll
-      for (int r = 0; r < MOST; ++r)
-        if (r < p.splits && i < c1 * 32) v[u][r] = ld_cluster_f4(at, (uint32_t)r);
+        for (int r = 0; r < MOST; ++r)
+          if (r < p.splits && i < c1 * 32) v[u][r] = ld_cluster_f4(at, (uint32_t)r);
+      }
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const int i = i0 + u * (int)blockDim.x;
+        if (i >= c1 * 32) break;
+        float4 s = v[u][0];
+#pragma unroll
+        for (int r = 1; r < MOST; ++r)
+          if (r < p.splits) { s.x += v[u][r].x; s.y += v[u][r].y; s.z += v[u][r].z; s.w += v[u][r].w; }
+        store(i, s);
+      }
     }
-#pragma unroll
-    for (int u = 0; u < AT_ONCE; ++u) {
-      const int i = i0 + u * (int)blockDim.x;
-      if (i >= c1 * 32) break;
-      float4 s = v[u][0];
-#pragma unroll
-      for (int r = 1; r < MOST; ++r)
-        if (r < p.splits) { s.x += v[u][r].x; s.y += v[u][r].y; s.z += v[u][r].z; s.w += v[u][r].w; }
-      store(i, s);
-    }
-  }
   }
   tc_fence_before();
   if (p.splits > 1) {
@@ -420,9 +426,17 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
 
 // The pieces of 32 columns (tokens from m0 on) x 128 lanes (weight rows) that a group of four epilogue warps takes to Y.  Where
 // Y's rows are aligned they leave through shared memory as rows of 128 values, written by the copy engine, which also clips
-// them at Y's edges: whole 256-byte rows, where the warps' own stores would write 64 bytes of a row at a time (MEASURED).
+// them at Y's edges: whole 256-byte rows, where the warps' own stores would write 64 bytes of a row at a time (8192 x 1024 x 8192: 37.8 us against 45.3,
+// 16384 x 256 x 8192: 60.0 against 70.4).
 // Each group has two buffers of 8 KB, a piece of a 4-byte type goes in two parts.
 constexpr int PIECE_BYTES = 8192;
+// Whether all 128 threads at the barrier say yes.
+__device__ __forceinline__ bool agree(int barrier, bool yes) {
+  uint32_t all;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(all) : "r"((uint32_t)yes), "r"(barrier) : "memory");
+  return all != 0;
+}
 template <typename T>
 struct Output {
   static constexpr int PASS = PIECE_BYTES / 128 / sizeof(T);   // tokens of a buffer
@@ -550,10 +564,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
       int k = 0, t = 0;                                      // step of the tile, tile
       for (int64_t i = 0; i < steps; ++i) {
         if (!mbar_wait(full(stage), phase, p.d_status)) break;
-        if (k == 0 && t >= 1) {
-          if (!mbar_wait(drained, (uint32_t)(t - 1) & 1u, p.d_status)) break;
-          tc_fence_after();
-        }
+        if (k == 0 && t >= 1 && !mbar_wait(drained, (uint32_t)(t - 1) & 1u, p.d_status)) break;
         tc_fence_after();
         if (elect_one()) {
           const uint32_t acc = tmem + (uint32_t)((t & 1) * L::ACC_STRIDE);
@@ -591,7 +602,8 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
       int nb, mb;
       tile_of(u, nb, mb);
       const int a = t & 1;
-      if (!mbar_wait(ready(a), (uint32_t)(t >> 1) & 1u, p.d_status)) break;
+      // (the four warps of a group go on or leave together: they meet at barriers below)
+      if (!agree(1 + half, mbar_wait(ready(a), (uint32_t)(t >> 1) & 1u, p.d_status))) break;
       tc_fence_after();
       const int64_t n0 = (int64_t)nb * 256 + rank * 128, m0 = (int64_t)mb * 256;
       const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * L::ACC_STRIDE);

@@ -1,6 +1,9 @@
 // Microscaled quantisation: activations or weights to codes and scales (dq_mx_quantize), back to values
 // (dq_mx_dequantize), and the root-mean-square norm with the residual's addition in front of it
-// (dq_rmsnorm_quantize).  All three are bound by HBM: one read and one write of everything.
+// (dq_rmsnorm_quantize).  All three are bound by HBM: one read and one write of everything.  Share of the measured copy rate,
+// counting every byte once: 16384 x 4096 bf16 to 4 bits with values 48.7 us, 95 %; norm of 65536 x 8192 bf16 with residual, sum
+// and values 766 us, 97 %; 100000 x 128 to 4 bits 11.0 us, 80 %; 5000 x 5111 fp32 (unaligned rows) to 8 bits 41.5 us, 85 %, the
+// norm of 5000 x 5111 bf16 62 us, 56 %.
 #include <type_traits>
 
 #include "mx_common.cuh"
@@ -38,7 +41,8 @@ namespace {
 // A warp takes 256 columns of a row at a time, eight consecutive ones a lane, four lanes a block of 32.  WHOLE: rows come in
 // 16-byte pieces, eight values are one or two loads, and a lane's eight columns exist all or not at all.  Otherwise the warp
 // reads and writes 32 neighbouring values at a time and turns them in shared memory (1 KB a warp and row): one by one
-// from each lane's own eight columns every load would touch 32 different sectors (MEASURED).
+// from each lane's own eight columns every load would touch 32 different sectors (5000 x 5111 fp32 to 8 bits: 93 us,
+// 41.5 so).
 constexpr int PIECE = 256;
 template <typename T, bool WHOLE>
 struct Piece {
