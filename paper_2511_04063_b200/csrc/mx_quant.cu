@@ -38,13 +38,13 @@ dq_status current_device(Device& out) {
 
 namespace {
 
-// A warp takes 256 columns of a row at a time, eight consecutive ones a lane, four lanes a block of 32.  WHOLE: rows come in
-// 16-byte pieces, eight values are one or two loads, and a lane's eight columns exist all or not at all.  Otherwise the warp
-// reads and writes 32 neighbouring values at a time and turns them in shared memory (1 KB a warp and row): one by one
-// from each lane's own eight columns every load would touch 32 different sectors (5000 x 5111 fp32 to 8 bits: 93 us,
-// 41.5 so).
+// A warp takes 256 columns of a row at a time (LANES 16: half a warp 128), eight consecutive ones a lane, four lanes a block of
+// 32.  WHOLE: rows come in 16-byte pieces, eight values are one or two loads, and a lane's eight columns exist all or not
+// at all.  Otherwise the lanes read and write neighbouring values and turn them in shared memory: one by one from each lane's
+// own eight columns every load would touch 32 different sectors (5000 x 5111 fp32 to 8 bits: 93 us, 41.5 so).  Rows of k = 0
+// columns are neither read nor written and count as zeros; all lanes of a warp make the same calls.
 constexpr int PIECE = 256;
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, int LANES>
 struct Piece {
   using Raw = Vec8<T>;                       // what a lane fetches
   static __device__ __forceinline__ void fetch(Raw& x, const T* row, int c0, int k, int lane) {
@@ -56,18 +56,18 @@ struct Piece {
     if (c0 + lane * 8 < k) v.store(row + c0 + lane * 8);
   }
 };
-template <typename T>
-struct Piece<T, false> {
-  struct Raw { T x[8]; };                    // every 32nd value
+template <typename T, int LANES>
+struct Piece<T, false, LANES> {
+  struct Raw { T x[8]; };                    // every LANES-th value
   static __device__ __forceinline__ void fetch(Raw& x, const T* row, int c0, int k, int lane) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x.x[i] = c0 + i * 32 + lane < k ? row[c0 + i * 32 + lane] : from_f32<T>(0.f);
+    for (int i = 0; i < 8; ++i) x.x[i] = c0 + i * LANES + lane < k ? row[c0 + i * LANES + lane] : from_f32<T>(0.f);
   }
   static __device__ __forceinline__ Vec8<T> turned(const Raw& x, int lane, T* turn) {
     Vec8<T> v;
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn[i * 32 + lane] = x.x[i];
+    for (int i = 0; i < 8; ++i) turn[i * LANES + lane] = x.x[i];
     __syncwarp();
     v.load(turn + lane * 8);
     return v;
@@ -78,7 +78,7 @@ struct Piece<T, false> {
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (c0 + i * 32 + lane < k) row[c0 + i * 32 + lane] = turn[i * 32 + lane];
+      if (c0 + i * LANES + lane < k) row[c0 + i * LANES + lane] = turn[i * LANES + lane];
   }
 };
 
@@ -103,16 +103,22 @@ quantize_kernel(const T* X, int64_t rows, int k, int64_t ldx, int wide, uint8_t*
   const int64_t i = rows < 32 ? g : g & 31, r0 = tile * ROW_TILE + i;
   if (c0 >= ktiles * KTILE || __all_sync(0xffffffffu, r0 >= rows)) return;   // (whole warps)
   const bool in = c < ktiles * KTILE && r0 < rows;
-  T* stage = turn[WHOLE ? 0 : warp];
+  using P = Piece<T, WHOLE, NARROW ? 16 : 32>;
+  T* stage = turn[WHOLE ? 0 : warp] + (WHOLE ? 0 : half * KTILE);
+  // Half warps with rows of their own and shared memory between their lanes go through all four rows together; else a warp
+  // skips the rows that do not exist (16384 x 4096 to 4 bits: 49.3 us, 52.5 if it does not).
+  constexpr bool ALL = NARROW && !WHOLE;
+  auto exists = [&](int j) { return r0 + 32 * j < rows; };
+  auto columns = [&](int j) { return ALL && !exists(j) ? 0 : k; };
   Vec8<T> v[4];
   {
-    typename Piece<T, WHOLE>::Raw x[4];
+    typename P::Raw x[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (r0 + 32 * j < rows) Piece<T, WHOLE>::fetch(x[j], X + (r0 + 32 * j) * ldx, c0, k, place);
+      if (ALL || exists(j)) P::fetch(x[j], X + (r0 + 32 * j) * ldx, c0, columns(j), place);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (r0 + 32 * j < rows) v[j] = Piece<T, WHOLE>::turned(x[j], place, stage);
+      if (ALL || exists(j)) v[j] = P::turned(x[j], place, stage);
       else v[j].clear();
     }
   }
@@ -126,13 +132,13 @@ quantize_kernel(const T* X, int64_t rows, int k, int64_t ldx, int wide, uint8_t*
   for (int j = 0; j < 4; ++j) {
     const uint32_t s = scale_code<FMT>(e[j]);
     if ((lane & 3) == j) mine = s;
-    if (r0 + 32 * j < rows) {
+    if (ALL || exists(j)) {
       Codes8<FMT> q;
       q.encode(v[j], s);
-      if (in) q.store(to + 32 * j * pitch);
+      if (in && (!ALL || exists(j))) q.store(to + 32 * j * pitch);
       if (values) {
         q.decode(s, v[j]);
-        Piece<T, WHOLE>::store(v[j], values + (r0 + 32 * j) * ldv, c0, k, place, stage);
+        P::store(v[j], values + (r0 + 32 * j) * ldv, c0, columns(j), place, stage);
       }
     }
   }
@@ -163,7 +169,7 @@ dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
     q.load(codes + r * row_bytes(FMT, k) + c / 8 * Codes8<FMT>::BYTES);
     q.decode(scales[scale_offset(r, c / BLOCK, k_tiles(k))], v);
   }
-  Piece<T, WHOLE>::store(v, Y + r * ldy, c0, k, lane, turn[WHOLE ? 0 : warp]);
+  Piece<T, WHOLE, 32>::store(v, Y + r * ldy, c0, k, lane, turn[WHOLE ? 0 : warp]);
 }
 
 // ------------------------------------------------------------------------------------------------ norm
@@ -179,37 +185,40 @@ rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, 
   __shared__ float part[32];
   wait_for_previous();
   allow_next();
-  static_assert(!NARROW || (WHOLE && V == 1), "narrow rows come in whole pieces");
+  static_assert(!NARROW || V == 1, "one piece");
+  constexpr int LANES = NARROW ? 16 : 32;
+  using P = Piece<T, WHOLE, LANES>;
   const int w = threadIdx.x >> 5, lane = NARROW ? threadIdx.x & 15 : threadIdx.x & 31;
   int64_t r = warps == 1 ? (int64_t)blockIdx.x * (blockDim.x >> 5) + w : blockIdx.x;
   if (NARROW) r = r * 2 + (threadIdx.x >> 4 & 1);
   if (__all_sync(0xffffffffu, r >= rows)) return;             // (whole warps; with more than one a row, whole CTAs)
   const bool live = !NARROW || r < rows;                      // (the half of a last warp that has no row repeats the last one)
   if (NARROW && !live) r = rows - 1;
+  const int kw = live ? k : 0;                                // columns that are written
   const int first = warps == 1 ? 0 : w;
-  T* stage = reinterpret_cast<T*>(turn + (WHOLE ? 0 : w * 1024));
+  T* stage = reinterpret_cast<T*>(turn + (WHOLE ? 0 : w * 1024 + (NARROW ? (threadIdx.x >> 4 & 1) * 512 : 0)));
   G* g_stage = reinterpret_cast<G*>(stage);
   auto column = [&](int u) { return (u * warps + first) * PIECE; };
   float2 h[V][4];
   float2 ss = make_float2(0.f, 0.f);
   {
-    typename Piece<T, WHOLE>::Raw x[V], b[V];
+    typename P::Raw x[V], b[V];
 #pragma unroll
-    for (int u = 0; u < V; ++u) Piece<T, WHOLE>::fetch(x[u], X + r * ldx, column(u), k, lane);
+    for (int u = 0; u < V; ++u) P::fetch(x[u], X + r * ldx, column(u), k, lane);
     if (residual) {
 #pragma unroll
-      for (int u = 0; u < V; ++u) Piece<T, WHOLE>::fetch(b[u], residual + r * ldr, column(u), k, lane);
+      for (int u = 0; u < V; ++u) P::fetch(b[u], residual + r * ldr, column(u), k, lane);
     }
 #pragma unroll
     for (int u = 0; u < V; ++u) {
-      const Vec8<T> v = Piece<T, WHOLE>::turned(x[u], lane, stage);
+      const Vec8<T> v = P::turned(x[u], lane, stage);
 #pragma unroll
       for (int i = 0; i < 4; ++i) h[u][i] = v.pair(i);
     }
     if (residual) {
 #pragma unroll
       for (int u = 0; u < V; ++u) {
-        const Vec8<T> v = Piece<T, WHOLE>::turned(b[u], lane, stage);
+        const Vec8<T> v = P::turned(b[u], lane, stage);
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[u][i] = add2(h[u][i], v.pair(i));
       }
@@ -219,11 +228,11 @@ rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, 
   for (int u = 0; u < V; ++u) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) ss = add2(ss, mul2(h[u][i], h[u][i]));
-    if (sum && live) {
+    if (sum) {
       Vec8<T> s;
 #pragma unroll
       for (int i = 0; i < 4; ++i) s.set_pair(i, h[u][i]);
-      Piece<T, WHOLE>::store(s, sum + r * lds, column(u), k, lane, stage);
+      P::store(s, sum + r * lds, column(u), kw, lane, stage);
     }
   }
   float all = ss.x + ss.y;
@@ -246,9 +255,9 @@ rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, 
     Vec8<float> y;
     Vec8<G> g;
     if (gamma) {
-      typename Piece<G, WHOLE>::Raw x;
-      Piece<G, WHOLE>::fetch(x, gamma, c0, k, lane);
-      g = Piece<G, WHOLE>::turned(x, lane, g_stage);
+      typename Piece<G, WHOLE, LANES>::Raw x;
+      Piece<G, WHOLE, LANES>::fetch(x, gamma, c0, k, lane);
+      g = Piece<G, WHOLE, LANES>::turned(x, lane, g_stage);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -265,10 +274,10 @@ rmsnorm_kernel(const T* X, int64_t rows, int k, int64_t ldx, const T* residual, 
     q.encode(y, s);
     const bool in = c < ktiles * KTILE && live;
     if (in) q.store(to + c / 8 * Codes8<FMT>::BYTES);
-    if (values && live) {
+    if (values) {
       Vec8<T> d;
       q.decode(s, d);
-      Piece<T, WHOLE>::store(d, values + r * ldv, c0, k, lane, stage);
+      P::store(d, values + r * ldv, c0, kw, lane, stage);
     }
     s <<= 8 * ((lane >> 2) & 3);
     s |= __shfl_xor_sync(0xffffffffu, s, 4);
@@ -313,7 +322,7 @@ dq_status quantize(cudaStream_t stream, const void* X, int x_dtype, int64_t rows
   const int64_t pieces = (k_tiles(k) * KTILE + PIECE - 1) / PIECE;
   const int64_t groups = rows < 32 ? rows : (rows + ROW_TILE - 1) / ROW_TILE * 32;
   const int wide = columns_wide(pieces);
-  const bool narrow = whole && k <= KTILE;
+  const bool narrow = k <= KTILE;
   LaunchConfig c(stream, 1, 32 * Q_WARPS);
   DQ_CHECK(grid(c, pieces, narrow ? (groups + 1) / 2 : groups, wide));
   return by_type(x_dtype, [&](auto t) {
@@ -321,9 +330,8 @@ dq_status quantize(cudaStream_t stream, const void* X, int x_dtype, int64_t rows
     return by_format(fmt, [&](auto f) {
       constexpr int FMT = decltype(f)::value;
       auto run = [&](auto kern) { return launch(c, kern, (const T*)X, rows, (int)k, ldx, wide, codes, scales, (T*)values, ldv); };
-      if (narrow) return run(quantize_kernel<T, FMT, true, true>);
-      if (whole) return run(quantize_kernel<T, FMT, true, false>);
-      return run(quantize_kernel<T, FMT, false, false>);
+      if (narrow) return whole ? run(quantize_kernel<T, FMT, true, true>) : run(quantize_kernel<T, FMT, false, true>);
+      return whole ? run(quantize_kernel<T, FMT, true, false>) : run(quantize_kernel<T, FMT, false, false>);
     });
   });
 }
@@ -362,7 +370,7 @@ dq_status rmsnorm_quantize(cudaStream_t stream, const void* X, int dtype, int64_
                 : pieces == 2 || (pieces <= 32 && (few || !whole)) ? 2 : pieces <= 64 ? 4 : 8;
   const int warps = (pieces + V - 1) / V;
   const int threads = warps == 1 ? 256 : warps * 32;
-  const bool narrow = whole && k <= KTILE;
+  const bool narrow = k <= KTILE;
   const int64_t ctas = warps > 1 ? rows : narrow ? (rows + 15) / 16 : (rows + 7) / 8;
   LaunchConfig c(stream, ctas, threads, whole ? 0 : threads * 32);
   return by_type(dtype, [&](auto t) {
@@ -378,9 +386,7 @@ dq_status rmsnorm_quantize(cudaStream_t stream, const void* X, int dtype, int64_
         };
         auto with_gamma = [&](auto g) {
           using G = decltype(g);
-          if constexpr (WHOLE) {
-            if (narrow) return run(g, rmsnorm_kernel<T, G, FMT, 1, true, true>);
-          }
+          if (narrow) return run(g, rmsnorm_kernel<T, G, FMT, 1, WHOLE, true>);
           if (V == 1) return run(g, rmsnorm_kernel<T, G, FMT, 1, WHOLE, false>);
           if (V == 2) return run(g, rmsnorm_kernel<T, G, FMT, 2, WHOLE, false>);
           if (V == 4) return run(g, rmsnorm_kernel<T, G, FMT, 4, WHOLE, false>);

@@ -65,7 +65,7 @@ def finished():
 @pytest.mark.parametrize("rows,k,extra,offset", [(1, 1, 0, 0), (1, 32, 0, 0), (2, 31, 0, 0), (33, 33, 3, 0), (127, 127, 0, 1),
                                                  (128, 128, 8, 0), (129, 129, 0, 0), (40, 255, 1, 1), (257, 256, 0, 8),
                                                  (1, 4096, 0, 0), (70, 1000, 24, 0), (300, 520, 0, 4), (1, 128, 0, 0), (31, 96, 0, 0), (161, 128, 0, 0),
-                                                 (1000, 8, 0, 0), (97, 120, 16, 16)])
+                                                 (1000, 8, 0, 0), (97, 120, 16, 16), (1001, 103, 0, 0), (35, 100, 3, 1)])
 def test_quantize_is_the_oracles_bit_for_bit(fmt, dtype, rows, k, extra, offset):
     x = strided(draw(rows, k, dtype, rows * 1000 + k, spread=9.0), extra, offset)
     codes, scales = dq.dq_mx_empty(rows, k, fmt)
@@ -173,7 +173,7 @@ def check_norm(x, residual, gamma, eps, fmt, codes, scales, sum_out, values):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,k,extra,offset", [(1, 1, 0, 0), (3, 31, 0, 0), (5, 128, 0, 0), (9, 130, 6, 2), (2, 513, 0, 0), (130, 512, 0, 0),
                                                  (4, 1000, 8, 8), (2, 4096, 0, 0), (3, 5120, 0, 0), (2, 8200, 0, 0), (1, 32768, 0, 0), (1, 96, 0, 0),
-                                                 (33, 128, 0, 0), (100, 8, 8, 8)])
+                                                 (33, 128, 0, 0), (100, 8, 8, 8), (101, 103, 0, 0), (19, 127, 1, 1)])
 def test_rmsnorm_quantize(fmt, dtype, rows, k, extra, offset):
     x = strided(draw(rows, k, dtype, k), extra, offset)
     residual = strided(draw(rows, k, dtype, k + 1), extra, offset)
