@@ -164,42 +164,46 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, uint32_t rank) {
 }
 
 // Rows [0, m) x values [c0, c0 + 8 groups) of X as a CTA's resident operand: codes of step i at codes + i X_BYTES in the K-major
-// 128-byte-swizzled order of the MMA's operands, its scale tiles at scales + i SF_BYTES.
+// 128-byte-swizzled order of the MMA's operands, its scale tiles at scales + i SF_BYTES.  A warp takes 256 values of a row at
+// a time, the `warps` warps in turn.
 template <int BN, bool A8, typename T>
-__device__ __forceinline__ void quantize_resident(const Params& p, uint8_t* codes, uint8_t* scales, int c0, int groups, int t, int threads) {
+__device__ __forceinline__ void quantize_resident(const Params& p, uint8_t* codes, uint8_t* scales, int c0, int groups, int warp, int warps,
+                                                  int lane) {
   using L = ClusterSmem<BN, A8, true>;
   constexpr int FMT = A8 ? DQ_MXFP8 : DQ_MXFP4, BYTES = Codes8<FMT>::BYTES, PER_STEP = 128 / BYTES;
-  const T* X = reinterpret_cast<const T*>(p.x);
-  const int total = (int)p.m * groups;                       // a multiple of 16: the lanes of a block stay together
   constexpr int AT_ONCE = 4;
-  for (int i0 = t; i0 < (total + 31) / 32 * 32; i0 += AT_ONCE * threads) {
+  const T* X = reinterpret_cast<const T*>(p.x);
+  const int pieces = (groups + 31) / 32, m = (int)p.m;
+  int row = warp / pieces, piece = warp % pieces;            // of the next load; then of the next store
+  auto step_on = [&](int& r, int& c) {
+    for (c += warps; c >= pieces; c -= pieces) ++r;
+  };
+  while (row < m) {
     Vec8<T> v[AT_ONCE];
+    int r = row, c = piece;
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
-      const int i = i0 + u * threads;
+      const int at = c0 + (c * 32 + lane) * 8;
       v[u].clear();
-      if (i < total) {
-        const T* row = X + (int64_t)(i / groups) * p.ldx;
-        const int c = c0 + i % groups * 8;
-        if (!p.x_vec) load_each(v[u], row, c, (int)p.k);
-        else if (c < p.k) v[u].load(row + c);
+      if (r < m && c * 32 + lane < groups) {
+        if (!p.x_vec) load_each(v[u], X + r * p.ldx, at, (int)p.k);
+        else if (at < p.k) v[u].load(X + r * p.ldx + at);
       }
+      step_on(r, c);
     }
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
-      const int i = i0 + u * threads;
-      if (i - (t & 31) >= total) break;                      // (whole warps)
+      if (row >= m) break;                                   // (whole warps)
       const uint32_t s = scale_code<FMT>(block_exponent(v[u].exponent()));
       Codes8<FMT> q;
       q.encode(v[u], s);
-      if (i < total) {
-        const int row = i / groups, g = i % groups, step = g / PER_STEP, byte = g % PER_STEP * BYTES;
+      const int g = piece * 32 + lane;
+      if (g < groups) {
+        const int step = g / PER_STEP, byte = g % PER_STEP * BYTES, block = g / 4;
         q.store(codes + step * L::X_BYTES + row * 128 + ((((byte >> 4) ^ row) & 7) << 4) + (byte & 15));
-        if ((i & 3) == 0) {
-          const int block = g / 4;
-          scales[block / 4 * TILE_BYTES + (row & 31) * 16 + (row >> 5) * 4 + (block & 3)] = (uint8_t)s;
-        }
+        if ((lane & 3) == 0) scales[block / 4 * TILE_BYTES + (row & 31) * 16 + (row >> 5) * 4 + (block & 3)] = (uint8_t)s;
       }
+      step_on(row, piece);
     }
   }
 }
@@ -229,7 +233,7 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     mbar_init(done, 1);
-    mbar_init(held, 8);
+    mbar_init(held, L::THREADS / 32 - 2);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_tensormap(&map_w); prefetch_tensormap(&map_ws);
     if (!FUSED) { prefetch_tensormap(&map_x); prefetch_tensormap(&map_xs); }
@@ -318,7 +322,7 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
       wait_for_previous();
       const int values = A8 ? 128 : 256;                     // of a step
       quantize_resident<BN, A8, T>(p, smem + (res - base), smem + (res_sf - base), k0 * values, kn * (values / 8),
-                                   (int)threadIdx.x - 64, L::THREADS - 64);
+                                   warp - 2, L::THREADS / 32 - 2, lane);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(held);
@@ -740,6 +744,8 @@ dq_status launch_cluster(cudaStream_t stream, const Device& dev, const Operands&
   DQ_CHECK((choose_splits<BN, A8, FUSED, T>(dev, tiles, p.stages, p.splits)));
   const int smem = cluster_smem<BN, A8, FUSED>(p.stages, p.splits);
   if (tiles * p.splits > 0x7fffffff || smem > MAX_SMEM) return DQ_ERR_UNSUPPORTED;
+  // FUSED: more than 8192 values a CTA cost more than the launch that they save (linear says how much)
+  if (FUSED && o.m > 1 && o.m * ((p.stages + p.splits - 1) / p.splits) * (L::KT * KTILE) > 8192) return DQ_ERR_UNSUPPORTED;
   DQ_CHECK(codes_map(&w, o.w_codes, DQ_MXFP4, o.n, o.k, 128, A8));
   DQ_CHECK(scales_map(&ws, o.w_scales, o.n, o.k, L::KT, 1));
   if (!FUSED) {
@@ -829,13 +835,14 @@ dq_status linear(cudaStream_t stream, const void* X, int x_dtype, int64_t m, int
   DQ_CHECK(current_device(dev));
   uint8_t* scales = workspace + m * row_bytes(a_fmt, k);
   Operands o{a_fmt, workspace, scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy};
-  // Few tokens are quantised by the product's own CTAs, each the part that it multiplies; from five on the CTAs' repeated work costs
-  // more than a launch (4096 x 4096: 1 token 5.4 us against 6.9 in two launches, 4 tokens 6.2 against 6.9, 16 tokens 8.7 against 7.0).
-  if (m <= 4) {
+  // Few tokens are quantised by the product's own CTAs, each the part that it multiplies, where that part is small: the CTAs of
+  // all weight tiles repeat the work (4096 x 4096, 1024 values a token and CTA: 1 token 5.4 us against 6.7 in two launches, 8
+  // tokens 6.5 against 6.8, 16 tokens 8.2 against 6.9; 1024 x 4096, 256 values: 16 tokens 4.4 against 5.0).
+  if (m <= 16) {
     o.x = X; o.ldx = ldx;
     o.x_vec = whole_pieces(X, ldx, k, x_dtype);
     const dq_status st = a_fmt == DQ_MXFP4 ? fused<false>(stream, dev, o, x_dtype) : fused<true>(stream, dev, o, x_dtype);
-    if (st != DQ_ERR_UNSUPPORTED) return st;                 // (too long a reduction for its tokens to stay in shared memory)
+    if (st != DQ_ERR_UNSUPPORTED) return st;                 // (too many values for that, or for their shared memory)
   }
   DQ_CHECK(quantize(stream, X, x_dtype, m, k, ldx, a_fmt, workspace, scales, nullptr, 0));
   o.weights_first = true;
