@@ -275,6 +275,7 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     __syncwarp();
   } else if (warp == 1) {
     constexpr uint32_t IDESC = scaled_idesc<A8>(128, BN);
+    wait_for_previous();                                     // (the limits of the waits below do not count that kernel's time)
     // The scales of a step are copied ahead of the MMAs of the step before it where that step has arrived: its copies then run
     // beside those MMAs (for few tokens the MMAs of a step take less time than the copies it waits for).
     bool ok = !FUSED || mbar_wait(held, 0, p.d_status);
@@ -318,8 +319,8 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     if (elect_one()) umma_commit(done);
     __syncwarp();
   } else {
+    wait_for_previous();
     if constexpr (FUSED) {
-      wait_for_previous();
       const int values = A8 ? 128 : 256;                     // of a step
       quantize_resident<BN, A8, T>(p, smem + (res - base), smem + (res_sf - base), k0 * values, kn * (values / 8),
                                    warp - 2, L::THREADS / 32 - 2, lane);
@@ -561,6 +562,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
   } else if (warp == 1) {
     if (leader) {
       constexpr uint32_t IDESC = scaled_idesc<A8>(256, 256);
+      wait_for_previous();                                   // (the limits of the waits below do not count that kernel's time)
       const int mine = pair < tiles ? (tiles - pair + pairs - 1) / pairs : 0;
       const int64_t steps = (int64_t)mine * p.stages;
       int stage = 0;
@@ -599,6 +601,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
     // Two warps for each quarter of the tensor-memory lanes; they take turns at the tile's eight pieces of 32 columns,
     // those that both accumulators cover first (accumulator 0 ends with them, accumulator 1 begins with them).
     constexpr int SHARED = L::SHARED / 32;
+    wait_for_previous();
     const int q = warp & 3, half = (warp - 2) >> 2;
     Output<T> out{&map_y, smem_raw + (epi - smem_u32(smem_raw)) + half * 2 * PIECE_BYTES, half, q, lane};
     int t = 0;
