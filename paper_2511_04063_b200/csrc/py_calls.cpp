@@ -111,8 +111,24 @@ bool format(PyObject* o, int& fmt) {
   fmt = (int)v;
   return true;
 }
-long long code_bytes(int fmt, long long rows, long long k) { return rows * ((k + 127) / 128) * (fmt == DQ_MXFP4 ? 64 : 128); }
+long long row_bytes(int fmt, long long k) { return (k + 127) / 128 * (fmt == DQ_MXFP4 ? 64 : 128); }
+long long code_bytes(int fmt, long long rows, long long k) { return rows * row_bytes(fmt, k); }
 long long scale_bytes(long long rows, long long k) { return (rows + 127) / 128 * ((k + 127) / 128) * 512; }
+
+// Codes of a [rows, k] matrix: a buffer of their size, whose rows, if it has two dimensions, are theirs (another k or format
+// would read on as if they were).
+bool codes_of(PyObject* t, const char* name, int fmt, long long rows, long long k, long long device, void*& p) {
+  PyObject* shape = PyObject_GetAttr(t, s_shape);
+  if (!shape) return false;
+  bool fits = true;
+  if (PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 2) fits = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 1)) == row_bytes(fmt, k);
+  Py_DECREF(shape);
+  if (!fits) {
+    PyErr_Format(PyExc_ValueError, "%s: rows of %lld bytes are needed for %lld values in this format", name, row_bytes(fmt, k), k);
+    return false;
+  }
+  return bytes(t, name, code_bytes(fmt, rows, k), device, p);
+}
 
 // The stream (None: torch's current one), after checking that the tensors' device is the current one.
 bool stream_of(PyObject* stream, const char* name, long long device, void*& s) {
@@ -154,7 +170,7 @@ PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int fmt;
   void *codes, *scales, *s;
   if (!count(n, 6) || !matrix(a[0], "X", x) || !format(a[1], fmt) ||
-      !bytes(a[2], "codes", code_bytes(fmt, x.rows, x.k), x.device, codes) ||
+      !codes_of(a[2], "codes", fmt, x.rows, x.k, x.device, codes) ||
       !bytes(a[3], "scales", scale_bytes(x.rows, x.k), x.device, scales) || !optional(a[4], "values", v, x) ||
       !stream_of(a[5], "dq_mx_quantize", x.device, s))
     return nullptr;
@@ -167,7 +183,7 @@ PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int fmt;
   void *codes, *scales, *s;
   if (!count(n, 5) || !matrix(a[3], "Y", y) || !format(a[2], fmt) ||
-      !bytes(a[0], "codes", code_bytes(fmt, y.rows, y.k), y.device, codes) ||
+      !codes_of(a[0], "codes", fmt, y.rows, y.k, y.device, codes) ||
       !bytes(a[1], "scales", scale_bytes(y.rows, y.k), y.device, scales) || !stream_of(a[4], "dq_mx_dequantize", y.device, s))
     return nullptr;
   DQ_CALL(entry.dequantize(fmt, codes, scales, y.rows, y.k, y.p, y.dtype, y.ld, s));
@@ -197,7 +213,7 @@ PyObject* rmsnorm_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (fp32) g_dtype = DQ_FP32;
     if (!bytes(a[1], "gamma", 0, x.device, gamma)) return nullptr;
   }
-  if (!bytes(a[4], "codes", code_bytes(fmt, x.rows, x.k), x.device, codes) ||
+  if (!codes_of(a[4], "codes", fmt, x.rows, x.k, x.device, codes) ||
       !bytes(a[5], "scales", scale_bytes(x.rows, x.k), x.device, scales) || !optional(a[6], "residual", r, x) ||
       !optional(a[7], "sum_out", h, x) || !optional(a[8], "values", v, x) || !stream_of(a[9], "dq_rmsnorm_quantize", x.device, s))
     return nullptr;
@@ -214,9 +230,9 @@ PyObject* matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const long long k = PyLong_AsLongLong(a[5]);
   if (k == -1 && PyErr_Occurred()) return nullptr;
   if (k < 0 || k > (1LL << 40)) { PyErr_SetString(PyExc_ValueError, "k: out of range"); return nullptr; }
-  if (!bytes(a[0], "a_codes", code_bytes(fmt, y.rows, k), y.device, ac) ||
+  if (!codes_of(a[0], "a_codes", fmt, y.rows, k, y.device, ac) ||
       !bytes(a[1], "a_scales", scale_bytes(y.rows, k), y.device, as) ||
-      !bytes(a[3], "w_codes", code_bytes(DQ_MXFP4, y.k, k), y.device, wc) ||
+      !codes_of(a[3], "w_codes", DQ_MXFP4, y.k, k, y.device, wc) ||
       !bytes(a[4], "w_scales", scale_bytes(y.k, k), y.device, ws) || !stream_of(a[7], "dq_mx_matmul", y.device, s))
     return nullptr;
   DQ_CALL(entry.matmul(fmt, ac, as, y.rows, wc, ws, y.k, k, y.p, y.dtype, y.ld, s));
@@ -232,7 +248,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     PyErr_Format(PyExc_ValueError, "Y: %lld rows on X's device are needed", x.rows);
     return nullptr;
   }
-  if (!bytes(a[2], "w_codes", code_bytes(DQ_MXFP4, y.k, x.k), x.device, wc) ||
+  if (!codes_of(a[2], "w_codes", DQ_MXFP4, y.k, x.k, x.device, wc) ||
       !bytes(a[3], "w_scales", scale_bytes(y.k, x.k), x.device, ws) ||
       !bytes(a[5], "workspace", code_bytes(fmt, x.rows, x.k) + scale_bytes(x.rows, x.k), x.device, work) ||
       !stream_of(a[6], "dq_mx_linear", x.device, s))

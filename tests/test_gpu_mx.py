@@ -395,6 +395,42 @@ def test_calls_in_a_graph_and_in_a_row():
     check_product(z, a, w, k)
 
 
+def test_two_streams_at_once():
+    """The same chain on two streams with buffers of their own: the results are those of one stream alone."""
+    m, k, n = 8, 2048, 1536
+    w = quantized(draw(n, k, torch.float32, 1), dq.DQ_MXFP4)[:2]
+    sets = []
+    for seed in (2, 3):
+        x = draw(m, k, torch.bfloat16, seed)
+        sets.append((x, *dq.dq_mx_empty(m, k, dq.DQ_MXFP8), torch.empty((m, n), dtype=torch.bfloat16, device="cuda"),
+                     torch.empty((m, n), dtype=torch.bfloat16, device="cuda"),
+                     torch.empty(dq.dq_mx_linear_workspace(dq.DQ_MXFP4, m, k), dtype=torch.uint8, device="cuda")))
+
+    def chain(s, stream=None):
+        x, codes, scales, y, z, work = s
+        dq.dq_rmsnorm_quantize(x, None, 1e-5, dq.DQ_MXFP8, codes, scales, stream=stream)
+        dq.dq_mx_matmul(codes, scales, dq.DQ_MXFP8, *w, k, y, stream=stream)
+        dq.dq_mx_linear(x, dq.DQ_MXFP4, *w, z, work, stream=stream)
+
+    want = []
+    for s in sets:
+        chain(s)
+        want.append((s[3].clone(), s[4].clone()))
+    torch.cuda.synchronize()
+    for s in sets:
+        s[3].zero_()
+        s[4].zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        for s, stream in zip(sets, streams):
+            chain(s, stream)
+    torch.cuda.synchronize()
+    finished()
+    for s, (y, z) in zip(sets, want):
+        assert torch.equal(s[3], y) and torch.equal(s[4], z)
+
+
 # ------------------------------------------------------------------------------------------------ refusals
 def test_refusals():
     x = draw(4, 64, torch.bfloat16, 1)
@@ -412,6 +448,7 @@ def test_refusals():
                  lambda: dq.dq_rmsnorm_quantize(x, torch.ones(63, device="cuda"), 1e-5, dq.DQ_MXFP4, codes, scales),
                  lambda: dq.dq_rmsnorm_quantize(x, None, 1e-5, dq.DQ_MXFP4, codes, scales, residual=x.float()),
                  lambda: dq.dq_mx_matmul(codes, scales, dq.DQ_MXFP4, codes, scales, 300, y),
+                 lambda: dq.dq_mx_matmul(*dq.dq_mx_empty(4, 256, dq.DQ_MXFP4), dq.DQ_MXFP4, *dq.dq_mx_empty(4, 256, dq.DQ_MXFP4), 64, y),
                  lambda: dq.dq_mx_linear(x, dq.DQ_MXFP4, codes, scales, y, scales[:8])):
         with pytest.raises(ValueError):
             call()
