@@ -52,13 +52,6 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
-// Whether a phase has completed, without waiting (the lanes of a warp agree on the answer).
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return __all_sync(0xffffffffu, ok != 0);
-}
 // After a wait that ran out: the last loads into the stages (`fills` of them were issued in all) have to land before the shared
 // memory may go to another CTA.
 template <int STAGES, typename Full>
@@ -276,37 +269,21 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   } else if (warp == 1) {
     constexpr uint32_t IDESC = scaled_idesc<A8>(128, BN);
     wait_for_previous();                                     // (the limits of the waits below do not count that kernel's time)
-    // The scales of a step are copied ahead of the MMAs of the step before it where that step has arrived: its copies then run
-    // beside those MMAs (for few tokens the MMAs of a step take less time than the copies it waits for).
-    bool ok = !FUSED || mbar_wait(held, 0, p.d_status);
-    auto copy = [&](int i) {
+    const bool ok = !FUSED || mbar_wait(held, 0, p.d_status);
+    for (int i = 0; i < kn && ok; ++i) {
+      const int st = i % STAGES;
+      if (!mbar_wait(full(st), (uint32_t)(i / STAGES) & 1u, p.d_status)) break;
       tc_fence_after();
       if (elect_one()) {
-        const int st = i % STAGES;
         const uint32_t sw = tmem + BN + (uint32_t)st * L::SCALE_COLS, sx = sw + 4 * KT;
-        const uint32_t ws = base + st * L::STAGE_BYTES + L::W_BYTES;
-        const uint32_t xs = FUSED ? res_sf + i * L::SF_BYTES : ws + L::SF_BYTES + L::X_BYTES;
+        const uint32_t at = base + st * L::STAGE_BYTES, ws = at + L::W_BYTES;
+        const uint32_t x = FUSED ? res + i * L::X_BYTES : ws + L::SF_BYTES, xs = FUSED ? res_sf + i * L::SF_BYTES : x + L::X_BYTES;
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
           copy_scales<1>(sw + 4 * t, scale_desc(ws + t * TILE_BYTES));
           copy_scales<1>(sx + 4 * t, scale_desc(xs + t * TILE_BYTES));
         }
-      }
-      __syncwarp();
-    };
-    int copied = 0;
-    for (int i = 0; i < kn && ok; ++i) {
-      if (copied == i) {
-        if (!mbar_wait(full(i % STAGES), (uint32_t)(i / STAGES) & 1u, p.d_status)) break;
-        copy(copied++);
-      }
-      if (copied < kn && mbar_test(full(copied % STAGES), (uint32_t)(copied / STAGES) & 1u)) copy(copied++);
-      if (elect_one()) {
-        const int st = i % STAGES;
-        const uint32_t sw = tmem + BN + (uint32_t)st * L::SCALE_COLS, sx = sw + 4 * KT;
-        const uint32_t at = base + st * L::STAGE_BYTES;
-        const uint64_t a = make_kmajor_sw128_desc(at);
-        const uint64_t b = make_kmajor_sw128_desc(FUSED ? res + i * L::X_BYTES : at + L::W_BYTES + L::SF_BYTES);
+        const uint64_t a = make_kmajor_sw128_desc(at), b = make_kmajor_sw128_desc(x);
 #pragma unroll
         for (int m = 0; m < Step<A8>::MMAS; ++m) {
           const int t = A8 ? 0 : m >> 1;
