@@ -6,7 +6,7 @@
 // weights' 4-bit codes to one 16-byte slot per 16 values while it brings them into shared memory.
 //
 // Two kernels.  cluster_kernel, for few tokens, is bound by bringing the weights in and by the MMA steps that consume them: one
-// takes about 140 cycles whatever its N is, 4 KB of 4-bit weights an SM (16 x 8192 x 8192: 9.7 us at 4 bits, 11.1 at 8, whose
+// takes about 140 cycles whatever its N is, 4 KB of 4-bit weights an SM (16 x 8192 x 8192: 9.1 us at 4 bits, 10.3 at 8, whose
 // steps hold half as much; the weights alone need 5.5 us of HBM).  pair_kernel, for many, is bound by the tensor cores: 85 %
 // (4 bits) and 87 % (8 bits) of their cycles active, 16384 x 8192 x 8192 in 365 us (6000 TFLOP/s) and 734 us (3000) from a cool
 // start, and by the 1000 W power limit (1.3 to 1.4 GHz, 408 and 832 us) when it lasts.
@@ -687,10 +687,9 @@ int cluster_smem(int stages, int splits) {
 }
 
 // Into how many CTAs the reduction of each of `tiles` tiles is split: as many as run at once, until every SM has one; for few
-// tokens until it has two, whose latencies hide each other's, as long as each keeps eight steps (16 x 8192 x 8192: 9.8 us with
-// two CTAs of 8 steps an SM against 11.1 with one of 16; one token, 4096 x 4096: 5.4 with one CTA of 4 steps against 5.8 with two
-// of 2).  Clusters have to find their SMs together: of 8 CTAs with an SM each, 15 run at once, not 18.  FUSED: at least as
-// many as make the tokens fit.
+// tokens until it has two, whose latencies hide each other's, as long as each keeps eight steps (16 x 8192 x 8192: 9.1 us with
+// two CTAs of 8 steps an SM against 10.3 with one of 16 at 4 bits, 10.3 against 12.3 at 8).  Clusters have to find their SMs
+// together: of 8 CTAs with an SM each, 15 run at once, not 18.  FUSED: at least as many as make the tokens fit.
 template <int BN, bool A8, bool FUSED, typename T>
 dq_status choose_splits(const Device& dev, int64_t tiles, int stages, int& splits) {
   using L = ClusterSmem<BN, A8, FUSED>;
@@ -759,7 +758,7 @@ dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o)
 // Above, pairs unless their one tile after another is longer than a cluster's share of the reduction.  Measured (4 to 50 us,
 // k 256 to 8192, n 512 to 13824, 80 to 1536 tokens): a pair's step takes 0.28 us, a cluster CTA's 0.38, and its epilogue over the
 // cluster as long as five of the pair's steps; with more tiles than SMs the clusters lose everywhere.
-// (256 x 8192 x 1000, 8 bits: clusters 16.0, pairs 22.2 us; 256 x 8192 x 11008: clusters 52.1, pairs 26.5.)
+// (256 x 8192 x 1000, 8 bits: clusters 10.3, pairs 22.2 us; 256 x 8192 x 11008: clusters 52.1, pairs 26.5.)
 template <bool A8>
 dq_status cluster_is_faster(const Device& dev, const Operands& o, bool& yes) {
   constexpr int KT = Step<A8>::KT;
@@ -816,8 +815,8 @@ dq_status linear(cudaStream_t stream, const void* X, int x_dtype, int64_t m, int
   uint8_t* scales = workspace + m * row_bytes(a_fmt, k);
   Operands o{a_fmt, workspace, scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy};
   // Few tokens are quantised by the product's own CTAs, each the part that it multiplies, where that part is small: the CTAs of
-  // all weight tiles repeat the work (4096 x 4096, 1024 values a token and CTA: 1 token 5.4 us against 6.7 in two launches, 8
-  // tokens 6.5 against 6.8, 16 tokens 8.2 against 6.9; 1024 x 4096, 256 values: 16 tokens 4.4 against 5.0).
+  // all weight tiles repeat the work (4096 x 4096, 1024 values a token and CTA: 1 token 5.1 us against 6.4 in two launches, 8
+  // tokens 6.1 against 6.5, 16 tokens 7.9 against 6.6; 1024 x 4096, 256 values: 16 tokens 4.3 against 5.0).
   if (m <= 16) {
     o.x = X; o.ldx = ldx;
     o.x_vec = whole_pieces(X, ldx, k, x_dtype);
