@@ -74,13 +74,12 @@ bool matrix(PyObject* t, const char* name, Matrix& m, const Matrix* like = nullp
     return false;
   }
   if (pair_of(PyObject_CallMethodNoArgs(t, s_stride), m.ld, step) != 1) return false;
-  if (step != 1 || m.ld < m.k) {
-    if ((step != 1 && m.k > 1) || (m.ld < m.k && m.rows > 1)) {
-      PyErr_Format(PyExc_ValueError, "%s: rows have to be contiguous and must not overlap", name);
-      return false;
-    }
-    m.ld = m.k;                                               // (one row, or one column)
+  // (a single column's step means nothing, nor does a single row's stride)
+  if ((step != 1 && m.k > 1) || (m.ld < m.k && m.rows > 1)) {
+    PyErr_Format(PyExc_ValueError, "%s: rows have to be contiguous and must not overlap", name);
+    return false;
   }
+  if (m.ld < m.k) m.ld = m.k;                                 // (one row)
   return address(t, m.p);
 }
 // None, or a matrix like `x`
