@@ -201,8 +201,9 @@ __device__ __forceinline__ void quantize_resident(const Params& p, uint8_t* code
   }
 }
 
+// (Two CTAs an SM where shared memory has room for them: the registers have to do, too.)
 template <int BN, bool A8, bool FUSED, typename T>
-__global__ void __launch_bounds__(ClusterSmem<BN, A8, FUSED>::THREADS)
+__global__ void __launch_bounds__(ClusterSmem<BN, A8, FUSED>::THREADS, 2) 
 cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws,
                const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_xs, const Params p) {
   using L = ClusterSmem<BN, A8, FUSED>;
@@ -340,39 +341,51 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   };
   if (p.splits == 1) {
     for (int i = threadIdx.x; i < cols * 32; i += blockDim.x) store(i, reinterpret_cast<const float4*>(smem)[i]);
-  } else {
-    // all loads of two pieces at once: one at a time they cost the cluster's latency each (128 x 4096 x 4096: 9.7 us, 8.4 so)
-    constexpr int AT_ONCE = 2, MOST = 8;
-    for (int i0 = (int)threadIdx.x + c0 * 32; i0 < c1 * 32; i0 += AT_ONCE * blockDim.x) {
-      float4 v[AT_ONCE][MOST];
-#pragma unroll
-      for (int u = 0; u < AT_ONCE; ++u) {
-        const int i = i0 + u * (int)blockDim.x;
-        const uint32_t at = base + (uint32_t)i * 16u;        // [token][32 pieces]
-#pragma unroll
-        for (int r = 0; r < MOST; ++r)
-          if (r < p.splits && i < c1 * 32) v[u][r] = ld_cluster_f4(at, (uint32_t)r);
-      }
-#pragma unroll
-      for (int u = 0; u < AT_ONCE; ++u) {
-        const int i = i0 + u * (int)blockDim.x;
-        if (i >= c1 * 32) break;
-        float4 s = v[u][0];
-#pragma unroll
-        for (int r = 1; r < MOST; ++r)
-          if (r < p.splits) { s.x += v[u][r].x; s.y += v[u][r].y; s.z += v[u][r].z; s.w += v[u][r].w; }
-        store(i, s);
-      }
-    }
-  }
-  tc_fence_before();
-  if (p.splits > 1) {
-    // the peers have read this CTA's sums; nothing else is handed over (a release would wait for the stores to Y)
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-  } else {
+    tc_fence_before();
     __syncthreads();
+  } else {
+    // All loads of two pieces at once: one at a time they cost the cluster's latency each (128 x 4096 x 4096: 9.7 us, 8.4 so).
+    // The cluster's closing barrier tells the peers that this CTA has read their sums, so that they may leave: its arrival
+    // releases, which orders those loads before it, and stands behind the last loads but in front of the last stores to Y,
+    // which it would wait for (16 x 8192 x 8192: 9.04 and 10.09 us at 4 and 8 bits, 9.16 and 10.33 behind them).  All threads
+    // make the same rounds; pieces past Y's edge are neither loaded nor stored.
+    constexpr int AT_ONCE = 2, MOST = 8;
+    const int end = c1 * 32, per_round = AT_ONCE * (int)blockDim.x;
+    int i0 = c0 * 32;
+    tc_fence_before();
+    do {
+      float4 sum[AT_ONCE];
+      auto piece = [&](int u) { return i0 + u * (int)blockDim.x + (int)threadIdx.x; };
+      auto wanted = [&](int i) { return i < end && n0 + (i & 31) * 4 < p.n; };
+      {
+        float4 v[AT_ONCE][MOST];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+          const uint32_t at = base + (uint32_t)piece(u) * 16u;   // [token][32 pieces]
+#pragma unroll
+          for (int r = 0; r < MOST; ++r)
+            if (r < p.splits && wanted(piece(u))) v[u][r] = ld_cluster_f4(at, (uint32_t)r);
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+          if (!wanted(piece(u))) continue;
+          sum[u] = v[u][0];
+#pragma unroll
+          for (int r = 1; r < MOST; ++r)
+            if (r < p.splits) { sum[u].x += v[u][r].x; sum[u].y += v[u][r].y; sum[u].z += v[u][r].z; sum[u].w += v[u][r].w; }
+        }
+      }
+      if (i0 + per_round >= end) {                             // (the last round)
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+      }
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u)
+        if (wanted(piece(u))) store(piece(u), sum[u]);
+      i0 += per_round;
+    } while (i0 < end);
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   }
   if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, L::TMEM); }
 }

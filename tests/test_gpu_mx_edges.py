@@ -93,3 +93,29 @@ def test_one_column_of_a_matrix(fmt, dtype, rows):
     finished()
     check_product(y, a, w, 1)
     only(whole, y, y.clone())
+
+
+# ------------------------------------------------------------------------------------------------ a tile's last weight rows
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("k", (512, 1100, 4096))     # 2 to 32 steps: the reduction split over 2 to 8 CTAs
+@pytest.mark.parametrize("m,n", [(1, 1), (1, 132), (7, 100), (16, 253), (17, 258), (40, 129), (64, 641), (100, 127), (128, 136)])
+def test_split_products_at_a_weight_remainder(fmt, k, m, n):
+    """The last weight rows do not fill a tile, so some threads of the cluster's sum have nothing to add; calls in a row,
+    whose CTAs take over one another's shared memory, agree."""
+    a_codes, a_scales, a = quantized(draw(m, k, torch.float32, m + k), fmt)
+    w_codes, w_scales, w = quantized(draw(n, k, torch.float32, n + k), dq.DQ_MXFP4)
+    outs = [torch.full((m, n + 3), 7.0, dtype=torch.float32, device="cuda") for _ in range(8)]
+    for y in outs:
+        dq.dq_mx_matmul(a_codes, a_scales, fmt, w_codes, w_scales, k, y[:, :n])
+    finished()
+    check_product(outs[0][:, :n], a, w, k)
+    for y in outs:
+        assert torch.equal(y, outs[0]) and bool((y[:, n:] == 7.0).all())
+    if m <= 16:
+        x = draw(m, k, torch.bfloat16, m)
+        work = torch.empty(dq.dq_mx_linear_workspace(fmt, m, k), dtype=torch.uint8, device="cuda")
+        y = torch.full((m, n + 3), 7.0, dtype=torch.float32, device="cuda")
+        dq.dq_mx_linear(x, fmt, w_codes, w_scales, y[:, :n], work)
+        finished()
+        check_product(y[:, :n], mx.dequantize(*mx.quantize(f64(x), fmt), fmt, k), w, k)
+        assert bool((y[:, n:] == 7.0).all())
