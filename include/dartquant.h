@@ -391,6 +391,14 @@ dq_status dq_mx_linear(const void* d_X, int32_t x_dtype, int64_t m, int64_t k, i
  * DQ_OK, or DQ_ERR_TIMEOUT once a bounded wait inside a product gave up (its output is then not valid). */
 dq_status dq_mx_status(void* cuda_stream);
 
+/* Failure detection self-test: dq_mx_matmul's product with its waits limited to limit_ns (1 .. 1e8) each, in which the warp
+ * that issues the MMAs waits at its pipeline step `step` (>= 0, of every CTA or CTA pair that has that many) for a barrier that
+ * nothing arrives at.  It gives up, what it has in flight ends, and the kernel returns; dq_mx_status then says DQ_ERR_TIMEOUT,
+ * and Y is not valid. */
+dq_status dq_mx_selftest_bounded_wait(int32_t a_fmt, const void* d_a_codes, const void* d_a_scales, int64_t m, const void* d_w_codes,
+                                      const void* d_w_scales, int64_t n, int64_t k, void* d_Y, int32_t y_dtype, int64_t ldy,
+                                      int64_t step, uint64_t limit_ns, void* cuda_stream);
+
 const char* dq_status_string(dq_status s);
 void dq_calib_destroy(dq_calib_t* h);
 

@@ -34,7 +34,7 @@ EXPORTED_SYMBOLS = (
     "dq_calib_set_orth_method", "dq_calib_set_objective", "dq_calib_run_epochs", "dq_calib_mma_flops", "dq_calib_set_keep_gradient",
     "dq_calib_set_backward_precision", "dq_calib_selftest_bounded_wait", "dq_calib_time_product",
     "dq_mx_row_bytes", "dq_mx_scale_bytes", "dq_mx_linear_workspace", "dq_mx_quantize", "dq_mx_dequantize", "dq_rmsnorm_quantize",
-    "dq_mx_matmul", "dq_mx_linear", "dq_mx_status",
+    "dq_mx_matmul", "dq_mx_linear", "dq_mx_status", "dq_mx_selftest_bounded_wait",
 )
 
 
@@ -104,6 +104,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
                                                 vp]),
                        ("dq_mx_matmul", [i32, vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, vp]),
                        ("dq_mx_linear", [vp, i32, i64, i64, i64, i32, vp, vp, i64, vp, i32, i64, vp, vp]),
+                       ("dq_mx_selftest_bounded_wait", [i32, vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, i64, C.c_uint64, vp]),
                        ("dq_mx_status", [vp])):
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = i32
@@ -421,6 +422,17 @@ def dq_mx_linear(X, a_fmt: int, w_codes, w_scales, Y, workspace, stream=None):
 def dq_mx_status(stream=None) -> int:
     """Synchronises the stream; the microscaled operators' status on the current device, which is cleared."""
     return int(load_library().dq_mx_status(_stream_ptr(stream)))
+
+
+def dq_mx_selftest_bounded_wait(a_codes, a_scales, a_fmt: int, w_codes, w_scales, k: int, Y, step: int, limit_ns: int, stream=None):
+    """A product that gives up waiting at a pipeline step: dq_mx_status says DQ_ERR_TIMEOUT afterwards, Y is not valid.  Runs
+    the ordinary product first, which checks the arguments."""
+    dq_mx_matmul(a_codes, a_scales, a_fmt, w_codes, w_scales, k, Y, stream)
+    import torch
+    dtype = {torch.float32: DQ_FP32, torch.bfloat16: DQ_BF16, torch.float16: DQ_FP16}[Y.dtype]
+    _check(load_library().dq_mx_selftest_bounded_wait(
+        a_fmt, a_codes.data_ptr(), a_scales.data_ptr(), Y.shape[0], w_codes.data_ptr(), w_scales.data_ptr(), Y.shape[1], k,
+        Y.data_ptr(), dtype, Y.stride(0), step, limit_ns, _stream_ptr(stream)), "dq_mx_selftest_bounded_wait")
 
 
 def dq_version() -> str:

@@ -18,6 +18,16 @@ inline dq_status quantised(const void* codes, const void* scales) {
   return aligned(codes, 32) && aligned(scales, 16) ? DQ_OK : DQ_ERR_UNSUPPORTED;
 }
 inline bool typed(const void* p, int dtype) { return aligned(p, dtype == DQ_FP32 ? 4 : 2); }
+inline dq_status product_args(int a_fmt, const void* a_codes, const void* a_scales, int64_t m, const void* w_codes, const void* w_scales,
+                              int64_t n, int64_t k, const void* Y, int y_dtype, int64_t ldy) {
+  DQ_CHECK(sizes(m, k));
+  DQ_CHECK(sizes(n, k));
+  if (n == 0 || !is_format(a_fmt) || !is_float(y_dtype) || ldy < n) return DQ_ERR_INVALID_ARG;
+  if (m == 0) return DQ_OK;
+  if (!Y || !typed(Y, y_dtype)) return DQ_ERR_INVALID_ARG;
+  DQ_CHECK(quantised(a_codes, a_scales));
+  return quantised(w_codes, w_scales);
+}
 }  // namespace
 
 extern "C" {
@@ -81,15 +91,20 @@ dq_status dq_rmsnorm_quantize(const void* d_X, const void* d_residual, int32_t d
 dq_status dq_mx_matmul(int32_t a_fmt, const void* d_a_codes, const void* d_a_scales, int64_t m, const void* d_w_codes,
                        const void* d_w_scales, int64_t n, int64_t k, void* d_Y, int32_t y_dtype, int64_t ldy,
                        void* cuda_stream) {
-  DQ_CHECK(sizes(m, k));
-  DQ_CHECK(sizes(n, k));
-  if (n == 0 || !is_format(a_fmt) || !is_float(y_dtype) || ldy < n) return DQ_ERR_INVALID_ARG;
+  DQ_CHECK(product_args(a_fmt, d_a_codes, d_a_scales, m, d_w_codes, d_w_scales, n, k, d_Y, y_dtype, ldy));
   if (m == 0) return DQ_OK;
-  if (!d_Y || !typed(d_Y, y_dtype)) return DQ_ERR_INVALID_ARG;
-  DQ_CHECK(quantised(d_a_codes, d_a_scales));
-  DQ_CHECK(quantised(d_w_codes, d_w_scales));
   return mx::matmul((cudaStream_t)cuda_stream, a_fmt, (const uint8_t*)d_a_codes, (const uint8_t*)d_a_scales, m,
                     (const uint8_t*)d_w_codes, (const uint8_t*)d_w_scales, n, k, d_Y, y_dtype, ldy);
+}
+
+dq_status dq_mx_selftest_bounded_wait(int32_t a_fmt, const void* d_a_codes, const void* d_a_scales, int64_t m, const void* d_w_codes,
+                                      const void* d_w_scales, int64_t n, int64_t k, void* d_Y, int32_t y_dtype, int64_t ldy,
+                                      int64_t step, uint64_t limit_ns, void* cuda_stream) {
+  if (step < 0 || limit_ns == 0 || limit_ns > 100000000ull) return DQ_ERR_INVALID_ARG;   // at most 0.1 s
+  DQ_CHECK(product_args(a_fmt, d_a_codes, d_a_scales, m, d_w_codes, d_w_scales, n, k, d_Y, y_dtype, ldy));
+  if (m == 0) return DQ_OK;
+  return mx::matmul_giving_up((cudaStream_t)cuda_stream, a_fmt, (const uint8_t*)d_a_codes, (const uint8_t*)d_a_scales, m,
+                              (const uint8_t*)d_w_codes, (const uint8_t*)d_w_scales, n, k, d_Y, y_dtype, ldy, step, limit_ns);
 }
 
 dq_status dq_mx_linear(const void* d_X, int32_t x_dtype, int64_t m, int64_t k, int64_t ldx, int32_t a_fmt,

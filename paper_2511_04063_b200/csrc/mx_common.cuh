@@ -262,6 +262,10 @@ dq_status rmsnorm_quantize(cudaStream_t stream, const void* X, int dtype, int64_
                            uint8_t* codes, uint8_t* scales, void* sum, int64_t lds, void* values, int64_t ldv);
 dq_status matmul(cudaStream_t stream, int a_fmt, const uint8_t* a_codes, const uint8_t* a_scales, int64_t m,
                  const uint8_t* w_codes, const uint8_t* w_scales, int64_t n, int64_t k, void* Y, int y_dtype, int64_t ldy);
+// the product whose issuing warp gives up waiting at a pipeline step (dq_mx_selftest_bounded_wait)
+dq_status matmul_giving_up(cudaStream_t stream, int a_fmt, const uint8_t* a_codes, const uint8_t* a_scales, int64_t m,
+                           const uint8_t* w_codes, const uint8_t* w_scales, int64_t n, int64_t k, void* Y, int y_dtype, int64_t ldy,
+                           int64_t step, uint64_t limit_ns);
 dq_status linear(cudaStream_t stream, const void* X, int x_dtype, int64_t m, int64_t k, int64_t ldx, int a_fmt,
                  const uint8_t* w_codes, const uint8_t* w_scales, int64_t n, void* Y, int y_dtype, int64_t ldy,
                  uint8_t* workspace);

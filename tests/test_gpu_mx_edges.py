@@ -119,3 +119,33 @@ def test_split_products_at_a_weight_remainder(fmt, k, m, n):
         finished()
         check_product(y[:, :n], mx.dequantize(*mx.quantize(f64(x), fmt), fmt, k), w, k)
         assert bool((y[:, n:] == 7.0).all())
+
+
+# ------------------------------------------------------------------------------------------------ a wait that runs out
+# Clusters (split, and whole with more steps than stages) and pairs (one tile, and several); the first step, one of the first
+# stages, one that reuses a stage, one of a second tile (steps at 4 bits; at 8 there are twice as many).
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("m,n,k,steps", [(16, 300, 4096, (0, 1)), (1, 25600, 4096, (0, 3, 9)), (100, 640, 2048, (0,)),
+                                         (300, 5000, 4096, (0, 4, 11)), (2048, 4096, 4096, (0, 7, 19))])
+def test_a_product_that_gives_up_waiting_returns_and_the_next_is_right(fmt, m, n, k, steps):
+    """Failure detection without a fault: the wait runs out after 20 ms, the status word says so, is cleared by being
+    read, and the calls after it, on the same SMs and the same tensor memory, are as before."""
+    a_codes, a_scales, _ = quantized(draw(m, k, torch.float32, m + k), fmt)
+    w_codes, w_scales, _ = quantized(draw(n, k, torch.float32, n + k), dq.DQ_MXFP4)
+    args = (a_codes, a_scales, fmt, w_codes, w_scales, k)
+    want = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
+    dq.dq_mx_matmul(*args, want)
+    finished()
+    y = torch.empty_like(want)
+    for step in (s * (1 + (fmt == dq.DQ_MXFP8)) for s in steps):
+        dq.dq_mx_selftest_bounded_wait(*args, y, step, 20_000_000)
+        assert dq.dq_mx_status() == dq.DQ_ERR_TIMEOUT
+        finished()
+        for _ in range(3):
+            y.zero_()
+            dq.dq_mx_matmul(*args, y)
+            assert torch.equal(y, want)
+        finished()
+    dq.dq_mx_selftest_bounded_wait(*args, y, 1 << 40, 20_000_000)      # no CTA has that many steps: nothing runs out
+    finished()
+    assert torch.equal(y, want)

@@ -92,3 +92,12 @@ def test_strides_that_no_row_needs(calls):
                           ((4, 1), (0, 7))):
         with pytest.raises(ValueError, match="contiguous"):
             module.quantize(Stand(shape, stride), 0, *held(*shape), None, None)
+
+
+def test_the_self_tests_limits(calls):
+    import paper_2511_04063_b200 as dq
+    st, p = dq.load_library().dq_mx_selftest_bounded_wait, 1 << 12
+    for step, limit in ((-1, 1000), (0, 0), (0, 10 ** 9)):
+        assert st(0, p, p, 4, p, p, 64, 64, p, 1, 64, step, limit, None) == dq.DQ_ERR_INVALID_ARG
+    assert st(0, p, p, 4, p, p, 64, 64, p, 1, 63, 0, 1000, None) == dq.DQ_ERR_INVALID_ARG
+    assert st(0, p, p, 0, p, p, 64, 64, p, 1, 64, 0, 1000, None) == dq.DQ_OK
