@@ -12,8 +12,18 @@ using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, voi
                               const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                               CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
+// The function encodes for the context that is current in the calling thread.  The runtime's own calls make the device's one
+// current where they need it; a host thread that has made none of them yet (because everything that this library looks up
+// was looked up in another thread) has to do so first.
+inline bool bind_thread() {
+  static thread_local bool bound = false;
+  int dev = -1;
+  if (!bound) bound = cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess;
+  return bound;
+}
 inline EncodeFn get_encode_fn() {
   static EncodeFn fn = nullptr;
+  if (!bind_thread()) return nullptr;
   if (fn) return fn;
   void* p = nullptr;
   cudaDriverEntryPointQueryResult qres;

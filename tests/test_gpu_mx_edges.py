@@ -1,5 +1,7 @@
 """Edges of the microscaled operators against the float64 oracle: views, remainders, orders and sizes at which one of
 their parts is used differently."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -149,3 +151,32 @@ def test_a_product_that_gives_up_waiting_returns_and_the_next_is_right(fmt, m, n
     dq.dq_mx_selftest_bounded_wait(*args, y, 1 << 40, 20_000_000)      # no CTA has that many steps: nothing runs out
     finished()
     assert torch.equal(y, want)
+
+
+# ------------------------------------------------------------------------------------------------ other host threads
+@pytest.mark.parametrize("m", (4, 40, 300))
+def test_products_from_a_thread_that_did_nothing_else(m):
+    """A host thread whose first use of the GPU is a product gives what the main thread gives."""
+    n, k = 2000, 1024
+    w_codes, w_scales, _ = quantized(draw(n, k, torch.float32, 1), dq.DQ_MXFP4)
+    a_codes, a_scales, _ = quantized(draw(m, k, torch.float32, 2), dq.DQ_MXFP8)
+    x = draw(m, k, torch.bfloat16, 3)
+    work = torch.empty(dq.dq_mx_linear_workspace(dq.DQ_MXFP4, m, k), dtype=torch.uint8, device="cuda")
+    y, z, other_y, other_z = (torch.zeros((m, n), dtype=torch.bfloat16, device="cuda") for _ in range(4))
+    stream = torch.cuda.current_stream()
+    errors = []
+
+    def calls(y, z):
+        try:
+            dq.dq_mx_matmul(a_codes, a_scales, dq.DQ_MXFP8, w_codes, w_scales, k, y, stream=stream)
+            dq.dq_mx_linear(x, dq.DQ_MXFP4, w_codes, w_scales, z, work, stream=stream)
+        except Exception as e:
+            errors.append(e)
+
+    calls(y, z)
+    thread = threading.Thread(target=calls, args=(other_y, other_z))
+    thread.start()
+    thread.join()
+    assert not errors
+    finished()
+    assert torch.equal(y, other_y) and torch.equal(z, other_z) and bool(y.any()) and bool(z.any())
