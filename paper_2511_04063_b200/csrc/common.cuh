@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "dartquant.h"
 
 namespace dq {
@@ -66,15 +68,15 @@ inline dq_status join_side(Ctx& ctx) {
 
 // Opt-in to more than 48 KB of dynamic shared memory.  The attribute belongs to the (function, device) pair,
 // so it is set once per device; one process may use the library on several devices.
-struct SmemOptIn { bool done[64] = {}; };
+struct SmemOptIn { std::atomic<bool> done[64] = {}; };
 template <typename Kernel>
 inline dq_status opt_in_dynamic_smem(Kernel kern, int bytes, SmemOptIn& table) {
   int dev = -1;
   DQ_CHECK_CUDA(cudaGetDevice(&dev));
   const bool tracked = dev >= 0 && dev < 64;
-  if (tracked && table.done[dev]) return DQ_OK;
+  if (tracked && table.done[dev].load(std::memory_order_acquire)) return DQ_OK;
   DQ_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-  if (tracked) table.done[dev] = true;
+  if (tracked) table.done[dev].store(true, std::memory_order_release);
   return DQ_OK;
 }
 

@@ -11,6 +11,7 @@
 #include <cuda_fp16.h>
 
 #include "common.cuh"
+#include "per_device.h"
 
 namespace dq {
 namespace mx {

@@ -739,23 +739,24 @@ int cluster_smem(int stages, int splits) {
 template <int BN, bool A8, bool FUSED, typename T>
 dq_status choose_splits(const Device& dev, int64_t tiles, int stages, int& splits) {
   using L = ClusterSmem<BN, A8, FUSED>;
-  static SmemOptIn attr;
-  static int known[64][9] = {};                              // clusters with an SM a CTA at once, by device and size; asked once
+  struct Clusters { int most[9]; };                          // that run at once with an SM a CTA, by their size
+  static PerDevice<Clusters> known;
   constexpr int ALONE = L::FIXED > MAX_SMEM / 2 + 1024 ? L::FIXED : MAX_SMEM / 2 + 1024;   // shared memory that leaves no room for two
   auto kern = cluster_kernel<BN, A8, FUSED, T>;
-  DQ_CHECK(opt_in_dynamic_smem(kern, FUSED ? MAX_SMEM : ALONE, attr));
+  Clusters clusters;
+  DQ_CHECK((dq_status)known.get(dev.index, clusters, [kern](Clusters& c) -> int {
+    DQ_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FUSED ? MAX_SMEM : ALONE));
+    for (int s = 2; s <= 8; s *= 2) {
+      LaunchConfig config(nullptr, s, L::THREADS, ALONE, s);
+      DQ_CHECK_CUDA(cudaOccupancyMaxActiveClusters(&c.most[s], kern, &config.cfg));
+    }
+    return DQ_OK;
+  }));
   splits = 1;
   for (int s = 2; s <= 8 && s <= stages; s *= 2) {
-    int& most = known[dev.index][s];
-    if (most == 0) {
-      LaunchConfig c(nullptr, s, L::THREADS, ALONE, s);
-      int n = 0;
-      DQ_CHECK_CUDA(cudaOccupancyMaxActiveClusters(&n, kern, &c.cfg));
-      most = n > 0 ? n : -1;
-    }
     const int smem = cluster_smem<BN, A8, FUSED>(stages, s);
     const bool two = BN <= 32 && smem <= MAX_SMEM / 2 - 1024 && stages >= s * 8;
-    if (cluster_smem<BN, A8, FUSED>(stages, splits) > MAX_SMEM || tiles <= (two ? 2 : 1) * most) splits = s;
+    if (cluster_smem<BN, A8, FUSED>(stages, splits) > MAX_SMEM || tiles <= (two ? 2 : 1) * clusters.most[s]) splits = s;
   }
   return DQ_OK;
 }

@@ -14,14 +14,12 @@ namespace mx {
 static __device__ int g_mx_status;
 
 dq_status current_device(Device& out) {
-  static Device known[64];
-  static bool done[64] = {};
+  static PerDevice<Device> known;
   int dev = -1;
   DQ_CHECK_CUDA(cudaGetDevice(&dev));
-  if (dev < 0 || dev >= 64) return DQ_ERR_UNSUPPORTED;
-  if (!done[dev]) {
+  if (dev < 0 || dev >= MAX_DEVICES) return DQ_ERR_UNSUPPORTED;
+  return (dq_status)known.get(dev, out, [dev](Device& d) -> int {
     int major = 0;
-    Device d;
     void* p = nullptr;
     DQ_CHECK_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
     if (major != 10) return DQ_ERR_UNSUPPORTED;
@@ -29,11 +27,8 @@ dq_status current_device(Device& out) {
     DQ_CHECK_CUDA(cudaGetSymbolAddress(&p, g_mx_status));
     d.d_status = (int*)p;
     d.index = dev;
-    known[dev] = d;
-    done[dev] = true;
-  }
-  out = known[dev];
-  return DQ_OK;
+    return DQ_OK;
+  });
 }
 
 namespace {

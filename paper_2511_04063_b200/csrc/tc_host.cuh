@@ -22,16 +22,16 @@ inline bool bind_thread() {
   return bound;
 }
 inline EncodeFn get_encode_fn() {
-  static EncodeFn fn = nullptr;
+  static std::atomic<EncodeFn> known{nullptr};
   if (!bind_thread()) return nullptr;
-  if (fn) return fn;
+  if (EncodeFn fn = known.load(std::memory_order_acquire)) return fn;
   void* p = nullptr;
   cudaDriverEntryPointQueryResult qres;
   if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) != cudaSuccess ||
       qres != cudaDriverEntryPointSuccess)
     return nullptr;
-  fn = reinterpret_cast<EncodeFn>(p);
-  return fn;
+  known.store(reinterpret_cast<EncodeFn>(p), std::memory_order_release);
+  return reinterpret_cast<EncodeFn>(p);
 }
 
 // bf16 tensor [batch][rows][k] (k contiguous, row stride ld elements), box = {64, box_rows, 1},

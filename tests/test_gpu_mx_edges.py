@@ -1,5 +1,8 @@
 """Edges of the microscaled operators against the float64 oracle: views, remainders, orders and sizes at which one of
 their parts is used differently."""
+import os
+import subprocess
+import sys
 import threading
 
 import numpy as np
@@ -180,3 +183,61 @@ def test_products_from_a_thread_that_did_nothing_else(m):
     assert not errors
     finished()
     assert torch.equal(y, other_y) and torch.equal(z, other_z) and bool(y.any()) and bool(z.any())
+
+
+# ------------------------------------------------------------------------------------------------ first calls of several threads
+FIRST_CALLS = """
+import threading
+import torch
+import paper_2511_04063_b200 as dq
+
+SHAPES = ((1, 4096, 4096), (40, 4096, 1000), (300, 4096, 2048), (100, 512, 700))
+THREADS = 8
+g = torch.Generator(device="cuda").manual_seed(1)
+x = {s: torch.randn(s[0], s[1], device="cuda", generator=g).bfloat16() for s in SHAPES}
+w = {s: (torch.randint(0, 256, (s[2], s[1] // 2), dtype=torch.uint8, device="cuda", generator=g),
+         torch.full((-(-s[2] // 128) * (s[1] // 128) * 512,), 127, dtype=torch.uint8, device="cuda")) for s in SHAPES}
+torch.cuda.synchronize()
+
+def outputs(stream):
+    out = []
+    for fmt in (dq.DQ_MXFP8, dq.DQ_MXFP4):
+        for s in SHAPES:
+            y = torch.empty(s[0], s[2], dtype=torch.bfloat16, device="cuda")
+            work = torch.empty(dq.dq_mx_linear_workspace(fmt, s[0], s[1]), dtype=torch.uint8, device="cuda")
+            dq.dq_mx_linear(x[s], fmt, *w[s], y, work, stream=stream)
+            out.append((y, work))
+    stream.synchronize()
+    return [y for y, _ in out]
+
+got, errors = [None] * THREADS, []
+ready = threading.Barrier(THREADS)
+streams = [torch.cuda.Stream() for _ in range(THREADS)]
+
+def first(i):
+    try:
+        ready.wait()
+        got[i] = outputs(streams[i])
+    except Exception as e:
+        errors.append(repr(e))
+
+threads = [threading.Thread(target=first, args=(i,)) for i in range(THREADS)]
+for t in threads:
+    t.start()
+for t in threads:
+    t.join()
+assert not errors, errors
+want = outputs(torch.cuda.current_stream())
+torch.cuda.synchronize()
+for ys in got:
+    for y, z in zip(ys, want):
+        assert torch.equal(y, z)
+assert dq.dq_mx_status() == dq.DQ_OK
+"""
+
+
+def test_first_calls_of_several_threads():
+    """A process whose first calls on the device come from eight threads at once."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    ran = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
+    assert ran.returncode == 0, ran.stderr[-3000:]
