@@ -1,4 +1,4 @@
-"""Builds libdartquant.so (sm_100a only, nvcc) and _calls.so (its Python calls, the host compiler) in-tree."""
+"""Builds libdartquant.so (sm_100a only, nvcc) and the module _calls (its Python calls, the host compiler) in-tree."""
 from __future__ import annotations
 
 import os
@@ -11,7 +11,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libdartquant.so")
-CALLS = os.path.join(HERE, "_calls.so")
+CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))   # of this interpreter
+UNTAGGED = os.path.join(HERE, "_calls.so")                                       # any interpreter would load it
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.cu", "gemm_ffma.cu", "qr_forward.cu", "qr_backward.cu", "tc_path.cu", "qr_tc.cu", "qr_panel_tc.cu", "qr128.cu", "token_sampling.cu", "eval_metrics.cu", "cayley_tc.cu", "objectives.cu", "qr128_inc.cu", "qr128_tc5.cu", "mx_quant.cu", "mx_matmul.cu", "mx_api.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -59,6 +60,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
                         "-I", INCLUDE, os.path.join(CSRC, "py_calls.cpp"), "-o", CALLS], capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("host compiler failed for py_calls.cpp:\n" + r.stderr)
+    if os.path.exists(UNTAGGED):
+        os.remove(UNTAGGED)
     return LIB
 
 
