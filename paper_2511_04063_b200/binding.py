@@ -351,7 +351,11 @@ def _mx():
     if _calls is None:
         import torch
         lib = load_library()
-        from . import _calls as calls
+        try:
+            from . import _calls as calls
+        except ImportError as e:
+            raise ImportError("the microscaled operators' Python calls are not built for this interpreter: run "
+                              "`python -m paper_2511_04063_b200.build` where its Python.h is installed") from e
         torch.cuda.current_device()
         calls.bind(tuple(C.cast(getattr(lib, n), C.c_void_p).value for n in
                          ("dq_mx_quantize", "dq_mx_dequantize", "dq_rmsnorm_quantize", "dq_mx_matmul", "dq_mx_linear")),

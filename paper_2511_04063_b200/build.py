@@ -5,6 +5,7 @@ import os
 import subprocess
 import sys
 import sysconfig
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -26,17 +27,11 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found")
 
 
-def _stale() -> bool:
-    if not (os.path.exists(LIB) and os.path.exists(CALLS)):
-        return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(INCLUDE, "dartquant.h")]
-    return any(os.path.getmtime(p) > t for p in deps)
+def _stale(target: str, deps: list[str]) -> bool:
+    return not os.path.exists(target) or any(os.path.getmtime(p) > os.path.getmtime(target) for p in deps)
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not _stale():
-        return LIB
+def _build_library(verbose: bool) -> None:
     os.makedirs(OBJ_DIR, exist_ok=True)
     nvcc = _nvcc()
 
@@ -56,12 +51,28 @@ def build(force: bool = False, verbose: bool = False) -> str:
                        capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stderr)
-    r = subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"],
-                        "-I", INCLUDE, os.path.join(CSRC, "py_calls.cpp"), "-o", CALLS], capture_output=True, text=True)
+
+
+def _build_calls(source: str) -> None:
+    """The Python calls of the microscaled operators; the only part that needs Python's headers."""
+    include = sysconfig.get_paths()["include"]
+    if not os.path.exists(os.path.join(include, "Python.h")):
+        warnings.warn("no Python.h in %s: the microscaled operators have no Python calls; everything else is built" % include)
+        return
+    r = subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-I", include,
+                        "-I", INCLUDE, source, "-o", CALLS], capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("host compiler failed for py_calls.cpp:\n" + r.stderr)
     if os.path.exists(UNTAGGED):
         os.remove(UNTAGGED)
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    header, calls = os.path.join(INCLUDE, "dartquant.h"), os.path.join(CSRC, "py_calls.cpp")
+    if force or _stale(LIB, [header, *(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != "py_calls.cpp")]):
+        _build_library(verbose)
+    if force or _stale(CALLS, [header, calls]):
+        _build_calls(calls)
     return LIB
 
 
