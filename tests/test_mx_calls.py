@@ -45,8 +45,8 @@ def held(rows, k, bits=4):
 
 @pytest.fixture()
 def calls():
-    """(the compiled calls, the list that their entries write to); the library is bound again afterwards."""
-    from paper_2511_04063_b200 import binding, build
+    """(the compiled calls, the list that their entries write to)"""
+    from paper_2511_04063_b200 import build
     build.build()
     from paper_2511_04063_b200 import _calls
     seen = []
@@ -57,8 +57,7 @@ def calls():
 
     entries = [C.CFUNCTYPE(I32, *a)(note) for a in ARGUMENTS]
     _calls.bind(tuple(C.cast(e, P).value for e in entries), TYPES, lambda: 0, lambda index: 0)
-    yield _calls, seen
-    binding._calls = None      # (the next operator call binds the library)
+    yield _calls, seen         # (and the entries live until the test has ended)
 
 
 @pytest.mark.parametrize("stride,ld", [((1, 1), 1), ((2, 2), 2), ((28, 7), 28), ((5000, 1), 5000), ((5000, 7), 5000)])
