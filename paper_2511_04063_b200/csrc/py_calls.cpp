@@ -86,7 +86,7 @@ bool matrix(PyObject* t, const char* name, Matrix& m, const Matrix* like = nullp
 bool optional(PyObject* t, const char* name, Matrix& m, const Matrix& x) { return t == Py_None || matrix(t, name, m, &x); }
 
 // A contiguous buffer of at least `least` bytes on a device.
-bool bytes(PyObject* t, const char* name, long long least, long long device, void*& p) {
+bool bytes(PyObject* t, const char* name, long long least, long long device, void*& p, long long* held = nullptr) {
   long long size, where;
   if (!as_int(PyObject_GetAttr(t, s_nbytes), size) || !call_int(t, s_get_device, where)) return false;
   PyObject* c = PyObject_CallMethodNoArgs(t, s_is_contiguous);
@@ -97,6 +97,7 @@ bool bytes(PyObject* t, const char* name, long long least, long long device, voi
     PyErr_Format(PyExc_ValueError, "%s: a contiguous buffer of at least %lld bytes on the inputs' device is needed", name, least);
     return false;
   }
+  if (held) *held = size;
   return address(t, p);
 }
 
@@ -115,18 +116,17 @@ long long code_bytes(int fmt, long long rows, long long k) { return rows * row_b
 long long scale_bytes(long long rows, long long k) { return (rows + 127) / 128 * ((k + 127) / 128) * 512; }
 
 // Codes of a [rows, k] matrix: a buffer of their size, whose rows, if it has two dimensions, are theirs (another k or format
-// would read on as if they were).
+// would read on as if they were).  Whatever type they have: rows are counted in bytes.
 bool codes_of(PyObject* t, const char* name, int fmt, long long rows, long long k, long long device, void*& p) {
+  long long held = 0;
+  if (!bytes(t, name, code_bytes(fmt, rows, k), device, p, &held)) return false;
   PyObject* shape = PyObject_GetAttr(t, s_shape);
   if (!shape) return false;
   bool fits = true;
-  if (PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 2) fits = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 1)) == row_bytes(fmt, k);
+  if (PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 2) fits = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0)) * row_bytes(fmt, k) == held;
   Py_DECREF(shape);
-  if (!fits) {
-    PyErr_Format(PyExc_ValueError, "%s: rows of %lld bytes are needed for %lld values in this format", name, row_bytes(fmt, k), k);
-    return false;
-  }
-  return bytes(t, name, code_bytes(fmt, rows, k), device, p);
+  if (!fits) PyErr_Format(PyExc_ValueError, "%s: rows of %lld bytes are needed for %lld values in this format", name, row_bytes(fmt, k), k);
+  return fits;
 }
 
 // The stream (None: torch's current one), after checking that the tensors' device is the current one.

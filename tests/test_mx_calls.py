@@ -100,3 +100,20 @@ def test_the_self_tests_limits(calls):
         assert st(0, p, p, 4, p, p, 64, 64, p, 1, 64, step, limit, None) == dq.DQ_ERR_INVALID_ARG
     assert st(0, p, p, 4, p, p, 64, 64, p, 1, 63, 0, 1000, None) == dq.DQ_ERR_INVALID_ARG
     assert st(0, p, p, 0, p, p, 64, 64, p, 1, 64, 0, 1000, None) == dq.DQ_OK
+
+
+def test_rows_of_codes_are_counted_in_bytes(calls):
+    """Two-dimensional codes have rows of their own; what counts is their bytes, whatever the elements' type."""
+    module, seen = calls
+    x, (codes, scales) = Stand((4, 256)), held(4, 256)               # rows of 128 bytes
+    module.quantize(x, 0, Stand((4, 32), dtype=torch.int32), scales, None, None)
+    module.quantize(x, 0, Stand((6, 128), dtype=torch.uint8), scales, None, None)
+    module.quantize(x, 0, Stand((512,), dtype=torch.uint8), scales, None, None)
+    module.quantize(x, 0, Stand((2, 2, 128), dtype=torch.uint8), scales, None, None)
+    assert len(seen) == 4
+    for shape, dtype in (((4, 128), torch.int16), ((4, 128), torch.float32), ((8, 64), torch.uint8), ((4, 256), torch.uint8),
+                         ((2, 64), torch.int32)):
+        with pytest.raises(ValueError, match="rows of 128 bytes"):
+            module.quantize(x, 0, Stand(shape, dtype=dtype), scales, None, None)
+    with pytest.raises(ValueError, match="at least"):
+        module.quantize(x, 0, Stand((3, 128), dtype=torch.uint8), scales, None, None)
