@@ -241,3 +241,30 @@ def test_first_calls_of_several_threads():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     ran = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
     assert ran.returncode == 0, ran.stderr[-3000:]
+
+
+# ------------------------------------------------------------------------------------------------ weights from the call before
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("m,n,k", [(1, 4096, 2048), (17, 4096, 2048), (40, 8192, 4096), (300, 8192, 4096), (600, 1000, 1031)])
+def test_linear_right_after_its_weights(fmt, m, n, k):
+    """Weights that the kernel directly before dq_mx_linear writes, over others of another size of value: its product may read
+    weights before its own quantisation of the tokens has ended, not before theirs."""
+    w = [draw(n, k, torch.bfloat16, 1) * 4.0 ** i for i in range(4)]
+    x = draw(m, k, torch.bfloat16, 2)
+    codes, scales = dq.dq_mx_empty(n, k, dq.DQ_MXFP4)
+    work = torch.empty(dq.dq_mx_linear_workspace(fmt, m, k), dtype=torch.uint8, device="cuda")
+    want = []
+    for v in w:
+        dq.dq_mx_quantize(v, dq.DQ_MXFP4, codes, scales)
+        torch.cuda.synchronize()
+        want.append(torch.empty((m, n), dtype=torch.float32, device="cuda"))
+        dq.dq_mx_linear(x, fmt, codes, scales, want[-1], work)
+        torch.cuda.synchronize()
+    assert not torch.equal(want[0], want[1])
+    got = [torch.empty_like(y) for _ in range(8) for y in want]
+    for i, y in enumerate(got):
+        dq.dq_mx_quantize(w[i % 4], dq.DQ_MXFP4, codes, scales)
+        dq.dq_mx_linear(x, fmt, codes, scales, y, work)
+    finished()
+    for i, y in enumerate(got):
+        assert torch.equal(y, want[i % 4])
