@@ -268,3 +268,41 @@ def test_linear_right_after_its_weights(fmt, m, n, k):
     finished()
     for i, y in enumerate(got):
         assert torch.equal(y, want[i % 4])
+
+
+# ------------------------------------------------------------------------------------------------ long rows of the norm
+# Relative error of y in fp32: at most 32 squares in a thread's sum, 5 additions across a warp and 5 across up to 32 warps, the
+# squares' own rounding and the mean's, half of it under the root, rsqrtf good to 2 units, three products: below 2^-18.
+Y_REL = 2.0 ** -18
+
+
+def check_norm(x, residual, gamma, eps, fmt, codes, scales, values):
+    """Scale and elements lie between those of y (1 - Y_REL) and y (1 + Y_REL)."""
+    rows, k = x.shape
+    _, y = mx.rmsnorm(f64(x), None if residual is None else f64(residual), None if gamma is None else f64(gamma), eps)
+    c, s = codes.cpu().numpy(), mx.unpack_scales(scales.cpu().numpy(), rows, k)
+    if fmt == dq.DQ_MXFP4:
+        c = np.stack((c & 15, c >> 4), -1).reshape(rows, -1)
+    _, lo = mx.quantize(y * (1 - Y_REL), fmt)
+    _, hi = mx.quantize(y * (1 + Y_REL), fmt)
+    assert ((s >= lo) & (s <= hi)).all()
+    pad = np.zeros((rows, c.shape[1]))
+    pad[:, :k] = np.abs(y)
+    v = np.ldexp(pad.reshape(rows, -1, 32), (127 - s.astype(np.int64))[..., None]).reshape(rows, -1)
+    mag = (c % mx.SIGN[fmt]).astype(np.int64)
+    assert (mag >= mx.nearest_code(v * (1 - Y_REL), fmt)).all() and (mag <= mx.nearest_code(v * (1 + Y_REL), fmt)).all()
+    assert torch.equal(values.cpu(), torch.from_numpy(mx.dequantize(c, s, fmt, k)).to(x.dtype))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16, torch.float16))
+@pytest.mark.parametrize("rows,k", [(3, 8195), (600, 8447), (2, 16385), (300, 16501), (3, 32767), (2, 16392), (2, 32760)])
+def test_rmsnorm_of_long_rows(fmt, dtype, rows, k):
+    """Four and eight pieces of 256 columns a warp: rows in whole pieces of 16 bytes, and rows that are not."""
+    x, r = draw(rows, k, dtype, k), draw(rows, k, dtype, k + 1)
+    gamma = (1 + 0.1 * draw(1, k, torch.float32, k + 2)[0]).to(dtype)
+    codes, scales = dq.dq_mx_empty(rows, k, fmt)
+    h, values = torch.empty_like(x), torch.empty_like(x)
+    dq.dq_rmsnorm_quantize(x, gamma, 1e-5, fmt, codes, scales, residual=r, sum_out=h, values=values)
+    check_norm(x, r, gamma, 1e-5, fmt, codes, scales, values)
+    assert torch.equal(h, (x.float() + r.float()).to(dtype))
