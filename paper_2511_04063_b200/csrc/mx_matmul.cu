@@ -755,7 +755,7 @@ dq_status choose_splits(const Device& dev, int64_t tiles, int stages, int& split
   splits = 1;
   for (int s = 2; s <= 8 && s <= stages; s *= 2) {
     const int smem = cluster_smem<BN, A8, FUSED>(stages, s);
-    const bool two = BN <= 32 && smem <= MAX_SMEM / 2 - 1024 && stages >= s * 8;
+    const bool two = smem <= MAX_SMEM / 2 - 1024 && stages >= s * 8;
     if (cluster_smem<BN, A8, FUSED>(stages, splits) > MAX_SMEM || tiles <= (two ? 2 : 1) * clusters.most[s]) splits = s;
   }
   return DQ_OK;
