@@ -343,7 +343,9 @@ dq_status dq_calib_time_product(dq_calib_t* h, int32_t nterms, int32_t reps, flo
  *   or DQ_FP16; 16-byte aligned rows are read and written fastest, no alignment beyond the type's is needed.
  * Calls are asynchronous on the given stream, allocate nothing, keep nothing and can be captured in a graph (make one call of
  *   each kind before, on each device: the first looks up what the device can run at once).  They use programmatic dependent
- *   launch: a kernel may be scheduled before the one in front of it has ended, but reads and writes nothing until then.
+ *   launch: a kernel may be scheduled before the one in front of it has ended, but reads and writes nothing until then, with
+ *   one exception: dq_mx_linear's product may read weights while the same call's quantisation still runs.  Any number of host
+ *   threads may call at the same time, each with streams, outputs and workspaces of its own.
  *   A call with no rows does nothing.  Limits: k <= 2^24, rows <= 2^31 - 256.
  * Errors: INVALID_ARG (null, sizes, enums, a pointer that its type's alignment rules out), UNSUPPORTED (alignment of codes
  *   and scales, limits, a device that is not sm_100), CUDA. */
@@ -369,7 +371,8 @@ dq_status dq_mx_dequantize(int32_t fmt, const void* d_codes, const void* d_scale
  * X, residual, sum and values have type `dtype`.  d_residual (nullable: h = x).  d_gamma (nullable: ones, as where gamma
  * was folded into the weights before a rotation): [k] of gamma_dtype, DQ_FP32 or `dtype`.  d_sum (nullable) receives
  * h rounded once, what the next layer adds to; it may be X or residual itself (equal row strides).  y is computed from
- * the unrounded h.  d_values (nullable) as in dq_mx_quantize.  k <= 32768. */
+ * the unrounded h.  The squares are summed in fp32: a row whose sum of squares passes its range (3.4e38) has
+ * y = 0.  d_values (nullable) as in dq_mx_quantize.  k <= 32768. */
 dq_status dq_rmsnorm_quantize(const void* d_X, const void* d_residual, int32_t dtype, int64_t rows, int64_t k, int64_t ldx,
                               int64_t ldr, const void* d_gamma, int32_t gamma_dtype, float eps, int32_t fmt, void* d_codes,
                               void* d_scales, void* d_sum, int64_t lds, void* d_values, int64_t ldv, void* cuda_stream);

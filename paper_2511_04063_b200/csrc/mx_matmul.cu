@@ -5,11 +5,13 @@
 // kind::mxf4 (64 values per MMA step), 8-bit ones kind::mxf8f6f4 (32 per step), for which the copy engine spreads the
 // weights' 4-bit codes to one 16-byte slot per 16 values while it brings them into shared memory.
 //
-// Two kernels.  cluster_kernel, for few tokens, is bound by bringing the weights in and by the MMA steps that consume them: one
-// takes about 140 cycles whatever its N is, 4 KB of 4-bit weights an SM (16 x 8192 x 8192: 9.1 us at 4 bits, 10.3 at 8, whose
-// steps hold half as much; the weights alone need 5.5 us of HBM).  pair_kernel, for many, is bound by the tensor cores: 85 %
-// (4 bits) and 87 % (8 bits) of their cycles active, 16384 x 8192 x 8192 in 365 us (6000 TFLOP/s) and 734 us (3000) from a cool
-// start, and by the 1000 W power limit (1.3 to 1.4 GHz, 408 and 832 us) when it lasts.
+// Two kernels.  cluster_kernel, for few tokens, is bound by bringing the weights in, by the MMAs that consume them and by the
+// latency at both ends: an MMA takes about 140 cycles whatever its N is (each adds to the sum of the one before it; whether
+// that or the pipe sets the time was not measured), 4 KB of 4-bit weights an SM.  16 x 8192 x 8192, weights from HBM: 9.1 us at
+// 4 bits, 4.1 of them an SM's 55 MMAs; 10.0 at 8 bits, whose MMAs hold half as much and are twice as many; the weights alone need
+// 5.5 us of HBM.  pair_kernel, for many, is bound by the tensor cores: 84 % (4 bits) and 87 % (8 bits) of their cycles active,
+// 16384 x 8192 x 8192 in 365 to 373 us (6000 TFLOP/s) and 734 to 742 us (3000) from a cool start, and by the 1000 W power limit
+// (1.25 to 1.4 GHz, 408 to 430 and 832 to 865 us) when it lasts.
 #include "mx_common.cuh"
 #include "tc_host.cuh"
 
@@ -359,7 +361,8 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     tc_fence_before();
     __syncthreads();
   } else {
-    // All loads of two pieces at once: one at a time they cost the cluster's latency each (128 x 4096 x 4096: 9.7 us, 8.4 so).
+    // All loads of two pieces at once: one at a time they cost the cluster's latency each (128 x 4096 x 4096: 9.7 us
+    // then, 8.4 so).
     // The cluster's closing barrier tells the peers that this CTA has read their sums, so that they may leave: its arrival
     // releases, which orders those loads before it, and stands behind the last loads but in front of the last stores to Y,
     // which it would wait for (16 x 8192 x 8192: 9.04 and 10.09 us at 4 and 8 bits, 9.16 and 10.33 behind them).  All threads
@@ -732,10 +735,13 @@ int cluster_smem(int stages, int splits) {
   return L::FIXED + (FUSED ? 1024 + (stages + splits - 1) / splits * L::RESIDENT : 0);
 }
 
-// Into how many CTAs the reduction of each of `tiles` tiles is split: as many as run at once, until every SM has one; for few
-// tokens until it has two, whose latencies hide each other's, as long as each keeps eight steps (16 x 8192 x 8192: 9.1 us with
-// two CTAs of 8 steps an SM against 10.3 with one of 16 at 4 bits, 10.3 against 12.3 at 8).  Clusters have to find their SMs
-// together: of 8 CTAs with an SM each, 15 run at once, not 18.  FUSED: at least as many as make the tokens fit.
+// Into how many CTAs the reduction of each of `tiles` tiles is split, in powers of two (the kernel takes any number up to 8;
+// others were not measured): as many as run at once, until every SM has one; where shared memory has room for two on an SM, up
+// to 32 tokens, until it has two, whose latencies hide each other's, as long as each keeps eight steps.  16 x 8192 x 8192 at
+// 4 bits: 9.1 us with two CTAs of 8 steps an SM, 10.1 with one of 16.  Any limit from 4 to 8 steps does: 1 x 1024 x 8192 at
+// 4 bits takes 3.0 us with either and 3.7 with none, 16 x 2048 x 8192 at 8 bits 5.9 with 8 and 5.5 with 4, the others within
+// 2 %.  Clusters have to find their SMs together: of 8 CTAs with an SM each, 15 run at once, not 18.  FUSED: at least as
+// many as make the tokens fit.
 template <int BN, bool A8, bool FUSED, typename T>
 dq_status choose_splits(const Device& dev, int64_t tiles, int stages, int& splits) {
   using L = ClusterSmem<BN, A8, FUSED>;
@@ -803,9 +809,11 @@ dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o)
 
 // Which kernel.  Up to 64 tokens a cluster's tile: weights are what counts, and a pair's tile would be three quarters empty.
 // Above, pairs unless their one tile after another is longer than a cluster's share of the reduction.  Measured (4 to 50 us,
-// k 256 to 8192, n 512 to 13824, 80 to 1536 tokens): a pair's step takes 0.28 us, a cluster CTA's 0.38, and its epilogue over the
-// cluster as long as five of the pair's steps; with more tiles than SMs the clusters lose everywhere.
-// (256 x 8192 x 1000, 8 bits: clusters 10.3, pairs 22.2 us; 256 x 8192 x 11008: clusters 52.1, pairs 26.5.)
+// k 256 to 8192, n 512 to 13824, 80 to 1536 tokens): a pair's step took 0.28 us, a cluster CTA's 0.38, and its epilogue over the
+// cluster as long as five of the pair's steps; with more tiles than SMs the clusters lose everywhere.  Both sides, us, 8 bits:
+// 256 x 8192 x 1000 clusters 9.3, pairs 22.3; 128 x 4096 x 4096 8.8 and 13.9; 256 x 8192 x 11008 35.7 and 26.7.  A cluster's step has
+// become shorter since, and near the border the rule still takes pairs where clusters would win: 100 x 2048 x 11008 8.8 and
+// 10.1, 300 x 4096 x 5120 12.6 and 15.1, 333 x 5111 x 5001 14.8 and 18.2 (4 bits: 11.0 and 12.0).
 template <bool A8>
 dq_status cluster_is_faster(const Device& dev, const Operands& o, bool& yes) {
   constexpr int KT = Step<A8>::KT;
@@ -872,8 +880,9 @@ dq_status linear(cudaStream_t stream, const void* X, int x_dtype, int64_t m, int
   uint8_t* scales = workspace + m * row_bytes(a_fmt, k);
   Operands o{a_fmt, workspace, scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy};
   // Few tokens are quantised by the product's own CTAs, each the part that it multiplies, where that part is small: the CTAs of
-  // all weight tiles repeat the work (4096 x 4096, 1024 values a token and CTA: 1 token 5.1 us against 6.4 in two launches, 8
-  // tokens 6.1 against 6.5, 16 tokens 7.9 against 6.6; 1024 x 4096, 256 values: 16 tokens 4.3 against 5.0).
+  // all weight tiles repeat the work.  Weights from HBM, 4 bits, one launch against two: k = n = 4096, 1024 values a token and
+  // CTA, 1 token 5.0 us against 6.2, 8 tokens 5.9 against 6.2, 16 tokens 7.6 against 6.2; k = 1024, n = 4096, 256 values, 16 tokens
+  // 4.4 against 4.5; k = n = 8192, 8 tokens 11.5 against 10.8.
   if (m <= 16) {
     o.x = X; o.ldx = ldx;
     o.x_vec = whole_pieces(X, ldx, k, x_dtype);

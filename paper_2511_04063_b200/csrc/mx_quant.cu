@@ -1,9 +1,10 @@
 // Microscaled quantisation: activations or weights to codes and scales (dq_mx_quantize), back to values
 // (dq_mx_dequantize), and the root-mean-square norm with the residual's addition in front of it
 // (dq_rmsnorm_quantize).  All three are bound by HBM: one read and one write of everything.  Share of the measured copy rate,
-// counting every byte once: 16384 x 4096 bf16 to 4 bits with values 48.7 us, 95 %; norm of 65536 x 8192 bf16 with residual, sum
-// and values 766 us, 97 %; 100000 x 128 to 4 bits 11.0 us, 80 %; 5000 x 5111 fp32 (unaligned rows) to 8 bits 41.5 us, 85 %, the
-// norm of 5000 x 5111 bf16 62 us, 56 %.
+// counting every byte once, over several GPUs: 16384 x 4096 bf16 to 4 bits with values 49 to 51 us, 91 to 95 %, codes and
+// scales alone 33.4 us, 78 %, back 38.5 us, 67 %; norm of 65536 x 8192 bf16 with residual, sum and values 766 to 803 us, 92 to
+// 97 %; 100000 x 128 to 4 bits with values 10.5 to 11.0 us, 80 to 84 %; 5000 x 5111 fp32 (unaligned rows) to 8 bits with values
+// 41 to 43 us, 83 to 86 %, the norm of 5000 x 5111 bf16 57 to 62 us, 56 to 62 %.
 #include <type_traits>
 
 #include "mx_common.cuh"
@@ -359,7 +360,10 @@ dq_status rmsnorm_quantize(cudaStream_t stream, const void* X, int dtype, int64_
   DQ_CHECK(current_device(dev));
   // Pieces a warp: one where there are few rows (latency), else four, or two where four would leave too few warps to keep HBM
   // busy or the rows are not in whole pieces (4096 x 1024: 9.4 us with two, 11.4 with four; 16384 x 8192: 185 with four,
-  // 207 with two; 5000 x 5111: 62 with two, 73 with four); eight where a CTA of 16 warps would not hold the row.
+  // 207 with two; 5000 x 5111: 62 with two, 73 with four); eight where a CTA of 16 warps would not hold the row.  Between 592
+  // and about 5000 rows of whole pieces, where four begin, neither is better throughout: 1200 x 4096 12.7 us with four and 10.9
+  // with two, 1777 x 5120 18.3 and 18.0, 600 x 5120 7.7 and 8.8, 3000 x 8192 39.7 and 42.1; from 9000 rows on four are
+  // better by 6 to 12 %, except for rows of 1280 and 2560 values (two better by 5 % and by nothing).
   const bool few = rows <= 4 * dev.sms || (pieces <= 4 && rows <= 64 * dev.sms);
   const int V = pieces == 1 || (rows <= 2 * dev.sms && pieces <= 32) ? 1
                 : pieces == 2 || (pieces <= 32 && (few || !whole)) ? 2 : pieces <= 64 ? 4 : 8;
