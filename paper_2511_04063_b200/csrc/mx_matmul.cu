@@ -7,8 +7,8 @@
 //
 // Two kernels.  cluster_kernel, for few tokens, is bound by bringing the weights in, by the MMAs that consume them and by the
 // latency at both ends: an MMA takes about 140 cycles whatever its N is (each adds to the sum of the one before it; whether
-// that or the pipe sets the time was not measured), 4 KB of 4-bit weights an SM.  16 x 8192 x 8192, weights from HBM: 9.1 us at
-// 4 bits, 4.1 of them an SM's 55 MMAs; 10.0 at 8 bits, whose MMAs hold half as much and are twice as many; the weights alone need
+// that or the pipe sets the time was not measured), 4 KB of 4-bit weights an SM.  16 x 8192 x 8192, weights from HBM: 8.8 us at
+// 4 bits, 4.1 of them an SM's 55 MMAs; 9.8 at 8 bits, whose MMAs hold half as much and are twice as many; the weights alone need
 // 5.5 us of HBM.  pair_kernel, for many, is bound by the tensor cores: 84 % (4 bits) and 87 % (8 bits) of their cycles active,
 // 16384 x 8192 x 8192 in 365 to 373 us (6000 TFLOP/s) and 734 to 742 us (3000) from a cool start, and by the 1000 W power limit
 // (1.25 to 1.4 GHz, 408 to 430 and 832 to 865 us) when it lasts.
@@ -164,6 +164,15 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, uint32_t rank) {
   return v;
 }
 
+// Arrives at the cluster's barrier once the warp's reads of its peers' shared memory have been performed, which is what `bits` has
+// to depend on: every lane's goes into a vote, and the arrival takes the vote's outcome.  The arrival itself is relaxed, it orders
+// nothing; a releasing one waits for the fence and the stores to Y, too (16 x 8192 x 8192, 4 and 8 bits: 8.8 and 9.8 us so, 9.1
+// and 10.0 to 10.3 released; 256 x 8192 x 1000, 8 bits: 8.7 and 9.3; 32 x 4096 x 4096, 8 bits, weights in L2: 4.5 and 4.9 to 5.3).
+__device__ __forceinline__ void cluster_arrive_after(uint32_t bits) {
+  const int unusual = __any_sync(0xffffffffu, bits == 0x7fdb97c5u);
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %0, 0;\n\t@p nanosleep.u32 1;\n\tbarrier.cluster.arrive.relaxed.aligned;\n\t}"
+               ::"r"(unusual) : "memory");
+}
 // Rows [0, m) x values [c0, c0 + 8 groups) of X as a CTA's resident operand: codes of step i at codes + i X_BYTES in the K-major
 // 128-byte-swizzled order of the MMA's operands, its scale tiles at scales + i SF_BYTES.  A warp takes 256 values of a row at
 // a time, the `warps` warps in turn.
@@ -280,7 +289,8 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     constexpr uint32_t IDESC = scaled_idesc<A8>(128, BN);
     wait_for_previous();                                     // (the limits of the waits below do not count that kernel's time)
     // One thread waits and issues: what it decides needs no agreement, and a step is shorter than where the warp waits together
-    // (64 x 8192 x 11008, 8 bits: 17.8 us against 22.2; 16 x 8192 x 8192: 10.0 against 10.6).
+    // (64 x 8192 x 11008, 8 bits: 17.8 us against 22.2; 16 x 8192 x 8192: 10.0 against 10.6, both with a
+    // releasing arrival at the end).
     if (elect_one()) {
       auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, p.d_status, p.wait_ns); };
       const int stop = p.fail_step < kn ? (int)p.fail_step : kn;
@@ -362,47 +372,36 @@ cluster_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     __syncthreads();
   } else {
     // All loads of two pieces at once: one at a time they cost the cluster's latency each (128 x 4096 x 4096: 9.7 us
-    // then, 8.4 so).
-    // The cluster's closing barrier tells the peers that this CTA has read their sums, so that they may leave: its arrival
-    // releases, which orders those loads before it, and stands behind the last loads but in front of the last stores to Y,
-    // which it would wait for (16 x 8192 x 8192: 9.04 and 10.09 us at 4 and 8 bits, 9.16 and 10.33 behind them).  All threads
-    // make the same rounds; pieces past Y's edge are neither loaded nor stored.
+    // then, 8.4 so).  Pieces past Y's edge are neither loaded nor stored.  What was loaded is gathered in `bits`: the peers may
+    // leave, and their shared memory with them, once the barrier at the end says that this CTA has read it.
     constexpr int AT_ONCE = 2, MOST = 8;
-    const int end = c1 * 32, per_round = AT_ONCE * (int)blockDim.x;
-    int i0 = c0 * 32;
+    uint32_t bits = 0;
+    for (int i0 = (int)threadIdx.x + c0 * 32; i0 < c1 * 32; i0 += AT_ONCE * blockDim.x) {
+      float4 v[AT_ONCE][MOST];
+      auto wanted = [&](int i) { return i < c1 * 32 && n0 + (i & 31) * 4 < p.n; };
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const int i = i0 + u * (int)blockDim.x;
+        const uint32_t at = base + (uint32_t)i * 16u;        // [token][32 pieces]
+#pragma unroll
+        for (int r = 0; r < MOST; ++r)
+          if (r < p.splits && wanted(i)) v[u][r] = ld_cluster_f4(at, (uint32_t)r);
+      }
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const int i = i0 + u * (int)blockDim.x;
+        if (!wanted(i)) continue;
+        float4 s = v[u][0];
+#pragma unroll
+        for (int r = 1; r < MOST; ++r)
+          if (r < p.splits) { s.x += v[u][r].x; s.y += v[u][r].y; s.z += v[u][r].z; s.w += v[u][r].w; }
+        bits ^= __float_as_uint(s.x) ^ __float_as_uint(s.y) ^ __float_as_uint(s.z) ^ __float_as_uint(s.w);
+        store(i, s);
+      }
+    }
     tc_fence_before();
-    do {
-      float4 sum[AT_ONCE];
-      auto piece = [&](int u) { return i0 + u * (int)blockDim.x + (int)threadIdx.x; };
-      auto wanted = [&](int i) { return i < end && n0 + (i & 31) * 4 < p.n; };
-      {
-        float4 v[AT_ONCE][MOST];
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-          const uint32_t at = base + (uint32_t)piece(u) * 16u;   // [token][32 pieces]
-#pragma unroll
-          for (int r = 0; r < MOST; ++r)
-            if (r < p.splits && wanted(piece(u))) v[u][r] = ld_cluster_f4(at, (uint32_t)r);
-        }
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-          if (!wanted(piece(u))) continue;
-          sum[u] = v[u][0];
-#pragma unroll
-          for (int r = 1; r < MOST; ++r)
-            if (r < p.splits) { sum[u].x += v[u][r].x; sum[u].y += v[u][r].y; sum[u].z += v[u][r].z; sum[u].w += v[u][r].w; }
-        }
-      }
-      if (i0 + per_round >= end) {                             // (the last round)
-        __syncwarp();
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-      }
-#pragma unroll
-      for (int u = 0; u < AT_ONCE; ++u)
-        if (wanted(piece(u))) store(piece(u), sum[u]);
-      i0 += per_round;
-    } while (i0 < end);
     __syncwarp();
+    cluster_arrive_after(bits);
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   }
   if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, L::TMEM); }
@@ -738,9 +737,9 @@ int cluster_smem(int stages, int splits) {
 // Into how many CTAs the reduction of each of `tiles` tiles is split, in powers of two (the kernel takes any number up to 8;
 // others were not measured): as many as run at once, until every SM has one; where shared memory has room for two on an SM, up
 // to 32 tokens, until it has two, whose latencies hide each other's, as long as each keeps eight steps.  16 x 8192 x 8192 at
-// 4 bits: 9.1 us with two CTAs of 8 steps an SM, 10.1 with one of 16.  Any limit from 4 to 8 steps does: 1 x 1024 x 8192 at
-// 4 bits takes 3.0 us with either and 3.7 with none, 16 x 2048 x 8192 at 8 bits 5.9 with 8 and 5.5 with 4, the others within
-// 2 %.  Clusters have to find their SMs together: of 8 CTAs with an SM each, 15 run at once, not 18.  FUSED: at least as
+// 4 bits: 8.8 us with two CTAs of 8 steps an SM, 9.9 with one of 16.  Any limit from 4 to 8 steps does: 1 x 1024 x 8192 at
+// 4 bits takes 2.9 us with either and 3.5 with none, 16 x 2048 x 8192 at 8 bits 5.4 with 8 and 5.2 with 4, the others the
+// same.  Clusters have to find their SMs together: of 8 CTAs with an SM each, 15 run at once, not 18.  FUSED: at least as
 // many as make the tokens fit.
 template <int BN, bool A8, bool FUSED, typename T>
 dq_status choose_splits(const Device& dev, int64_t tiles, int stages, int& splits) {
@@ -811,9 +810,9 @@ dq_status launch_pair(cudaStream_t stream, const Device& dev, const Operands& o)
 // Above, pairs unless their one tile after another is longer than a cluster's share of the reduction.  Measured (4 to 50 us,
 // k 256 to 8192, n 512 to 13824, 80 to 1536 tokens): a pair's step took 0.28 us, a cluster CTA's 0.38, and its epilogue over the
 // cluster as long as five of the pair's steps; with more tiles than SMs the clusters lose everywhere.  Both sides, us, 8 bits:
-// 256 x 8192 x 1000 clusters 9.3, pairs 22.3; 128 x 4096 x 4096 8.8 and 13.9; 256 x 8192 x 11008 35.7 and 26.7.  A cluster's step has
+// 256 x 8192 x 1000 clusters 8.7, pairs 22.6; 128 x 4096 x 4096 8.2 and 13.9; 256 x 8192 x 11008 35.3 and 26.4.  A cluster's step has
 // become shorter since, and near the border the rule still takes pairs where clusters would win: 100 x 2048 x 11008 8.8 and
-// 10.1, 300 x 4096 x 5120 12.6 and 15.1, 333 x 5111 x 5001 14.8 and 18.2 (4 bits: 11.0 and 12.0).
+// 10.0, 300 x 4096 x 5120 12.5 and 15.0, 333 x 5111 x 5001 14.7 and 18.1 (4 bits: 11.0 and 12.0).
 template <bool A8>
 dq_status cluster_is_faster(const Device& dev, const Operands& o, bool& yes) {
   constexpr int KT = Step<A8>::KT;
@@ -881,8 +880,8 @@ dq_status linear(cudaStream_t stream, const void* X, int x_dtype, int64_t m, int
   Operands o{a_fmt, workspace, scales, w_codes, w_scales, m, n, k, Y, y_dtype, ldy};
   // Few tokens are quantised by the product's own CTAs, each the part that it multiplies, where that part is small: the CTAs of
   // all weight tiles repeat the work.  Weights from HBM, 4 bits, one launch against two: k = n = 4096, 1024 values a token and
-  // CTA, 1 token 5.0 us against 6.2, 8 tokens 5.9 against 6.2, 16 tokens 7.6 against 6.2; k = 1024, n = 4096, 256 values, 16 tokens
-  // 4.4 against 4.5; k = n = 8192, 8 tokens 11.5 against 10.8.
+  // CTA, 1 token 4.7 us against 6.1, 8 tokens 5.7 against 6.0, 16 tokens 7.5 against 6.0; k = 1024, n = 4096, 256 values, 16 tokens
+  // 4.2 against 4.3; k = n = 8192, 8 tokens 10.9 against 10.1.
   if (m <= 16) {
     o.x = X; o.ldx = ldx;
     o.x_vec = whole_pieces(X, ldx, k, x_dtype);
