@@ -63,8 +63,6 @@ def _build_calls(source: str) -> None:
                         "-I", INCLUDE, source, "-o", CALLS], capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("host compiler failed for py_calls.cpp:\n" + r.stderr)
-    if os.path.exists(UNTAGGED):
-        os.remove(UNTAGGED)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -73,6 +71,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
         _build_library(verbose)
     if force or _stale(CALLS, [header, calls]):
         _build_calls(calls)
+    if os.path.exists(UNTAGGED):
+        os.remove(UNTAGGED)
     return LIB
 
 

@@ -21,6 +21,12 @@ def test_the_module_carries_the_interpreters_tag():
     assert _calls.__file__ == build.CALLS
 
 
+def test_an_untagged_module_does_not_stay():
+    open(build.UNTAGGED, "w").close()
+    build.build()
+    assert not os.path.exists(build.UNTAGGED)
+
+
 def test_without_pythons_headers_the_library_is_still_built(monkeypatch, tmp_path):
     missing = str(tmp_path / "_calls.so")
     monkeypatch.setattr(build, "CALLS", missing)
