@@ -402,6 +402,101 @@ dq_status dq_mx_selftest_bounded_wait(int32_t a_fmt, const void* d_a_codes, cons
                                       const void* d_w_scales, int64_t n, int64_t k, void* d_Y, int32_t y_dtype, int64_t ldy,
                                       int64_t step, uint64_t limit_ns, void* cuda_stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Attention over a key/value cache in 4 bits (the paper evaluates its rotations with keys and values quantised so, per token
+ * and head, asymmetrically, behind the online Hadamard rotation of queries and keys).
+ *
+ * Cache: pages of page_size tokens (a power of two, 16 .. 4096), [n_pages][heads][dq_kv_page_bytes], of head_dim 64, 128 or
+ * 256, in groups of 16 tokens: key codes [16][head_dim / 2], key parameters [16] (scale, offset: two bf16), the same of the
+ * values.  Two codes a byte, the even dimension in the low half.  value = offset + scale * code with
+ *   offset = the largest bf16 number <= min x,  scale = the smallest bf16 number >= (max x - offset) / 15 (formed in fp32),
+ *   code = round-to-nearest-even((x - offset) / scale); 0 where scale is 0.
+ * A head of a token with a NaN, an infinity or a range past fp32's gets NaN parameters and reads back as NaN.  d_pages: 128-byte
+ * aligned.
+ * d_table [n_seqs][table_width]: the pages of a sequence, in order; an index outside [0, n_pages) is no page: what would be
+ * written there is dropped, and keys there take no part.  Pages may be shared between sequences as long as no call writes to
+ * one from two.  d_lengths [n_seqs]: tokens (slots) of a sequence, those of the call included; taken as 0 where negative and as
+ * table_width * page_size where above.  Both are read on the device when the call runs.
+ * Tokens of a call: sequence b has rows d_starts[b] .. d_starts[b + 1] - 1 of the call's tensors (d_starts [n_seqs + 1], not
+ * decreasing), or tokens / n_seqs each where d_starts is NULL.  They are its last: token i of n has slot length - n + i, and
+ * sees the slots up to its own.  Rows that belong to no sequence are left as they are.
+ * Tensors of heads (dq_heads_t): [token][head][head_dim] with contiguous values and any strides, counted in values, so that
+ * views of a fused projection can be given; heads that start on 16-byte boundaries are read and written fastest.
+ * Calls behave as the microscaled operators' do: asynchronous, nothing allocated or kept, capturable, dependent launch; a wait
+ * that gives up (dq_kv_attention's, 1 s) is reported by dq_mx_status.
+ * Errors: INVALID_ARG (null, sizes, enums, heads that do not fit, a pointer that its type's alignment rules out), UNSUPPORTED
+ * (head_dim, page_size, alignment of pages and workspace, limits, a type, a device that is not sm_100), CUDA. */
+typedef struct {
+  void* d_data;
+  int64_t token_stride, head_stride; /* in values */
+  int32_t heads;
+} dq_heads_t;
+
+typedef struct {
+  void* d_pages;
+  int64_t n_pages;
+  const int32_t* d_table;
+  const int32_t* d_lengths;
+  int32_t n_seqs, table_width, heads, head_dim, page_size;
+} dq_kv_cache_t;
+
+/* Bytes of a page of one head, of dq_kv_attention's and dq_kv_evict's workspaces; -1 for arguments out of range. */
+int64_t dq_kv_page_bytes(int32_t page_size, int32_t head_dim);
+int64_t dq_kv_attention_workspace(int32_t head_dim);
+int64_t dq_kv_evict_workspace(int32_t n_seqs, int32_t heads, int32_t keep);
+
+/* Queries and keys of each head, in one pass:
+ *   DQ_QK_NORM:     h = x / sqrt(mean x^2 + eps) * gamma (gamma: [head_dim] of gamma_dtype, DQ_FP32 or `dtype`; NULL: ones)
+ *   rotation:       pairs (a, b) of the first rot_dim values, (i, i + rot_dim / 2), or (2 i, 2 i + 1) with DQ_QK_NEIGHBOURS, to
+ *                   (a cos t - b sin t, b cos t + a sin t) with t = position * inv_freq[i], formed in 64 bits
+ *   DQ_QK_HADAMARD: y = h H / sqrt(head_dim) with Sylvester's H (head_dim 64, 128, 256), which keeps q . k
+ * computed in fp32, rounded once.  d_positions [tokens], d_inv_freq [rot_dim / 2]; rot_dim 0: no rotation.  K and K_out may be
+ * NULL.  An output may be its input.  head_dim and rot_dim: multiples of 16, head_dim at most 256. */
+enum { DQ_QK_NORM = 1, DQ_QK_NEIGHBOURS = 2, DQ_QK_HADAMARD = 4 };
+dq_status dq_qk_norm_rope(const dq_heads_t* Q, const dq_heads_t* K, int32_t dtype, int64_t tokens, int32_t head_dim,
+                          const int32_t* d_positions, const float* d_inv_freq, int32_t rot_dim, const void* d_q_gamma,
+                          const void* d_k_gamma, int32_t gamma_dtype, float eps, int32_t flags, const dq_heads_t* Q_out,
+                          const dq_heads_t* K_out, void* cuda_stream);
+
+/* Quantises the call's keys and values into their slots.  k_values, v_values (nullable; may be K and V): what the codes stand
+ * for, rounded once to `dtype`.  d_slot_positions (nullable, [n_seqs][heads][ld_slots], ld_slots >= table_width * page_size):
+ * the slots' positions, from d_positions [tokens], or the slots' own numbers where that is NULL. */
+dq_status dq_kv_append(const dq_heads_t* K, const dq_heads_t* V, int32_t dtype, int64_t tokens, const dq_kv_cache_t* cache,
+                       const int32_t* d_starts, const dq_heads_t* k_values, const dq_heads_t* v_values, const int32_t* d_positions,
+                       int32_t* d_slot_positions, int64_t ld_slots, void* cuda_stream);
+
+/* The keys and values of the sequences' last tokens, as the cache holds them, rounded once to `dtype` (zeros where there is no page
+ * or no slot). */
+dq_status dq_kv_dequantize(const dq_kv_cache_t* cache, const int32_t* d_starts, int64_t tokens, const dq_heads_t* K,
+                           const dq_heads_t* V, int32_t dtype, void* cuda_stream);
+
+/* out = softmax(scale * q k^T) v over the slots that each query sees; query head j reads kv head j / (Q's heads / cache's heads).
+ * dtype: DQ_BF16 or DQ_FP16.  A query that sees nothing gets zeros.  d_lse (nullable, [tokens][Q's heads]): the natural logarithm of the
+ * sums of exp(scale * q . k), -infinity for a query that sees nothing.  d_workspace: dq_kv_attention_workspace bytes, 16-byte
+ * aligned, set to zero once before its first use (every call leaves it ready for the next); calls that overlap on the GPU need one each.
+ * Results do not depend on the run. */
+dq_status dq_kv_attention(const dq_heads_t* Q, int32_t dtype, int64_t tokens, const dq_kv_cache_t* cache, const int32_t* d_starts,
+                          float scale, const dq_heads_t* out, float* d_lse, void* d_workspace, void* cuda_stream);
+
+/* The probability that each slot received, added up: for the slots of sequence b and kv head h,
+ *   weights_out[b][h][slot] = (slot < length - n ? weights[b][h][slot] : 0) + sum over the n queries and the query heads of h that see
+ *   the slot of exp(scale * q . k - lse)
+ * with dq_kv_attention's d_lse.  [n_seqs][heads][ld_slots], ld_slots >= table_width * page_size; d_weights NULL: zeros; d_weights_out may
+ * be d_weights.  Slots from the length on are left as they are.  Results do not depend on the run. */
+dq_status dq_kv_attention_weights(const dq_heads_t* Q, int32_t dtype, int64_t tokens, const float* d_lse, const dq_kv_cache_t* cache,
+                                  const int32_t* d_starts, float scale, const float* d_weights, float* d_weights_out,
+                                  int64_t ld_slots, void* cuda_stream);
+
+/* Leaves the sequences min(length, keep) slots: in each head those whose position is above the head's largest less `recent`, then
+ * those with the largest weights (a NaN last); of equals the lower slots.  Kept slots from `keep` on move, in order, into the
+ * slots below that are given up, with their codes, weights and positions, so a head's slots are in no order of positions
+ * afterwards, and the heads of a sequence keep different tokens.  d_lengths_out [n_seqs] receives the new lengths.  The outputs may be the
+ * inputs (d_lengths_out the cache's lengths); entries from the new length on are left as they are.  0 <= recent <= keep, keep > 0.
+ * d_workspace: dq_kv_evict_workspace bytes; calls that overlap on the GPU need one each. */
+dq_status dq_kv_evict(const dq_kv_cache_t* cache, const float* d_weights, const int32_t* d_positions, int64_t ld_slots, int32_t keep,
+                      int32_t recent, float* d_weights_out, int32_t* d_positions_out, int32_t* d_lengths_out, void* d_workspace,
+                      void* cuda_stream);
+
 const char* dq_status_string(dq_status s);
 void dq_calib_destroy(dq_calib_t* h);
 

@@ -19,6 +19,7 @@ DQ_ORTH_QR, DQ_ORTH_CAYLEY = 0, 1
 DQ_OBJ_WHIP, DQ_OBJ_VARIANCE, DQ_OBJ_KURTOSIS, DQ_OBJ_QUANT = 0, 1, 2, 3
 DQ_FP32, DQ_BF16, DQ_FP16 = 0, 1, 2
 DQ_MXFP4, DQ_MXFP8 = 0, 1
+DQ_QK_NORM, DQ_QK_NEIGHBOURS, DQ_QK_HADAMARD = 1, 2, 4
 DQ_PATH_FP32, DQ_PATH_BF16_TC = 0, 1
 DQ_MEAN_TOKENS, DQ_SUM_TOKENS = 0, 1
 DQ_SGD, DQ_SGD_MOMENTUM, DQ_ADAM = 0, 1, 2
@@ -35,6 +36,8 @@ EXPORTED_SYMBOLS = (
     "dq_calib_set_backward_precision", "dq_calib_selftest_bounded_wait", "dq_calib_time_product",
     "dq_mx_row_bytes", "dq_mx_scale_bytes", "dq_mx_linear_workspace", "dq_mx_quantize", "dq_mx_dequantize", "dq_rmsnorm_quantize",
     "dq_mx_matmul", "dq_mx_linear", "dq_mx_status", "dq_mx_selftest_bounded_wait",
+    "dq_kv_page_bytes", "dq_kv_attention_workspace", "dq_kv_evict_workspace", "dq_qk_norm_rope", "dq_kv_append", "dq_kv_dequantize",
+    "dq_kv_attention", "dq_kv_attention_weights", "dq_kv_evict",
 )
 
 
@@ -42,6 +45,16 @@ class dq_calib_config(C.Structure):
     _fields_ = [("d", C.c_int32), ("n_tokens", C.c_int64), ("batch", C.c_int32), ("x_dtype", C.c_int32),
                 ("path", C.c_int32), ("reduction", C.c_int32), ("optimizer", C.c_int32), ("lr", C.c_float),
                 ("ldx", C.c_int64)]
+
+
+class dq_heads_t(C.Structure):
+    _fields_ = [("d_data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("heads", C.c_int32)]
+
+
+class dq_kv_cache_t(C.Structure):
+    _fields_ = [("d_pages", C.c_void_p), ("n_pages", C.c_int64), ("d_table", C.c_void_p), ("d_lengths", C.c_void_p),
+                ("n_seqs", C.c_int32), ("table_width", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_size", C.c_int32)]
 
 
 class DartQuantError(RuntimeError):
@@ -98,6 +111,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.dq_calib_time_product.restype = i32
     lib.dq_calib_set_backward_precision.argtypes = [vp, i32]
     lib.dq_calib_set_backward_precision.restype = i32
+    heads, cache = C.POINTER(dq_heads_t), C.POINTER(dq_kv_cache_t)
     for name, args in (("dq_mx_quantize", [vp, i32, i64, i64, i64, i32, vp, vp, vp, i64, vp]),
                        ("dq_mx_dequantize", [i32, vp, vp, i64, i64, vp, i32, i64, vp]),
                        ("dq_rmsnorm_quantize", [vp, vp, i32, i64, i64, i64, i64, vp, i32, C.c_float, i32, vp, vp, vp, i64, vp, i64,
@@ -105,11 +119,18 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
                        ("dq_mx_matmul", [i32, vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, vp]),
                        ("dq_mx_linear", [vp, i32, i64, i64, i64, i32, vp, vp, i64, vp, i32, i64, vp, vp]),
                        ("dq_mx_selftest_bounded_wait", [i32, vp, vp, i64, vp, vp, i64, i64, vp, i32, i64, i64, C.c_uint64, vp]),
-                       ("dq_mx_status", [vp])):
+                       ("dq_mx_status", [vp]),
+                       ("dq_qk_norm_rope", [heads, heads, i32, i64, i32, vp, vp, i32, vp, vp, i32, C.c_float, i32, heads, heads, vp]),
+                       ("dq_kv_append", [heads, heads, i32, i64, cache, vp, heads, heads, vp, vp, i64, vp]),
+                       ("dq_kv_dequantize", [cache, vp, i64, heads, heads, i32, vp]),
+                       ("dq_kv_attention", [heads, i32, i64, cache, vp, C.c_float, heads, vp, vp, vp]),
+                       ("dq_kv_attention_weights", [heads, i32, i64, vp, cache, vp, C.c_float, vp, vp, i64, vp]),
+                       ("dq_kv_evict", [cache, vp, vp, i64, i32, i32, vp, vp, vp, vp, vp])):
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = i32
     for name, args in (("dq_mx_row_bytes", [i32, i64]), ("dq_mx_scale_bytes", [i64, i64]),
-                       ("dq_mx_linear_workspace", [i32, i64, i64])):
+                       ("dq_mx_linear_workspace", [i32, i64, i64]), ("dq_kv_page_bytes", [i32, i32]),
+                       ("dq_kv_attention_workspace", [i32]), ("dq_kv_evict_workspace", [i32, i32, i32])):
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = i64
     lib.dq_calib_launch_count.argtypes = [vp]
@@ -354,12 +375,15 @@ def _mx():
         try:
             from . import _calls as calls
         except ImportError as e:
-            raise ImportError("the microscaled operators' Python calls are not built for this interpreter: run "
+            raise ImportError("the microscaled and key/value cache operators' Python calls are not built for this interpreter: run "
                               "`python -m paper_2511_04063_b200.build` where its Python.h is installed") from e
         torch.cuda.current_device()
         calls.bind(tuple(C.cast(getattr(lib, n), C.c_void_p).value for n in
                          ("dq_mx_quantize", "dq_mx_dequantize", "dq_rmsnorm_quantize", "dq_mx_matmul", "dq_mx_linear")),
                    (torch.float32, torch.bfloat16, torch.float16), torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        calls.bind_kv(tuple(C.cast(getattr(lib, n), C.c_void_p).value for n in
+                            ("dq_qk_norm_rope", "dq_kv_append", "dq_kv_dequantize", "dq_kv_attention", "dq_kv_attention_weights",
+                             "dq_kv_evict", "dq_kv_attention_workspace", "dq_kv_evict_workspace")), torch.int32)
         _calls = calls
     return _calls
 
@@ -437,6 +461,108 @@ def dq_mx_selftest_bounded_wait(a_codes, a_scales, a_fmt: int, w_codes, w_scales
     _check(load_library().dq_mx_selftest_bounded_wait(
         a_fmt, a_codes.data_ptr(), a_scales.data_ptr(), Y.shape[0], w_codes.data_ptr(), w_scales.data_ptr(), Y.shape[1], k,
         Y.data_ptr(), dtype, Y.stride(0), step, limit_ns, _stream_ptr(stream)), "dq_mx_selftest_bounded_wait")
+
+
+# ---------------------------------------------------------------------------
+# Attention over a key/value cache in 4 bits (include/dartquant.h says what the calls compute).  Tensors of heads are
+# [tokens, heads, head_dim] with contiguous values and any other strides; indices are int32, sums and weights float32.
+# ---------------------------------------------------------------------------
+def dq_kv_page_bytes(page_size: int, head_dim: int) -> int:
+    return int(load_library().dq_kv_page_bytes(page_size, head_dim))
+
+
+def dq_kv_attention_workspace(head_dim: int) -> int:
+    return int(load_library().dq_kv_attention_workspace(head_dim))
+
+
+def dq_kv_evict_workspace(n_seqs: int, heads: int, keep: int) -> int:
+    return int(load_library().dq_kv_evict_workspace(n_seqs, heads, keep))
+
+
+def dq_kv_pages(n_pages: int, heads: int, head_dim: int, page_size: int, device="cuda"):
+    """Memory of n_pages pages of page_size tokens (a power of two from 16 on): uint8 [n_pages, heads, bytes]."""
+    import torch
+    size = dq_kv_page_bytes(page_size, head_dim)
+    if size < 0:
+        raise ValueError("pages of %r tokens of %r values: a power of two from 16 to 4096 and 64, 128 or 256 are needed"
+                         % (page_size, head_dim))
+    return torch.empty((n_pages, heads, size), dtype=torch.uint8, device=device)
+
+
+class dq_kv_cache:
+    """A cache: pages (dq_kv_pages), table (int32 [n_seqs, pages of a sequence]: which page holds its tokens, -1: none) and
+    lengths (int32 [n_seqs], a call's own tokens counted).  Holds the tensors; their contents may change between calls."""
+
+    __slots__ = ("pages", "table", "lengths", "head_dim", "page_size", "heads", "n_seqs", "slots", "_struct", "_call")
+
+    def __init__(self, pages, table, lengths, head_dim: int):
+        import torch
+        if pages.dtype != torch.uint8 or pages.dim() != 3 or not pages.is_contiguous() or not pages.is_cuda:
+            raise ValueError("pages: a contiguous CUDA tensor [n_pages, heads, bytes] of uint8 is needed")
+        if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous() or table.device != pages.device:
+            raise ValueError("table: a contiguous int32 tensor [n_seqs, pages of a sequence] on the pages' device is needed")
+        if lengths.dtype != torch.int32 or lengths.shape != table.shape[:1] or not lengths.is_contiguous() or lengths.device != pages.device:
+            raise ValueError("lengths: a contiguous int32 tensor [n_seqs] on the pages' device is needed")
+        page_size = pages.shape[2] // (head_dim + 8) if head_dim > 0 else 0
+        if dq_kv_page_bytes(page_size, head_dim) != pages.shape[2]:
+            raise ValueError("pages: %d bytes are no page of heads of %r values" % (pages.shape[2], head_dim))
+        if pages.shape[1] < 1 or table.shape[1] < 1:
+            raise ValueError("a cache has at least one head, and a table at least one column")
+        self.pages, self.table, self.lengths, self.head_dim, self.page_size = pages, table, lengths, head_dim, page_size
+        self.heads, self.n_seqs, self.slots = pages.shape[1], table.shape[0], table.shape[1] * page_size
+        self._struct = dq_kv_cache_t(pages.data_ptr(), pages.shape[0], table.data_ptr(), lengths.data_ptr(), table.shape[0],
+                                     table.shape[1], pages.shape[1], head_dim, page_size)
+        self._call = (C.addressof(self._struct), pages.get_device())
+
+
+def dq_qk_norm_rope(Q, K, positions, inv_freq, Q_out, K_out, q_gamma=None, k_gamma=None, eps: float = 1e-6, flags: int = DQ_QK_NORM,
+                    stream=None):
+    """Queries and keys of each head: norm (DQ_QK_NORM), rotation by position, Hadamard rotation (DQ_QK_HADAMARD).  positions:
+    [tokens]; inv_freq: [rotated values / 2], or None; gamma: [head_dim] of Q's type or float32; K and K_out may be None, outputs
+    their inputs."""
+    status = (_calls or _mx()).qk_norm_rope(Q, K, positions, inv_freq, Q_out, K_out, q_gamma, k_gamma, eps, flags, stream)
+    if status != DQ_OK:
+        raise DartQuantError(status, "dq_qk_norm_rope")
+
+
+def dq_kv_append(K, V, cache, starts=None, k_values=None, v_values=None, positions=None, slot_positions=None, stream=None):
+    """Quantises K and V into the cache, as each sequence's last tokens: rows starts[b] to starts[b + 1], or equally many each.
+    k_values, v_values (may be K and V): what the codes stand for.  slot_positions ([n_seqs, heads, cache.slots]) receives
+    positions ([tokens]; None: the slots' numbers)."""
+    status = (_calls or _mx()).append(K, V, cache, starts, k_values, v_values, positions, slot_positions, stream)
+    if status != DQ_OK:
+        raise DartQuantError(status, "dq_kv_append")
+
+
+def dq_kv_dequantize(cache, K, V, starts=None, stream=None):
+    """K and V = what the cache holds for each sequence's last tokens."""
+    status = (_calls or _mx()).kv_dequantize(cache, K, V, starts, stream)
+    if status != DQ_OK:
+        raise DartQuantError(status, "dq_kv_dequantize")
+
+
+def dq_kv_attention(Q, cache, scale: float, out, workspace, starts=None, lse=None, stream=None):
+    """out = softmax(scale q k^T) v of each sequence's last tokens over its cache.  workspace: dq_kv_attention_workspace(head_dim)
+    bytes, zeros before their first use.  lse ([tokens, Q's heads]): the logarithms of the sums."""
+    status = (_calls or _mx()).attention(Q, cache, scale, out, workspace, starts, lse, stream)
+    if status != DQ_OK:
+        raise DartQuantError(status, "dq_kv_attention")
+
+
+def dq_kv_attention_weights(Q, lse, cache, scale: float, weights_out, weights=None, starts=None, stream=None):
+    """weights_out ([n_seqs, heads, cache.slots]) = weights (None: zeros; new slots start at zero) + the probability that each
+    slot received from these queries.  weights_out may be weights."""
+    status = (_calls or _mx()).attention_weights(Q, lse, cache, scale, weights_out, weights, starts, stream)
+    if status != DQ_OK:
+        raise DartQuantError(status, "dq_kv_attention_weights")
+
+
+def dq_kv_evict(cache, weights, positions, keep: int, recent: int, weights_out, positions_out, lengths_out, workspace, stream=None):
+    """Leaves each head of a sequence its `recent` last positions and the slots with the largest weights, `keep` in all, in the slots
+    below `keep`.  The outputs may be the inputs (lengths_out: cache.lengths).  workspace: dq_kv_evict_workspace(...) bytes."""
+    status = (_calls or _mx()).evict(cache, weights, positions, keep, recent, weights_out, positions_out, lengths_out, workspace, stream)
+    if status != DQ_OK:
+        raise DartQuantError(status, "dq_kv_evict")
 
 
 def dq_version() -> str:

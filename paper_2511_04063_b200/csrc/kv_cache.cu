@@ -1,0 +1,347 @@
+// The key/value cache in 4 bits: writing (dq_kv_append), reading back (dq_kv_dequantize) and eviction (dq_kv_evict).
+//
+// Quantiser, for the D values of a token's key or value in one head:
+//     offset = the largest bf16 number <= min x,   scale = the smallest bf16 number >= (max x - offset) / 15,
+//     code = rint((x - offset) / scale), 0 where scale is 0
+// Rounding outwards keeps every value inside the grid, so no code is clamped, and bf16's range is that of the inputs.  A head
+// with a NaN or an infinity, or a range past fp32's, gets a scale of NaN and reads back as NaN.
+//
+// Bound by HBM: 2 D bytes read and D / 2 + 4 written for each key and each value in 16 bits (and 2 D where the values that the
+// codes stand for are asked for).  A lane takes 16 values, D / 16 lanes a head; a CTA takes some tokens, for which it finds
+// sequence, slot and page first.
+#include "kv_common.cuh"
+
+namespace dq {
+namespace kv {
+namespace {
+
+using mx::Vec8;
+using mx::from_f32;
+using mx::to_f32;
+
+constexpr int THREADS = 256;
+constexpr int TILE = 32;      // tokens of a CTA at most
+
+__device__ __forceinline__ float bf16_below(float v) {
+  const uint32_t w = __float_as_uint(v), cut = w & 0xffff0000u;
+  return __uint_as_float((int)w < 0 && cut != w ? cut + 0x10000u : cut);
+}
+
+template <typename T>
+__device__ __forceinline__ void load16(float (&x)[16], const T* p, bool vec) {
+  if (vec) {
+    Vec8<T> a, b;
+    a.load(p);
+    b.load(p + 8);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 u = a.pair(i), w = b.pair(i);
+      x[2 * i] = u.x; x[2 * i + 1] = u.y;
+      x[8 + 2 * i] = w.x; x[8 + 2 * i + 1] = w.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = to_f32(p[i]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store16(const float (&x)[16], T* p, bool vec) {
+  if (vec) {
+    Vec8<T> a, b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a.set_pair(i, make_float2(x[2 * i], x[2 * i + 1]));
+      b.set_pair(i, make_float2(x[8 + 2 * i], x[8 + 2 * i + 1]));
+    }
+    a.store(p);
+    b.store(p + 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[i] = from_f32<T>(x[i]);
+  }
+}
+
+// Where the tokens of a CTA lie: the first kv head's group of a token's slot (null: in no page), and whether it is a sequence's.
+struct Place { uint8_t* group; int in_group, there; };
+__device__ __forceinline__ Place place_of(const AppendArgs& a, int64_t t, int dim) {
+  Place at{nullptr, 0, 0};
+  const int b = t < a.batch.tokens ? a.batch.sequence(t) : -1;
+  if (b < 0) return at;
+  int64_t first;
+  int n;
+  a.batch.range(b, first, n);
+  if (t < first || t >= first + n) return at;
+  at.there = 1;
+  const int length = a.cache.length(b);
+  const int64_t slot = length - n + (t - first);
+  if (slot < 0) return at;
+  at.in_group = (int)slot & (GROUP - 1);
+  const int64_t page = a.cache.page_of(b, (int)slot);
+  if (page >= 0) at.group = a.cache.group_at(page, 0, (int)slot, dim);
+  if (a.slot_positions)
+    for (int h = 0; h < a.cache.heads; ++h)
+      a.slot_positions[((int64_t)b * a.cache.heads + h) * a.ld_slots + slot] = a.positions ? a.positions[t] : (int)slot;
+  return at;
+}
+
+// WRITE: values are quantised into the cache; otherwise read back from it.
+template <typename T, int DIM, bool WRITE>
+__global__ void __launch_bounds__(THREADS) append_kernel(const AppendArgs a, int tile) {
+  constexpr int LANES = DIM / 16, GROUPS = THREADS / LANES, HALF = GROUP * (DIM / 2 + 4);
+  __shared__ Place s_place[TILE];
+  const int l = threadIdx.x % LANES;
+  const int64_t t0 = (int64_t)blockIdx.x * tile;
+  const int heads = a.cache.heads, jobs = tile * 2 * heads;
+  mx::wait_for_previous();
+  if ((int)threadIdx.x < tile) s_place[threadIdx.x] = place_of(a, t0 + threadIdx.x, DIM);
+  __syncthreads();
+  for (int j0 = 0; j0 < jobs; j0 += GROUPS) {   // all lanes of a warp go round equally often
+    const int j = j0 + threadIdx.x / LANES;
+    const int i = j / (2 * heads), which = j % (2 * heads), h = which < heads ? which : which - heads;
+    const bool value = which >= heads;
+    const Place at = j < jobs ? s_place[i] : Place{nullptr, 0, 0};
+    const Heads& src = value ? a.v : a.k;
+    const int64_t t = t0 + i;
+    uint8_t* group = at.group ? at.group + h * a.cache.page_bytes + (value ? HALF : 0) : nullptr;
+    float x[16];
+    if constexpr (!WRITE) {
+      if (!at.there) continue;
+      float scale = 0.f, offset = 0.f;
+      uint2 w = make_uint2(0u, 0u);
+      if (group) {
+        w = *reinterpret_cast<const uint2*>(group + at.in_group * (DIM / 2) + l * 8);
+        const uint32_t p = *reinterpret_cast<const uint32_t*>(group + GROUP * (DIM / 2) + at.in_group * 4);
+        scale = scale_of(p);
+        offset = offset_of(p);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = __fadd_rn(offset, __fmul_rn(scale, (float)(((e < 8 ? w.x : w.y) >> (4 * (e & 7))) & 15u)));
+      store16<T>(x, reinterpret_cast<T*>(src.p) + t * src.token + h * src.head + l * 16, src.vec);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = 0.f;
+      if (at.there) load16<T>(x, reinterpret_cast<const T*>(src.p) + t * src.token + h * src.head + l * 16, src.vec);
+      float lo = x[0], hi = x[0], most = x[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) {
+        lo = fminf(lo, x[e]);
+        hi = fmaxf(hi, x[e]);
+        most = mx::larger(most, x[e]);
+      }
+#pragma unroll
+      for (int d = 1; d < LANES; d <<= 1) {
+        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+        most = mx::larger(most, __shfl_xor_sync(0xffffffffu, most, d));
+      }
+      float offset = bf16_below(lo + 0.f);                       // (-0 becomes 0)
+      float scale = 0.f - bf16_below(-((hi - offset) / 15.f));
+      const bool good = fabsf(most) <= 3.402823466e38f && scale <= 3.402823466e38f;
+      uint32_t w[2] = {0u, 0u};
+      if (good && scale > 0.f) {
+        const float inverse = 1.f / scale;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float d = x[e] - offset;
+          // the quotient by the reciprocal is off by three roundings, 15 x 3 x 2^-24 at most: near a half, where that could
+          // decide, and where the reciprocal is out of range, the division itself
+          float q = d * inverse, c = rintf(q);
+          if (!(fabsf(fabsf(q - c) - 0.5f) > 1e-5f)) c = rintf(__fdiv_rn(d, scale));
+          w[e >> 3] |= (uint32_t)c << (4 * (e & 7));
+          x[e] = __fadd_rn(offset, __fmul_rn(scale, c));
+        }
+      } else {
+        if (!good) scale = offset = __uint_as_float(0x7fc00000u);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = offset;
+      }
+      if (group) {
+        *reinterpret_cast<uint2*>(group + at.in_group * (DIM / 2) + l * 8) = make_uint2(w[0], w[1]);
+        if (l == 0)
+          *reinterpret_cast<uint32_t*>(group + GROUP * (DIM / 2) + at.in_group * 4) =
+              (__float_as_uint(scale) >> 16) | (__float_as_uint(offset) & 0xffff0000u);
+      }
+      const Heads& dst = value ? a.v_values : a.k_values;
+      if (at.there && dst.p) store16<T>(x, reinterpret_cast<T*>(dst.p) + t * dst.token + h * dst.head + l * 16, dst.vec);
+    }
+  }
+  mx::allow_next();
+}
+
+template <bool WRITE>
+dq_status run_append(cudaStream_t stream, int dtype, int dim, const AppendArgs& a) {
+  // about two rounds of heads a CTA, so that its search of sequences and pages is worth one
+  const int groups = THREADS / (dim / 16);
+  const int tile = max(1, min(TILE, (2 * groups) / (2 * a.cache.heads)));
+  return by_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    return by_dim(dim, [&](auto d) {
+      mx::LaunchConfig c(stream, (a.batch.tokens + tile - 1) / tile, THREADS);
+      return mx::launch(c, append_kernel<T, decltype(d)::value, WRITE>, a, tile);
+    });
+  });
+}
+
+// ------------------------------------------------------------------------------------------------ eviction
+// One CTA for each (sequence, kv head) finds the `keep` slots that stay: the order is (protected, weight, lower slot first).  A
+// radix selection over the weights' order-preserving bits, 8 at a time, finds the key of the last one that stays and how many of
+// its equals do.  Slots from `keep` on that stay move into the slots below that do not, the i-th into the i-th: what is moved is
+// read from slots that nothing writes, so no order between the moves is needed, and a sequence that is over its budget by a
+// few tokens moves a few.
+constexpr int SELECT = 1024;
+
+__device__ __forceinline__ uint32_t order_key(float w, int position, int64_t guarded_above) {
+  if ((int64_t)position > guarded_above) return 0xffffffffu;
+  if (w != w) return 0u;
+  const uint32_t u = __float_as_uint(w + 0.f);                 // (-0 becomes 0)
+  return (int)u < 0 ? ~u : u | 0x80000000u;
+}
+
+__global__ void __launch_bounds__(SELECT) evict_select_kernel(const EvictArgs a) {
+  __shared__ int s_count[256], s_sum[SELECT / 32][3], s_pick[2], s_newest[SELECT / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t row = blockIdx.x;                              // sequence x heads + head
+  const int b = (int)(row / a.cache.heads);
+  mx::wait_for_previous();
+  const int n = a.cache.length(b), keep = min(n, a.keep);
+  const float* weights = a.weights + row * a.ld_slots;
+  const int* positions = a.positions + row * a.ld_slots;
+  int* ws = a.workspace + row * evict_stride(a.keep);
+  int64_t guarded_above = 0;
+  uint32_t last = 0u;      // the key of the last slot that stays
+  int equals = n;          // how many slots with that key stay
+  if (n > keep) {
+    int newest = INT_MIN;
+    for (int i = tid; i < n; i += SELECT) newest = max(newest, positions[i]);
+    newest = __reduce_max_sync(0xffffffffu, newest);
+    if (lane == 0) s_newest[warp] = newest;
+    __syncthreads();
+    for (int w = 0; w < SELECT / 32; ++w) newest = max(newest, s_newest[w]);
+    guarded_above = (int64_t)newest - a.recent;
+    int wanted = keep;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      if (tid < 256) s_count[tid] = 0;
+      __syncthreads();
+      const uint32_t known = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
+      for (int i = tid; i < n; i += SELECT) {
+        const uint32_t key = order_key(weights[i], positions[i], guarded_above);
+        if ((key & known) == last) atomicAdd(&s_count[(key >> shift) & 255u], 1);
+      }
+      __syncthreads();
+      if (warp == 0) {   // from the largest digit down: the first at which the count reaches what is wanted
+        int sum = 0;
+        int c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += c[i] = s_count[255 - (lane * 8 + i)];
+        int upto = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, upto, d);
+          if (lane >= d) upto += v;
+        }
+        int before = upto - sum;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (before < wanted && before + c[i] >= wanted) { s_pick[0] = 255 - (lane * 8 + i); s_pick[1] = wanted - before; }
+          before += c[i];
+        }
+      }
+      __syncthreads();
+      last |= (uint32_t)s_pick[0] << shift;
+      wanted = s_pick[1];
+    }
+    equals = wanted;
+  }
+  float* weights_out = a.weights_out + row * a.ld_slots;
+  int* positions_out = a.positions_out + row * a.ld_slots;
+  int same = 0, holes = 0, movers = 0;                          // so far
+  for (int i0 = 0; i0 < n; i0 += SELECT) {
+    const int i = i0 + tid;
+    float w = 0.f;
+    int position = 0;
+    uint32_t key = 0u;
+    if (i < n) {
+      w = weights[i];
+      position = positions[i];
+      key = order_key(w, position, guarded_above);
+    }
+    const uint32_t below = (1u << lane) - 1u;
+    const bool equal = i < n && n > keep && key == last;
+    uint32_t votes = __ballot_sync(0xffffffffu, equal);
+    __syncthreads();
+    if (lane == 0) s_sum[warp][0] = __popc(votes);
+    __syncthreads();
+    int before = same + __popc(votes & below);
+    for (int v = 0; v < SELECT / 32; ++v) { if (v < warp) before += s_sum[v][0]; same += s_sum[v][0]; }
+    const bool stays = i < n && (n <= keep || key > last || (equal && before < equals));
+    const bool hole = i < keep && !stays, mover = i >= keep && stays;
+    const uint32_t h_votes = __ballot_sync(0xffffffffu, hole), m_votes = __ballot_sync(0xffffffffu, mover);
+    if (lane == 0) { s_sum[warp][1] = __popc(h_votes); s_sum[warp][2] = __popc(m_votes); }
+    __syncthreads();
+    int h_before = holes + __popc(h_votes & below), m_before = movers + __popc(m_votes & below);
+    for (int v = 0; v < SELECT / 32; ++v) {
+      if (v < warp) { h_before += s_sum[v][1]; m_before += s_sum[v][2]; }
+      holes += s_sum[v][1];
+      movers += s_sum[v][2];
+    }
+    if (hole) ws[4 + 2 * h_before + 1] = i;
+    if (mover) ws[4 + 2 * m_before] = i;
+    if (stays && i < keep) { weights_out[i] = w; positions_out[i] = position; }
+  }
+  if (tid == 0) ws[0] = movers;
+  __syncthreads();
+  for (int i = tid; i < movers; i += SELECT) {
+    const int from = ws[4 + 2 * i], to = ws[4 + 2 * i + 1];
+    weights_out[to] = weights[from];
+    positions_out[to] = positions[from];
+  }
+  mx::allow_next();
+}
+
+template <int DIM>
+__global__ void __launch_bounds__(THREADS) evict_move_kernel(const EvictArgs a, int parts) {
+  constexpr int LANES = DIM / 16, GROUPS = THREADS / LANES, HALF = GROUP * (DIM / 2 + 4);
+  const int64_t row = blockIdx.x / parts;
+  const int part = blockIdx.x % parts, b = (int)(row / a.cache.heads), h = (int)(row % a.cache.heads);
+  const int l = threadIdx.x % LANES;
+  mx::wait_for_previous();
+  const int* ws = a.workspace + row * evict_stride(a.keep);
+  const int moves = ws[0];
+  for (int i = part * GROUPS + threadIdx.x / LANES; i < moves; i += parts * GROUPS) {
+    const int from = ws[4 + 2 * i], to = ws[4 + 2 * i + 1];
+    const int64_t from_page = a.cache.page_of(b, from), to_page = a.cache.page_of(b, to);
+    if (from_page < 0 || to_page < 0) continue;
+    const int half = l >= LANES / 2 ? HALF : 0, chunk = l % (LANES / 2);
+    const uint8_t* src = a.cache.group_at(from_page, h, from, DIM) + half;
+    uint8_t* dst = a.cache.group_at(to_page, h, to, DIM) + half;
+    const int f = from & (GROUP - 1), t = to & (GROUP - 1);
+    const uint4 codes = *reinterpret_cast<const uint4*>(src + f * (DIM / 2) + chunk * 16);
+    uint32_t p = 0u;
+    if (chunk == 0) p = *reinterpret_cast<const uint32_t*>(src + GROUP * (DIM / 2) + f * 4);
+    *reinterpret_cast<uint4*>(dst + t * (DIM / 2) + chunk * 16) = codes;
+    if (chunk == 0) *reinterpret_cast<uint32_t*>(dst + GROUP * (DIM / 2) + t * 4) = p;
+  }
+  if (h == 0 && part == 0 && threadIdx.x == 0) a.lengths_out[b] = min(a.cache.length(b), a.keep);   // (may be the lengths themselves)
+  mx::allow_next();
+}
+
+}  // namespace
+
+dq_status append(cudaStream_t stream, int dtype, int dim, const AppendArgs& a) { return run_append<true>(stream, dtype, dim, a); }
+dq_status dequantize(cudaStream_t stream, int dtype, int dim, const AppendArgs& a) { return run_append<false>(stream, dtype, dim, a); }
+
+dq_status evict(cudaStream_t stream, const mx::Device& dev, int dim, const EvictArgs& a) {
+  const int64_t rows = (int64_t)a.cache.n_seqs * a.cache.heads;
+  {
+    mx::LaunchConfig c(stream, rows, SELECT);
+    DQ_CHECK(mx::launch(c, evict_select_kernel, a));
+  }
+  // eight CTAs an SM at most, and none without a round of moves
+  const int groups = THREADS / (dim / 16);
+  const int parts = (int)max((int64_t)1, min((int64_t)(a.keep + groups - 1) / groups, (8 * (int64_t)dev.sms + rows - 1) / rows));
+  mx::LaunchConfig c(stream, rows * parts, THREADS);
+  return by_dim(dim, [&](auto d) { return mx::launch(c, evict_move_kernel<decltype(d)::value>, a, parts); });
+}
+
+}  // namespace kv
+}  // namespace dq
