@@ -122,7 +122,7 @@ class Cache:
             if r is not None:
                 c, s, o = r
                 v[slot], there[slot] = s * c + o, True
-                m[slot] = np.abs(s * (c.astype(np.float64) - 8)) + np.abs(o + 8 * s)
+                m[slot] = np.abs(s * c) + np.abs(o)
         return v, m, there
 
     def length(self, b):
@@ -131,7 +131,8 @@ class Cache:
 
 def attention(cache, b, h, q, scale):
     """q [n][group][dim] of a sequence's last n tokens: dict of out, lse, p [n][group][slots] and error magnitudes: `terms` of the
-    output (sum of p times the values' terms) and `logits` (the largest sum of magnitudes behind a logit that is seen)."""
+    output (sum of p times the values' terms), `logits` (the largest sum of magnitudes behind a logit that is seen) and `largest` (of the
+    values' terms)."""
     n, length = q.shape[0], cache.length(b)
     k, k_terms, there = cache.exact(b, h, length, 0)
     v, v_terms, _ = cache.exact(b, h, length, 1)
@@ -150,7 +151,7 @@ def attention(cache, b, h, q, scale):
             p[i, g, seen] = e / e.sum()
             out[i, g], terms[i, g] = p[i, g, seen] @ v[seen], p[i, g, seen] @ v_terms[seen]
             logits[i, g] = (k_terms[seen] @ np.abs(q[i, g])).max() * abs(scale)
-    return dict(out=out, lse=lse, p=p, terms=terms, logits=logits)
+    return dict(out=out, lse=lse, p=p, terms=terms, logits=logits, largest=np.nanmax(v_terms, initial=0.0))
 
 
 def evict(weights, positions, length, keep, recent):

@@ -3,19 +3,21 @@
 //
 //     S = scale q k^T over the slots a query sees,   O = softmax(S) v,   lse = log sum exp S
 //
-// With k = ks c + ko for codes c = 0 .. 15,   q . k = ks (q . (c - 8)) + (ko + 8 ks) sum q,   and
-// sum_t p_t v_t = sum_t (p_t vs_t) (c_t - 8) + sum_t p_t (vo_t + 8 vs_t):   the matrix instructions multiply the codes, centred so
-// that the sums stay small, and the parameters enter once for each key.  c - 8 is formed in place: four bits or'ed into the
-// mantissa of 128 (bf16) or 1024 (fp16), less 136 or 1032.
+// With k = ks c + ko for codes c = 0 .. 15,   q . k = ks (q . c) + ko sum q   and   sum_t p_t v_t = sum_t (p_t vs_t) c_t + sum_t p_t vo_t:
+// the matrix instructions multiply the codes, and the parameters enter once for each key.  Four bits alone are an fp16 number,
+// the subnormal c 2^-24 (c 2^-20 four bits further up), which the tensor cores multiply exactly: one AND turns two codes into two
+// operands, and the powers of two are taken out with the parameters.  (Bits or'ed into the mantissa of 1024, less 1032, are three
+// instructions; with them a token over 131072 slots took 107 us.)
 //
 // The keys are the rows (M) of the instructions and the query rows their columns (N = 8), so that the eight or fewer query heads
 // of a kv head fill a tile: S^T = K Q^T, O^T = V^T P^T with mma.m16n8k16.  Any order of the dimensions serves the first product
 // as long as Q has the same, any order of the keys the second as long as P has: a thread takes neighbouring codes of a key, as
 // they lie, in both.  P^T comes out of the first product transposed and is turned by movmatrix.
-// P vs is rounded to bf16 for the second product (relative error 2^-9 a term, as the output's own rounding); for fp16 queries it
-// is held in two bf16 numbers (2^-17), because the output has 11 bits.
-#include <type_traits>
-
+//
+// Roundings to 16 bits.  A query row is multiplied by a power of two that brings its largest value to 2^14 and rounded to fp16: exact
+// for fp16's 11 and bf16's 8 bits, save values below 2^-24 of the largest.  P vs is divided by the power of two of the stage's
+// largest vs and rounded to fp16 (2^-11 a term; below 2^-20 of the row's largest 2^-31 of it).  A stage's sum of P vs c starts
+// from zero and is added in fp32: the instructions' own sums truncate, which over a long axis would add up.
 #include "kv_common.cuh"
 #include "tc_gemm.cuh"
 
@@ -26,30 +28,13 @@ namespace {
 constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
 constexpr int STAGE = 2 * GROUP;   // keys of a pipeline stage: the maximum of a row is looked at once for 32 keys
 
-template <typename T>
-__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
-template <>
-__device__ __forceinline__ void mma<__nv_bfloat16>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-template <>
-__device__ __forceinline__ void mma<__half>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Codes in bits 0-3 and 16-19, as c - 8.
-template <typename T> __device__ __forceinline__ uint32_t centred(uint32_t w);
-template <> __device__ __forceinline__ uint32_t centred<__nv_bfloat16>(uint32_t w) {
-  const uint32_t v = (w & 0x000f000fu) | 0x43004300u, eight = 0x43084308u;   // 136
-  const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&eight));
-  return *reinterpret_cast<const uint32_t*>(&d);
-}
-template <> __device__ __forceinline__ uint32_t centred<__half>(uint32_t w) {
-  const uint32_t v = (w & 0x000f000fu) | 0x64006400u, eight = 0x64086408u;   // 1032
-  const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&eight));
-  return *reinterpret_cast<const uint32_t*>(&d);
-}
+// Two codes as fp16 numbers, c 2^-24: bits 0-3 and 16-19; c 2^-20: bits 4-7 and 20-23.
+__device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000fu; }
+__device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
 __device__ __forceinline__ uint32_t transposed(uint32_t v) {
   uint32_t d;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
@@ -60,8 +45,8 @@ __device__ __forceinline__ float exp2_of(float v) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(v));
   return d;
 }
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+__device__ __forceinline__ uint32_t half_pair(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 template <int WORDS>
@@ -79,38 +64,32 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[WORDS], const uint8_t* 
 // 64 bytes apart modulo 128 so that a quarter of a warp reads its keys without bank conflicts.
 __device__ __forceinline__ int key_of(int r) { const int c = (r & 7) >> 1; return (r & 8) + ((r & 1) ? (c ^ 1) + 4 : c); }
 
-// Eight query values as B fragments of a word's two k steps: (d, d + 4) for d = 0 .. 3.
+// Eight values of a row, zeros where there is none.
 template <typename T>
-__device__ __forceinline__ void query_words(uint32_t (&b)[4], float& sum, const T* p, bool there, bool vec) {
-  uint32_t w[4] = {0u, 0u, 0u, 0u};
+__device__ __forceinline__ void load_values(float (&v)[8], const T* p, bool there, bool vec) {
+  mx::Vec8<T> x;
+  x.clear();
   if (there) {
-    if (vec) {
-      const uint4 v = *reinterpret_cast<const uint4*>(p);
-      w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-    } else {
+    if (vec) x.load(p);
+    else
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        w[i] = (uint32_t)reinterpret_cast<const uint16_t*>(p)[2 * i] | ((uint32_t)reinterpret_cast<const uint16_t*>(p)[2 * i + 1] << 16);
-    }
+      for (int i = 0; i < 4; ++i) x.set_pair(i, make_float2(mx::to_f32(p[2 * i]), mx::to_f32(p[2 * i + 1])));
   }
-  b[0] = __byte_perm(w[0], w[2], 0x5410);
-  b[1] = __byte_perm(w[0], w[2], 0x7632);
-  b[2] = __byte_perm(w[1], w[3], 0x5410);
-  b[3] = __byte_perm(w[1], w[3], 0x7632);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    T v[2];
-    memcpy(v, &w[i], 4);
-    sum += mx::to_f32(v[0]) + mx::to_f32(v[1]);
+    const float2 f = x.pair(i);
+    v[2 * i] = f.x; v[2 * i + 1] = f.y;
   }
 }
 
-// A warp's query rows: tile of 8 NT rows (row r: token r / group, head r % group) as B fragments, and the sums of columns 2 c, 2 c + 1.
+// A warp's query rows: tile of 8 NT rows (row r: token r / group, head r % group) as B fragments.  Dimensions whose codes lie four
+// bits up are held 2^-4 smaller.  For the columns 2 c and 2 c + 1: `by`, what takes the powers of two out of a product, and the
+// sum of the row.
 template <typename T, int DIM, int NT>
 struct Queries {
   static constexpr int WORDS = DIM / 32;
   uint32_t b[NT][WORDS][4];
-  float sum[NT][2];
+  float by[NT][2], sum[NT][2];
   __device__ __forceinline__ void load(const Heads& q, int64_t first, int rows, int row0, int h, int group, int lane) {
     const int c = lane & 3;
 #pragma unroll
@@ -119,18 +98,38 @@ struct Queries {
       const bool there = r < rows;
       const int i = there ? r / group : 0;
       const T* p = reinterpret_cast<const T*>(q.p) + (first + i) * q.token + (int64_t)(h * group + (there ? r - i * group : 0)) * q.head;
-      float s = 0.f;
+      float v[WORDS][8], s = 0.f, most = 0.f;
 #pragma unroll
-      for (int w = 0; w < WORDS; ++w) query_words<T>(b[nt][w], s, p + (c * WORDS + w) * 8, there, q.vec);
+      for (int w = 0; w < WORDS; ++w) {
+        load_values<T>(v[w], p + (c * WORDS + w) * 8, there, q.vec);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          s += v[w][e];
+          most = fmaxf(most, fabsf(v[w][e]));
+        }
+      }
       s += __shfl_xor_sync(0xffffffffu, s, 1);
       s += __shfl_xor_sync(0xffffffffu, s, 2);
-      sum[nt][0] = __shfl_sync(0xffffffffu, s, c * 8);
-      sum[nt][1] = __shfl_sync(0xffffffffu, s, c * 8 + 4);
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      // the largest value's exponent field, within what keeps both factors normal numbers; a row that is not finite stays so
+      const int field = min(max((int)mx::exponent_field(most), 14), 244);
+      const float up = __uint_as_float((uint32_t)(268 - field) << 23), up4 = up * 0.0625f;
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[nt][w][e] = half_pair(v[w][e] * (e & 1 ? up4 : up), v[w][e + 4] * (e & 1 ? up4 : up));
+      const float down = __uint_as_float((uint32_t)(field + 10) << 23);   // 2^24 / up
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        sum[nt][j] = __shfl_sync(0xffffffffu, s, c * 8 + 4 * j);
+        by[nt][j] = __shfl_sync(0xffffffffu, down, c * 8 + 4 * j);
+      }
     }
   }
 };
 
-// q . (c - 8) of a group's 16 keys and the tile's rows: acc[nt] = (key_of(g), columns 2 c, 2 c + 1), (key_of(g + 8), the same).
+// (q . c) of a group's 16 keys and the tile's rows, without q.by: acc[nt] = (key_of(g), columns 2 c, 2 c + 1), (key_of(g + 8), the same).
 template <typename T, int DIM, int NT>
 __device__ __forceinline__ void key_products(float (&acc)[NT][4], const uint8_t* codes, const Queries<T, DIM, NT>& q, int lane) {
   constexpr int WORDS = DIM / 32;
@@ -146,10 +145,10 @@ __device__ __forceinline__ void key_products(float (&acc)[NT][4], const uint8_t*
   for (int w = 0; w < WORDS; ++w)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const uint32_t a0 = centred<T>(k0[w] >> (8 * e)), a1 = centred<T>(k1[w] >> (8 * e));
-      const uint32_t a2 = centred<T>(k0[w] >> (8 * e + 4)), a3 = centred<T>(k1[w] >> (8 * e + 4));
+      const uint32_t x0 = k0[w] >> (8 * e), x1 = k1[w] >> (8 * e);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mma<T>(acc[nt], a0, a1, a2, a3, q.b[nt][w][2 * e], q.b[nt][w][2 * e + 1]);
+      for (int nt = 0; nt < NT; ++nt)
+        mma(acc[nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), q.b[nt][w][2 * e], q.b[nt][w][2 * e + 1]);
     }
 }
 
@@ -174,19 +173,21 @@ __device__ __forceinline__ void describe(Item& it, const AttentionArgs& a, int b
 }
 
 // ------------------------------------------------------------------------------------------------ few rows
-// A CTA takes an equal share of all stages of all items, whatever the sequences' lengths: one producer warp brings groups in by bulk copies, a
-// ring of stages ahead; each of the other warps takes whole stages in turn, with its own maximum, sum and O^T, joined in shared memory at an
-// item's end.  An item that crosses CTAs is left in the workspace in parts, and the CTA that finishes last joins them, in order.
+// A CTA takes an equal share of all stages of all items, whatever the sequences' lengths, and its warps take them in turn, each with its
+// own maximum, sum and O^T, joined in shared memory at an item's end.  A warp brings its stages in by bulk copies into two places of
+// its own: while it works on one the other is on its way, across items too.  An item that crosses CTAs is left in the workspace in parts,
+// and the CTA that finishes last joins them, in order.
 template <int DIM, int NT>
 struct Few {
   static constexpr int ROWS = 8 * NT;
   static constexpr int WARPS = DIM == 256 || (DIM == 128 && NT == 2) ? 8 : 16;
-  static constexpr int SLOTS = DIM == 256 ? 16 : 32;
-  static constexpr int THREADS = (WARPS + 1) * 32;
+  static constexpr int SLOTS = 2;
+  static constexpr int THREADS = WARPS * 32;
   static constexpr int GROUP_BYTES = GROUP * (DIM + 8), STAGE_BYTES = 2 * GROUP_BYTES;
   static constexpr int PAD = DIM + 4;                                  // floats of a row of O, against bank conflicts
+  static constexpr int RING_BYTES = WARPS * SLOTS * STAGE_BYTES;
   static constexpr int JOIN_BYTES = WARPS * ROWS * PAD * 4;
-  static constexpr int SMEM = SLOTS * STAGE_BYTES + JOIN_BYTES;
+  static constexpr int SMEM = RING_BYTES + JOIN_BYTES;
   static constexpr int PART = ROWS * (DIM + 2);                        // floats of a part in the workspace: O, maxima, sums
 };
 constexpr int MAX_CTAS = 256;
@@ -194,24 +195,45 @@ constexpr int TICKET_BYTES = MAX_CTAS * 4;
 constexpr int LEAST_STAGES = 8;                                        // of a CTA
 constexpr float SLACK = 8.f;                                           // a maximum may grow by this (in powers of two) before O is rescaled
 
+// A walk over the items in the order (sequence, head, tile).
+template <int ROWS>
+struct Walk {
+  Item it;
+  int seq;
+  int64_t index, begin;                                                // of the sequence's items; the item's first unit
+  __device__ __forceinline__ void start(const AttentionArgs& a, const Share& s) {
+    seq = s.seq;
+    describe<ROWS>(it, a, seq);
+    index = (s.lo - s.before) / it.stages;
+    begin = s.before + index * it.stages;
+  }
+  __device__ __forceinline__ void next(const AttentionArgs& a) {
+    begin += it.stages;
+    if (++index < (int64_t)it.tiles * a.cache.heads) return;
+    index = 0;
+    do {
+      if (++seq == a.batch.n_seqs) return;
+      describe<ROWS>(it, a, seq);
+    } while (it.tiles == 0);
+  }
+};
+
 template <typename T, int DIM, int NT>
 __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const AttentionArgs a) {
   using F = Few<DIM, NT>;
   constexpr int ROWS = F::ROWS, WARPS = F::WARPS, SLOTS = F::SLOTS, VW = DIM / 64;
   extern __shared__ __align__(128) uint8_t smem[];
-  float* joined = reinterpret_cast<float*>(smem + SLOTS * F::STAGE_BYTES);
-  __shared__ __align__(8) uint64_t s_full[SLOTS], s_empty[SLOTS];
-  __shared__ int s_valid[SLOTS];
+  float* joined = reinterpret_cast<float*>(smem + F::RING_BYTES);
+  __shared__ __align__(8) uint64_t s_full[WARPS][SLOTS];
+  __shared__ int s_valid[WARPS][SLOTS];
+  struct Fetch { Walk<ROWS> walk; int64_t unit; int issued; };
+  __shared__ Fetch s_fetch[WARPS];                                     // of what a warp brings in next; its first lane's
   __shared__ Share s_share;
-  __shared__ int64_t s_sums[WARPS + 1];
+  __shared__ int64_t s_sums[WARPS];
   __shared__ float s_max[WARPS][ROWS], s_sum[WARPS][ROWS];
   __shared__ int s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t full0 = tc::smem_u32(s_full), empty0 = tc::smem_u32(s_empty);
-  if (tid < SLOTS) {
-    tc::mbar_init(full0 + tid * 8, 1);
-    tc::mbar_init(empty0 + tid * 8, 1);
-  }
+  if (tid < WARPS * SLOTS) tc::mbar_init(tc::smem_u32(&s_full[0][0]) + tid * 8, 1);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   mx::wait_for_previous();
   mx::allow_next();
@@ -223,79 +245,51 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
   const Share share = s_share;
   if (share.lo >= share.hi) return;
 
-  // Items in the order (sequence, head, tile); both kinds of warps walk the same way.
-  Item it;
-  int seq = share.seq;
-  describe<ROWS>(it, a, seq);
-  int64_t index = (share.lo - share.before) / it.stages;                // of the sequence's items
-  int64_t begin = share.before + index * it.stages;                     // the item's first unit
-  auto next = [&]() {
-    begin += it.stages;
-    if (++index == (int64_t)it.tiles * a.cache.heads) {
-      index = 0;
-      do {
-        if (++seq == a.batch.n_seqs) return;
-        describe<ROWS>(it, a, seq);
-      } while (it.tiles == 0);
-    }
+  const uint32_t full0 = tc::smem_u32(&s_full[warp][0]);
+  uint8_t* const ring = smem + warp * SLOTS * F::STAGE_BYTES;
+  Walk<ROWS> at;
+  at.start(a, share);
+  auto fetch = [&](Fetch& f) {                                          // the warp's next stage, by its first lane
+    if (f.unit >= share.hi) return;
+    while (f.unit >= f.walk.begin + f.walk.it.stages) f.walk.next(a);
+    const Item& it = f.walk.it;
+    const int h = (int)(f.walk.index / it.tiles), slot = (int)(f.unit - f.walk.begin) * STAGE, place = f.issued % SLOTS;
+    const int64_t p0 = slot < it.length ? a.cache.page_of(it.b, slot) : -1;
+    const int64_t p1 = slot + GROUP < it.length ? a.cache.shift > 4 ? p0 : a.cache.page_of(it.b, slot + GROUP) : -1;
+    const bool joint = a.cache.shift > 4 && p1 >= 0;                    // both groups in one page, one behind the other
+    const uint32_t dst = tc::smem_u32(ring + place * F::STAGE_BYTES), bar = full0 + place * 8;
+    auto copy = [&](uint32_t to, const uint8_t* from, uint32_t bytes) {
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                   ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+    };
+    s_valid[warp][place] = (p0 >= 0 ? 1 : 0) | (p1 >= 0 ? 2 : 0);
+    tc::mbar_expect_tx(bar, ((p0 >= 0) + (p1 >= 0)) * F::GROUP_BYTES);
+    if (p0 >= 0) copy(dst, a.cache.group_at(p0, h, slot, DIM), joint ? F::STAGE_BYTES : F::GROUP_BYTES);
+    if (p1 >= 0 && !joint) copy(dst + F::GROUP_BYTES, a.cache.group_at(p1, h, slot + GROUP, DIM), F::GROUP_BYTES);
+    f.unit += WARPS;
+    ++f.issued;
   };
-  int64_t count = 0;                                                    // stages of this CTA so far
-
-  if (warp == WARPS) {   // ------------------------------------------------ producer
-    bool alive = true;
-    while (alive) {
-      const int h = (int)(index / it.tiles);
-      const int64_t s0 = max(begin, share.lo) - begin, s1 = min(begin + it.stages, share.hi) - begin;
-      for (int64_t at = s0; at < s1 && alive; at += 32) {               // a lane looks a stage's pages up
-        int64_t page[2] = {-1, -1};
-        const int slot0 = (int)(at + lane) * STAGE;
-        if (at + lane < s1) {
-          if (slot0 < it.length) page[0] = a.cache.page_of(it.b, slot0);
-          if (slot0 + GROUP < it.length) page[1] = a.cache.shift > 4 ? page[0] : a.cache.page_of(it.b, slot0 + GROUP);
-        }
-        for (int j = 0; j < 32 && at + j < s1; ++j, ++count) {
-          const int ring = (int)(count % SLOTS);
-          const int64_t p0 = __shfl_sync(0xffffffffu, page[0], j), p1 = __shfl_sync(0xffffffffu, page[1], j);
-          alive = __all_sync(0xffffffffu, tc::mbar_wait(empty0 + ring * 8, (uint32_t)(count / SLOTS + 1) & 1u, a.d_status));
-          if (!alive) break;
-          if (lane == 0) {
-            const int slot = (int)(at + j) * STAGE;
-            const uint32_t dst = tc::smem_u32(smem + ring * F::STAGE_BYTES), bar = full0 + ring * 8;
-            auto copy = [&](uint32_t to, const uint8_t* from, uint32_t bytes) {
-              asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                           ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
-            };
-            const bool joint = a.cache.shift > 4 && p1 >= 0;             // both groups in one page, one behind the other
-            s_valid[ring] = (p0 >= 0 ? 1 : 0) | (p1 >= 0 ? 2 : 0);
-            tc::mbar_expect_tx(bar, ((p0 >= 0) + (p1 >= 0)) * F::GROUP_BYTES);
-            if (p0 >= 0) copy(dst, a.cache.group_at(p0, h, slot, DIM), joint ? F::STAGE_BYTES : F::GROUP_BYTES);
-            if (p1 >= 0 && !joint) copy(dst + F::GROUP_BYTES, a.cache.group_at(p1, h, slot + GROUP, DIM), F::GROUP_BYTES);
-          }
-          __syncwarp();
-        }
-      }
-      if (begin + it.stages >= share.hi) break;
-      next();
-    }
-    if (!alive)   // no copy is left on its way into memory that may go to another CTA
-      for (int64_t j = max((int64_t)0, count - SLOTS); j < count; ++j)
-        tc::mbar_wait(full0 + (int)(j % SLOTS) * 8, (uint32_t)(j / SLOTS) & 1u, a.d_status);
-    return;
+  if (lane == 0) {
+    Fetch& f = s_fetch[warp];
+    f.walk = at;
+    f.unit = share.lo + warp;
+    f.issued = 0;
+    for (int i = 0; i < SLOTS; ++i) fetch(f);
   }
+  __syncwarp();
 
-  // ------------------------------------------------------------------------ the others
   const int g = lane >> 2, c = lane & 3;
   const float to_log2 = a.scale * LOG2E;
-  auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory"); };
   bool alive = true;
+  int turn = 0;                                                         // stages of this warp so far
   Queries<T, DIM, NT> q;
+  int64_t unit = share.lo + warp;                                       // this warp's next
   while (true) {
-    const int h = (int)(index / it.tiles), row0 = (int)(index % it.tiles) * ROWS;
-    const int64_t s0 = max(begin, share.lo) - begin, s1 = min(begin + it.stages, share.hi) - begin;
+    const Item& it = at.it;
+    const int64_t begin = at.begin;
+    const int h = (int)(at.index / it.tiles), row0 = (int)(at.index % it.tiles) * ROWS;
     const bool starts = begin >= share.lo, ends = begin + it.stages <= share.hi;
-    int64_t k = s0 + (warp - count % WARPS + WARPS) % WARPS;            // this warp's first stage of the segment
-    int64_t n_count = count + (k - s0);
-    count += s1 - s0;
+    const int64_t until = min(begin + it.stages, share.hi);
     float top[NT][2], sum[NT][2], off[NT][2], o[NT][VW * 4][4];
     int sees[NT][2];
 #pragma unroll
@@ -315,15 +309,16 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
       for (int i = 0; i < VW * 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.f;
-    if (k < s1) q.load(a.q, it.first, it.rows, row0, h, a.group, lane);
+    if (unit < until) q.load(a.q, it.first, it.rows, row0, h, a.group, lane);
 
-    for (; k < s1; k += WARPS, n_count += WARPS) {
-      const int ring = (int)(n_count % SLOTS);
-      if (alive) alive = __all_sync(0xffffffffu, tc::mbar_wait(full0 + ring * 8, (uint32_t)(n_count / SLOTS) & 1u, a.d_status));
-      const int slot0 = (int)k * STAGE;
-      if (alive && slot0 < most) {
-        const uint8_t* stage = smem + ring * F::STAGE_BYTES;
-        const int valid = s_valid[ring];
+    for (; unit < until; unit += WARPS) {
+      const int place = turn % SLOTS;
+      if (alive) alive = __all_sync(0xffffffffu, tc::mbar_wait(full0 + place * 8, (uint32_t)(turn / SLOTS) & 1u, a.d_status));
+      if (!alive) continue;
+      const int slot0 = (int)(unit - begin) * STAGE;
+      if (slot0 < most) {
+        const uint8_t* stage = ring + place * F::STAGE_BYTES;
+        const int valid = s_valid[warp][place];
         const bool masked = slot0 + STAGE > least || valid != 3;
         float s[2][NT][4];
 #pragma unroll
@@ -333,19 +328,26 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const uint32_t p = *reinterpret_cast<const uint32_t*>(group + GROUP * (DIM / 2) + key_of(g + 8 * e) * 4);
-            const float ks = scale_of(p) * to_log2, kz = offset_of(p) * to_log2 + 8.f * ks;
+            const float ks = scale_of(p) * to_log2, ko = offset_of(p) * to_log2;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int j = 0; j < 2; ++j) s[u][nt][2 * e + j] = s[u][nt][2 * e + j] * ks + kz * q.sum[nt][j];
+              for (int j = 0; j < 2; ++j) s[u][nt][2 * e + j] = s[u][nt][2 * e + j] * (ks * q.by[nt][j]) + ko * q.sum[nt][j];
           }
         }
+        uint32_t vp[2][2];                                              // the values' parameters; a masked key's may be anything
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            vp[u][e] = *reinterpret_cast<const uint32_t*>(stage + u * F::GROUP_BYTES + GROUP * (DIM + 4) + key_of(g + 8 * e) * 4);
         if (masked)
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int slot = (valid >> u & 1) ? slot0 + u * GROUP + key_of(g + 8 * e) : INT_MAX;
+              if (slot >= it.length) vp[u][e] = 0u;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -382,14 +384,32 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
                 o[nt][i][2 + j] *= by;
               }
             }
+        // the exponent field of the stage's largest vs (a NaN's does not count): vs 2^(6 - field + 127) < 2^7, and with p < 2^SLACK
+        // P stays below 2^15
+        uint32_t field = 7u;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t f = vp[u][e] >> 7 & 255u;
+            field = max(field, f == 255u ? 0u : f);
+          }
+        field = __reduce_max_sync(0xffffffffu, field);
+        const float shrink = __uint_as_float((260u - field) << 23), grow = __uint_as_float((field - 6u) << 23);
+        float part[NT][VW * 4][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < VW * 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) part[nt][i][j] = 0.f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const uint8_t* group = stage + u * F::GROUP_BYTES + GROUP * (DIM / 2 + 4);
-          uint32_t b[NT][2], b_low[NT][2];
+          uint32_t b[NT][2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(group + GROUP * (DIM / 2) + key_of(g + 8 * e) * 4);
-            const float vs = scale_of(w), vz = offset_of(w) + 8.f * vs;
+            const float vs = scale_of(vp[u][e]) * shrink, vo = offset_of(vp[u][e]);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               float pv[2];
@@ -397,15 +417,12 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
               for (int j = 0; j < 2; ++j) {
                 const float x = s[u][nt][2 * e + j], m = top[nt][j];
                 const float p = exp2_of(x - (m == -INFINITY ? 0.f : m));
-                const bool gone = masked && x == -INFINITY;              // its parameters may be anything
+                const bool gone = masked && x == -INFINITY;              // (its value may be a NaN that others see)
                 sum[nt][j] += p;
-                off[nt][j] += gone ? 0.f : p * vz;
+                off[nt][j] += gone ? 0.f : p * vo;
                 pv[j] = gone ? 0.f : p * vs;
               }
-              const uint32_t high = bf16_pair(pv[0], pv[1]);
-              b[nt][e] = transposed(high);
-              if (!std::is_same<T, __nv_bfloat16>::value)
-                b_low[nt][e] = transposed(bf16_pair(pv[0] - scale_of(high), pv[1] - offset_of(high)));
+              b[nt][e] = transposed(half_pair(pv[0], pv[1]));
             }
           }
           uint32_t x[4][VW];
@@ -417,19 +434,26 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
             const uint32_t lo23 = __byte_perm(x[2][w], x[3][w], 0x5410), hi23 = __byte_perm(x[2][w], x[3][w], 0x7632);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint32_t a0 = centred<__nv_bfloat16>(lo01 >> (4 * i)), a1 = centred<__nv_bfloat16>(hi01 >> (4 * i));
-              const uint32_t a2 = centred<__nv_bfloat16>(lo23 >> (4 * i)), a3 = centred<__nv_bfloat16>(hi23 >> (4 * i));
+              const uint32_t a0 = lo01 >> (i & 2 ? 8 : 0), a1 = hi01 >> (i & 2 ? 8 : 0), a2 = lo23 >> (i & 2 ? 8 : 0), a3 = hi23 >> (i & 2 ? 8 : 0);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
-                mma<__nv_bfloat16>(o[nt][w * 4 + i], a0, a1, a2, a3, b[nt][0], b[nt][1]);
-                if (!std::is_same<T, __nv_bfloat16>::value) mma<__nv_bfloat16>(o[nt][w * 4 + i], a0, a1, a2, a3, b_low[nt][0], b_low[nt][1]);
+                if (i & 1) mma(part[nt][w * 4 + i], high_codes(a0), high_codes(a1), high_codes(a2), high_codes(a3), b[nt][0], b[nt][1]);
+                else mma(part[nt][w * 4 + i], low_codes(a0), low_codes(a1), low_codes(a2), low_codes(a3), b[nt][0], b[nt][1]);
               }
             }
           }
         }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < VW * 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[nt][i][j] += part[nt][i][j] * grow;
       }
+      ++turn;
+      __syncwarp();                                                     // all lanes have read the stage
+      if (lane == 0) fetch(s_fetch[warp]);
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(empty0 + ring * 8);
     }
 
     // ---- the item's rows over the warps
@@ -444,7 +468,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
         }
         if (g == 0) { s_max[warp][nt * 8 + 2 * c + j] = top[nt][j]; s_sum[warp][nt * 8 + 2 * c + j] = sum[nt][j]; }
       }
-    sync();
+    __syncthreads();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -455,18 +479,18 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
         for (int w = 0; w < WARPS; ++w) m = fmaxf(m, s_max[w][r]);
         const float by = top[nt][j] == -INFINITY ? 1.f : exp2_of(top[nt][j] - m);
         float* row = joined + (warp * ROWS + r) * F::PAD + g * (DIM / 8);
+        constexpr float LOW = 16777216.f, HIGH = 1048576.f;             // 2^24 and 2^20: of the codes
 #pragma unroll
-        for (int i = 0; i < VW; ++i) {
-          float4 v;
-          v.x = (o[nt][4 * i][j] + off[nt][j]) * by; v.y = (o[nt][4 * i + 1][j] + off[nt][j]) * by;
-          v.z = (o[nt][4 * i + 2][j] + off[nt][j]) * by; v.w = (o[nt][4 * i + 3][j] + off[nt][j]) * by;
-          *reinterpret_cast<float4*>(row + 8 * i) = v;
-          v.x = (o[nt][4 * i][2 + j] + off[nt][j]) * by; v.y = (o[nt][4 * i + 1][2 + j] + off[nt][j]) * by;
-          v.z = (o[nt][4 * i + 2][2 + j] + off[nt][j]) * by; v.w = (o[nt][4 * i + 3][2 + j] + off[nt][j]) * by;
-          *reinterpret_cast<float4*>(row + 8 * i + 4) = v;
-        }
+        for (int i = 0; i < VW; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float4 v;
+            v.x = (o[nt][4 * i][2 * e + j] * LOW + off[nt][j]) * by; v.y = (o[nt][4 * i + 1][2 * e + j] * HIGH + off[nt][j]) * by;
+            v.z = (o[nt][4 * i + 2][2 * e + j] * LOW + off[nt][j]) * by; v.w = (o[nt][4 * i + 3][2 * e + j] * HIGH + off[nt][j]) * by;
+            *reinterpret_cast<float4*>(row + 8 * i + 4 * e) = v;
+          }
       }
-    sync();
+    __syncthreads();
     const int cta = blockIdx.x;
     const int first_cta = starts ? cta : cta_of(begin, share.total, share.ctas);
     const int last_cta = ends ? cta : cta_of(begin + it.stages - 1, share.total, share.ctas);
@@ -505,9 +529,9 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
     if (!whole) {
       int* ticket = reinterpret_cast<int*>(a.workspace) + first_cta;
       __threadfence();
-      sync();
+      __syncthreads();
       if (tid == 0) s_last = atomicAdd(ticket, 1) == last_cta - first_cta;
-      sync();
+      __syncthreads();
       if (s_last) {
         __threadfence();
         if (tid == 0) *ticket = 0;                                       // for the next call
@@ -529,10 +553,12 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
         }
       }
     }
-    sync();
+    __syncthreads();
     if (begin + it.stages >= share.hi) break;
-    next();
+    at.next(a);
   }
+  if (!alive && lane == 0)   // no copy is left on its way into memory that may go to another CTA
+    for (int i = turn; i < s_fetch[warp].issued; ++i) tc::mbar_wait(full0 + (i % SLOTS) * 8, (uint32_t)(i / SLOTS) & 1u, a.d_status);
 }
 
 template <typename T, int DIM, int NT>
@@ -583,12 +609,12 @@ __global__ void __launch_bounds__(W_WARPS * 32) weights_kernel(const AttentionAr
     float got[2] = {0.f, 0.f};
     if (page >= 0) {
       const uint8_t* group = a.cache.group_at(page, h, slot0, DIM);
-      float ks[2], kz[2];
+      float ks[2], ko[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const uint32_t p = *reinterpret_cast<const uint32_t*>(group + GROUP * (DIM / 2) + key_of(g + 8 * e) * 4);
         ks[e] = scale_of(p) * to_log2;
-        kz[e] = offset_of(p) * to_log2 + 8.f * ks[e];
+        ko[e] = offset_of(p) * to_log2;
       }
       // rows before the first one that sees slot0 see nothing here
       const int row_first = max(0, slot0 - (length - n)) * a.group / 8 * 8;
@@ -605,7 +631,7 @@ __global__ void __launch_bounds__(W_WARPS * 32) weights_kernel(const AttentionAr
           const float lse = a.lse[(first + i) * a.q.heads + h * a.group + r - i * a.group] * LOG2E;
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            if (slot0 + key_of(g + 8 * e) < sees) got[e] += exp2_of(s[0][2 * e + j] * ks[e] + kz[e] * q.sum[0][j] - lse);
+            if (slot0 + key_of(g + 8 * e) < sees) got[e] += exp2_of(s[0][2 * e + j] * (ks[e] * q.by[0][j]) + (ko[e] * q.sum[0][j] - lse));
         }
       }
     }

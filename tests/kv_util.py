@@ -65,15 +65,16 @@ def attend(cache, q, scale, starts=None, work=None, out=None, lse=None):
 
 
 def logit_bound(logits, dim):
-    """A logit is a sum of dim exact products (a code's four bits times a query's 8 or 11) in fp32, in steps that may truncate, times a
-    scale, plus an offset times the sum of the query: off by at most (dim / 16 + 24) 2^-23 of the magnitudes' sum."""
+    """A logit is a sum of dim exact products (a code's four bits times a query's 8 or 11; queries below 2^-24 of their row's largest are
+    off by 2^-35 of it) in fp32, in steps that may truncate, times a scale, plus an offset times the sum of the query: off by at most (dim / 16 + 24) 2^-23 of the magnitudes' sum."""
     return (dim / 16 + 24) * 2.0 ** -23 * logits + 2.0 ** -22
 
 
 def check_attention(c, b, q, first, n, group, scale, out, lse):
     """Rows first .. first + n of out and lse against the oracle.  p = exp(S - top) / l is off by twice the logits' error relatively
-    (S and l), by 2^-20 for the exponentials, sums and joins, and by half a bf16 step where it is rounded for the product (two bf16
-    numbers, 2^-17, for fp16 queries); the output is then rounded once."""
+    (S and l), by 2^-20 for the exponentials, sums and joins, and by half an fp16 step, 2^-11, where it is rounded for the product:
+    of a term that is at least 2^-20 of what a key with p = 1 and the largest scale of its stage has (2^6 .. 2^7, fp16's normal numbers
+    begin at 2^-14), else by 2^-25 / 2^6 of the latter; the output is then rounded once."""
     dtype = q.dtype
     for h in range(c.heads):
         heads = slice(h * group, (h + 1) * group)
@@ -84,7 +85,7 @@ def check_attention(c, b, q, first, n, group, scale, out, lse):
         assert (np.isneginf(got) == empty).all()
         full = ~empty
         assert (np.abs(got[full] - r["lse"][full]) <= e[full] + 2.0 ** -21 * (1 + np.abs(r["lse"][full]))).all()
-        rounding = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -17
-        bound = (2 * e[..., None] + 2.0 ** -20 + rounding) * r["terms"] * 1.01 + UNIT[dtype] * np.abs(r["out"]) * 1.01 + LEAST[dtype]
+        bound = (2 * e[..., None] + 2.0 ** -20 + 2.0 ** -11) * r["terms"] * 1.01 + UNIT[dtype] * np.abs(r["out"]) * 1.01 + LEAST[dtype]
+        bound += c.length(b) * 2.0 ** -31 * r["largest"]
         got = f64(out[first:first + n, heads])
         assert (np.abs(got - r["out"]) <= bound).all(), float((np.abs(got - r["out"]) / bound).max())
