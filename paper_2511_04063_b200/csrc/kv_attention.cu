@@ -32,6 +32,11 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The same with a sum that starts from zero.
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 // Two codes as fp16 numbers, c 2^-24: bits 0-3 and 16-19; c 2^-20: bits 4-7 and 20-23.
 __device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000fu; }
 __device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
@@ -83,14 +88,14 @@ __device__ __forceinline__ void load_values(float (&v)[8], const T* p, bool ther
 }
 
 // A warp's query rows: tile of 8 NT rows (row r: token r / group, head r % group) as B fragments.  Dimensions whose codes lie four
-// bits up are held 2^-4 smaller.  For the columns 2 c and 2 c + 1: `by`, what takes the powers of two out of a product, and the
-// sum of the row.
+// bits up are held 2^-4 smaller.  For the columns 2 c and 2 c + 1: `by`, what takes the powers of two out of a product, and the sum of
+// the row, both times `factor`.
 template <typename T, int DIM, int NT>
 struct Queries {
   static constexpr int WORDS = DIM / 32;
   uint32_t b[NT][WORDS][4];
   float by[NT][2], sum[NT][2];
-  __device__ __forceinline__ void load(const Heads& q, int64_t first, int rows, int row0, int h, int group, int lane) {
+  __device__ __forceinline__ void load(const Heads& q, int64_t first, int rows, int row0, int h, int group, float factor, int lane) {
     const int c = lane & 3;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -122,8 +127,8 @@ struct Queries {
       const float down = __uint_as_float((uint32_t)(field + 10) << 23);   // 2^24 / up
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        sum[nt][j] = __shfl_sync(0xffffffffu, s, c * 8 + 4 * j);
-        by[nt][j] = __shfl_sync(0xffffffffu, down, c * 8 + 4 * j);
+        sum[nt][j] = __shfl_sync(0xffffffffu, s, c * 8 + 4 * j) * factor;
+        by[nt][j] = __shfl_sync(0xffffffffu, down, c * 8 + 4 * j) * factor;
       }
     }
   }
@@ -138,96 +143,106 @@ __device__ __forceinline__ void key_products(float (&acc)[NT][4], const uint8_t*
   load_words<WORDS>(k0, codes + key_of(g) * (DIM / 2) + c * (DIM / 8));
   load_words<WORDS>(k1, codes + key_of(g + 8) * (DIM / 2) + c * (DIM / 8));
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[nt][i] = 0.f;
-#pragma unroll
   for (int w = 0; w < WORDS; ++w)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const uint32_t x0 = k0[w] >> (8 * e), x1 = k1[w] >> (8 * e);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-        mma(acc[nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), q.b[nt][w][2 * e], q.b[nt][w][2 * e + 1]);
+      for (int nt = 0; nt < NT; ++nt) {
+        const uint32_t b0 = q.b[nt][w][2 * e], b1 = q.b[nt][w][2 * e + 1];
+        if (w == 0 && e == 0) mma_first(acc[nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), b0, b1);
+        else mma(acc[nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), b0, b1);
+      }
     }
 }
 
-// What an item of work is: a tile of query rows of a sequence and kv head, with `stages` stages of keys.
-struct Item {
-  int b, h, tile;
-  int64_t first;
-  int n, length, rows, tiles;
-  int64_t stages;
-};
-
-// Sequence b's units of work: every tile of rows of every kv head, with the stages of its keys (one at least: rows that see
-// nothing are written too).
+// An item of work is a tile of query rows of a sequence and kv head; it has `stages` stages of keys (one at least: rows that see nothing
+// are written too).
 template <int ROWS>
-__device__ __forceinline__ void describe(Item& it, const AttentionArgs& a, int b) {
-  it.b = b;
-  a.batch.range(b, it.first, it.n);
-  it.length = a.cache.length(b);
-  it.rows = it.n * a.group;
-  it.tiles = (it.rows + ROWS - 1) / ROWS;
-  it.stages = max(1, (it.length + STAGE - 1) / STAGE);
-}
+struct Sequence {
+  int64_t first;
+  int n, length, tiles, stages;
+  __device__ __forceinline__ void describe(const AttentionArgs& a, int b) {
+    a.batch.range(b, first, n);
+    length = a.cache.length(b);
+    tiles = (int)(((int64_t)n * a.group + ROWS - 1) / ROWS);
+    stages = max(1, (length + STAGE - 1) / STAGE);
+  }
+};
 
 // ------------------------------------------------------------------------------------------------ few rows
 // A CTA takes an equal share of all stages of all items, whatever the sequences' lengths, and its warps take them in turn, each with its
 // own maximum, sum and O^T, joined in shared memory at an item's end.  A warp brings its stages in by bulk copies into two places of
 // its own: while it works on one the other is on its way, across items too.  An item that crosses CTAs is left in the workspace in parts,
 // and the CTA that finishes last joins them, in order.
+constexpr int MAX_CTAS = 640;
+constexpr int TICKET_BYTES = MAX_CTAS * 4;
+#ifndef FEW_WARPS
+#define FEW_WARPS 8
+#endif
 template <int DIM, int NT>
 struct Few {
   static constexpr int ROWS = 8 * NT;
-  static constexpr int WARPS = DIM == 256 || (DIM == 128 && NT == 2) ? 8 : 16;
+  static constexpr int WARPS = DIM == 256 || (DIM == 128 && NT == 2) ? FEW_WARPS / 2 : FEW_WARPS;
+  static constexpr int PER_SM = 16 / FEW_WARPS;
   static constexpr int SLOTS = 2;
   static constexpr int THREADS = WARPS * 32;
   static constexpr int GROUP_BYTES = GROUP * (DIM + 8), STAGE_BYTES = 2 * GROUP_BYTES;
   static constexpr int PAD = DIM + 4;                                  // floats of a row of O, against bank conflicts
   static constexpr int RING_BYTES = WARPS * SLOTS * STAGE_BYTES;
-  static constexpr int JOIN_BYTES = WARPS * ROWS * PAD * 4;
+  static constexpr int O_BYTES = WARPS * ROWS * PAD * 4, PARTS_BYTES = 2 * 148 * PER_SM * ROWS * 4;
+  static constexpr int JOIN_BYTES = O_BYTES > PARTS_BYTES ? O_BYTES : PARTS_BYTES;   // the warps' O; factors and sums of an item's parts
   static constexpr int SMEM = RING_BYTES + JOIN_BYTES;
   static constexpr int PART = ROWS * (DIM + 2);                        // floats of a part in the workspace: O, maxima, sums
 };
-constexpr int MAX_CTAS = 256;
-constexpr int TICKET_BYTES = MAX_CTAS * 4;
-constexpr int LEAST_STAGES = 8;                                        // of a CTA
+#ifndef LEAST
+#define LEAST 8
+#endif
+constexpr int LEAST_STAGES = LEAST;                                        // of a CTA
 constexpr float SLACK = 8.f;                                           // a maximum may grow by this (in powers of two) before O is rescaled
 
 // A walk over the items in the order (sequence, head, tile).
 template <int ROWS>
 struct Walk {
-  Item it;
-  int seq;
-  int64_t index, begin;                                                // of the sequence's items; the item's first unit
-  __device__ __forceinline__ void start(const AttentionArgs& a, const Share& s) {
-    seq = s.seq;
-    describe<ROWS>(it, a, seq);
-    index = (s.lo - s.before) / it.stages;
-    begin = s.before + index * it.stages;
+  Sequence<ROWS> s;
+  int b, h, tile;
+  int64_t begin;                                                       // the item's first unit
+  __device__ __forceinline__ void start(const AttentionArgs& a, const Share& share) {
+    b = share.seq;
+    s.describe(a, b);
+    const int64_t index = (share.lo - share.before) / s.stages;        // of the sequence's items
+    h = (int)(index / s.tiles);
+    tile = (int)(index - (int64_t)h * s.tiles);
+    begin = share.before + index * s.stages;
   }
   __device__ __forceinline__ void next(const AttentionArgs& a) {
-    begin += it.stages;
-    if (++index < (int64_t)it.tiles * a.cache.heads) return;
-    index = 0;
+    begin += s.stages;
+    if (++tile < s.tiles) return;
+    tile = 0;
+    if (++h < a.cache.heads) return;
+    h = 0;
     do {
-      if (++seq == a.batch.n_seqs) return;
-      describe<ROWS>(it, a, seq);
-    } while (it.tiles == 0);
+      if (++b == a.batch.n_seqs) return;
+      s.describe(a, b);
+    } while (s.tiles == 0);
   }
 };
 
 template <typename T, int DIM, int NT>
-__global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const AttentionArgs a) {
+__global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) few_kernel(const AttentionArgs a) {
   using F = Few<DIM, NT>;
   constexpr int ROWS = F::ROWS, WARPS = F::WARPS, SLOTS = F::SLOTS, VW = DIM / 64;
   extern __shared__ __align__(128) uint8_t smem[];
   float* joined = reinterpret_cast<float*>(smem + F::RING_BYTES);
   __shared__ __align__(8) uint64_t s_full[WARPS][SLOTS];
   __shared__ int s_valid[WARPS][SLOTS];
-  struct Fetch { Walk<ROWS> walk; int64_t unit; int issued; };
-  __shared__ Fetch s_fetch[WARPS];                                     // of what a warp brings in next; its first lane's
+  struct Fetch {                                                       // what a warp brings in next
+    const uint8_t* group[32][2];
+    int used, left, issued;                                            // of the list
+    int slot, end;                                                     // within the item, behind the list
+    Walk<ROWS> walk;
+  };
+  __shared__ Fetch s_fetch[WARPS];
   __shared__ Share s_share;
   __shared__ int64_t s_sums[WARPS];
   __shared__ float s_max[WARPS][ROWS], s_sum[WARPS][ROWS];
@@ -238,58 +253,102 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
   mx::wait_for_previous();
   mx::allow_next();
   find_share(&s_share, a.batch.n_seqs, LEAST_STAGES, s_sums, [&](int b) {
-    Item it;
-    describe<ROWS>(it, a, b);
-    return (int64_t)it.tiles * a.cache.heads * it.stages;
+    Sequence<ROWS> s;
+    s.describe(a, b);
+    return (int64_t)s.tiles * a.cache.heads * s.stages;
   });
   const Share share = s_share;
   if (share.lo >= share.hi) return;
 
   const uint32_t full0 = tc::smem_u32(&s_full[warp][0]);
   uint8_t* const ring = smem + warp * SLOTS * F::STAGE_BYTES;
+  const uint32_t ring0 = tc::smem_u32(ring);
   Walk<ROWS> at;
   at.start(a, share);
-  auto fetch = [&](Fetch& f) {                                          // the warp's next stage, by its first lane
-    if (f.unit >= share.hi) return;
-    while (f.unit >= f.walk.begin + f.walk.it.stages) f.walk.next(a);
-    const Item& it = f.walk.it;
-    const int h = (int)(f.walk.index / it.tiles), slot = (int)(f.unit - f.walk.begin) * STAGE, place = f.issued % SLOTS;
-    const int64_t p0 = slot < it.length ? a.cache.page_of(it.b, slot) : -1;
-    const int64_t p1 = slot + GROUP < it.length ? a.cache.shift > 4 ? p0 : a.cache.page_of(it.b, slot + GROUP) : -1;
-    const bool joint = a.cache.shift > 4 && p1 >= 0;                    // both groups in one page, one behind the other
-    const uint32_t dst = tc::smem_u32(ring + place * F::STAGE_BYTES), bar = full0 + place * 8;
-    auto copy = [&](uint32_t to, const uint8_t* from, uint32_t bytes) {
-      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                   ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
-    };
-    s_valid[warp][place] = (p0 >= 0 ? 1 : 0) | (p1 >= 0 ? 2 : 0);
-    tc::mbar_expect_tx(bar, ((p0 >= 0) + (p1 >= 0)) * F::GROUP_BYTES);
-    if (p0 >= 0) copy(dst, a.cache.group_at(p0, h, slot, DIM), joint ? F::STAGE_BYTES : F::GROUP_BYTES);
-    if (p1 >= 0 && !joint) copy(dst + F::GROUP_BYTES, a.cache.group_at(p1, h, slot + GROUP, DIM), F::GROUP_BYTES);
-    f.unit += WARPS;
-    ++f.issued;
+  // the slots of an item that are this CTA's, for a walk that stands at it
+  auto end_of = [&](const Walk<ROWS>& w) { return (int)(min(w.begin + w.s.stages, share.hi) - w.begin) * STAGE; };
+  // The next stages of the warp, up to 32 of one item: a lane looks one's pages up and leaves the addresses of its groups (null: no
+  // page) in the warp's list.
+  Fetch& f = s_fetch[warp];
+  auto refill = [&]() {
+    int slot = f.slot;
+    while (slot >= f.end && f.walk.begin + f.walk.s.stages < share.hi) {
+      __syncwarp();
+      if (lane == 0) {
+        slot -= f.walk.s.stages * STAGE;                                // (the warp's stages go on through all items)
+        f.walk.next(a);
+        f.end = end_of(f.walk);
+        f.slot = slot;
+      }
+      __syncwarp();
+      slot = f.slot;
+    }
+    const Walk<ROWS>& w = f.walk;
+    const int mine = slot + lane * (WARPS * STAGE), length = w.s.length;
+    const uint8_t *p0 = nullptr, *p1 = nullptr;
+    if (mine < min(f.end, length)) {
+      const int64_t page = a.cache.page_of(w.b, mine);
+      if (page >= 0) p0 = a.cache.group_at(page, w.h, mine, DIM);
+      if (mine + GROUP < length) {
+        if (a.cache.shift > 4) p1 = p0 ? p0 + F::GROUP_BYTES : nullptr;
+        else {
+          const int64_t other = a.cache.page_of(w.b, mine + GROUP);
+          if (other >= 0) p1 = a.cache.group_at(other, w.h, mine + GROUP, DIM);
+        }
+      }
+    }
+    f.group[lane][0] = p0;
+    f.group[lane][1] = p1;
+    const int left = slot < f.end ? (f.end - slot + WARPS * STAGE - 1) / (WARPS * STAGE) : 0;
+    __syncwarp();
+    if (lane == 0) {
+      f.left = min(left, 32);
+      f.used = 0;
+      f.slot = slot + f.left * (WARPS * STAGE);
+    }
+    __syncwarp();
   };
+  auto fetch = [&](int place) {                                         // the warp's next stage; false: there is none
+    if (f.used == f.left) refill();
+    const int i = f.used;
+    if (i == f.left) return;
+    __syncwarp();
+    if (lane == 0) {
+      const uint8_t *p0 = f.group[i][0], *p1 = f.group[i][1];
+      const uint32_t dst = ring0 + place * F::STAGE_BYTES, bar = full0 + place * 8;
+      auto copy = [&](uint32_t to, const uint8_t* from, uint32_t bytes) {
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                     ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+      };
+      f.used = i + 1;
+      ++f.issued;
+      s_valid[warp][place] = (p0 ? 1 : 0) | (p1 ? 2 : 0);
+      tc::mbar_expect_tx(bar, ((p0 ? 1 : 0) + (p1 ? 1 : 0)) * F::GROUP_BYTES);
+      if (p1 == p0 + F::GROUP_BYTES && p0) copy(dst, p0, F::STAGE_BYTES);   // one behind the other
+      else {
+        if (p0) copy(dst, p0, F::GROUP_BYTES);
+        if (p1) copy(dst + F::GROUP_BYTES, p1, F::GROUP_BYTES);
+      }
+    }
+    __syncwarp();
+  };
+  int slot0 = (int)(share.lo - at.begin + warp) * STAGE;                // this warp's next, within the item
   if (lane == 0) {
-    Fetch& f = s_fetch[warp];
     f.walk = at;
-    f.unit = share.lo + warp;
-    f.issued = 0;
-    for (int i = 0; i < SLOTS; ++i) fetch(f);
+    f.slot = slot0; f.end = end_of(at); f.used = f.left = f.issued = 0;
   }
   __syncwarp();
+  for (int i = 0; i < SLOTS; ++i) fetch(i);
 
   const int g = lane >> 2, c = lane & 3;
-  const float to_log2 = a.scale * LOG2E;
   bool alive = true;
   int turn = 0;                                                         // stages of this warp so far
   Queries<T, DIM, NT> q;
-  int64_t unit = share.lo + warp;                                       // this warp's next
   while (true) {
-    const Item& it = at.it;
-    const int64_t begin = at.begin;
-    const int h = (int)(at.index / it.tiles), row0 = (int)(at.index % it.tiles) * ROWS;
-    const bool starts = begin >= share.lo, ends = begin + it.stages <= share.hi;
-    const int64_t until = min(begin + it.stages, share.hi);
+    const int64_t begin = at.begin, first = at.s.first;
+    const int h = at.h, row0 = at.tile * ROWS, rows = at.s.n * a.group, length = at.s.length;
+    const bool starts = begin >= share.lo, ends = begin + at.s.stages <= share.hi;
+    const int end = end_of(at);
     float top[NT][2], sum[NT][2], off[NT][2], o[NT][VW * 4][4];
     int sees[NT][2];
 #pragma unroll
@@ -298,24 +357,23 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
       for (int j = 0; j < 2; ++j) {
         top[nt][j] = -INFINITY; sum[nt][j] = off[nt][j] = 0.f;
         const int r = row0 + nt * 8 + 2 * c + j;
-        sees[nt][j] = r < it.rows ? max(it.length - it.n + r / a.group + 1, 0) : 0;
+        sees[nt][j] = r < rows ? max(length - at.s.n + r / a.group + 1, 0) : 0;
       }
     // all valid rows see the stages before the first row's end, none those past the last one's
-    const int least = max(it.length - it.n + row0 / a.group + 1, 0);
-    const int most = max(it.length - it.n + (min(row0 + ROWS, it.rows) - 1) / a.group + 1, 0);
+    const int least = max(length - at.s.n + row0 / a.group + 1, 0);
+    const int most = max(length - at.s.n + (min(row0 + ROWS, rows) - 1) / a.group + 1, 0);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int i = 0; i < VW * 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.f;
-    if (unit < until) q.load(a.q, it.first, it.rows, row0, h, a.group, lane);
+    if (slot0 < end) q.load(a.q, first, rows, row0, h, a.group, a.scale * LOG2E, lane);
 
-    for (; unit < until; unit += WARPS) {
+    for (; slot0 < end; slot0 += WARPS * STAGE) {
       const int place = turn % SLOTS;
       if (alive) alive = __all_sync(0xffffffffu, tc::mbar_wait(full0 + place * 8, (uint32_t)(turn / SLOTS) & 1u, a.d_status));
       if (!alive) continue;
-      const int slot0 = (int)(unit - begin) * STAGE;
       if (slot0 < most) {
         const uint8_t* stage = ring + place * F::STAGE_BYTES;
         const int valid = s_valid[warp][place];
@@ -328,7 +386,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const uint32_t p = *reinterpret_cast<const uint32_t*>(group + GROUP * (DIM / 2) + key_of(g + 8 * e) * 4);
-            const float ks = scale_of(p) * to_log2, ko = offset_of(p) * to_log2;
+            const float ks = scale_of(p), ko = offset_of(p);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -347,7 +405,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int slot = (valid >> u & 1) ? slot0 + u * GROUP + key_of(g + 8 * e) : INT_MAX;
-              if (slot >= it.length) vp[u][e] = 0u;
+              if (slot >= length) vp[u][e] = 0u;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -384,25 +442,28 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
                 o[nt][i][2 + j] *= by;
               }
             }
-        // the exponent field of the stage's largest vs (a NaN's does not count): vs 2^(6 - field + 127) < 2^7, and with p < 2^SLACK
-        // P stays below 2^15
-        uint32_t field = 7u;
+        // the exponent field of the stage's largest vs: vs 2^(6 - field + 127) < 2^7, and with p < 2^SLACK P stays below 2^15
+        uint32_t field = max(max(vp[0][0] & 0x7f80u, vp[0][1] & 0x7f80u), max(vp[1][0] & 0x7f80u, vp[1][1] & 0x7f80u));
+        field = max(__reduce_max_sync(0xffffffffu, field) >> 7, 7u);
+        const bool odd = field == 255u;
+        if (odd) {                                                      // a NaN does not count: not all rows may see it
+          field = 7u;
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t f = vp[u][e] >> 7 & 255u;
-            field = max(field, f == 255u ? 0u : f);
-          }
-        field = __reduce_max_sync(0xffffffffu, field);
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t f = vp[u][e] >> 7 & 255u;
+              field = max(field, f == 255u ? 0u : f);
+            }
+          field = __reduce_max_sync(0xffffffffu, field);
+        }
         const float shrink = __uint_as_float((260u - field) << 23), grow = __uint_as_float((field - 6u) << 23);
-        float part[NT][VW * 4][4];
+        float base[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < VW * 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) part[nt][i][j] = 0.f;
+          for (int j = 0; j < 2; ++j) base[nt][j] = top[nt][j] == -INFINITY ? 0.f : top[nt][j];
+        float part[NT][VW * 4][4];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const uint8_t* group = stage + u * F::GROUP_BYTES + GROUP * (DIM / 2 + 4);
@@ -412,17 +473,26 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
             const float vs = scale_of(vp[u][e]) * shrink, vo = offset_of(vp[u][e]);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              float pv[2];
+              float p[2];
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
-                const float x = s[u][nt][2 * e + j], m = top[nt][j];
-                const float p = exp2_of(x - (m == -INFINITY ? 0.f : m));
-                const bool gone = masked && x == -INFINITY;              // (its value may be a NaN that others see)
-                sum[nt][j] += p;
-                off[nt][j] += gone ? 0.f : p * vo;
-                pv[j] = gone ? 0.f : p * vs;
+                p[j] = exp2_of(s[u][nt][2 * e + j] - base[nt][j]);
+                sum[nt][j] += p[j];
               }
-              b[nt][e] = transposed(half_pair(pv[0], pv[1]));
+              if (!odd) {
+                off[nt][0] += p[0] * vo;
+                off[nt][1] += p[1] * vo;
+                b[nt][e] = half_pair(p[0] * vs, p[1] * vs);
+              } else {                                                  // (a NaN times the zero of a row that does not see it)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                  const bool gone = masked && s[u][nt][2 * e + j] == -INFINITY;
+                  off[nt][j] += gone ? 0.f : p[j] * vo;
+                  p[j] = gone ? 0.f : p[j] * vs;
+                }
+                b[nt][e] = half_pair(p[0], p[1]);
+              }
+              b[nt][e] = transposed(b[nt][e]);
             }
           }
           uint32_t x[4][VW];
@@ -437,8 +507,12 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
               const uint32_t a0 = lo01 >> (i & 2 ? 8 : 0), a1 = hi01 >> (i & 2 ? 8 : 0), a2 = lo23 >> (i & 2 ? 8 : 0), a3 = hi23 >> (i & 2 ? 8 : 0);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
-                if (i & 1) mma(part[nt][w * 4 + i], high_codes(a0), high_codes(a1), high_codes(a2), high_codes(a3), b[nt][0], b[nt][1]);
-                else mma(part[nt][w * 4 + i], low_codes(a0), low_codes(a1), low_codes(a2), low_codes(a3), b[nt][0], b[nt][1]);
+                auto add = [&](uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3) {
+                  if (u == 0) mma_first(part[nt][w * 4 + i], c0, c1, c2, c3, b[nt][0], b[nt][1]);
+                  else mma(part[nt][w * 4 + i], c0, c1, c2, c3, b[nt][0], b[nt][1]);
+                };
+                if (i & 1) add(high_codes(a0), high_codes(a1), high_codes(a2), high_codes(a3));
+                else add(low_codes(a0), low_codes(a1), low_codes(a2), low_codes(a3));
               }
             }
           }
@@ -452,8 +526,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
       }
       ++turn;
       __syncwarp();                                                     // all lanes have read the stage
-      if (lane == 0) fetch(s_fetch[warp]);
-      __syncwarp();
+      fetch(place);
     }
 
     // ---- the item's rows over the warps
@@ -493,22 +566,22 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
     __syncthreads();
     const int cta = blockIdx.x;
     const int first_cta = starts ? cta : cta_of(begin, share.total, share.ctas);
-    const int last_cta = ends ? cta : cta_of(begin + it.stages - 1, share.total, share.ctas);
+    const int last_cta = ends ? cta : cta_of(begin + at.s.stages - 1, share.total, share.ctas);
     const bool whole = first_cta == last_cta;
     float* parts = reinterpret_cast<float*>(a.workspace + TICKET_BYTES);
     auto part_of = [&](int i) { return parts + ((int64_t)i * 2 + (i == first_cta ? 1 : 0)) * F::PART; };
     auto write = [&](int r, int d, float4 v, float m, float l) {         // row r of the tile, dimensions d .. d + 3
       const int row = row0 + r;
-      if (row >= it.rows) return;
+      if (row >= rows) return;
       const int i = row / a.group, head = h * a.group + row - i * a.group;
       const float by = l == 0.f ? 0.f : 1.f / l;
-      T* p = reinterpret_cast<T*>(a.out.p) + (it.first + i) * a.out.token + head * a.out.head + d;
+      T* p = reinterpret_cast<T*>(a.out.p) + (first + i) * a.out.token + head * a.out.head + d;
       T y[4] = {mx::from_f32<T>(v.x * by), mx::from_f32<T>(v.y * by), mx::from_f32<T>(v.z * by), mx::from_f32<T>(v.w * by)};
       if (a.out.vec) { uint2 w; memcpy(&w, y, 8); *reinterpret_cast<uint2*>(p) = w; }
       else
 #pragma unroll
         for (int e = 0; e < 4; ++e) p[e] = y[e];
-      if (d == 0 && a.lse) a.lse[(it.first + i) * a.q.heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+      if (d == 0 && a.lse) a.lse[(first + i) * a.q.heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
     };
     for (int x = tid; x < ROWS * (DIM / 4); x += WARPS * 32) {
       const int r = x / (DIM / 4), d = x % (DIM / 4) * 4;
@@ -535,30 +608,46 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, 1) few_kernel(const Att
       if (s_last) {
         __threadfence();
         if (tid == 0) *ticket = 0;                                       // for the next call
+        // what each part's rows count for, by a thread each; then the sums
+        const int n_parts = last_cta - first_cta + 1;
+        float* by = joined;                                              // [part][row]
+        for (int x = tid; x < n_parts * ROWS; x += WARPS * 32) by[x] = __ldcg(part_of(first_cta + x / ROWS) + ROWS * DIM + x % ROWS);
+        __syncthreads();
+        if (tid < ROWS) {
+          float m = -INFINITY;
+          for (int i = 0; i < n_parts; ++i) m = fmaxf(m, by[i * ROWS + tid]);
+          s_max[0][tid] = m;
+        }
+        __syncthreads();
+        for (int x = tid; x < n_parts * ROWS; x += WARPS * 32) {
+          const float l = __ldcg(part_of(first_cta + x / ROWS) + ROWS * (DIM + 1) + x % ROWS);
+          const float f = l == 0.f ? 0.f : by[x] == -INFINITY ? 1.f : exp2_of(by[x] - s_max[0][x % ROWS]);
+          by[x] = f;
+          by[n_parts * ROWS + x] = l * f;
+        }
+        __syncthreads();
         for (int x = tid; x < ROWS * (DIM / 4); x += WARPS * 32) {
           const int r = x / (DIM / 4), d = x % (DIM / 4) * 4;
-          float m = -INFINITY, l = 0.f;
+          float l = 0.f;
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int i = first_cta; i <= last_cta; ++i) m = fmaxf(m, __ldcg(part_of(i) + ROWS * DIM + r));
-#pragma unroll 4
-          for (int i = first_cta; i <= last_cta; ++i) {
-            const float* p = part_of(i);
-            const float pl = __ldcg(p + ROWS * (DIM + 1) + r), pm = __ldcg(p + ROWS * DIM + r);
-            const float4 t = __ldcg(reinterpret_cast<const float4*>(p + r * DIM + d));
-            const float by = pl == 0.f ? 0.f : pm == -INFINITY ? 1.f : exp2_of(pm - m);
-            l += pl * by;
-            v.x += t.x * by; v.y += t.y * by; v.z += t.z * by; v.w += t.w * by;
+#pragma unroll 8
+          for (int i = 0; i < n_parts; ++i) {
+            const float4 t = __ldcg(reinterpret_cast<const float4*>(part_of(first_cta + i) + r * DIM + d));
+            const float f = by[i * ROWS + r];
+            l += by[(n_parts + i) * ROWS + r];
+            v.x += t.x * f; v.y += t.y * f; v.z += t.z * f; v.w += t.w * f;
           }
-          write(r, d, v, m, l);
+          write(r, d, v, s_max[0][r], l);
         }
       }
     }
     __syncthreads();
-    if (begin + it.stages >= share.hi) break;
+    if (begin + at.s.stages >= share.hi) break;
+    slot0 -= at.s.stages * STAGE;
     at.next(a);
   }
   if (!alive && lane == 0)   // no copy is left on its way into memory that may go to another CTA
-    for (int i = turn; i < s_fetch[warp].issued; ++i) tc::mbar_wait(full0 + (i % SLOTS) * 8, (uint32_t)(i / SLOTS) & 1u, a.d_status);
+    for (int i = turn; i < f.issued; ++i) tc::mbar_wait(full0 + (i % SLOTS) * 8, (uint32_t)(i / SLOTS) & 1u, a.d_status);
 }
 
 template <typename T, int DIM, int NT>
@@ -570,7 +659,7 @@ dq_status run_few(cudaStream_t stream, const mx::Device& dev, const AttentionArg
   const int64_t rows = a.batch.tokens * a.group, tiles = rows / F::ROWS + a.batch.n_seqs;
   const int64_t stages = max((int64_t)1, ((int64_t)a.cache.width << a.cache.shift) / STAGE);
   const int64_t most = (tiles * a.cache.heads * stages + LEAST_STAGES - 1) / LEAST_STAGES;
-  mx::LaunchConfig c(stream, min((int64_t)min(dev.sms, MAX_CTAS), max((int64_t)1, most)), F::THREADS, F::SMEM);
+  mx::LaunchConfig c(stream, min((int64_t)min(dev.sms, 148) * F::PER_SM, max((int64_t)1, most)), F::THREADS, F::SMEM);
   return mx::launch(c, few_kernel<T, DIM, NT>, a);
 }
 
@@ -585,7 +674,6 @@ __global__ void __launch_bounds__(W_WARPS * 32) weights_kernel(const AttentionAr
   __shared__ Share s_share;
   __shared__ int64_t s_sums[W_WARPS];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-  const float to_log2 = a.scale * LOG2E;
   mx::wait_for_previous();
   find_share(&s_share, a.batch.n_seqs, 1, s_sums, [&](int b) { return (int64_t)a.cache.heads * ((a.cache.length(b) + W_TILE - 1) / W_TILE); });
   const Share share = s_share;
@@ -613,14 +701,14 @@ __global__ void __launch_bounds__(W_WARPS * 32) weights_kernel(const AttentionAr
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const uint32_t p = *reinterpret_cast<const uint32_t*>(group + GROUP * (DIM / 2) + key_of(g + 8 * e) * 4);
-        ks[e] = scale_of(p) * to_log2;
-        ko[e] = offset_of(p) * to_log2;
+        ks[e] = scale_of(p);
+        ko[e] = offset_of(p);
       }
       // rows before the first one that sees slot0 see nothing here
       const int row_first = max(0, slot0 - (length - n)) * a.group / 8 * 8;
       for (int row0 = row_first; row0 < rows; row0 += 8) {
         Queries<T, DIM, 1> q;
-        q.load(a.q, first, rows, row0, h, a.group, lane);
+        q.load(a.q, first, rows, row0, h, a.group, a.scale * LOG2E, lane);
         float s[1][4];
         key_products<T, DIM, 1>(s, group, q, lane);
 #pragma unroll
