@@ -29,12 +29,12 @@ constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
 constexpr int STAGE = 2 * GROUP;   // keys of a pipeline stage: the maximum of a row is looked at once for 32 keys
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // The same with a sum that starts from zero.
 __device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
                : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 // Two codes as fp16 numbers, c 2^-24: bits 0-3 and 16-19; c 2^-20: bits 4-7 and 20-23.
@@ -42,7 +42,7 @@ __device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000
 __device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
 __device__ __forceinline__ uint32_t transposed(uint32_t v) {
   uint32_t d;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
   return d;
 }
 __device__ __forceinline__ float exp2_of(float v) {
@@ -50,6 +50,17 @@ __device__ __forceinline__ float exp2_of(float v) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(v));
   return d;
 }
+// Two fp32 operations in one instruction.
+using mx::add2;
+using mx::mul2;
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\t"
+      "mov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 __device__ __forceinline__ uint32_t half_pair(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -94,7 +105,7 @@ template <typename T, int DIM, int NT>
 struct Queries {
   static constexpr int WORDS = DIM / 32;
   uint32_t b[NT][WORDS][4];
-  float by[NT][2], sum[NT][2];
+  float2 by[NT], sum[NT];
   __device__ __forceinline__ void load(const Heads& q, int64_t first, int rows, int row0, int h, int group, float factor, int lane) {
     const int c = lane & 3;
 #pragma unroll
@@ -125,23 +136,22 @@ struct Queries {
 #pragma unroll
         for (int e = 0; e < 4; ++e) b[nt][w][e] = half_pair(v[w][e] * (e & 1 ? up4 : up), v[w][e + 4] * (e & 1 ? up4 : up));
       const float down = __uint_as_float((uint32_t)(field + 10) << 23);   // 2^24 / up
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        sum[nt][j] = __shfl_sync(0xffffffffu, s, c * 8 + 4 * j) * factor;
-        by[nt][j] = __shfl_sync(0xffffffffu, down, c * 8 + 4 * j) * factor;
-      }
+      sum[nt] = make_float2(__shfl_sync(0xffffffffu, s, c * 8) * factor, __shfl_sync(0xffffffffu, s, c * 8 + 4) * factor);
+      by[nt] = make_float2(__shfl_sync(0xffffffffu, down, c * 8) * factor, __shfl_sync(0xffffffffu, down, c * 8 + 4) * factor);
     }
   }
 };
 
-// (q . c) of a group's 16 keys and the tile's rows, without q.by: acc[nt] = (key_of(g), columns 2 c, 2 c + 1), (key_of(g + 8), the same).
+// (q . c) of a group's 16 keys and the tile's rows, without q.by: acc[nt][e] = key_of(g + 8 e), columns 2 c, 2 c + 1.  Two sums side by
+// side, because each instruction waits for the one that its sum comes from.
 template <typename T, int DIM, int NT>
-__device__ __forceinline__ void key_products(float (&acc)[NT][4], const uint8_t* codes, const Queries<T, DIM, NT>& q, int lane) {
+__device__ __forceinline__ void key_products(float2 (&acc)[NT][2], const uint8_t* codes, const Queries<T, DIM, NT>& q, int lane) {
   constexpr int WORDS = DIM / 32;
   const int g = lane >> 2, c = lane & 3;
   uint32_t k0[WORDS], k1[WORDS];
   load_words<WORDS>(k0, codes + key_of(g) * (DIM / 2) + c * (DIM / 8));
   load_words<WORDS>(k1, codes + key_of(g + 8) * (DIM / 2) + c * (DIM / 8));
+  float d[2][NT][4];
 #pragma unroll
   for (int w = 0; w < WORDS; ++w)
 #pragma unroll
@@ -150,10 +160,15 @@ __device__ __forceinline__ void key_products(float (&acc)[NT][4], const uint8_t*
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const uint32_t b0 = q.b[nt][w][2 * e], b1 = q.b[nt][w][2 * e + 1];
-        if (w == 0 && e == 0) mma_first(acc[nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), b0, b1);
-        else mma(acc[nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), b0, b1);
+        if (w == 0) mma_first(d[e][nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), b0, b1);
+        else mma(d[e][nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), b0, b1);
       }
     }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      acc[nt][e] = add2(make_float2(d[0][nt][2 * e], d[0][nt][2 * e + 1]), make_float2(d[1][nt][2 * e], d[1][nt][2 * e + 1]));
 }
 
 // An item of work is a tile of query rows of a sequence and kv head; it has `stages` stages of keys (one at least: rows that see nothing
@@ -349,13 +364,15 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
     const int h = at.h, row0 = at.tile * ROWS, rows = at.s.n * a.group, length = at.s.length;
     const bool starts = begin >= share.lo, ends = begin + at.s.stages <= share.hi;
     const int end = end_of(at);
-    float top[NT][2], sum[NT][2], off[NT][2], o[NT][VW * 4][4];
+    float top[NT][2];
+    float2 sum[NT], off[NT], o[NT][VW * 4][2];
     int sees[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        top[nt][j] = -INFINITY; sum[nt][j] = off[nt][j] = 0.f;
+        top[nt][j] = -INFINITY;
+        sum[nt] = off[nt] = both(0.f);
         const int r = row0 + nt * 8 + 2 * c + j;
         sees[nt][j] = r < rows ? max(length - at.s.n + r / a.group + 1, 0) : 0;
       }
@@ -367,7 +384,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
 #pragma unroll
       for (int i = 0; i < VW * 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.f;
+        for (int e = 0; e < 2; ++e) o[nt][i][e] = both(0.f);
     if (slot0 < end) q.load(a.q, first, rows, row0, h, a.group, a.scale * LOG2E, lane);
 
     for (; slot0 < end; slot0 += WARPS * STAGE) {
@@ -378,7 +395,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
         const uint8_t* stage = ring + place * F::STAGE_BYTES;
         const int valid = s_valid[warp][place];
         const bool masked = slot0 + STAGE > least || valid != 3;
-        float s[2][NT][4];
+        float2 s[2][NT][2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const uint8_t* group = stage + u * F::GROUP_BYTES;
@@ -388,9 +405,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
             const uint32_t p = *reinterpret_cast<const uint32_t*>(group + GROUP * (DIM / 2) + key_of(g + 8 * e) * 4);
             const float ks = scale_of(p), ko = offset_of(p);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int j = 0; j < 2; ++j) s[u][nt][2 * e + j] = s[u][nt][2 * e + j] * (ks * q.by[nt][j]) + ko * q.sum[nt][j];
+            for (int nt = 0; nt < NT; ++nt) s[u][nt][e] = fma2(s[u][nt][e], mul2(both(ks), q.by[nt]), mul2(both(ko), q.sum[nt]));
           }
         }
         uint32_t vp[2][2];                                              // the values' parameters; a masked key's may be anything
@@ -407,10 +422,10 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
               const int slot = (valid >> u & 1) ? slot0 + u * GROUP + key_of(g + 8 * e) : INT_MAX;
               if (slot >= length) vp[u][e] = 0u;
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                  if (slot >= sees[nt][j]) s[u][nt][2 * e + j] = -INFINITY;
+              for (int nt = 0; nt < NT; ++nt) {
+                if (slot >= sees[nt][0]) s[u][nt][e].x = -INFINITY;
+                if (slot >= sees[nt][1]) s[u][nt][e].y = -INFINITY;
+              }
             }
         // maxima over the stage's keys; O is rescaled where one has grown by more than SLACK
         bool grown = false;
@@ -419,7 +434,8 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            float m = fmaxf(fmaxf(s[0][nt][j], s[0][nt][2 + j]), fmaxf(s[1][nt][j], s[1][nt][2 + j]));
+            auto at_j = [&](int u, int e) { return j ? s[u][nt][e].y : s[u][nt][e].x; };
+            float m = fmaxf(fmaxf(at_j(0, 0), at_j(0, 1)), fmaxf(at_j(1, 0), at_j(1, 1)));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -428,20 +444,23 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
           }
         if (__any_sync(0xffffffffu, grown))
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt) {
+            float by[2];
+            const float l[2] = {sum[nt].x, sum[nt].y};
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               const float m = fmaxf(top[nt][j], now[nt][j]);
-              const float by = top[nt][j] == -INFINITY ? (sum[nt][j] == 0.f ? 0.f : 1.f) : exp2_of(top[nt][j] - m);
+              by[j] = top[nt][j] == -INFINITY ? (l[j] == 0.f ? 0.f : 1.f) : exp2_of(top[nt][j] - m);
               top[nt][j] = m;
-              sum[nt][j] *= by;
-              off[nt][j] *= by;
-#pragma unroll
-              for (int i = 0; i < VW * 4; ++i) {
-                o[nt][i][j] *= by;
-                o[nt][i][2 + j] *= by;
-              }
             }
+            const float2 f = make_float2(by[0], by[1]);
+            sum[nt] = mul2(sum[nt], f);
+            off[nt] = mul2(off[nt], f);
+#pragma unroll
+            for (int i = 0; i < VW * 4; ++i)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) o[nt][i][e] = mul2(o[nt][i][e], f);
+          }
         // the exponent field of the stage's largest vs: vs 2^(6 - field + 127) < 2^7, and with p < 2^SLACK P stays below 2^15
         uint32_t field = max(max(vp[0][0] & 0x7f80u, vp[0][1] & 0x7f80u), max(vp[1][0] & 0x7f80u, vp[1][1] & 0x7f80u));
         field = max(__reduce_max_sync(0xffffffffu, field) >> 7, 7u);
@@ -458,11 +477,10 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
           field = __reduce_max_sync(0xffffffffu, field);
         }
         const float shrink = __uint_as_float((260u - field) << 23), grow = __uint_as_float((field - 6u) << 23);
-        float base[NT][2];
+        float2 base[NT];                                                // less the maximum
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) base[nt][j] = top[nt][j] == -INFINITY ? 0.f : top[nt][j];
+          base[nt] = make_float2(top[nt][0] == -INFINITY ? 0.f : -top[nt][0], top[nt][1] == -INFINITY ? 0.f : -top[nt][1]);
         float part[NT][VW * 4][4];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -473,26 +491,19 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
             const float vs = scale_of(vp[u][e]) * shrink, vo = offset_of(vp[u][e]);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              float p[2];
-#pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                p[j] = exp2_of(s[u][nt][2 * e + j] - base[nt][j]);
-                sum[nt][j] += p[j];
-              }
+              float2 p = add2(s[u][nt][e], base[nt]), r, v;
+              p = make_float2(exp2_of(p.x), exp2_of(p.y));
+              sum[nt] = add2(sum[nt], p);
               if (!odd) {
-                off[nt][0] += p[0] * vo;
-                off[nt][1] += p[1] * vo;
-                b[nt][e] = half_pair(p[0] * vs, p[1] * vs);
+                off[nt] = fma2(p, both(vo), off[nt]);
+                v = mul2(p, both(vs));
               } else {                                                  // (a NaN times the zero of a row that does not see it)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                  const bool gone = masked && s[u][nt][2 * e + j] == -INFINITY;
-                  off[nt][j] += gone ? 0.f : p[j] * vo;
-                  p[j] = gone ? 0.f : p[j] * vs;
-                }
-                b[nt][e] = half_pair(p[0], p[1]);
+                const bool x = masked && s[u][nt][e].x == -INFINITY, y = masked && s[u][nt][e].y == -INFINITY;
+                r = make_float2(x ? 0.f : p.x * vo, y ? 0.f : p.y * vo);
+                off[nt] = add2(off[nt], r);
+                v = make_float2(x ? 0.f : p.x * vs, y ? 0.f : p.y * vs);
               }
-              b[nt][e] = transposed(b[nt][e]);
+              b[nt][e] = transposed(half_pair(v.x, v.y));
             }
           }
           uint32_t x[4][VW];
@@ -522,7 +533,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
 #pragma unroll
           for (int i = 0; i < VW * 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[nt][i][j] += part[nt][i][j] * grow;
+            for (int e = 0; e < 2; ++e) o[nt][i][e] = fma2(make_float2(part[nt][i][2 * e], part[nt][i][2 * e + 1]), both(grow), o[nt][i][e]);
       }
       ++turn;
       __syncwarp();                                                     // all lanes have read the stage
@@ -530,37 +541,38 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
     }
 
     // ---- the item's rows over the warps
+    float l[NT][2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) {
-          sum[nt][j] += __shfl_xor_sync(0xffffffffu, sum[nt][j], d);
-          off[nt][j] += __shfl_xor_sync(0xffffffffu, off[nt][j], d);
-        }
-        if (g == 0) { s_max[warp][nt * 8 + 2 * c + j] = top[nt][j]; s_sum[warp][nt * 8 + 2 * c + j] = sum[nt][j]; }
+      for (int d = 4; d < 32; d <<= 1) {
+        sum[nt] = add2(sum[nt], make_float2(__shfl_xor_sync(0xffffffffu, sum[nt].x, d), __shfl_xor_sync(0xffffffffu, sum[nt].y, d)));
+        off[nt] = add2(off[nt], make_float2(__shfl_xor_sync(0xffffffffu, off[nt].x, d), __shfl_xor_sync(0xffffffffu, off[nt].y, d)));
       }
+      l[nt][0] = sum[nt].x; l[nt][1] = sum[nt].y;
+      if (g == 0)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) { s_max[warp][nt * 8 + 2 * c + j] = top[nt][j]; s_sum[warp][nt * 8 + 2 * c + j] = l[nt][j]; }
+    }
     __syncthreads();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int r = nt * 8 + 2 * c + j;
-        if (s_sum[warp][r] == 0.f) continue;
+        if (l[nt][j] == 0.f) continue;
         float m = -INFINITY;
         for (int w = 0; w < WARPS; ++w) m = fmaxf(m, s_max[w][r]);
         const float by = top[nt][j] == -INFINITY ? 1.f : exp2_of(top[nt][j] - m);
         float* row = joined + (warp * ROWS + r) * F::PAD + g * (DIM / 8);
-        constexpr float LOW = 16777216.f, HIGH = 1048576.f;             // 2^24 and 2^20: of the codes
+        const float low = 16777216.f * by, high = 1048576.f * by, o0 = (j ? off[nt].y : off[nt].x) * by;   // 2^24 and 2^20: of the codes
 #pragma unroll
         for (int i = 0; i < VW; ++i)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float4 v;
-            v.x = (o[nt][4 * i][2 * e + j] * LOW + off[nt][j]) * by; v.y = (o[nt][4 * i + 1][2 * e + j] * HIGH + off[nt][j]) * by;
-            v.z = (o[nt][4 * i + 2][2 * e + j] * LOW + off[nt][j]) * by; v.w = (o[nt][4 * i + 3][2 * e + j] * HIGH + off[nt][j]) * by;
-            *reinterpret_cast<float4*>(row + 8 * i + 4 * e) = v;
+            auto at_j = [&](int k) { const float2 v = o[nt][4 * i + k][e]; return j ? v.y : v.x; };
+            *reinterpret_cast<float4*>(row + 8 * i + 4 * e) =
+                make_float4(at_j(0) * low + o0, at_j(1) * high + o0, at_j(2) * low + o0, at_j(3) * high + o0);
           }
       }
     __syncthreads();
@@ -709,17 +721,22 @@ __global__ void __launch_bounds__(W_WARPS * 32) weights_kernel(const AttentionAr
       for (int row0 = row_first; row0 < rows; row0 += 8) {
         Queries<T, DIM, 1> q;
         q.load(a.q, first, rows, row0, h, a.group, a.scale * LOG2E, lane);
-        float s[1][4];
+        float2 s[1][2];
         key_products<T, DIM, 1>(s, group, q, lane);
+        float lse[2];
+        int sees[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int r = row0 + 2 * c + j;
-          if (r >= rows) continue;
-          const int i = r / a.group, sees = length - n + i + 1;
-          const float lse = a.lse[(first + i) * a.q.heads + h * a.group + r - i * a.group] * LOG2E;
+          const int r = row0 + 2 * c + j, i = r / a.group;
+          lse[j] = r < rows ? a.lse[(first + i) * a.q.heads + h * a.group + r - i * a.group] * LOG2E : 0.f;
+          sees[j] = r < rows ? length - n + i + 1 : 0;
+        }
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (slot0 + key_of(g + 8 * e) < sees) got[e] += exp2_of(s[0][2 * e + j] * (ks[e] * q.by[0][j]) + (ko[e] * q.sum[0][j] - lse));
+        for (int e = 0; e < 2; ++e) {
+          const float2 x = fma2(s[0][e], mul2(both(ks[e]), q.by[0]), mul2(both(ko[e]), q.sum[0]));
+          const int slot = slot0 + key_of(g + 8 * e);
+          if (slot < sees[0]) got[e] += exp2_of(x.x - lse[0]);
+          if (slot < sees[1]) got[e] += exp2_of(x.y - lse[1]);
         }
       }
     }
