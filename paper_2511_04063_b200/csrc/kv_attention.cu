@@ -3,7 +3,7 @@
 //
 //     S = scale q k^T over the slots a query sees,   O = softmax(S) v,   lse = log sum exp S
 //
-// With k = ks c + ko for codes c = 0 .. 15,   q . k = ks (q . c) + ko sum q   and   sum_t p_t v_t = sum_t (p_t vs_t) c_t + sum_t p_t vo_t:
+// With k = ks c + ko for codes c = 0 .. 15,   q . k = ks (q . c) + ko sum q   and   sum_t p_t v_t = sum_t (p_t vs_t) (c_t - 8) + sum_t p_t (vo_t + 8 vs_t):
 // the matrix instructions multiply the codes, and the parameters enter once for each key.  Four bits alone are an fp16 number,
 // the subnormal c 2^-24 (c 2^-20 four bits further up), which the tensor cores multiply exactly: one AND turns two codes into two
 // operands, and the powers of two are taken out with the parameters.  (Bits or'ed into the mantissa of 1024, less 1032, are three
@@ -15,9 +15,9 @@
 // they lie, in both.  P^T comes out of the first product transposed and is turned by movmatrix.
 //
 // Roundings to 16 bits.  A query row is multiplied by a power of two that brings its largest value to 2^14 and rounded to fp16: exact
-// for fp16's 11 and bf16's 8 bits, save values below 2^-24 of the largest.  P vs is divided by the power of two of the stage's
-// largest vs and rounded to fp16 (2^-11 a term; below 2^-20 of the row's largest 2^-31 of it).  A stage's sum of P vs c starts
-// from zero and is added in fp32: the instructions' own sums truncate, which over a long axis would add up.
+// for fp16's 11 and bf16's 8 bits, save values below 2^-24 of the largest.  P vs is divided by the power of two of the largest vs so
+// far and rounded to fp16 (2^-11 a term; below 2^-20 of the row's largest 2^-31 of it).  The values' codes are centred (one more
+// instruction, in a pipe that has room) because the instructions' own sums truncate: over a long axis sums of 0 .. 15 would drift.
 #include "kv_common.cuh"
 #include "tc_gemm.cuh"
 
@@ -32,6 +32,10 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma(float2 (&d)[2], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0].x), "+f"(d[0].y), "+f"(d[1].x), "+f"(d[1].y) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 // The same with a sum that starts from zero.
 __device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
@@ -40,6 +44,13 @@ __device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a
 // Two codes as fp16 numbers, c 2^-24: bits 0-3 and 16-19; c 2^-20: bits 4-7 and 20-23.
 __device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000fu; }
 __device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
+// The same less 8.
+__device__ __forceinline__ uint32_t less(uint32_t w, uint32_t eight) {
+  const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&w), *reinterpret_cast<const __half2*>(&eight));
+  return *reinterpret_cast<const uint32_t*>(&d);
+}
+__device__ __forceinline__ uint32_t low_centred(uint32_t w) { return less(low_codes(w), 0x00080008u); }
+__device__ __forceinline__ uint32_t high_centred(uint32_t w) { return less(high_codes(w), 0x00800080u); }
 __device__ __forceinline__ uint32_t transposed(uint32_t v) {
   uint32_t d;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
@@ -98,77 +109,81 @@ __device__ __forceinline__ void load_values(float (&v)[8], const T* p, bool ther
   }
 }
 
-// A warp's query rows: tile of 8 NT rows (row r: token r / group, head r % group) as B fragments.  Dimensions whose codes lie four
-// bits up are held 2^-4 smaller.  For the columns 2 c and 2 c + 1: `by`, what takes the powers of two out of a product, and the sum of
-// the row, both times `factor`.
-template <typename T, int DIM, int NT>
+// Eight query rows from row0 on (row r: token r / group, head r % group) as B fragments.  Dimensions whose codes lie four bits up
+// are held 2^-4 smaller.  For the columns 2 c and 2 c + 1: `by`, what takes the powers of two out of a product, and the sum of the
+// row, both times `factor`.
+template <typename T, int DIM>
 struct Queries {
   static constexpr int WORDS = DIM / 32;
-  uint32_t b[NT][WORDS][4];
-  float2 by[NT], sum[NT];
+  uint4 b[WORDS];
+  float2 by, sum;
   __device__ __forceinline__ void load(const Heads& q, int64_t first, int rows, int row0, int h, int group, float factor, int lane) {
-    const int c = lane & 3;
+    const int c = lane & 3, r = row0 + (lane >> 2);
+    const bool there = r < rows;
+    const int i = there ? r / group : 0;
+    const T* p = reinterpret_cast<const T*>(q.p) + (first + i) * q.token + (int64_t)(h * group + (there ? r - i * group : 0)) * q.head;
+    float v[WORDS][8], s = 0.f, most = 0.f;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int r = row0 + nt * 8 + (lane >> 2);
-      const bool there = r < rows;
-      const int i = there ? r / group : 0;
-      const T* p = reinterpret_cast<const T*>(q.p) + (first + i) * q.token + (int64_t)(h * group + (there ? r - i * group : 0)) * q.head;
-      float v[WORDS][8], s = 0.f, most = 0.f;
+    for (int w = 0; w < WORDS; ++w) {
+      load_values<T>(v[w], p + (c * WORDS + w) * 8, there, q.vec);
 #pragma unroll
-      for (int w = 0; w < WORDS; ++w) {
-        load_values<T>(v[w], p + (c * WORDS + w) * 8, there, q.vec);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          s += v[w][e];
-          most = fmaxf(most, fabsf(v[w][e]));
-        }
+      for (int e = 0; e < 8; ++e) {
+        s += v[w][e];
+        most = fmaxf(most, fabsf(v[w][e]));
       }
-      s += __shfl_xor_sync(0xffffffffu, s, 1);
-      s += __shfl_xor_sync(0xffffffffu, s, 2);
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      // the largest value's exponent field, within what keeps both factors normal numbers; a row that is not finite stays so
-      const int field = min(max((int)mx::exponent_field(most), 14), 244);
-      const float up = __uint_as_float((uint32_t)(268 - field) << 23), up4 = up * 0.0625f;
-#pragma unroll
-      for (int w = 0; w < WORDS; ++w)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) b[nt][w][e] = half_pair(v[w][e] * (e & 1 ? up4 : up), v[w][e + 4] * (e & 1 ? up4 : up));
-      const float down = __uint_as_float((uint32_t)(field + 10) << 23);   // 2^24 / up
-      sum[nt] = make_float2(__shfl_sync(0xffffffffu, s, c * 8) * factor, __shfl_sync(0xffffffffu, s, c * 8 + 4) * factor);
-      by[nt] = make_float2(__shfl_sync(0xffffffffu, down, c * 8) * factor, __shfl_sync(0xffffffffu, down, c * 8 + 4) * factor);
     }
+    s += __shfl_xor_sync(0xffffffffu, s, 1);
+    s += __shfl_xor_sync(0xffffffffu, s, 2);
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    // the largest value's exponent field, within what keeps both factors normal numbers; a row that is not finite stays so
+    const int field = min(max((int)mx::exponent_field(most), 14), 244);
+    const float up = __uint_as_float((uint32_t)(268 - field) << 23), up4 = up * 0.0625f;
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w)
+      b[w] = make_uint4(half_pair(v[w][0] * up, v[w][4] * up), half_pair(v[w][1] * up4, v[w][5] * up4),
+                        half_pair(v[w][2] * up, v[w][6] * up), half_pair(v[w][3] * up4, v[w][7] * up4));
+    const float down = __uint_as_float((uint32_t)(field + 10) << 23);   // 2^24 / up
+    sum = make_float2(__shfl_sync(0xffffffffu, s, c * 8) * factor, __shfl_sync(0xffffffffu, s, c * 8 + 4) * factor);
+    by = make_float2(__shfl_sync(0xffffffffu, down, c * 8) * factor, __shfl_sync(0xffffffffu, down, c * 8 + 4) * factor);
   }
 };
 
-// (q . c) of a group's 16 keys and the tile's rows, without q.by: acc[nt][e] = key_of(g + 8 e), columns 2 c, 2 c + 1.  Two sums side by
-// side, because each instruction waits for the one that its sum comes from.
-template <typename T, int DIM, int NT>
-__device__ __forceinline__ void key_products(float2 (&acc)[NT][2], const uint8_t* codes, const Queries<T, DIM, NT>& q, int lane) {
+// (q . c) of the 16 keys of N groups and the tile's rows, without q.by: acc[u][nt][e] = key_of(g + 8 e), columns 2 c, 2 c + 1.
+// query(nt, w): the B fragments of a word.  Two sums a group side by side, because each instruction waits for the one that its sum
+// comes from.
+template <int DIM, int NT, int N, typename Q>
+__device__ __forceinline__ void key_products(float2 (&acc)[N][NT][2], const uint8_t* codes, Q query, int lane) {
   constexpr int WORDS = DIM / 32;
   const int g = lane >> 2, c = lane & 3;
-  uint32_t k0[WORDS], k1[WORDS];
-  load_words<WORDS>(k0, codes + key_of(g) * (DIM / 2) + c * (DIM / 8));
-  load_words<WORDS>(k1, codes + key_of(g + 8) * (DIM / 2) + c * (DIM / 8));
-  float d[2][NT][4];
+  uint32_t k[N][2][WORDS];
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      load_words<WORDS>(k[u][e], codes + u * (GROUP * (DIM + 8)) + key_of(g + 8 * e) * (DIM / 2) + c * (DIM / 8));
+  float d[N][2][NT][4];
 #pragma unroll
   for (int w = 0; w < WORDS; ++w)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const uint32_t x0 = k0[w] >> (8 * e), x1 = k1[w] >> (8 * e);
+    for (int nt = 0; nt < NT; ++nt) {
+      const uint4 b = query(nt, w);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const uint32_t b0 = q.b[nt][w][2 * e], b1 = q.b[nt][w][2 * e + 1];
-        if (w == 0) mma_first(d[e][nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), b0, b1);
-        else mma(d[e][nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), b0, b1);
-      }
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t x0 = k[u][0][w] >> (8 * e), x1 = k[u][1][w] >> (8 * e), b0 = e ? b.z : b.x, b1 = e ? b.w : b.y;
+          if (w == 0) mma_first(d[u][e][nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), b0, b1);
+          else mma(d[u][e][nt], low_codes(x0), low_codes(x1), high_codes(x0), high_codes(x1), b0, b1);
+        }
     }
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
+  for (int u = 0; u < N; ++u)
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      acc[nt][e] = add2(make_float2(d[0][nt][2 * e], d[0][nt][2 * e + 1]), make_float2(d[1][nt][2 * e], d[1][nt][2 * e + 1]));
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        acc[u][nt][e] = add2(make_float2(d[u][0][nt][2 * e], d[u][0][nt][2 * e + 1]), make_float2(d[u][1][nt][2 * e], d[u][1][nt][2 * e + 1]));
 }
 
 // An item of work is a tile of query rows of a sequence and kv head; it has `stages` stages of keys (one at least: rows that see nothing
@@ -192,28 +207,21 @@ struct Sequence {
 // and the CTA that finishes last joins them, in order.
 constexpr int MAX_CTAS = 640;
 constexpr int TICKET_BYTES = MAX_CTAS * 4;
-#ifndef FEW_WARPS
-#define FEW_WARPS 8
-#endif
 template <int DIM, int NT>
 struct Few {
   static constexpr int ROWS = 8 * NT;
-  static constexpr int WARPS = DIM == 256 || (DIM == 128 && NT == 2) ? FEW_WARPS / 2 : FEW_WARPS;
-  static constexpr int PER_SM = 16 / FEW_WARPS;
+  // two CTAs an SM: while one joins its warps the other works (64 ragged sequences up to 16384 slots: 171 us; one CTA of twice the
+  // warps 190; more warps of fewer registers, 20 or 18 an SM, 185 and 200)
+  static constexpr int WARPS = DIM * NT > 128 ? 6 : 8, PER_SM = 2;
   static constexpr int SLOTS = 2;
   static constexpr int THREADS = WARPS * 32;
   static constexpr int GROUP_BYTES = GROUP * (DIM + 8), STAGE_BYTES = 2 * GROUP_BYTES;
   static constexpr int PAD = DIM + 4;                                  // floats of a row of O, against bank conflicts
-  static constexpr int RING_BYTES = WARPS * SLOTS * STAGE_BYTES;
-  static constexpr int O_BYTES = WARPS * ROWS * PAD * 4, PARTS_BYTES = 2 * 148 * PER_SM * ROWS * 4;
-  static constexpr int JOIN_BYTES = O_BYTES > PARTS_BYTES ? O_BYTES : PARTS_BYTES;   // the warps' O; factors and sums of an item's parts
-  static constexpr int SMEM = RING_BYTES + JOIN_BYTES;
+  static_assert(8 * PAD * 4 <= STAGE_BYTES, "a warp leaves eight rows of O where its last stage was");
+  static constexpr int SMEM = WARPS * SLOTS * STAGE_BYTES;
   static constexpr int PART = ROWS * (DIM + 2);                        // floats of a part in the workspace: O, maxima, sums
 };
-#ifndef LEAST
-#define LEAST 8
-#endif
-constexpr int LEAST_STAGES = LEAST;                                        // of a CTA
+constexpr int LEAST_STAGES = 8;                                        // of a CTA
 constexpr float SLACK = 8.f;                                           // a maximum may grow by this (in powers of two) before O is rescaled
 
 // A walk over the items in the order (sequence, head, tile).
@@ -248,7 +256,6 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
   using F = Few<DIM, NT>;
   constexpr int ROWS = F::ROWS, WARPS = F::WARPS, SLOTS = F::SLOTS, VW = DIM / 64;
   extern __shared__ __align__(128) uint8_t smem[];
-  float* joined = reinterpret_cast<float*>(smem + F::RING_BYTES);
   __shared__ __align__(8) uint64_t s_full[WARPS][SLOTS];
   __shared__ int s_valid[WARPS][SLOTS];
   struct Fetch {                                                       // what a warp brings in next
@@ -261,6 +268,10 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
   __shared__ Share s_share;
   __shared__ int64_t s_sums[WARPS];
   __shared__ float s_max[WARPS][ROWS], s_sum[WARPS][ROWS];
+  __shared__ int s_place[WARPS];                                       // the place that a warp's O is left in
+  __shared__ uint4 s_query[2][NT][DIM / 32][32];                       // this item's queries and the next one's
+  __shared__ float2 s_by[2][NT][4], s_qsum[2][NT][4];
+  __shared__ float s_join[WARPS * 32 / ROWS][ROWS];
   __shared__ int s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid < WARPS * SLOTS) tc::mbar_init(tc::smem_u32(&s_full[0][0]) + tid * 8, 1);
@@ -358,7 +369,20 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
   const int g = lane >> 2, c = lane & 3;
   bool alive = true;
   int turn = 0;                                                         // stages of this warp so far
-  Queries<T, DIM, NT> q;
+  int page = 0;                                                         // of the queries
+  auto load_queries = [&](const Walk<ROWS>& w, int into) {              // by the first NT warps
+    if (warp >= NT) return;
+    Queries<T, DIM> q;
+    q.load(a.q, w.s.first, w.s.n * a.group, w.tile * ROWS + warp * 8, w.h, a.group, a.scale * LOG2E, lane);
+#pragma unroll
+    for (int i = 0; i < DIM / 32; ++i) s_query[into][warp][i][lane] = q.b[i];
+    if (g == 0) {
+      s_by[into][warp][c] = q.by;
+      s_qsum[into][warp][c] = q.sum;
+    }
+  };
+  load_queries(at, 0);
+  __syncthreads();
   while (true) {
     const int64_t begin = at.begin, first = at.s.first;
     const int h = at.h, row0 = at.tile * ROWS, rows = at.s.n * a.group, length = at.s.length;
@@ -385,7 +409,11 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
       for (int i = 0; i < VW * 4; ++i)
 #pragma unroll
         for (int e = 0; e < 2; ++e) o[nt][i][e] = both(0.f);
-    if (slot0 < end) q.load(a.q, first, rows, row0, h, a.group, a.scale * LOG2E, lane);
+    float2 q_by[NT], q_sum[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) { q_by[nt] = s_by[page][nt][c]; q_sum[nt] = s_qsum[page][nt][c]; }
+    uint32_t scale_field = 7u;                                          // the largest vs's so far
+    bool left = false;                                                  // a place is free for O, and not filled again yet
 
     for (; slot0 < end; slot0 += WARPS * STAGE) {
       const int place = turn % SLOTS;
@@ -396,18 +424,16 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
         const int valid = s_valid[warp][place];
         const bool masked = slot0 + STAGE > least || valid != 3;
         float2 s[2][NT][2];
+        key_products<DIM, NT, 2>(s, stage, [&](int nt, int w) { return s_query[page][nt][w][lane]; }, lane);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const uint8_t* group = stage + u * F::GROUP_BYTES;
-          key_products<T, DIM, NT>(s[u], group, q, lane);
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const uint32_t p = *reinterpret_cast<const uint32_t*>(group + GROUP * (DIM / 2) + key_of(g + 8 * e) * 4);
+            const uint32_t p = *reinterpret_cast<const uint32_t*>(stage + u * F::GROUP_BYTES + GROUP * (DIM / 2) + key_of(g + 8 * e) * 4);
             const float ks = scale_of(p), ko = offset_of(p);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[u][nt][e] = fma2(s[u][nt][e], mul2(both(ks), q.by[nt]), mul2(both(ko), q.sum[nt]));
+            for (int nt = 0; nt < NT; ++nt) s[u][nt][e] = fma2(s[u][nt][e], mul2(both(ks), q_by[nt]), mul2(both(ko), q_sum[nt]));
           }
-        }
         uint32_t vp[2][2];                                              // the values' parameters; a masked key's may be anything
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -427,8 +453,23 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
                 if (slot >= sees[nt][1]) s[u][nt][e].y = -INFINITY;
               }
             }
-        // maxima over the stage's keys; O is rescaled where one has grown by more than SLACK
-        bool grown = false;
+        // the exponent field of the stage's largest vs: vs 2^(6 - scale_field + 127) < 2^7, and with p < 2^SLACK P stays below 2^15
+        uint32_t field = max(max(vp[0][0] & 0x7f80u, vp[0][1] & 0x7f80u), max(vp[1][0] & 0x7f80u, vp[1][1] & 0x7f80u));
+        field = __reduce_max_sync(0xffffffffu, field) >> 7;
+        const bool odd = field == 255u;
+        if (odd) {                                                      // a NaN does not count: not all rows may see it
+          field = 0u;
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t f = vp[u][e] >> 7 & 255u;
+              field = max(field, f == 255u ? 0u : f);
+            }
+          field = __reduce_max_sync(0xffffffffu, field);
+        }
+        // maxima over the stage's keys; O is rescaled where one has grown by more than SLACK, or the largest vs
+        bool grown = field > scale_field;
         float now[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -442,7 +483,10 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
             now[nt][j] = m;
             grown |= m > top[nt][j] + SLACK;
           }
-        if (__any_sync(0xffffffffu, grown))
+        if (__any_sync(0xffffffffu, grown)) {
+          const uint32_t wider = max(field, scale_field) - scale_field;
+          const float scaled = wider > 126u ? 0.f : __uint_as_float((127u - wider) << 23);
+          scale_field += wider;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             float by[2];
@@ -453,42 +497,28 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
               by[j] = top[nt][j] == -INFINITY ? (l[j] == 0.f ? 0.f : 1.f) : exp2_of(top[nt][j] - m);
               top[nt][j] = m;
             }
-            const float2 f = make_float2(by[0], by[1]);
+            float2 f = make_float2(by[0], by[1]);
             sum[nt] = mul2(sum[nt], f);
             off[nt] = mul2(off[nt], f);
+            f = mul2(f, both(scaled));
 #pragma unroll
             for (int i = 0; i < VW * 4; ++i)
 #pragma unroll
               for (int e = 0; e < 2; ++e) o[nt][i][e] = mul2(o[nt][i][e], f);
           }
-        // the exponent field of the stage's largest vs: vs 2^(6 - field + 127) < 2^7, and with p < 2^SLACK P stays below 2^15
-        uint32_t field = max(max(vp[0][0] & 0x7f80u, vp[0][1] & 0x7f80u), max(vp[1][0] & 0x7f80u, vp[1][1] & 0x7f80u));
-        field = max(__reduce_max_sync(0xffffffffu, field) >> 7, 7u);
-        const bool odd = field == 255u;
-        if (odd) {                                                      // a NaN does not count: not all rows may see it
-          field = 7u;
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t f = vp[u][e] >> 7 & 255u;
-              field = max(field, f == 255u ? 0u : f);
-            }
-          field = __reduce_max_sync(0xffffffffu, field);
         }
-        const float shrink = __uint_as_float((260u - field) << 23), grow = __uint_as_float((field - 6u) << 23);
+        const float shrink = __uint_as_float((260u - scale_field) << 23);
         float2 base[NT];                                                // less the maximum
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
           base[nt] = make_float2(top[nt][0] == -INFINITY ? 0.f : -top[nt][0], top[nt][1] == -INFINITY ? 0.f : -top[nt][1]);
-        float part[NT][VW * 4][4];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const uint8_t* group = stage + u * F::GROUP_BYTES + GROUP * (DIM / 2 + 4);
           uint32_t b[NT][2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float vs = scale_of(vp[u][e]) * shrink, vo = offset_of(vp[u][e]);
+            const float v1 = scale_of(vp[u][e]), vs = v1 * shrink, vo = offset_of(vp[u][e]) + 8.f * v1;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               float2 p = add2(s[u][nt][e], base[nt]), r, v;
@@ -518,26 +548,17 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
               const uint32_t a0 = lo01 >> (i & 2 ? 8 : 0), a1 = hi01 >> (i & 2 ? 8 : 0), a2 = lo23 >> (i & 2 ? 8 : 0), a3 = hi23 >> (i & 2 ? 8 : 0);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
-                auto add = [&](uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3) {
-                  if (u == 0) mma_first(part[nt][w * 4 + i], c0, c1, c2, c3, b[nt][0], b[nt][1]);
-                  else mma(part[nt][w * 4 + i], c0, c1, c2, c3, b[nt][0], b[nt][1]);
-                };
-                if (i & 1) add(high_codes(a0), high_codes(a1), high_codes(a2), high_codes(a3));
-                else add(low_codes(a0), low_codes(a1), low_codes(a2), low_codes(a3));
+                if (i & 1) mma(o[nt][w * 4 + i], high_centred(a0), high_centred(a1), high_centred(a2), high_centred(a3), b[nt][0], b[nt][1]);
+                else mma(o[nt][w * 4 + i], low_centred(a0), low_centred(a1), low_centred(a2), low_centred(a3), b[nt][0], b[nt][1]);
               }
             }
           }
         }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int i = 0; i < VW * 4; ++i)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) o[nt][i][e] = fma2(make_float2(part[nt][i][2 * e], part[nt][i][2 * e + 1]), both(grow), o[nt][i][e]);
       }
       ++turn;
       __syncwarp();                                                     // all lanes have read the stage
-      fetch(place);
+      left = slot0 + WARPS * STAGE >= end;                              // the last one's place takes O first
+      if (!left) fetch(place);
     }
 
     // ---- the item's rows over the warps
@@ -554,27 +575,14 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
 #pragma unroll
         for (int j = 0; j < 2; ++j) { s_max[warp][nt * 8 + 2 * c + j] = top[nt][j]; s_sum[warp][nt * 8 + 2 * c + j] = l[nt][j]; }
     }
-    __syncthreads();
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int r = nt * 8 + 2 * c + j;
-        if (l[nt][j] == 0.f) continue;
-        float m = -INFINITY;
-        for (int w = 0; w < WARPS; ++w) m = fmaxf(m, s_max[w][r]);
-        const float by = top[nt][j] == -INFINITY ? 1.f : exp2_of(top[nt][j] - m);
-        float* row = joined + (warp * ROWS + r) * F::PAD + g * (DIM / 8);
-        const float low = 16777216.f * by, high = 1048576.f * by, o0 = (j ? off[nt].y : off[nt].x) * by;   // 2^24 and 2^20: of the codes
-#pragma unroll
-        for (int i = 0; i < VW; ++i)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            auto at_j = [&](int k) { const float2 v = o[nt][4 * i + k][e]; return j ? v.y : v.x; };
-            *reinterpret_cast<float4*>(row + 8 * i + 4 * e) =
-                make_float4(at_j(0) * low + o0, at_j(1) * high + o0, at_j(2) * low + o0, at_j(3) * high + o0);
-          }
-      }
+    const int place = (turn + SLOTS - 1) % SLOTS;                       // of the last stage
+    if (lane == 0) s_place[warp] = place;
+    const bool more = begin + at.s.stages < share.hi;
+    if (more && warp < NT) {
+      Walk<ROWS> following = at;
+      following.next(a);
+      load_queries(following, page ^ 1);
+    }
     __syncthreads();
     const int cta = blockIdx.x;
     const int first_cta = starts ? cta : cta_of(begin, share.total, share.ctas);
@@ -595,65 +603,96 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
         for (int e = 0; e < 4; ++e) p[e] = y[e];
       if (d == 0 && a.lse) a.lse[(first + i) * a.q.heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
     };
-    for (int x = tid; x < ROWS * (DIM / 4); x += WARPS * 32) {
-      const int r = x / (DIM / 4), d = x % (DIM / 4) * 4;
-      float m = -INFINITY, l = 0.f;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int w = 0; w < WARPS; ++w) m = fmaxf(m, s_max[w][r]);
-      for (int w = 0; w < WARPS; ++w) {
-        if (s_sum[w][r] == 0.f) continue;
-        l += s_sum[w][r] * (s_max[w][r] == -INFINITY ? 1.f : exp2_of(s_max[w][r] - m));
-        const float4 t = *reinterpret_cast<const float4*>(joined + (w * ROWS + r) * F::PAD + d);
-        v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = nt * 8 + 2 * c + j;
+        if (l[nt][j] == 0.f) continue;
+        float m = -INFINITY;
+        for (int w = 0; w < WARPS; ++w) m = fmaxf(m, s_max[w][r]);
+        const float by = top[nt][j] == -INFINITY ? 1.f : exp2_of(top[nt][j] - m);
+        float* row = reinterpret_cast<float*>(ring + place * F::STAGE_BYTES) + (2 * c + j) * F::PAD + g * (DIM / 8);
+        // out of the codes' 2^24 and 2^20, and the scales' power of two
+        const float grow = __uint_as_float((scale_field - 6u) << 23) * by, o0 = (j ? off[nt].y : off[nt].x) * by;
+        const float low = 16777216.f * grow, high = 1048576.f * grow;
+#pragma unroll
+        for (int i = 0; i < VW; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            auto at_j = [&](int k) { const float2 v = o[nt][4 * i + k][e]; return j ? v.y : v.x; };
+            *reinterpret_cast<float4*>(row + 8 * i + 4 * e) =
+                make_float4(at_j(0) * low + o0, at_j(1) * high + o0, at_j(2) * low + o0, at_j(3) * high + o0);
+          }
       }
-      if (whole) { write(r, d, v, m, l); continue; }
-      float* p = part_of(cta);
-      __stcg(reinterpret_cast<float4*>(p + r * DIM + d), v);
-      if (d == 0) { __stcg(p + ROWS * DIM + r, m); __stcg(p + ROWS * (DIM + 1) + r, l); }
+      __syncthreads();
+      for (int x = tid; x < 8 * (DIM / 4); x += WARPS * 32) {
+        const int r = nt * 8 + x / (DIM / 4), d = x % (DIM / 4) * 4;
+        float m = -INFINITY, all = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 0; w < WARPS; ++w) m = fmaxf(m, s_max[w][r]);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+          if (s_sum[w][r] == 0.f) continue;
+          all += s_sum[w][r] * (s_max[w][r] == -INFINITY ? 1.f : exp2_of(s_max[w][r] - m));
+          const float4 t = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + (w * SLOTS + s_place[w]) * F::STAGE_BYTES) +
+                                                            (x / (DIM / 4)) * F::PAD + d);
+          v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
+        }
+        if (whole) { write(r, d, v, m, all); continue; }
+        float* p = part_of(cta);
+        __stcg(reinterpret_cast<float4*>(p + r * DIM + d), v);
+        if (d == 0) { __stcg(p + ROWS * DIM + r, m); __stcg(p + ROWS * (DIM + 1) + r, all); }
+      }
+      if (!whole && nt == NT - 1) __threadfence();
+      __syncthreads();
+    }
+    if (left) {                                                         // the stage after next comes where O was
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      fetch(place);
     }
     if (!whole) {
       int* ticket = reinterpret_cast<int*>(a.workspace) + first_cta;
-      __threadfence();
-      __syncthreads();
       if (tid == 0) s_last = atomicAdd(ticket, 1) == last_cta - first_cta;
       __syncthreads();
       if (s_last) {
         __threadfence();
         if (tid == 0) *ticket = 0;                                       // for the next call
-        // what each part's rows count for, by a thread each; then the sums
-        const int n_parts = last_cta - first_cta + 1;
-        float* by = joined;                                              // [part][row]
-        for (int x = tid; x < n_parts * ROWS; x += WARPS * 32) by[x] = __ldcg(part_of(first_cta + x / ROWS) + ROWS * DIM + x % ROWS);
+        // each row's maximum and sum, over the parts by many threads; then O
+        constexpr int AT_ONCE = WARPS * 32 / ROWS;
+        const int row = tid % ROWS, mine = tid / ROWS;
+        float m = -INFINITY, all = 0.f;
+        for (int i = first_cta + mine; i <= last_cta; i += AT_ONCE) m = fmaxf(m, __ldcg(part_of(i) + ROWS * DIM + row));
+        s_join[mine][row] = m;
         __syncthreads();
-        if (tid < ROWS) {
-          float m = -INFINITY;
-          for (int i = 0; i < n_parts; ++i) m = fmaxf(m, by[i * ROWS + tid]);
-          s_max[0][tid] = m;
-        }
+        for (int i = 0; i < AT_ONCE; ++i) m = fmaxf(m, s_join[i][row]);
         __syncthreads();
-        for (int x = tid; x < n_parts * ROWS; x += WARPS * 32) {
-          const float l = __ldcg(part_of(first_cta + x / ROWS) + ROWS * (DIM + 1) + x % ROWS);
-          const float f = l == 0.f ? 0.f : by[x] == -INFINITY ? 1.f : exp2_of(by[x] - s_max[0][x % ROWS]);
-          by[x] = f;
-          by[n_parts * ROWS + x] = l * f;
+        for (int i = first_cta + mine; i <= last_cta; i += AT_ONCE) {
+          const float pm = __ldcg(part_of(i) + ROWS * DIM + row), pl = __ldcg(part_of(i) + ROWS * (DIM + 1) + row);
+          all += pl == 0.f ? 0.f : pl * (pm == -INFINITY ? 1.f : exp2_of(pm - m));
         }
+        s_join[mine][row] = all;
+        if (mine == 0) s_max[0][row] = m;
         __syncthreads();
         for (int x = tid; x < ROWS * (DIM / 4); x += WARPS * 32) {
           const int r = x / (DIM / 4), d = x % (DIM / 4) * 4;
-          float l = 0.f;
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          m = s_max[0][r];
 #pragma unroll 8
-          for (int i = 0; i < n_parts; ++i) {
-            const float4 t = __ldcg(reinterpret_cast<const float4*>(part_of(first_cta + i) + r * DIM + d));
-            const float f = by[i * ROWS + r];
-            l += by[(n_parts + i) * ROWS + r];
-            v.x += t.x * f; v.y += t.y * f; v.z += t.z * f; v.w += t.w * f;
+          for (int i = first_cta; i <= last_cta; ++i) {
+            const float pm = __ldcg(part_of(i) + ROWS * DIM + r);
+            const float4 t = __ldcg(reinterpret_cast<const float4*>(part_of(i) + r * DIM + d));
+            const float by = pm == -INFINITY ? 1.f : exp2_of(pm - m);    // (where there is no sum O is zero)
+            v.x += t.x * by; v.y += t.y * by; v.z += t.z * by; v.w += t.w * by;
           }
-          write(r, d, v, s_max[0][r], l);
+          all = 0.f;
+          for (int i = 0; i < AT_ONCE; ++i) all += s_join[i][r];
+          write(r, d, v, m, all);
         }
+        __syncthreads();
       }
     }
-    __syncthreads();
+    page ^= 1;
     if (begin + at.s.stages >= share.hi) break;
     slot0 -= at.s.stages * STAGE;
     at.next(a);
@@ -719,10 +758,10 @@ __global__ void __launch_bounds__(W_WARPS * 32) weights_kernel(const AttentionAr
       // rows before the first one that sees slot0 see nothing here
       const int row_first = max(0, slot0 - (length - n)) * a.group / 8 * 8;
       for (int row0 = row_first; row0 < rows; row0 += 8) {
-        Queries<T, DIM, 1> q;
+        Queries<T, DIM> q;
         q.load(a.q, first, rows, row0, h, a.group, a.scale * LOG2E, lane);
-        float2 s[1][2];
-        key_products<T, DIM, 1>(s, group, q, lane);
+        float2 s[1][1][2];
+        key_products<DIM, 1, 1>(s, group, [&](int, int w) { return q.b[w]; }, lane);
         float lse[2];
         int sees[2];
 #pragma unroll
@@ -733,7 +772,7 @@ __global__ void __launch_bounds__(W_WARPS * 32) weights_kernel(const AttentionAr
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float2 x = fma2(s[0][e], mul2(both(ks[e]), q.by[0]), mul2(both(ko[e]), q.sum[0]));
+          const float2 x = fma2(s[0][0][e], mul2(both(ks[e]), q.by), mul2(both(ko[e]), q.sum));
           const int slot = slot0 + key_of(g + 8 * e);
           if (slot < sees[0]) got[e] += exp2_of(x.x - lse[0]);
           if (slot < sees[1]) got[e] += exp2_of(x.y - lse[1]);
