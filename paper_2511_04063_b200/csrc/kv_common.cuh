@@ -78,6 +78,18 @@ struct Share {
 // The CTA that has unit x: lo(i) = floor(i total / ctas).
 __device__ __forceinline__ int cta_of(int64_t x, int64_t total, int ctas) { return (int)(((x + 1) * ctas - 1) / total); }
 
+// Two fp32 operations in one instruction.
+using mx::add2;
+using mx::mul2;
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\t"
+      "mov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
 // Called by a whole CTA of `threads` threads.  `least`: units that are worth a CTA.
 template <typename F>
 __device__ void find_share(Share* out, int n_seqs, int64_t least, int64_t* warp_sums, F cost) {
@@ -148,7 +160,7 @@ struct RopeArgs {
   const int* positions;
   const float* inv_freq;
   const void *q_gamma, *k_gamma;
-  int gamma_fp32, flags, splits;
+  int gamma_fp32, gamma_vec, flags, splits;
   float eps;
 };
 dq_status rope(cudaStream_t stream, int dtype, const RopeArgs& a);
