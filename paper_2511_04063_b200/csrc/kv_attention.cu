@@ -141,7 +141,7 @@ struct Queries {
 // (q . c) of the 16 keys of N groups and the tile's rows, without q.by: acc[u][nt][e] = key_of(g + 8 e), columns 2 c, 2 c + 1.
 // query(nt, w): the B fragments of a word.  Two sums a group side by side, because each instruction waits for the one that its sum
 // comes from.
-template <int DIM, int NT, int N, typename Q>
+template <int DIM, int NT, int N, int STRIDE, typename Q>
 __device__ __forceinline__ void key_products(float2 (&acc)[N][NT][2], const uint8_t* codes, Q query, int lane) {
   constexpr int WORDS = DIM / 32;
   const int g = lane >> 2, c = lane & 3;
@@ -150,7 +150,7 @@ __device__ __forceinline__ void key_products(float2 (&acc)[N][NT][2], const uint
   for (int u = 0; u < N; ++u)
 #pragma unroll
     for (int e = 0; e < 2; ++e)
-      load_words<WORDS>(k[u][e], codes + u * (GROUP * (DIM + 8)) + key_of(g + 8 * e) * (DIM / 2) + c * (DIM / 8));
+      load_words<WORDS>(k[u][e], codes + u * STRIDE + key_of(g + 8 * e) * (DIM / 2) + c * (DIM / 8));
   float d[N][2][NT][4];
 #pragma unroll
   for (int w = 0; w < WORDS; ++w)
@@ -175,8 +175,8 @@ __device__ __forceinline__ void key_products(float2 (&acc)[N][NT][2], const uint
         acc[u][nt][e] = add2(make_float2(d[u][0][nt][2 * e], d[u][0][nt][2 * e + 1]), make_float2(d[u][1][nt][2 * e], d[u][1][nt][2 * e + 1]));
 }
 
-// An item of work is a tile of query rows of a sequence and kv head; it has `stages` stages of keys (one at least: rows that see nothing
-// are written too).
+// An item of work is a tile of ROWS query rows of a sequence and kv head; it has `stages` stages of keys (one at least: rows that see
+// nothing are written too).  ROWS 0: all rows, and no item without keys.
 template <int ROWS>
 struct Sequence {
   int64_t first;
@@ -184,34 +184,15 @@ struct Sequence {
   __device__ __forceinline__ void describe(const AttentionArgs& a, int b) {
     a.batch.range(b, first, n);
     length = a.cache.length(b);
-    tiles = (int)(((int64_t)n * a.group + ROWS - 1) / ROWS);
-    stages = max(1, (length + STAGE - 1) / STAGE);
+    stages = (length + STAGE - 1) / STAGE;
+    if constexpr (ROWS == 0) tiles = min(stages, 1);
+    else {
+      tiles = (int)(((int64_t)n * a.group + ROWS - 1) / ROWS);
+      stages = max(stages, 1);
+    }
   }
+  __device__ __forceinline__ int64_t units(const AttentionArgs& a) const { return (int64_t)tiles * a.cache.heads * stages; }
 };
-
-// ------------------------------------------------------------------------------------------------ few rows
-// A CTA takes an equal share of all stages of all items, whatever the sequences' lengths, and its warps take them in turn, each with its
-// own maximum, sum and O^T, joined in shared memory at an item's end.  A warp brings its stages in by bulk copies into two places of
-// its own: while it works on one the other is on its way, across items too.  An item that crosses CTAs is left in the workspace in parts,
-// and the CTA that finishes last joins them, in order.
-constexpr int MAX_CTAS = 640;
-constexpr int TICKET_BYTES = MAX_CTAS * 4;
-template <int DIM, int NT>
-struct Few {
-  static constexpr int ROWS = 8 * NT;
-  // two CTAs an SM: while one joins its warps the other works (64 ragged sequences up to 16384 slots: 171 us; one CTA of twice the
-  // warps 190; more warps of fewer registers, 20 or 18 an SM, 185 and 200)
-  static constexpr int WARPS = DIM * NT > 128 ? 6 : 8, PER_SM = 2;
-  static constexpr int SLOTS = 2;
-  static constexpr int THREADS = WARPS * 32;
-  static constexpr int GROUP_BYTES = GROUP * (DIM + 8), STAGE_BYTES = 2 * GROUP_BYTES;
-  static constexpr int PAD = DIM + 4;                                  // floats of a row of O, against bank conflicts
-  static_assert(8 * PAD * 4 <= STAGE_BYTES, "a warp leaves eight rows of O where its last stage was");
-  static constexpr int SMEM = WARPS * SLOTS * STAGE_BYTES;
-  static constexpr int PART = ROWS * (DIM + 2);                        // floats of a part in the workspace: O, maxima, sums
-};
-constexpr int LEAST_STAGES = 8;                                        // of a CTA
-constexpr float SLACK = 8.f;                                           // a maximum may grow by this (in powers of two) before O is rescaled
 
 // A walk over the items in the order (sequence, head, tile).
 template <int ROWS>
@@ -238,61 +219,43 @@ struct Walk {
       s.describe(a, b);
     } while (s.tiles == 0);
   }
+  // the slots of the item that are a CTA's
+  __device__ __forceinline__ int end(const Share& share) const { return (int)(min(begin + s.stages, share.hi) - begin) * STAGE; }
 };
 
-template <typename T, int DIM, int NT>
-__global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) few_kernel(const AttentionArgs a) {
-  using F = Few<DIM, NT>;
-  constexpr int ROWS = F::ROWS, WARPS = F::WARPS, SLOTS = F::SLOTS, VW = DIM / 64;
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ __align__(8) uint64_t s_full[WARPS][SLOTS];
-  __shared__ int s_valid[WARPS][SLOTS];
-  struct Fetch {                                                       // what a warp brings in next
-    const uint8_t* group[32][2];
-    int used, left, issued;                                            // of the list
-    int slot, end;                                                     // within the item, behind the list
+// A warp's stages of its CTA's share, every WARPS-th, brought into PLACES places of its own by bulk copies ahead of their use, across
+// items.  KEYS: without the values.
+template <int DIM, int ROWS, int WARPS, int PLACES, bool KEYS>
+struct Stream {
+  static constexpr int WHOLE = GROUP * (DIM + 8), GROUP_BYTES = KEYS ? WHOLE / 2 : WHOLE, STAGE_BYTES = 2 * GROUP_BYTES;
+  struct List {                                                         // in shared memory
+    const uint8_t* group[32][2];                                        // of the next stages (null: no page)
+    uint64_t full[PLACES];                                              // barriers: a place has been filled
+    int valid[PLACES];                                                  // which of its groups have been
+    int used, left, issued;                                             // of the list
+    int slot, end;                                                      // within the item, behind the list
     Walk<ROWS> walk;
   };
-  __shared__ Fetch s_fetch[WARPS];
-  __shared__ Share s_share;
-  __shared__ int64_t s_sums[WARPS];
-  __shared__ float s_max[WARPS][ROWS], s_sum[WARPS][ROWS];
-  __shared__ int s_place[WARPS];                                       // the place that a warp's O is left in
-  __shared__ uint4 s_query[2][NT][DIM / 32][32];                       // this item's queries and the next one's
-  __shared__ float2 s_by[2][NT][4], s_qsum[2][NT][4];
-  __shared__ float s_join[WARPS * 32 / ROWS][ROWS];
-  __shared__ int s_last;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid < WARPS * SLOTS) tc::mbar_init(tc::smem_u32(&s_full[0][0]) + tid * 8, 1);
-  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  mx::wait_for_previous();
-  mx::allow_next();
-  find_share(&s_share, a.batch.n_seqs, LEAST_STAGES, s_sums, [&](int b) {
-    Sequence<ROWS> s;
-    s.describe(a, b);
-    return (int64_t)s.tiles * a.cache.heads * s.stages;
-  });
-  const Share share = s_share;
-  if (share.lo >= share.hi) return;
+  const AttentionArgs& a;
+  const Share& share;
+  List& f;
+  uint8_t* ring;
+  int lane, turn = 0;                                                   // stages so far
+  bool alive = true;
 
-  const uint32_t full0 = tc::smem_u32(&s_full[warp][0]);
-  uint8_t* const ring = smem + warp * SLOTS * F::STAGE_BYTES;
-  const uint32_t ring0 = tc::smem_u32(ring);
-  Walk<ROWS> at;
-  at.start(a, share);
-  // the slots of an item that are this CTA's, for a walk that stands at it
-  auto end_of = [&](const Walk<ROWS>& w) { return (int)(min(w.begin + w.s.stages, share.hi) - w.begin) * STAGE; };
-  // The next stages of the warp, up to 32 of one item: a lane looks one's pages up and leaves the addresses of its groups (null: no
-  // page) in the warp's list.
-  Fetch& f = s_fetch[warp];
-  auto refill = [&]() {
+  __device__ __forceinline__ uint32_t bar(int place) const { return tc::smem_u32(&f.full[place]); }
+  __device__ __forceinline__ int place() const { return turn % PLACES; }
+  __device__ __forceinline__ const uint8_t* stage() const { return ring + place() * STAGE_BYTES; }
+
+  // A lane looks the pages of one of the next 32 stages of an item up.
+  __device__ __forceinline__ void refill() {
     int slot = f.slot;
     while (slot >= f.end && f.walk.begin + f.walk.s.stages < share.hi) {
       __syncwarp();
       if (lane == 0) {
         slot -= f.walk.s.stages * STAGE;                                // (the warp's stages go on through all items)
         f.walk.next(a);
-        f.end = end_of(f.walk);
+        f.end = f.walk.end(share);
         f.slot = slot;
       }
       __syncwarp();
@@ -305,7 +268,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
       const int64_t page = a.cache.page_of(w.b, mine);
       if (page >= 0) p0 = a.cache.group_at(page, w.h, mine, DIM);
       if (mine + GROUP < length) {
-        if (a.cache.shift > 4) p1 = p0 ? p0 + F::GROUP_BYTES : nullptr;
+        if (a.cache.shift > 4) p1 = p0 ? p0 + WHOLE : nullptr;
         else {
           const int64_t other = a.cache.page_of(w.b, mine + GROUP);
           if (other >= 0) p1 = a.cache.group_at(other, w.h, mine + GROUP, DIM);
@@ -322,42 +285,112 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
       f.slot = slot + f.left * (WARPS * STAGE);
     }
     __syncwarp();
-  };
-  auto fetch = [&](int place) {                                         // the warp's next stage; false: there is none
+  }
+  // The warp's next stage, if there is one, into a place that no lane reads any more.
+  __device__ __forceinline__ void fetch(int place) {
     if (f.used == f.left) refill();
     const int i = f.used;
     if (i == f.left) return;
     __syncwarp();
     if (lane == 0) {
       const uint8_t *p0 = f.group[i][0], *p1 = f.group[i][1];
-      const uint32_t dst = ring0 + place * F::STAGE_BYTES, bar = full0 + place * 8;
+      const uint32_t dst = tc::smem_u32(ring + place * STAGE_BYTES), full = bar(place);
       auto copy = [&](uint32_t to, const uint8_t* from, uint32_t bytes) {
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                     ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+                     ::"r"(to), "l"(from), "r"(bytes), "r"(full) : "memory");
       };
       f.used = i + 1;
       ++f.issued;
-      s_valid[warp][place] = (p0 ? 1 : 0) | (p1 ? 2 : 0);
-      tc::mbar_expect_tx(bar, ((p0 ? 1 : 0) + (p1 ? 1 : 0)) * F::GROUP_BYTES);
-      if (p1 == p0 + F::GROUP_BYTES && p0) copy(dst, p0, F::STAGE_BYTES);   // one behind the other
+      f.valid[place] = (p0 ? 1 : 0) | (p1 ? 2 : 0);
+      tc::mbar_expect_tx(full, ((p0 ? 1 : 0) + (p1 ? 1 : 0)) * GROUP_BYTES);
+      if (!KEYS && p0 && p1 == p0 + WHOLE) copy(dst, p0, STAGE_BYTES);   // one behind the other
       else {
-        if (p0) copy(dst, p0, F::GROUP_BYTES);
-        if (p1) copy(dst + F::GROUP_BYTES, p1, F::GROUP_BYTES);
+        if (p0) copy(dst, p0, GROUP_BYTES);
+        if (p1) copy(dst + GROUP_BYTES, p1, GROUP_BYTES);
       }
     }
     __syncwarp();
-  };
-  int slot0 = (int)(share.lo - at.begin + warp) * STAGE;                // this warp's next, within the item
-  if (lane == 0) {
-    f.walk = at;
-    f.slot = slot0; f.end = end_of(at); f.used = f.left = f.issued = 0;
   }
-  __syncwarp();
-  for (int i = 0; i < SLOTS; ++i) fetch(i);
+  // From the first slot of the share's first item that is this warp's.  The barriers are ready.
+  __device__ __forceinline__ void start(const Walk<ROWS>& walk, int slot) {
+    if (lane == 0) {
+      f.walk = walk;
+      f.slot = slot; f.end = walk.end(share); f.used = f.left = f.issued = 0;
+    }
+    __syncwarp();
+    for (int i = 0; i < PLACES; ++i) fetch(i);
+  }
+  // Whether the warp's next stage is there.
+  __device__ __forceinline__ bool wait() {
+    if (alive) alive = __all_sync(0xffffffffu, tc::mbar_wait(bar(place()), (uint32_t)(turn / PLACES) & 1u, a.d_status));
+    return alive;
+  }
+  // After a wait that gave up: no copy is left on its way into memory that may go to another CTA.
+  __device__ __forceinline__ void end() {
+    if (!alive && lane == 0)
+      for (int i = turn; i < f.issued; ++i) tc::mbar_wait(bar(i % PLACES), (uint32_t)(i / PLACES) & 1u, a.d_status);
+  }
+};
+
+// ------------------------------------------------------------------------------------------------ few rows
+// A CTA takes an equal share of all stages of all items, whatever the sequences' lengths, and its warps take them in turn, each with its
+// own maximum, sum and O^T, joined in shared memory at an item's end.  A warp brings its stages in by bulk copies into two places of
+// its own: while it works on one the other is on its way, across items too.  An item that crosses CTAs is left in the workspace in parts,
+// and the CTA that finishes last joins them, in order.
+constexpr int MAX_CTAS = 640;
+constexpr int TICKET_BYTES = MAX_CTAS * 4;
+template <int DIM, int NT>
+struct Few {
+  static constexpr int ROWS = 8 * NT;
+  // two CTAs an SM: while one joins its warps the other works (64 ragged sequences up to 16384 slots: 171 us; one CTA of twice the
+  // warps 190; more warps of fewer registers, 20 or 18 an SM, 185 and 200)
+  static constexpr int WARPS = DIM * NT > 128 ? 6 : 8, PER_SM = 2;
+  static constexpr int PLACES = 2;
+  static constexpr int THREADS = WARPS * 32;
+  using Stages = Stream<DIM, ROWS, WARPS, PLACES, false>;
+  static constexpr int GROUP_BYTES = Stages::GROUP_BYTES, STAGE_BYTES = Stages::STAGE_BYTES;
+  static constexpr int PAD = DIM + 4;                                  // floats of a row of O, against bank conflicts
+  static_assert(8 * PAD * 4 <= STAGE_BYTES, "a warp leaves eight rows of O where its last stage was");
+  static constexpr int SMEM = WARPS * PLACES * STAGE_BYTES;
+  static constexpr int PART = ROWS * (DIM + 2);                        // floats of a part in the workspace: O, maxima, sums
+};
+constexpr int LEAST_STAGES = 8;                                        // of a CTA
+constexpr float SLACK = 8.f;                                           // a maximum may grow by this (in powers of two) before O is rescaled
+
+template <typename T, int DIM, int NT>
+__global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) few_kernel(const AttentionArgs a) {
+  using F = Few<DIM, NT>;
+  constexpr int ROWS = F::ROWS, WARPS = F::WARPS, PLACES = F::PLACES, VW = DIM / 64;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ typename F::Stages::List s_list[WARPS];
+  __shared__ Share s_share;
+  __shared__ int64_t s_sums[WARPS];
+  __shared__ float s_max[WARPS][ROWS], s_sum[WARPS][ROWS];
+  __shared__ int s_place[WARPS];                                       // the place that a warp's O is left in
+  __shared__ uint4 s_query[2][NT][DIM / 32][32];                       // this item's queries and the next one's
+  __shared__ float2 s_by[2][NT][4], s_qsum[2][NT][4];
+  __shared__ float s_join[WARPS * 32 / ROWS][ROWS];
+  __shared__ int s_last;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid < WARPS * PLACES) tc::mbar_init(tc::smem_u32(&s_list[tid / PLACES].full[tid % PLACES]), 1);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  mx::wait_for_previous();
+  mx::allow_next();
+  find_share(&s_share, a.batch.n_seqs, LEAST_STAGES, s_sums, [&](int b) {
+    Sequence<ROWS> s;
+    s.describe(a, b);
+    return s.units(a);
+  });
+  const Share share = s_share;
+  if (share.lo >= share.hi) return;
+
+  Walk<ROWS> at;
+  at.start(a, share);
+  int slot0 = (int)(share.lo - at.begin + warp) * STAGE;                // this warp's next, within the item
+  typename F::Stages stages{a, share, s_list[warp], smem + warp * PLACES * F::STAGE_BYTES, lane};
+  stages.start(at, slot0);
 
   const int g = lane >> 2, c = lane & 3;
-  bool alive = true;
-  int turn = 0;                                                         // stages of this warp so far
   int page = 0;                                                         // of the queries
   auto load_queries = [&](const Walk<ROWS>& w, int into) {              // by the first NT warps
     if (warp >= NT) return;
@@ -376,7 +409,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
     const int64_t begin = at.begin, first = at.s.first;
     const int h = at.h, row0 = at.tile * ROWS, rows = at.s.n * a.group, length = at.s.length;
     const bool starts = begin >= share.lo, ends = begin + at.s.stages <= share.hi;
-    const int end = end_of(at);
+    const int end = at.end(share);
     float top[NT][2];
     float2 sum[NT], off[NT], o[NT][VW * 4][2];
     int sees[NT][2];
@@ -405,15 +438,14 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
     bool left = false;                                                  // a place is free for O, and not filled again yet
 
     for (; slot0 < end; slot0 += WARPS * STAGE) {
-      const int place = turn % SLOTS;
-      if (alive) alive = __all_sync(0xffffffffu, tc::mbar_wait(full0 + place * 8, (uint32_t)(turn / SLOTS) & 1u, a.d_status));
-      if (!alive) continue;
+      if (!stages.wait()) continue;
+      const int place = stages.place();
       if (slot0 < most) {
-        const uint8_t* stage = ring + place * F::STAGE_BYTES;
-        const int valid = s_valid[warp][place];
+        const uint8_t* stage = stages.stage();
+        const int valid = s_list[warp].valid[place];
         const bool masked = slot0 + STAGE > least || valid != 3;
         float2 s[2][NT][2];
-        key_products<DIM, NT, 2>(s, stage, [&](int nt, int w) { return s_query[page][nt][w][lane]; }, lane);
+        key_products<DIM, NT, 2, F::GROUP_BYTES>(s, stage, [&](int nt, int w) { return s_query[page][nt][w][lane]; }, lane);
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -544,10 +576,10 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
           }
         }
       }
-      ++turn;
+      ++stages.turn;
       __syncwarp();                                                     // all lanes have read the stage
       left = slot0 + WARPS * STAGE >= end;                              // the last one's place takes O first
-      if (!left) fetch(place);
+      if (!left) stages.fetch(place);
     }
 
     // ---- the item's rows over the warps
@@ -564,7 +596,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
 #pragma unroll
         for (int j = 0; j < 2; ++j) { s_max[warp][nt * 8 + 2 * c + j] = top[nt][j]; s_sum[warp][nt * 8 + 2 * c + j] = l[nt][j]; }
     }
-    const int place = (turn + SLOTS - 1) % SLOTS;                       // of the last stage
+    const int place = (stages.turn + PLACES - 1) % PLACES;                       // of the last stage
     if (lane == 0) s_place[warp] = place;
     const bool more = begin + at.s.stages < share.hi;
     if (more && warp < NT) {
@@ -601,7 +633,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
         float m = -INFINITY;
         for (int w = 0; w < WARPS; ++w) m = fmaxf(m, s_max[w][r]);
         const float by = top[nt][j] == -INFINITY ? 1.f : exp2_of(top[nt][j] - m);
-        float* row = reinterpret_cast<float*>(ring + place * F::STAGE_BYTES) + (2 * c + j) * F::PAD + g * (DIM / 8);
+        float* row = reinterpret_cast<float*>(stages.ring + place * F::STAGE_BYTES) + (2 * c + j) * F::PAD + g * (DIM / 8);
         // out of the codes' 2^24 and 2^20, and the scales' power of two
         const float grow = __uint_as_float((scale_field - 6u) << 23) * by, o0 = (j ? off[nt].y : off[nt].x) * by;
         const float low = 16777216.f * grow, high = 1048576.f * grow;
@@ -624,7 +656,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
         for (int w = 0; w < WARPS; ++w) {
           if (s_sum[w][r] == 0.f) continue;
           all += s_sum[w][r] * (s_max[w][r] == -INFINITY ? 1.f : exp2_of(s_max[w][r] - m));
-          const float4 t = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + (w * SLOTS + s_place[w]) * F::STAGE_BYTES) +
+          const float4 t = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + (w * PLACES + s_place[w]) * F::STAGE_BYTES) +
                                                             (x / (DIM / 4)) * F::PAD + d);
           v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
         }
@@ -638,7 +670,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
     }
     if (left) {                                                         // the stage after next comes where O was
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      fetch(place);
+      stages.fetch(place);
     }
     if (!whole) {
       int* ticket = reinterpret_cast<int*>(a.workspace) + first_cta;
@@ -686,8 +718,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
     slot0 -= at.s.stages * STAGE;
     at.next(a);
   }
-  if (!alive && lane == 0)   // no copy is left on its way into memory that may go to another CTA
-    for (int i = turn; i < f.issued; ++i) tc::mbar_wait(full0 + (i % SLOTS) * 8, (uint32_t)(i / SLOTS) & 1u, a.d_status);
+  stages.end();
 }
 
 template <typename T, int DIM, int NT>
@@ -705,81 +736,330 @@ dq_status run_few(cudaStream_t stream, const mx::Device& dev, const AttentionArg
 
 // ------------------------------------------------------------------------------------------------ weights
 // W[slot] = (old slot ? W[slot] : 0) + sum over the kv head's query rows of exp(S - lse): the first product again, with the
-// rows' sums known.  A CTA takes tiles of 128 keys, a warp 16 of them for all rows, so that each weight is summed by one warp in
-// one order.
-constexpr int W_WARPS = 8, W_TILE = W_WARPS * GROUP;
+// rows' sums known.  Each weight is summed in one order, whatever the run.
 
-template <typename T, int DIM>
-__global__ void __launch_bounds__(W_WARPS * 32) weights_kernel(const AttentionArgs a) {
-  __shared__ Share s_share;
-  __shared__ int64_t s_sums[W_WARPS];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-  mx::wait_for_previous();
-  find_share(&s_share, a.batch.n_seqs, 1, s_sums, [&](int b) { return (int64_t)a.cache.heads * ((a.cache.length(b) + W_TILE - 1) / W_TILE); });
-  const Share share = s_share;
-  int seq = share.seq;
-  int64_t before = share.before;
-  for (int64_t unit = share.lo; unit < share.hi; ++unit) {
-    int length = a.cache.length(seq);
-    int64_t tiles = (length + W_TILE - 1) / W_TILE;
-    while (unit >= before + tiles * a.cache.heads) {
-      before += tiles * a.cache.heads;
-      length = a.cache.length(++seq);
-      tiles = (length + W_TILE - 1) / W_TILE;
-    }
-    int64_t first;
-    int n;
-    a.batch.range(seq, first, n);
-    const int h = (int)((unit - before) / tiles), rows = n * a.group;
-    const int slot0 = (int)((unit - before) % tiles) * W_TILE + warp * GROUP;
-    if (slot0 >= length) continue;
-    const int64_t page = a.cache.page_of(seq, slot0);
-    float got[2] = {0.f, 0.f};
-    if (page >= 0) {
-      const uint8_t* group = a.cache.group_at(page, h, slot0, DIM);
-      float ks[2], ko[2];
+// A tile of 8 rows in shared memory, as the product and the exponentials want it.
+template <int DIM>
+struct Rows {
+  uint4 b[DIM / 32][32];
+  float2 by[4], sum[4], minus_lse[4];                                  // of columns 2 c, 2 c + 1; no row: an lse of infinity
+  int2 sees[4];
+  int least, most;                                                     // slots that all rows see, that any does
+  template <typename T>
+  __device__ __forceinline__ void bring(const AttentionArgs& a, int64_t first, int n, int length, int h, int r0, int lane) {
+    const int rows = n * a.group, c = lane & 3;
+    Queries<T, DIM> q;
+    q.load(a.q, first, rows, r0, h, a.group, a.scale * LOG2E, lane);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint32_t p = *reinterpret_cast<const uint32_t*>(group + GROUP * (DIM / 2) + key_of(g + 8 * e) * 4);
-        ks[e] = scale_of(p);
-        ko[e] = offset_of(p);
+    for (int w = 0; w < DIM / 32; ++w) b[w][lane] = q.b[w];
+    if (lane < 4) {
+      float lse[2];
+      int slots[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = r0 + 2 * c + j, t = r / a.group;
+        lse[j] = r < rows ? a.lse[(first + t) * a.q.heads + h * a.group + r - t * a.group] * -LOG2E : -INFINITY;
+        slots[j] = r < rows ? length - n + t + 1 : 0;
       }
-      // rows before the first one that sees slot0 see nothing here
-      const int row_first = max(0, slot0 - (length - n)) * a.group / 8 * 8;
-      for (int row0 = row_first; row0 < rows; row0 += 8) {
-        Queries<T, DIM> q;
-        q.load(a.q, first, rows, row0, h, a.group, a.scale * LOG2E, lane);
-        float2 s[1][1][2];
-        key_products<DIM, 1, 1>(s, group, [&](int, int w) { return q.b[w]; }, lane);
-        float lse[2];
-        int sees[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int r = row0 + 2 * c + j, i = r / a.group;
-          lse[j] = r < rows ? a.lse[(first + i) * a.q.heads + h * a.group + r - i * a.group] * LOG2E : 0.f;
-          sees[j] = r < rows ? length - n + i + 1 : 0;
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float2 x = fma2(s[0][0][e], mul2(both(ks[e]), q.by), mul2(both(ko[e]), q.sum));
-          const int slot = slot0 + key_of(g + 8 * e);
-          if (slot < sees[0]) got[e] += exp2_of(x.x - lse[0]);
-          if (slot < sees[1]) got[e] += exp2_of(x.y - lse[1]);
-        }
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      got[e] += __shfl_xor_sync(0xffffffffu, got[e], 1);
-      got[e] += __shfl_xor_sync(0xffffffffu, got[e], 2);
-      const int slot = slot0 + key_of(g + 8 * e);
-      if (c == 0 && slot < length) {
-        const int64_t at = ((int64_t)seq * a.cache.heads + h) * a.ld_slots + slot;
-        a.weights_out[at] = (a.weights && slot < length - n ? a.weights[at] : 0.f) + got[e];
+      by[c] = q.by;
+      sum[c] = q.sum;
+      minus_lse[c] = make_float2(lse[0], lse[1]);
+      sees[c] = make_int2(slots[0], slots[1]);
+      if (c == 0) {
+        least = slots[0];
+        most = r0 < rows ? length - n + (min(r0 + 8, rows) - 1) / a.group + 1 : 0;
       }
     }
   }
+  // The probabilities of products s of a key (parameters ks, ko), added to got.
+  __device__ __forceinline__ void add(float2& got, float2 s, float ks, float ko, int slot, bool masked, int c) const {
+    const float2 x = fma2(s, mul2(both(ks), by[c]), fma2(both(ko), sum[c], minus_lse[c]));
+    float2 p = make_float2(exp2_of(x.x), exp2_of(x.y));
+    if (masked) {
+      if (slot >= sees[c].x) p.x = 0.f;
+      if (slot >= sees[c].y) p.y = 0.f;
+    }
+    got = add2(got, p);
+  }
+};
+// A weight from the lanes of its key: the sum of their columns.
+__device__ __forceinline__ float over_columns(float2 got) {
+  float w = got.x + got.y;
+  w += __shfl_xor_sync(0xffffffffu, w, 1);
+  return w + __shfl_xor_sync(0xffffffffu, w, 2);
+}
+
+// Few rows: bound by HBM.  The keys come as in few_kernel; the first two tiles of rows lie in shared memory, of this item and the next.
+template <int DIM>
+struct FewWeights {
+  static constexpr int WARPS = DIM == 256 ? 8 : 10, PER_SM = 2, PLACES = DIM == 256 ? 2 : 4, TILES = 2;
+  using Stages = Stream<DIM, 0, WARPS, PLACES, true>;
+  static constexpr int SMEM = WARPS * PLACES * Stages::STAGE_BYTES;
+};
+template <typename T, int DIM>
+__global__ void __launch_bounds__(FewWeights<DIM>::WARPS * 32, FewWeights<DIM>::PER_SM) few_weights_kernel(const AttentionArgs a) {
+  using F = FewWeights<DIM>;
+  using Stages = typename F::Stages;
+  constexpr int WARPS = F::WARPS, PLACES = F::PLACES;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ typename Stages::List s_list[WARPS];
+  __shared__ Rows<DIM> s_rows[2][F::TILES];
+  __shared__ Share s_share;
+  __shared__ int64_t s_sums[WARPS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  if (tid < WARPS * PLACES) tc::mbar_init(tc::smem_u32(&s_list[tid / PLACES].full[tid % PLACES]), 1);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  mx::wait_for_previous();
   mx::allow_next();
+  find_share(&s_share, a.batch.n_seqs, LEAST_STAGES, s_sums, [&](int b) {
+    Sequence<0> s;
+    s.describe(a, b);
+    return s.units(a);
+  });
+  const Share share = s_share;
+  if (share.lo >= share.hi) return;
+  Walk<0> at;
+  at.start(a, share);
+  int slot0 = (int)(share.lo - at.begin + warp) * STAGE, page = 0;
+  Stages stages{a, share, s_list[warp], smem + warp * PLACES * Stages::STAGE_BYTES, lane};
+  stages.start(at, slot0);
+  auto bring = [&](const Walk<0>& w, int into) {
+    if (warp < F::TILES) s_rows[into][warp].template bring<T>(a, w.s.first, w.s.n, w.s.length, w.h, warp * 8, lane);
+  };
+  bring(at, 0);
+  __syncthreads();
+  while (true) {
+    const int n = at.s.n, rows = n * a.group, length = at.s.length, end = at.end(share);
+    const int64_t row = ((int64_t)at.b * a.cache.heads + at.h) * a.ld_slots;
+    for (; slot0 < end; slot0 += WARPS * STAGE) {
+      // the weights that are added to: lane l has that of key l of the stage
+      const float old = a.weights && slot0 + lane < length - n ? a.weights[row + slot0 + lane] : 0.f;
+      if (!stages.wait()) continue;
+      const uint8_t* stage = stages.stage();
+      const int valid = s_list[warp].valid[stages.place()];
+      float2 got[2][2] = {};
+      float ks[2][2], ko[2][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t p = *reinterpret_cast<const uint32_t*>(stage + u * Stages::GROUP_BYTES + GROUP * (DIM / 2) + key_of(g + 8 * e) * 4);
+          ks[u][e] = scale_of(p);
+          ko[u][e] = offset_of(p);
+        }
+      auto add = [&](const Rows<DIM>& r) {
+        if (r.most <= slot0) return;
+        float2 s[2][1][2];
+        key_products<DIM, 1, 2, Stages::GROUP_BYTES>(s, stage, [&](int, int w) { return r.b[w][lane]; }, lane);
+        const bool masked = slot0 + STAGE > r.least;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) r.add(got[u][e], s[u][0][e], ks[u][e], ko[u][e], slot0 + u * GROUP + key_of(g + 8 * e), masked, c);
+      };
+      for (int i = 0; i < min(F::TILES, (rows + 7) / 8); ++i) add(s_rows[page][i]);
+      for (int r0 = 8 * F::TILES; r0 < rows; r0 += 8) {                 // a sequence with more rows than most have
+        Queries<T, DIM> q;
+        q.load(a.q, at.s.first, rows, r0, at.h, a.group, a.scale * LOG2E, lane);
+        float2 s[2][1][2];
+        key_products<DIM, 1, 2, Stages::GROUP_BYTES>(s, stage, [&](int, int w) { return q.b[w]; }, lane);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = r0 + 2 * c + j, t = r / a.group, sees = r < rows ? length - n + t + 1 : 0;
+          const float lse = r < rows ? a.lse[(at.s.first + t) * a.q.heads + at.h * a.group + r - t * a.group] * LOG2E : 0.f;
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float x = (j ? s[u][0][e].y : s[u][0][e].x) * (ks[u][e] * (j ? q.by.y : q.by.x)) + (ko[u][e] * (j ? q.sum.y : q.sum.x) - lse);
+              if (slot0 + u * GROUP + key_of(g + 8 * e) < sees) got[u][e].x += exp2_of(x);
+            }
+        }
+      }
+      // from the lanes of the keys' rows to a lane a key
+      float mine = 0.f;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float w = over_columns(got[u][e]);
+          // key_of(r) for r = 8 e + g: c' = r / 2 % 4 for even r, (c' ^ 1) + 4 for odd ones
+          const int key = lane & 15, low = key & 7, from = low < 4 ? 2 * low : 2 * ((low - 4) ^ 1) + 1;
+          const float v = __shfl_sync(0xffffffffu, w, from * 4);
+          if ((lane >> 4) == u && ((key >> 3) & 1) == e) mine = (valid >> u & 1) ? v : 0.f;
+        }
+      if (slot0 + lane < length) a.weights_out[row + slot0 + lane] = old + mine;
+      const int place = stages.place();
+      ++stages.turn;
+      __syncwarp();
+      stages.fetch(place);
+    }
+    if (at.begin + at.s.stages >= share.hi) break;
+    slot0 -= at.s.stages * STAGE;
+    at.next(a);
+    bring(at, page ^ 1);
+    page ^= 1;
+    __syncthreads();
+  }
+  stages.end();
+}
+
+// Many rows: bound by the exponentials (16 a cycle and SM) and the instructions of the product.  A warp holds 32 keys as fragments (D =
+// 256: 16) and goes over the rows, 128 at a time from shared memory; SETS warps share the same keys and take the tiles of rows in turn,
+// more of them where the keys are too few for all SMs.
+template <int DIM>
+struct ManyWeights {
+  static constexpr int WARPS = DIM == 64 ? 16 : 12, N = DIM == 256 ? 1 : 2, WORDS = DIM / 32;
+  static constexpr int KEYS = WARPS * N * GROUP;                       // of a CTA whose warps all have keys of their own
+  static constexpr int TILES = 16;                                     // of 8 rows, in shared memory at once
+  static constexpr int SMEM = 2 * TILES * (int)sizeof(Rows<DIM>);
+};
+template <typename T, int DIM>
+__global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_kernel(const AttentionArgs a) {
+  using W = ManyWeights<DIM>;
+  constexpr int WARPS = W::WARPS, N = W::N, WORDS = W::WORDS, AT_ONCE = W::TILES * 8;
+  extern __shared__ __align__(128) uint8_t smem[];
+  Rows<DIM>* const rows_at = reinterpret_cast<Rows<DIM>*>(smem);       // [2][TILES]
+  __shared__ Share s_share;
+  __shared__ int64_t s_sums[WARPS];
+  __shared__ float s_got[WARPS][N][2][8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+  mx::wait_for_previous();
+  mx::allow_next();
+  auto share_of = [&](int keys) {
+    find_share(&s_share, a.batch.n_seqs, 1, s_sums, [&](int b) { return (int64_t)a.cache.heads * ((a.cache.length(b) + keys - 1) / keys); });
+    return s_share;
+  };
+  int sets = 1;
+  Share share = share_of(W::KEYS);
+  while (sets < 4 && share.total * sets < 4 * (int64_t)gridDim.x) sets *= 2;
+  if (sets > 1) {
+    __syncthreads();
+    share = share_of(W::KEYS / sets);
+  }
+  if (share.lo >= share.hi) return;
+  const int keys = W::KEYS / sets, set = warp % sets;
+  int seq = share.seq, n = 0, length = 0, tiles = 0;
+  int64_t first = 0;
+  auto describe = [&]() {
+    length = a.cache.length(seq);
+    tiles = (length + keys - 1) / keys;
+    a.batch.range(seq, first, n);
+  };
+  describe();
+  int h = (int)((share.lo - share.before) / tiles), tile = (int)((share.lo - share.before) % tiles);
+
+  for (int64_t unit = share.lo; unit < share.hi; ++unit) {
+    const int rows = n * a.group, base = tile * keys, slot0 = base + (warp / sets) * N * GROUP;
+    // this warp's keys, as fragments
+    uint32_t k[N][WORDS][2][4];
+    float ks[N][2], ko[N][2];
+    bool there[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int slot = slot0 + u * GROUP;
+      const int64_t page = slot < length ? a.cache.page_of(seq, slot) : -1;
+      there[u] = page >= 0;
+      uint32_t x[2][WORDS], p[2] = {0u, 0u};
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) x[e][w] = 0u;
+      if (there[u]) {
+        const uint8_t* group = a.cache.group_at(page, h, slot, DIM);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          load_words<WORDS>(x[e], group + key_of(g + 8 * e) * (DIM / 2) + c * (DIM / 8));
+          p[e] = *reinterpret_cast<const uint32_t*>(group + GROUP * (DIM / 2) + key_of(g + 8 * e) * 4);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        ks[u][e] = scale_of(p[e]);
+        ko[u][e] = offset_of(p[e]);
+      }
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          k[u][w][e][0] = low_codes(x[0][w] >> (8 * e)); k[u][w][e][1] = low_codes(x[1][w] >> (8 * e));
+          k[u][w][e][2] = high_codes(x[0][w] >> (8 * e)); k[u][w][e][3] = high_codes(x[1][w] >> (8 * e));
+        }
+    }
+    float2 got[N][2];
+#pragma unroll
+    for (int u = 0; u < N; ++u) got[u][0] = got[u][1] = both(0.f);
+    auto bring = [&](int row0, int into) {                              // rows row0 .. row0 + 127
+      for (int i = warp; i < W::TILES && row0 + i * 8 < rows; i += WARPS)
+        rows_at[into * W::TILES + i].template bring<T>(a, first, n, length, h, row0 + i * 8, lane);
+    };
+    // rows before the first one that sees these keys see nothing of them
+    const int row_first = (int)(max((int64_t)0, (int64_t)base - (length - n)) * a.group / AT_ONCE * AT_ONCE);
+    int page = 0;
+    __syncthreads();
+    bring(row_first, 0);
+    __syncthreads();
+    for (int row0 = row_first; row0 < rows; row0 += AT_ONCE, page ^= 1) {
+      if (row0 + AT_ONCE < rows) bring(row0 + AT_ONCE, page ^ 1);
+      const int count = min(W::TILES, (rows - row0 + 7) / 8);
+      for (int i = set; i < count; i += sets) {
+        const Rows<DIM>& q = rows_at[page * W::TILES + i];
+        if (q.most <= slot0) continue;
+        float d[N][2][4];
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+          const uint4 b = q.b[w][lane];
+#pragma unroll
+          for (int u = 0; u < N; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t* x = k[u][w][e];
+              if (w == 0) mma_first(d[u][e], x[0], x[1], x[2], x[3], e ? b.z : b.x, e ? b.w : b.y);
+              else mma(d[u][e], x[0], x[1], x[2], x[3], e ? b.z : b.x, e ? b.w : b.y);
+            }
+        }
+        const bool masked = slot0 + N * GROUP > q.least;
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            q.add(got[u][e], add2(make_float2(d[u][0][2 * e], d[u][0][2 * e + 1]), make_float2(d[u][1][2 * e], d[u][1][2 * e + 1])), ks[u][e],
+                  ko[u][e], slot0 + u * GROUP + key_of(g + 8 * e), masked, c);
+      }
+      if (row0 + AT_ONCE < rows) __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float w = over_columns(got[u][e]);
+        if (c == 0) s_got[warp][u][e][g] = there[u] ? w : 0.f;
+      }
+    __syncthreads();
+    if (set == 0 && c == 0)
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int slot = slot0 + u * GROUP + key_of(g + 8 * e);
+          if (slot < length) {
+            const int64_t at = ((int64_t)seq * a.cache.heads + h) * a.ld_slots + slot;
+            float w = a.weights && slot < length - n ? a.weights[at] : 0.f;
+            for (int i = 0; i < sets; ++i) w += s_got[warp + i][u][e][g];
+            a.weights_out[at] = w;
+          }
+        }
+    if (++tile == tiles) {
+      tile = 0;
+      if (++h == a.cache.heads) {
+        h = 0;
+        do {
+          if (++seq == a.batch.n_seqs) return;
+          describe();
+        } while (tiles == 0);
+      }
+    }
+  }
 }
 
 }  // namespace
@@ -798,11 +1078,26 @@ dq_status attention(cudaStream_t stream, const mx::Device& dev, int dtype, int d
 }
 
 dq_status attention_weights(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AttentionArgs& a) {
-  const int64_t most = (int64_t)a.cache.n_seqs * a.cache.heads * ((((int64_t)a.cache.width << a.cache.shift) + W_TILE - 1) / W_TILE);
-  mx::LaunchConfig c(stream, min((int64_t)dev.sms * 4, max((int64_t)1, most)), W_WARPS * 32);
+  // up to two tiles of rows a sequence: the keys' way from HBM is what takes time
+  const bool few = a.batch.tokens * a.group <= (int64_t)16 * a.cache.n_seqs;
+  const int64_t slots = (int64_t)a.cache.width << a.cache.shift, rows = (int64_t)a.cache.n_seqs * a.cache.heads;
   auto run = [&](auto t) {
     using T = decltype(t);
-    return by_dim(dim, [&](auto d) { return mx::launch(c, weights_kernel<T, decltype(d)::value>, a); });
+    return by_dim(dim, [&](auto d) {
+      constexpr int DIM = decltype(d)::value;
+      static SmemOptIn opted_few, opted_many;
+      if (few) {
+        using F = FewWeights<DIM>;
+        DQ_CHECK(opt_in_dynamic_smem(few_weights_kernel<T, DIM>, F::SMEM, opted_few));
+        const int64_t most = (rows * ((slots + STAGE - 1) / STAGE) + LEAST_STAGES - 1) / LEAST_STAGES;
+        mx::LaunchConfig c(stream, min((int64_t)dev.sms * F::PER_SM, max((int64_t)1, most)), F::WARPS * 32, F::SMEM);
+        return mx::launch(c, few_weights_kernel<T, DIM>, a);
+      }
+      using W = ManyWeights<DIM>;
+      DQ_CHECK(opt_in_dynamic_smem(many_weights_kernel<T, DIM>, W::SMEM, opted_many));
+      mx::LaunchConfig c(stream, min((int64_t)dev.sms, max((int64_t)1, rows * ((slots * 4 + W::KEYS - 1) / W::KEYS))), W::WARPS * 32, W::SMEM);
+      return mx::launch(c, many_weights_kernel<T, DIM>, a);
+    });
   };
   return dtype == DQ_BF16 ? run(__nv_bfloat16()) : run(__half());
 }
