@@ -416,7 +416,7 @@ dq_status dq_mx_selftest_bounded_wait(int32_t a_fmt, const void* d_a_codes, cons
  * d_table [n_seqs][table_width]: the pages of a sequence, in order; an index outside [0, n_pages) is no page: what would be
  * written there is dropped, and keys there take no part.  Pages may be shared between sequences as long as no call writes to
  * one from two.  d_lengths [n_seqs]: tokens (slots) of a sequence, those of the call included; taken as 0 where negative and as
- * table_width * page_size where above.  Both are read on the device when the call runs.
+ * table_width * page_size (at most 2^30) where above.  Both are read on the device when the call runs.
  * Tokens of a call: sequence b has rows d_starts[b] .. d_starts[b + 1] - 1 of the call's tensors (d_starts [n_seqs + 1], not
  * decreasing), or tokens / n_seqs each where d_starts is NULL.  They are its last: token i of n has slot length - n + i, and
  * sees the slots up to its own.  Rows that belong to no sequence are left as they are.

@@ -5,7 +5,7 @@
 using namespace dq;
 
 namespace {
-constexpr int64_t MAX_TOKENS = ((int64_t)1 << 31) - 256, MAX_STRIDE = (int64_t)1 << 40;
+constexpr int64_t MAX_TOKENS = ((int64_t)1 << 31) - 256, MAX_STRIDE = (int64_t)1 << 40, MAX_SLOTS = (int64_t)1 << 30;
 inline bool is_float(int t) { return t == DQ_FP32 || t == DQ_BF16 || t == DQ_FP16; }
 inline bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
@@ -31,7 +31,7 @@ dq_status cache_of(const dq_kv_cache_t* c, kv::Cache& out) {
   int shift;
   if (!c || c->n_seqs < 0 || c->heads <= 0 || c->heads > 65536 || c->table_width <= 0 || c->n_pages < 0) return DQ_ERR_INVALID_ARG;
   if (!cache_dim(c->head_dim) || !log2_of(c->page_size, shift)) return DQ_ERR_UNSUPPORTED;
-  if ((int64_t)c->table_width << shift > MAX_TOKENS || (int64_t)c->n_seqs * c->heads > MAX_TOKENS) return DQ_ERR_UNSUPPORTED;
+  if ((int64_t)c->table_width << shift > MAX_SLOTS || (int64_t)c->n_seqs * c->heads > MAX_TOKENS) return DQ_ERR_UNSUPPORTED;
   if (c->n_pages > MAX_TOKENS) return DQ_ERR_UNSUPPORTED;
   if (c->n_seqs > 0 && (!c->d_table || !c->d_lengths || (c->n_pages > 0 && !c->d_pages))) return DQ_ERR_INVALID_ARG;
   if (!aligned(c->d_table, 4) || !aligned(c->d_lengths, 4)) return DQ_ERR_INVALID_ARG;
@@ -65,6 +65,7 @@ dq_status attended(const dq_heads_t* Q, int dtype, int64_t tokens, const dq_kv_c
   DQ_CHECK(heads(Q, dtype, tokens, cache->head_dim, a.q));
   if (a.q.heads % cache->heads || !(scale > -INFINITY && scale < INFINITY)) return DQ_ERR_INVALID_ARG;
   a.group = a.q.heads / cache->heads;
+  a.group_shift = a.group & (a.group - 1) ? -1 : __builtin_ctz((unsigned)a.group);
   if (tokens * a.group > MAX_TOKENS) return DQ_ERR_UNSUPPORTED;
   a.scale = scale;
   return DQ_OK;

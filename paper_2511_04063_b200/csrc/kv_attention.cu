@@ -82,7 +82,7 @@ __device__ __forceinline__ int key_of(int r) { const int c = (r & 7) >> 1; retur
 
 // Eight values of a row, zeros where there is none.
 template <typename T>
-__device__ __forceinline__ void load_values(float (&v)[8], const T* p, bool there, bool vec) {
+__device__ __forceinline__ void load_values(float2 (&v)[4], const T* p, bool there, bool vec) {
   mx::Vec8<T> x;
   x.clear();
   if (there) {
@@ -92,35 +92,35 @@ __device__ __forceinline__ void load_values(float (&v)[8], const T* p, bool ther
       for (int i = 0; i < 4; ++i) x.set_pair(i, make_float2(mx::to_f32(p[2 * i]), mx::to_f32(p[2 * i + 1])));
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = x.pair(i);
-    v[2 * i] = f.x; v[2 * i + 1] = f.y;
-  }
+  for (int i = 0; i < 4; ++i) v[i] = x.pair(i);
 }
 
 // Eight query rows from row0 on (row r: token r / group, head r % group) as B fragments.  Dimensions whose codes lie four bits up
 // are held 2^-4 smaller.  For the columns 2 c and 2 c + 1: `by`, what takes the powers of two out of a product, and the sum of the
-// row, both times `factor`.
+// row, both times scale log2 e.
 template <typename T, int DIM>
 struct Queries {
   static constexpr int WORDS = DIM / 32;
   uint4 b[WORDS];
   float2 by, sum;
-  __device__ __forceinline__ void load(const Heads& q, int64_t first, int rows, int row0, int h, int group, float factor, int lane) {
+  __device__ __forceinline__ void load(const AttentionArgs& a, int64_t first, int rows, int row0, int h, int lane) {
     const int c = lane & 3, r = row0 + (lane >> 2);
     const bool there = r < rows;
-    const int i = there ? r / group : 0;
-    const T* p = reinterpret_cast<const T*>(q.p) + (first + i) * q.token + (int64_t)(h * group + (there ? r - i * group : 0)) * q.head;
-    float v[WORDS][8], s = 0.f, most = 0.f;
+    const int i = there ? a.token_of(r) : 0;
+    const T* p = reinterpret_cast<const T*>(a.q.p) + (first + i) * a.q.token + (int64_t)(h * a.group + (there ? r - i * a.group : 0)) * a.q.head;
+    const float factor = a.scale * LOG2E;
+    float2 v[WORDS][4], sums = both(0.f);
+    float most = 0.f;
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
-      load_values<T>(v[w], p + (c * WORDS + w) * 8, there, q.vec);
+      load_values<T>(v[w], p + (c * WORDS + w) * 8, there, a.q.vec);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        s += v[w][e];
-        most = fmaxf(most, fabsf(v[w][e]));
+      for (int e = 0; e < 4; ++e) {
+        sums = add2(sums, v[w][e]);
+        most = fmaxf(most, fmaxf(fabsf(v[w][e].x), fabsf(v[w][e].y)));
       }
     }
+    float s = sums.x + sums.y;
     s += __shfl_xor_sync(0xffffffffu, s, 1);
     s += __shfl_xor_sync(0xffffffffu, s, 2);
     most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
@@ -128,10 +128,12 @@ struct Queries {
     // the largest value's exponent field, within what keeps both factors normal numbers; a row that is not finite stays so
     const int field = min(max((int)mx::exponent_field(most), 14), 244);
     const float up = __uint_as_float((uint32_t)(268 - field) << 23), up4 = up * 0.0625f;
+    const float2 ups = make_float2(up, up4);
 #pragma unroll
-    for (int w = 0; w < WORDS; ++w)
-      b[w] = make_uint4(half_pair(v[w][0] * up, v[w][4] * up), half_pair(v[w][1] * up4, v[w][5] * up4),
-                        half_pair(v[w][2] * up, v[w][6] * up), half_pair(v[w][3] * up4, v[w][7] * up4));
+    for (int w = 0; w < WORDS; ++w) {
+      const float2 d01 = mul2(v[w][0], ups), d23 = mul2(v[w][1], ups), d45 = mul2(v[w][2], ups), d67 = mul2(v[w][3], ups);
+      b[w] = make_uint4(half_pair(d01.x, d45.x), half_pair(d01.y, d45.y), half_pair(d23.x, d67.x), half_pair(d23.y, d67.y));
+    }
     const float down = __uint_as_float((uint32_t)(field + 10) << 23);   // 2^24 / up
     sum = make_float2(__shfl_sync(0xffffffffu, s, c * 8) * factor, __shfl_sync(0xffffffffu, s, c * 8 + 4) * factor);
     by = make_float2(__shfl_sync(0xffffffffu, down, c * 8) * factor, __shfl_sync(0xffffffffu, down, c * 8 + 4) * factor);
@@ -395,7 +397,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
   auto load_queries = [&](const Walk<ROWS>& w, int into) {              // by the first NT warps
     if (warp >= NT) return;
     Queries<T, DIM> q;
-    q.load(a.q, w.s.first, w.s.n * a.group, w.tile * ROWS + warp * 8, w.h, a.group, a.scale * LOG2E, lane);
+    q.load(a, w.s.first, w.s.n * a.group, w.tile * ROWS + warp * 8, w.h, lane);
 #pragma unroll
     for (int i = 0; i < DIM / 32; ++i) s_query[into][warp][i][lane] = q.b[i];
     if (g == 0) {
@@ -420,11 +422,11 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
         top[nt][j] = -INFINITY;
         sum[nt] = off[nt] = both(0.f);
         const int r = row0 + nt * 8 + 2 * c + j;
-        sees[nt][j] = r < rows ? max(length - at.s.n + r / a.group + 1, 0) : 0;
+        sees[nt][j] = r < rows ? max(length - at.s.n + a.token_of(r) + 1, 0) : 0;
       }
     // all valid rows see the stages before the first row's end, none those past the last one's
-    const int least = max(length - at.s.n + row0 / a.group + 1, 0);
-    const int most = max(length - at.s.n + (min(row0 + ROWS, rows) - 1) / a.group + 1, 0);
+    const int least = max(length - at.s.n + a.token_of(row0) + 1, 0);
+    const int most = max(length - at.s.n + a.token_of(min(row0 + ROWS, rows) - 1) + 1, 0);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -614,7 +616,7 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
     auto write = [&](int r, int d, float4 v, float m, float l) {         // row r of the tile, dimensions d .. d + 3
       const int row = row0 + r;
       if (row >= rows) return;
-      const int i = row / a.group, head = h * a.group + row - i * a.group;
+      const int i = a.token_of(row), head = h * a.group + row - i * a.group;
       const float by = l == 0.f ? 0.f : 1.f / l;
       T* p = reinterpret_cast<T*>(a.out.p) + (first + i) * a.out.token + head * a.out.head + d;
       T y[4] = {mx::from_f32<T>(v.x * by), mx::from_f32<T>(v.y * by), mx::from_f32<T>(v.z * by), mx::from_f32<T>(v.w * by)};
@@ -749,7 +751,7 @@ struct Rows {
   __device__ __forceinline__ void bring(const AttentionArgs& a, int64_t first, int n, int length, int h, int r0, int lane) {
     const int rows = n * a.group, c = lane & 3;
     Queries<T, DIM> q;
-    q.load(a.q, first, rows, r0, h, a.group, a.scale * LOG2E, lane);
+    q.load(a, first, rows, r0, h, lane);
 #pragma unroll
     for (int w = 0; w < DIM / 32; ++w) b[w][lane] = q.b[w];
     if (lane < 4) {
@@ -757,7 +759,7 @@ struct Rows {
       int slots[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int r = r0 + 2 * c + j, t = r / a.group;
+        const int r = r0 + 2 * c + j, t = a.token_of(r);
         lse[j] = r < rows ? a.lse[(first + t) * a.q.heads + h * a.group + r - t * a.group] * -LOG2E : -INFINITY;
         slots[j] = r < rows ? length - n + t + 1 : 0;
       }
@@ -767,13 +769,13 @@ struct Rows {
       sees[c] = make_int2(slots[0], slots[1]);
       if (c == 0) {
         least = slots[0];
-        most = r0 < rows ? length - n + (min(r0 + 8, rows) - 1) / a.group + 1 : 0;
+        most = r0 < rows ? length - n + a.token_of(min(r0 + 8, rows) - 1) + 1 : 0;
       }
     }
   }
   // The probabilities of products s of a key (parameters ks, ko), added to got.
-  __device__ __forceinline__ void add(float2& got, float2 s, float ks, float ko, int slot, bool masked, int c) const {
-    const float2 x = fma2(s, mul2(both(ks), by[c]), fma2(both(ko), sum[c], minus_lse[c]));
+  __device__ __forceinline__ void add(float2& got, float2 s, float2 ks, float2 ko, int slot, bool masked, int c) const {
+    const float2 x = fma2(s, mul2(ks, by[c]), fma2(ko, sum[c], minus_lse[c]));
     float2 p = make_float2(exp2_of(x.x), exp2_of(x.y));
     if (masked) {
       if (slot >= sees[c].x) p.x = 0.f;
@@ -855,17 +857,17 @@ __global__ void __launch_bounds__(FewWeights<DIM>::WARPS * 32, FewWeights<DIM>::
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) r.add(got[u][e], s[u][0][e], ks[u][e], ko[u][e], slot0 + u * GROUP + key_of(g + 8 * e), masked, c);
+          for (int e = 0; e < 2; ++e) r.add(got[u][e], s[u][0][e], both(ks[u][e]), both(ko[u][e]), slot0 + u * GROUP + key_of(g + 8 * e), masked, c);
       };
       for (int i = 0; i < min(F::TILES, (rows + 7) / 8); ++i) add(s_rows[page][i]);
       for (int r0 = 8 * F::TILES; r0 < rows; r0 += 8) {                 // a sequence with more rows than most have
         Queries<T, DIM> q;
-        q.load(a.q, at.s.first, rows, r0, at.h, a.group, a.scale * LOG2E, lane);
+        q.load(a, at.s.first, rows, r0, at.h, lane);
         float2 s[2][1][2];
         key_products<DIM, 1, 2, Stages::GROUP_BYTES>(s, stage, [&](int, int w) { return q.b[w]; }, lane);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int r = r0 + 2 * c + j, t = r / a.group, sees = r < rows ? length - n + t + 1 : 0;
+          const int r = r0 + 2 * c + j, t = a.token_of(r), sees = r < rows ? length - n + t + 1 : 0;
           const float lse = r < rows ? a.lse[(at.s.first + t) * a.q.heads + at.h * a.group + r - t * a.group] * LOG2E : 0.f;
 #pragma unroll
           for (int u = 0; u < 2; ++u)
@@ -905,8 +907,9 @@ __global__ void __launch_bounds__(FewWeights<DIM>::WARPS * 32, FewWeights<DIM>::
 }
 
 // Many rows: bound by the exponentials (16 a cycle and SM) and the instructions of the product.  A warp holds 32 keys as fragments (D =
-// 256: 16) and goes over the rows, 128 at a time from shared memory; SETS warps share the same keys and take the tiles of rows in turn,
-// more of them where the keys are too few for all SMs.
+// 256: 16) and goes over the rows, 128 at a time from shared memory.  Bringing rows in costs a warp several times what a tile of them
+// does afterwards, so the warps of a CTA hold different keys; the CTAs of a cluster hold the same and take blocks of 128 rows in turn.
+// Where that leaves too few units for all SMs, `sets` warps of a CTA share keys too, and take a block's tiles in turn.
 template <int DIM>
 struct ManyWeights {
   static constexpr int WARPS = DIM == 64 ? 16 : 12, N = DIM == 256 ? 1 : 2, WORDS = DIM / 32;
@@ -914,8 +917,18 @@ struct ManyWeights {
   static constexpr int TILES = 16;                                     // of 8 rows, in shared memory at once
   static constexpr int SMEM = 2 * TILES * (int)sizeof(Rows<DIM>);
 };
+__device__ __forceinline__ float load_of_rank(const float* p, int rank) {
+  uint32_t at;
+  float v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 template <typename T, int DIM>
-__global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_kernel(const AttentionArgs a) {
+__global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_kernel(const AttentionArgs a, int cluster) {
   using W = ManyWeights<DIM>;
   constexpr int WARPS = W::WARPS, N = W::N, WORDS = W::WORDS, AT_ONCE = W::TILES * 8;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -932,28 +945,33 @@ __global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_
   };
   int sets = 1;
   Share share = share_of(W::KEYS);
-  while (sets < 4 && share.total * sets < 4 * (int64_t)gridDim.x) sets *= 2;
+  const int clusters = gridDim.x / cluster, rank = blockIdx.x % cluster;
+  while (sets < 4 && share.total * sets < clusters) sets *= 2;
   if (sets > 1) {
     __syncthreads();
     share = share_of(W::KEYS / sets);
   }
-  if (share.lo >= share.hi) return;
+  // the clusters take the units in turn: neighbours cost about the same, the sequences do not
   const int keys = W::KEYS / sets, set = warp % sets;
-  int seq = share.seq, n = 0, length = 0, tiles = 0;
-  int64_t first = 0;
+  int seq = 0, n = 0, length = 0, tiles = 0;
+  int64_t first = 0, before = 0;
   auto describe = [&]() {
     length = a.cache.length(seq);
     tiles = (length + keys - 1) / keys;
     a.batch.range(seq, first, n);
   };
   describe();
-  int h = (int)((share.lo - share.before) / tiles), tile = (int)((share.lo - share.before) % tiles);
-
-  for (int64_t unit = share.lo; unit < share.hi; ++unit) {
+  for (int64_t unit = blockIdx.x / cluster; unit < share.total; unit += clusters) {
+    while (unit >= before + (int64_t)tiles * a.cache.heads) {
+      before += (int64_t)tiles * a.cache.heads;
+      ++seq;
+      describe();
+    }
+    const int h = (int)((unit - before) / tiles), tile = (int)((unit - before) - (int64_t)h * tiles);
     const int rows = n * a.group, base = tile * keys, slot0 = base + (warp / sets) * N * GROUP;
     // this warp's keys, as fragments
     uint32_t k[N][WORDS][2][4];
-    float ks[N][2], ko[N][2];
+    float2 ks[N][2], ko[N][2];
     bool there[N];
 #pragma unroll
     for (int u = 0; u < N; ++u) {
@@ -975,8 +993,8 @@ __global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        ks[u][e] = scale_of(p[e]);
-        ko[u][e] = offset_of(p[e]);
+        ks[u][e] = both(scale_of(p[e]));
+        ko[u][e] = both(offset_of(p[e]));
       }
 #pragma unroll
       for (int w = 0; w < WORDS; ++w)
@@ -994,13 +1012,13 @@ __global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_
         rows_at[into * W::TILES + i].template bring<T>(a, first, n, length, h, row0 + i * 8, lane);
     };
     // rows before the first one that sees these keys see nothing of them
-    const int row_first = (int)(max((int64_t)0, (int64_t)base - (length - n)) * a.group / AT_ONCE * AT_ONCE);
+    const int row_first = (int)(max((int64_t)0, (int64_t)base - (length - n)) * a.group / AT_ONCE + rank) * AT_ONCE, step = cluster * AT_ONCE;
     int page = 0;
     __syncthreads();
     bring(row_first, 0);
     __syncthreads();
-    for (int row0 = row_first; row0 < rows; row0 += AT_ONCE, page ^= 1) {
-      if (row0 + AT_ONCE < rows) bring(row0 + AT_ONCE, page ^ 1);
+    for (int row0 = row_first; row0 < rows; row0 += step, page ^= 1) {
+      if (row0 + step < rows) bring(row0 + step, page ^ 1);
       const int count = min(W::TILES, (rows - row0 + 7) / 8);
       for (int i = set; i < count; i += sets) {
         const Rows<DIM>& q = rows_at[page * W::TILES + i];
@@ -1026,7 +1044,7 @@ __global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_
             q.add(got[u][e], add2(make_float2(d[u][0][2 * e], d[u][0][2 * e + 1]), make_float2(d[u][1][2 * e], d[u][1][2 * e + 1])), ks[u][e],
                   ko[u][e], slot0 + u * GROUP + key_of(g + 8 * e), masked, c);
       }
-      if (row0 + AT_ONCE < rows) __syncthreads();
+      if (row0 + step < rows) __syncthreads();
     }
 #pragma unroll
     for (int u = 0; u < N; ++u)
@@ -1035,8 +1053,9 @@ __global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_
         const float w = over_columns(got[u][e]);
         if (c == 0) s_got[warp][u][e][g] = there[u] ? w : 0.f;
       }
-    __syncthreads();
-    if (set == 0 && c == 0)
+    if (cluster > 1) cluster_sync();
+    else __syncthreads();
+    if (set == 0 && rank == 0 && c == 0)
 #pragma unroll
       for (int u = 0; u < N; ++u)
 #pragma unroll
@@ -1045,20 +1064,12 @@ __global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_
           if (slot < length) {
             const int64_t at = ((int64_t)seq * a.cache.heads + h) * a.ld_slots + slot;
             float w = a.weights && slot < length - n ? a.weights[at] : 0.f;
-            for (int i = 0; i < sets; ++i) w += s_got[warp + i][u][e][g];
+            for (int i = 0; i < sets; ++i)
+              for (int r = 0; r < cluster; ++r) w += cluster > 1 ? load_of_rank(&s_got[warp + i][u][e][g], r) : s_got[warp + i][u][e][g];
             a.weights_out[at] = w;
           }
         }
-    if (++tile == tiles) {
-      tile = 0;
-      if (++h == a.cache.heads) {
-        h = 0;
-        do {
-          if (++seq == a.batch.n_seqs) return;
-          describe();
-        } while (tiles == 0);
-      }
-    }
+    if (cluster > 1) cluster_sync();                                    // the others' sums have been read
   }
 }
 
@@ -1095,8 +1106,24 @@ dq_status attention_weights(cudaStream_t stream, const mx::Device& dev, int dtyp
       }
       using W = ManyWeights<DIM>;
       DQ_CHECK(opt_in_dynamic_smem(many_weights_kernel<T, DIM>, W::SMEM, opted_many));
-      mx::LaunchConfig c(stream, min((int64_t)dev.sms, max((int64_t)1, rows * ((slots * 4 + W::KEYS - 1) / W::KEYS))), W::WARPS * 32, W::SMEM);
-      return mx::launch(c, many_weights_kernel<T, DIM>, a);
+      // CTAs of a cluster: two blocks of rows or more for each
+      const int64_t each = a.batch.tokens * a.group / a.cache.n_seqs;
+      const int cluster = each >= 8 * W::TILES * 8 ? 4 : each >= 4 * W::TILES * 8 ? 2 : 1;
+      const int64_t units = max((int64_t)1, rows * ((slots * 4 + W::KEYS - 1) / W::KEYS));
+      // no more clusters than run at once: they find their SMs together, 33 or so of four and not 37
+      struct Clusters { int most[5]; };
+      static PerDevice<Clusters> known;
+      Clusters clusters;
+      DQ_CHECK((dq_status)known.get(dev.index, clusters, [&](Clusters& out) -> int {
+        out.most[1] = dev.sms;
+        for (int s = 2; s <= 4; s *= 2) {
+          mx::LaunchConfig config(nullptr, s, W::WARPS * 32, W::SMEM, s);
+          DQ_CHECK_CUDA(cudaOccupancyMaxActiveClusters(&out.most[s], many_weights_kernel<T, DIM>, &config.cfg));
+        }
+        return DQ_OK;
+      }));
+      mx::LaunchConfig c(stream, min((int64_t)max(clusters.most[cluster], 1), units) * cluster, W::WARPS * 32, W::SMEM, cluster);
+      return mx::launch(c, many_weights_kernel<T, DIM>, a, cluster);
     });
   };
   return dtype == DQ_BF16 ? run(__nv_bfloat16()) : run(__half());

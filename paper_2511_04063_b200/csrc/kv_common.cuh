@@ -186,8 +186,10 @@ struct AttentionArgs {
   const float* weights;    // [n_seqs][kv heads][ld_slots]
   float* weights_out;
   int64_t ld_slots;
-  int group;               // query heads of a kv head
+  int group, group_shift;  // query heads of a kv head; their logarithm, -1 if they are no power of two
   int* d_status;
+  // the token of a kv head's query row: rows are (token, head of the group)
+  __device__ __forceinline__ int token_of(int row) const { return group_shift >= 0 ? row >> group_shift : row / group; }
 };
 int64_t attention_workspace(int dim);
 dq_status attention(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AttentionArgs& a);
