@@ -25,7 +25,6 @@ namespace dq {
 namespace kv {
 namespace {
 
-constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
 constexpr int STAGE = 2 * GROUP;   // keys of a pipeline stage: the maximum of a row is looked at once for 32 keys
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -41,29 +40,10 @@ __device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
                : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-// Two codes as fp16 numbers, c 2^-24: bits 0-3 and 16-19; c 2^-20: bits 4-7 and 20-23.
-__device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000fu; }
-__device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
-// The same less 8.
-__device__ __forceinline__ uint32_t less(uint32_t w, uint32_t eight) {
-  const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&w), *reinterpret_cast<const __half2*>(&eight));
-  return *reinterpret_cast<const uint32_t*>(&d);
-}
-__device__ __forceinline__ uint32_t low_centred(uint32_t w) { return less(low_codes(w), 0x00080008u); }
-__device__ __forceinline__ uint32_t high_centred(uint32_t w) { return less(high_codes(w), 0x00800080u); }
 __device__ __forceinline__ uint32_t transposed(uint32_t v) {
   uint32_t d;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
   return d;
-}
-__device__ __forceinline__ float exp2_of(float v) {
-  float d;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(v));
-  return d;
-}
-__device__ __forceinline__ uint32_t half_pair(float a, float b) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
 }
 template <int WORDS>
 __device__ __forceinline__ void load_words(uint32_t (&w)[WORDS], const uint8_t* p) {
@@ -339,8 +319,6 @@ struct Stream {
 // own maximum, sum and O^T, joined in shared memory at an item's end.  A warp brings its stages in by bulk copies into two places of
 // its own: while it works on one the other is on its way, across items too.  An item that crosses CTAs is left in the workspace in parts,
 // and the CTA that finishes last joins them, in order.
-constexpr int MAX_CTAS = 640;
-constexpr int TICKET_BYTES = MAX_CTAS * 4;
 template <int DIM, int NT>
 struct Few {
   static constexpr int ROWS = 8 * NT;
@@ -732,7 +710,7 @@ dq_status run_few(cudaStream_t stream, const mx::Device& dev, const AttentionArg
   const int64_t rows = a.batch.tokens * a.group, tiles = rows / F::ROWS + a.batch.n_seqs;
   const int64_t stages = max((int64_t)1, ((int64_t)a.cache.width << a.cache.shift) / STAGE);
   const int64_t most = (tiles * a.cache.heads * stages + LEAST_STAGES - 1) / LEAST_STAGES;
-  mx::LaunchConfig c(stream, min((int64_t)min(dev.sms, 148) * F::PER_SM, max((int64_t)1, most)), F::THREADS, F::SMEM);
+  mx::LaunchConfig c(stream, min((int64_t)min(dev.sms, MAX_SMS) * F::PER_SM, max((int64_t)1, most)), F::THREADS, F::SMEM);
   return mx::launch(c, few_kernel<T, DIM, NT>, a);
 }
 
@@ -1073,11 +1051,17 @@ __global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_
   }
 }
 
+#ifndef PROMPT_ROWS
+#define PROMPT_ROWS 64
+#endif
 }  // namespace
 
-int64_t attention_workspace(int dim) { return TICKET_BYTES + (int64_t)MAX_CTAS * 2 * 16 * (dim + 2) * 4; }
+int64_t attention_workspace(int dim) {
+  return TICKET_BYTES + max((int64_t)MAX_CTAS * 2 * 16 * (dim + 2), MAX_SMS * prompt_part(dim)) * 4;
+}
 
 dq_status attention(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AttentionArgs& a) {
+  if (a.batch.tokens * a.group >= (int64_t)PROMPT_ROWS * a.batch.n_seqs) return prompt_attention(stream, dev, dtype, dim, a);
   auto by_rows = [&](auto t) {
     using T = decltype(t);
     const bool two = a.batch.tokens * a.group > (int64_t)8 * a.batch.n_seqs;

@@ -90,6 +90,27 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
+constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
+__device__ __forceinline__ float exp2_of(float v) {
+  float d;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(v));
+  return d;
+}
+__device__ __forceinline__ uint32_t half_pair(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Two codes as fp16 numbers, c 2^-24: bits 0-3 and 16-19; c 2^-20: bits 4-7 and 20-23.
+__device__ __forceinline__ uint32_t low_codes(uint32_t w) { return w & 0x000f000fu; }
+__device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0x00f000f0u; }
+// The same less 8.
+__device__ __forceinline__ uint32_t less(uint32_t w, uint32_t eight) {
+  const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&w), *reinterpret_cast<const __half2*>(&eight));
+  return *reinterpret_cast<const uint32_t*>(&d);
+}
+__device__ __forceinline__ uint32_t low_centred(uint32_t w) { return less(low_codes(w), 0x00080008u); }
+__device__ __forceinline__ uint32_t high_centred(uint32_t w) { return less(high_codes(w), 0x00800080u); }
+
 // Called by a whole CTA of `threads` threads.  `least`: units that are worth a CTA.
 template <typename F>
 __device__ void find_share(Share* out, int n_seqs, int64_t least, int64_t* warp_sums, F cost) {
@@ -191,7 +212,12 @@ struct AttentionArgs {
   // the token of a kv head's query row: rows are (token, head of the group)
   __device__ __forceinline__ int token_of(int row) const { return group_shift >= 0 ? row >> group_shift : row / group; }
 };
+// dq_kv_attention's workspace: a counter for each CTA (zero between calls), then parts of items that several CTAs work on.
+constexpr int MAX_SMS = 160, MAX_CTAS = 2 * MAX_SMS, TICKET_BYTES = MAX_CTAS * 4;
+inline int64_t prompt_part(int dim) { return (int64_t)(dim == 256 ? 128 : 256) * (dim + 2); }   // floats of a part
 int64_t attention_workspace(int dim);
+// the same for many query rows a sequence
+dq_status prompt_attention(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AttentionArgs& a);
 dq_status attention(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AttentionArgs& a);
 dq_status attention_weights(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AttentionArgs& a);
 
