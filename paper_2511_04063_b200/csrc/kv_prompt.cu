@@ -26,7 +26,10 @@ struct Prompt {
   static constexpr int TILES = DIM == 256 ? 1 : 2;                     // of 128 rows
   static constexpr int STAGES = DIM == 64 ? 3 : DIM == 128 ? 2 : 1;    // of keys and values
   static constexpr int ROWS = TILES * 128;
-  static constexpr int UNPACK = 4 * TILES, ISSUE = UNPACK + 4, THREADS = 32 * (ISSUE + 1);   // first warps of the roles
+  static constexpr int UNPACK = 4 * TILES, ISSUE = UNPACK + 4, THREADS = 32 * (ISSUE + 4);   // first warps of the roles
+  // registers of a thread of each role's four warps; together no more than the launch's (65536 / THREADS each)
+  static constexpr int ROW_REGS = DIM == 256 ? 224 : 192, UNPACK_REGS = DIM == 256 ? 152 : 80, ISSUE_REGS = 48;
+  static_assert(TILES * ROW_REGS + UNPACK_REGS + ISSUE_REGS <= 65536 / THREADS / 8 * 8 * (TILES + 2), "");
   static constexpr int TILE_BYTES = 128 * DIM * 2, BOX = 128 * 128;    // a box: 128 rows of 64 values
   static constexpr int Q_AT = 0, K_AT = TILES * TILE_BYTES, V_AT = K_AT + STAGES * TILE_BYTES, END = V_AT + STAGES * TILE_BYTES;
   static constexpr int SMEM = END + 1024;
@@ -69,6 +72,9 @@ __device__ __forceinline__ void store16(uint32_t at, const uint4& v) {
 __device__ __forceinline__ uint32_t piece_at(uint32_t tile, int row, int w) {
   return tile + (uint32_t)((w >> 3) * Prompt<128>::BOX + row * 128 + (((w & 7) ^ (row & 7)) << 4));
 }
+
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 template <typename T, int DIM>
 __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const AttentionArgs a, int splits) {
@@ -138,61 +144,65 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
   const uint32_t tmem = s_tmem;
 
   bool ok = true;
-  if (warp == P::ISSUE) {   // ------------------------------------------------ products
-    auto wait = [&](uint32_t at, int phase) { return __all_sync(0xffffffffu, tc::mbar_wait(at, (uint32_t)phase & 1u, a.d_status)); };
-    constexpr uint32_t SCORES = idesc_f16(KEYS), VALUES = idesc_f16(DIM) | tc::IDESC_B_MN_MAJOR;
-    auto scores = [&](int m, int i) {
-      const uint64_t q = tc::make_kmajor_sw128_desc(smem + P::Q_AT + m * P::TILE_BYTES);
-      const uint64_t k = tc::make_kmajor_sw128_desc(smem + P::K_AT + (i % STAGES) * P::TILE_BYTES);
-      if (elect_one()) {
-#pragma unroll
-        for (int s = 0; s < DIM / 16; ++s) {
-          const uint32_t step = ((s >> 2) * P::BOX + (s & 3) * 32) >> 4;
-          mma_ss(tmem + m * 128, q + step, k + step, SCORES, s > 0);
-        }
-        tc::umma_commit(s_full(m));
-      }
-      __syncwarp();
-    };
-    auto commit = [&](uint32_t at) {
-      if (elect_one()) tc::umma_commit(at);
-      __syncwarp();
-    };
-    if (key_tiles > 0) ok = wait(q_full, 0) && wait(k_full(0), 0);
-    tc::tc_fence_after();
-    if (ok && key_tiles > 0) {
-      for (int m = 0; m < TILES; ++m) scores(m, 0);
-      commit(k_empty(0));
-    }
-    for (int i = 0; i < key_tiles && ok; ++i) {
-      const int s = i % STAGES, s1 = (i + 1) % STAGES;
-      const uint64_t v = tc::make_mnmajor_sw128_desc(smem + P::V_AT + s * P::TILE_BYTES, P::BOX);
-      ok = wait(v_full(s), i / STAGES);
-      for (int m = 0; m < TILES && ok; ++m) {
-        ok = wait(p_full(m), i);
-        if (!ok) break;
-        tc::tc_fence_after();
+  if (warp >= P::ISSUE) {   // ------------------------------------------------ products, by one warp
+    fewer_registers<P::ISSUE_REGS>();   // (all four warps of a role: registers move by fours)
+    if (warp == P::ISSUE) {
+      auto wait = [&](uint32_t at, int phase) { return __all_sync(0xffffffffu, tc::mbar_wait(at, (uint32_t)phase & 1u, a.d_status)); };
+      constexpr uint32_t SCORES = idesc_f16(KEYS), VALUES = idesc_f16(DIM) | tc::IDESC_B_MN_MAJOR;
+      auto scores = [&](int m, int i) {
+        const uint64_t q = tc::make_kmajor_sw128_desc(smem + P::Q_AT + m * P::TILE_BYTES);
+        const uint64_t k = tc::make_kmajor_sw128_desc(smem + P::K_AT + (i % STAGES) * P::TILE_BYTES);
         if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < KEYS / 16; ++k)
-            mma_ts(tmem + P::O_COLUMN + m * DIM, tmem + m * 128 + (k >> 1) * 32 + (k & 1) * 8, v + ((k * 16 * 128) >> 4), VALUES, i > 0 || k > 0);
-          tc::umma_commit(pv_done(m));
+          for (int s = 0; s < DIM / 16; ++s) {
+            const uint32_t step = ((s >> 2) * P::BOX + (s & 3) * 32) >> 4;
+            mma_ss(tmem + m * 128, q + step, k + step, SCORES, s > 0);
+          }
+          tc::umma_commit(s_full(m));
         }
         __syncwarp();
-        if (m == TILES - 1) commit(v_empty(s));
-        if (i + 1 < key_tiles) {   // the next scores go over this P: it has to have been read
-          if (m == 0) ok = wait(k_full(s1), (i + 1) / STAGES);
-          ok = ok && wait(pv_done(m), i);
+      };
+      auto commit = [&](uint32_t at) {
+        if (elect_one()) tc::umma_commit(at);
+        __syncwarp();
+      };
+      if (key_tiles > 0) ok = wait(q_full, 0) && wait(k_full(0), 0);
+      tc::tc_fence_after();
+      if (ok && key_tiles > 0) {
+        for (int m = 0; m < TILES; ++m) scores(m, 0);
+        commit(k_empty(0));
+      }
+      for (int i = 0; i < key_tiles && ok; ++i) {
+        const int s = i % STAGES, s1 = (i + 1) % STAGES;
+        const uint64_t v = tc::make_mnmajor_sw128_desc(smem + P::V_AT + s * P::TILE_BYTES, P::BOX);
+        ok = wait(v_full(s), i / STAGES);
+        for (int m = 0; m < TILES && ok; ++m) {
+          ok = wait(p_full(m), i);
           if (!ok) break;
           tc::tc_fence_after();
-          scores(m, i + 1);
-          if (m == TILES - 1) commit(k_empty(s1));
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < KEYS / 16; ++k)
+              mma_ts(tmem + P::O_COLUMN + m * DIM, tmem + m * 128 + (k >> 1) * 32 + (k & 1) * 8, v + ((k * 16 * 128) >> 4), VALUES, i > 0 || k > 0);
+            tc::umma_commit(pv_done(m));
+          }
+          __syncwarp();
+          if (m == TILES - 1) commit(v_empty(s));
+          if (i + 1 < key_tiles) {   // the next scores go over this P: it has to have been read
+            if (m == 0) ok = wait(k_full(s1), (i + 1) / STAGES);
+            ok = ok && wait(pv_done(m), i);
+            if (!ok) break;
+            tc::tc_fence_after();
+            scores(m, i + 1);
+            if (m == TILES - 1) commit(k_empty(s1));
+          }
         }
       }
+      commit(drained);   // nothing is in flight when tensor and shared memory are given up
+      ok = wait(drained, 0) && ok;
     }
-    commit(drained);   // nothing is in flight when tensor and shared memory are given up
-    ok = wait(drained, 0) && ok;
   } else if (warp >= P::UNPACK) {   // ---------------------------------------- codes to operands
+    if constexpr (P::UNPACK_REGS < 65536 / P::THREADS / 8 * 8) fewer_registers<P::UNPACK_REGS>();
     const int t = tid - P::UNPACK * 32, w4 = warp - P::UNPACK;
     uint32_t k[WORDS], v[WORDS], kp = 0u, vp = 0u;
     bool there = false;
@@ -263,6 +273,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
       if (i + 1 < key_tiles) fetch(i + 1);
     }
   } else {   // ---------------------------------------------------------------- rows
+    more_registers<P::ROW_REGS>();
     const int m = warp >> 2, r = (warp & 3) * 32 + lane, row = row0 + m * 128 + r;
     const bool there = row < rows;
     const int token = there ? a.token_of(row) : 0, head = h * a.group + (there ? row - token * a.group : 0);
@@ -327,33 +338,28 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
       const Params& p = s_params[s];
       const uint32_t valid = p.valid;
       const bool masked = slot0 + KEYS > least || valid != 255u;
-      // scores of 32 keys from a column on, without `by`
-      auto scores = [&](float2 (&x)[16], int c) {
-        uint32_t v[32];
-        tc::tmem_ld32(s_at + c, v);
-        tc::tmem_ld_wait();
+      uint32_t raw[4][32];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float4 ks = *reinterpret_cast<const float4*>(p.ks + c + 4 * e), ko = *reinterpret_cast<const float4*>(p.ko + c + 4 * e);
-          x[2 * e] = fma2(make_float2(ko.x, ko.y), both(sum_by), mul2(make_float2(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1])), make_float2(ks.x, ks.y)));
-          x[2 * e + 1] = fma2(make_float2(ko.z, ko.w), both(sum_by), mul2(make_float2(__uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3])), make_float2(ks.z, ks.w)));
-        }
-        if (masked)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const bool none = !(valid >> ((c + 2 * e) >> 4) & 1u);
-            if (none || slot0 + c + 2 * e >= sees) x[e].x = -INFINITY;
-            if (none || slot0 + c + 2 * e + 1 >= sees) x[e].y = -INFINITY;
-          }
-      };
+      for (int c = 0; c < 4; ++c) tc::tmem_ld32(s_at + 32 * c, raw[c]);
+      float2 x[KEYS / 2];                                               // scores, without `by`
       float now = -INFINITY;
-#pragma unroll 1
-      for (int c = 0; c < KEYS; c += 32) {
-        float2 x[16];
-        scores(x, c);
+      tc::tmem_ld_wait();
 #pragma unroll
-        for (int e = 0; e < 16; ++e) now = fmaxf(now, fmaxf(x[e].x, x[e].y));
+      for (int e = 0; e < KEYS / 4; ++e) {
+        const float4 ks = *reinterpret_cast<const float4*>(p.ks + 4 * e), ko = *reinterpret_cast<const float4*>(p.ko + 4 * e);
+        const uint32_t* v = &raw[e >> 3][(e & 7) * 4];
+        x[2 * e] = fma2(make_float2(ko.x, ko.y), both(sum_by), mul2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), make_float2(ks.x, ks.y)));
+        x[2 * e + 1] = fma2(make_float2(ko.z, ko.w), both(sum_by), mul2(make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])), make_float2(ks.z, ks.w)));
       }
+      if (masked)
+#pragma unroll
+        for (int e = 0; e < KEYS / 2; ++e) {
+          const bool none = !(valid >> (e >> 3) & 1u);
+          if (none || slot0 + 2 * e >= sees) x[e].x = -INFINITY;
+          if (none || slot0 + 2 * e + 1 >= sees) x[e].y = -INFINITY;
+        }
+#pragma unroll
+      for (int e = 0; e < KEYS / 2; ++e) now = fmaxf(now, fmaxf(x[e].x, x[e].y));
       now *= by;
       const uint32_t wider = p.field - field;
       field = p.field;
@@ -377,31 +383,31 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
         }
       }
       const float base = top == -INFINITY ? 0.f : -top;
-#pragma unroll 1
-      for (int c = 0; c < KEYS; c += 32) {
-        float2 x[16];
-        scores(x, c);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
         uint32_t packed[16];
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          const float4 vs = *reinterpret_cast<const float4*>(p.vs + c + 2 * e), vo = *reinterpret_cast<const float4*>(p.vo + c + 2 * e);
+          const float4 vs = *reinterpret_cast<const float4*>(p.vs + 32 * c + 2 * e), vo = *reinterpret_cast<const float4*>(p.vo + 32 * c + 2 * e);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const float2 u = j ? make_float2(vs.z, vs.w) : make_float2(vs.x, vs.y), o = j ? make_float2(vo.z, vo.w) : make_float2(vo.x, vo.y);
-            float2 q = fma2(x[e + j], both(by), both(base)), pv, po;
+            const float2 z = x[16 * c + e + j];
+            float2 q = fma2(z, both(by), both(base)), pv, po;
             q = make_float2(exp2_of(q.x), exp2_of(q.y));
             sum = add2(sum, q);
             pv = mul2(q, u);
-            po = mul2(q, o);
-            if (masked) {   // (a NaN times the zero of a row that does not see it)
-              if (x[e + j].x == -INFINITY) pv.x = po.x = 0.f;
-              if (x[e + j].y == -INFINITY) pv.y = po.y = 0.f;
+            if (!masked) off = fma2(q, o, off);
+            else {   // (a NaN times the zero of a row that does not see it)
+              po = mul2(q, o);
+              if (z.x == -INFINITY) pv.x = po.x = 0.f;
+              if (z.y == -INFINITY) pv.y = po.y = 0.f;
+              off = add2(off, po);
             }
-            off = add2(off, po);
             packed[e + j] = half_pair(pv.x, pv.y);
           }
         }
-        tmem_st16(s_at + c, packed);
+        tmem_st16(s_at + 32 * c, packed);
       }
       tmem_st_wait();
       tc::tc_fence_before();
@@ -453,43 +459,44 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
       } else if (there && a.lse) a.lse[(first + token) * a.q.heads + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * LN2;
     }
     tc::tc_fence_before();
-  }
-  __syncthreads();
-  if (splits > 1) {   // the CTA that finishes an item last joins its parts, in order
-    int* ticket = reinterpret_cast<int*>(a.workspace) + (blockIdx.x - part);
-    if (tid == 0) s_last = atomicAdd(ticket, 1) == splits - 1;
-    __syncthreads();
-    if (s_last) {
-      __threadfence();
-      if (tid == 0) *ticket = 0;
-      const float* parts = reinterpret_cast<const float*>(a.workspace + TICKET_BYTES) + (int64_t)(blockIdx.x - part) * P::PART;
-      for (int r = tid; r < P::ROWS && row0 + r < rows; r += P::THREADS) {
-        const int row = row0 + r, token = a.token_of(row), head = h * a.group + row - token * a.group;
-        float top = -INFINITY, l = 0.f;
-        for (int i = 0; i < splits; ++i) top = fmaxf(top, __ldcg(parts + (int64_t)i * P::PART + (int64_t)DIM * P::ROWS + r));
-        for (int i = 0; i < splits; ++i) {
-          const float* p = parts + (int64_t)i * P::PART;
-          const float pl = __ldcg(p + (int64_t)(DIM + 1) * P::ROWS + r), pm = __ldcg(p + (int64_t)DIM * P::ROWS + r);
-          l += pl == 0.f ? 0.f : pl * (pm == -INFINITY ? 1.f : exp2_of(pm - top));
-        }
-        const float over = l == 0.f ? 0.f : 1.f / l;
-        T* out = reinterpret_cast<T*>(a.out.p) + (first + token) * a.out.token + (int64_t)head * a.out.head;
-        if (a.lse) a.lse[(first + token) * a.q.heads + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * LN2;
-        for (int d = 0; d < DIM; d += 8) {
-          float o[8] = {};
+    if (splits > 1) {   // the CTA that finishes an item last joins its parts, in order; a thread a row (only these warps have registers)
+      int* ticket = reinterpret_cast<int*>(a.workspace) + (blockIdx.x - part);
+      asm volatile("bar.sync 2, %0;" ::"n"(P::ROWS) : "memory");
+      if (tid == 0) s_last = atomicAdd(ticket, 1) == splits - 1;
+      asm volatile("bar.sync 2, %0;" ::"n"(P::ROWS) : "memory");
+      if (s_last) {
+        __threadfence();
+        if (tid == 0) *ticket = 0;
+        if (there) {
+          const float* parts = reinterpret_cast<const float*>(a.workspace + TICKET_BYTES) + (int64_t)(blockIdx.x - part) * P::PART + m * 128 + r;
+          float all_top = -INFINITY, l = 0.f;
+          for (int i = 0; i < splits; ++i) all_top = fmaxf(all_top, __ldcg(parts + (int64_t)i * P::PART + (int64_t)DIM * P::ROWS));
           for (int i = 0; i < splits; ++i) {
             const float* p = parts + (int64_t)i * P::PART;
-            const float pm = __ldcg(p + (int64_t)DIM * P::ROWS + r);
-            const float f = pm == -INFINITY ? 1.f : exp2_of(pm - top);  // (where there is no sum O is zero)
-#pragma unroll
-            for (int x = 0; x < 8; ++x) o[x] += __ldcg(p + (int64_t)(d + x) * P::ROWS + r) * f;
+            const float pl = __ldcg(p + (int64_t)(DIM + 1) * P::ROWS), pm = __ldcg(p + (int64_t)DIM * P::ROWS);
+            l += pl == 0.f ? 0.f : pl * (pm == -INFINITY ? 1.f : exp2_of(pm - all_top));
           }
+          const float over = l == 0.f ? 0.f : 1.f / l;
+          T* out = reinterpret_cast<T*>(a.out.p) + (first + token) * a.out.token + (int64_t)head * a.out.head;
+          if (a.lse) a.lse[(first + token) * a.q.heads + head] = l == 0.f ? -INFINITY : (all_top + log2f(l)) * LN2;
+#pragma unroll 1
+          for (int d = 0; d < DIM; d += 16) {
+            float o[16] = {};
+            for (int i = 0; i < splits; ++i) {
+              const float* p = parts + (int64_t)i * P::PART;
+              const float pm = __ldcg(p + (int64_t)DIM * P::ROWS);
+              const float f = pm == -INFINITY ? 1.f : exp2_of(pm - all_top);   // (where there is no sum O is zero)
 #pragma unroll
-          for (int x = 0; x < 8; ++x) out[d + x] = mx::from_f32<T>(o[x] * over);
+              for (int x = 0; x < 16; ++x) o[x] += __ldcg(p + (int64_t)(d + x) * P::ROWS) * f;
+            }
+#pragma unroll
+            for (int x = 0; x < 16; ++x) out[d + x] = mx::from_f32<T>(o[x] * over);
+          }
         }
       }
     }
   }
+  __syncthreads();
   if (warp == P::ISSUE) {
     tc::tc_fence_after();
     tc::tmem_dealloc(tmem, 512);

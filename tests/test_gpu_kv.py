@@ -252,6 +252,66 @@ def test_attention_of_chunks(dtype, dim):
     attention_case(3, [200, 90, 40, 64], [77, 90, 50, 1], 2, 3, dim, 32, dtype)
 
 
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("dim", (64, 128, 256))
+def test_attention_of_chunks_over_a_long_axis(dtype, dim):
+    """Many rows of few sequences: a tile's keys are cut between CTAs, with parts that a row sees nothing of."""
+    attention_case(5, [1500], [90], 1, 2, dim, 64, dtype)
+    attention_case(6, [700, 1030], [300, 20], 2, 1, dim, 16, dtype)
+
+
+def test_attention_of_chunks_does_not_depend_on_the_run():
+    rng = np.random.default_rng(15)
+    c, cache = filled(rng, [1300, 90], 2, 128, 64)
+    q = put(rng.standard_normal((200, 4, 128)), torch.bfloat16)
+    work, starts = workspace(128), starts_of([150, 50])
+    first = attend(cache, q, 0.1, starts, work=work)
+    check_attention(c, 0, q, 0, 150, 2, 0.1, *first)
+    check_attention(c, 1, q, 150, 50, 2, 0.1, *first)
+    for _ in range(10):
+        again = attend(cache, q, 0.1, starts, work=work)
+        assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1])
+    few = attend(cache, q[:2], 0.1, starts_of([1, 1]), work=work)      # the other kernels' counters are as they were
+    check_attention(c, 0, q, 0, 1, 2, 0.1, *few)
+    for scale in (0.0, -0.3):
+        out, lse = attend(cache, q, scale, starts, work=work)
+        check_attention(c, 1, q, 150, 50, 2, scale, out, lse)
+        few = attend(cache, q[150:151], scale, torch.tensor([0, 0, 1], dtype=torch.int32, device="cuda"))
+        check_attention(c, 1, q[150:151], 0, 1, 2, scale, *few)
+
+
+def test_chunks_with_missing_pages_and_values_that_are_not_numbers():
+    rng = np.random.default_rng(16)
+    for dim in (64, 128, 256):
+        c, _ = filled(rng, [300], 1, dim, 16)
+        c.table[0, [2, 9, 17]] = -1, len(c.pages), -7
+        q = put(rng.standard_normal((100, 2, dim)), torch.float16)
+        out, lse = attend(on_device(c), q, 0.1)
+        check_attention(c, 0, q, 0, 100, 2, 0.1, out, lse)
+        for second in (0, 1):
+            bad = kv.Cache(len(c.pages), 1, dim, 16, c.table, [300])
+            bad.pages = c.pages.copy()
+            bad.write(0, 0, 250, second, np.full(dim, np.nan))          # tokens 200 .. 299: the first 50 do not see it
+            out, lse = attend(on_device(bad), q, 0.1)
+            seen = kv.Cache(len(c.pages), 1, dim, 16, c.table, [250])
+            seen.pages = c.pages
+            check_attention(seen, 0, q[:50], 0, 50, 2, 0.1, out[:50], lse[:50])
+            assert bool(torch.isnan(out[50:]).all()) and bool(torch.isnan(lse[50:]).all()) == (second == 0)
+
+
+def test_chunks_of_views():
+    rng = np.random.default_rng(17)
+    c, cache = filled(rng, [90], 2, 128, 16)
+    whole = put(rng.standard_normal((70, 12, 129)), torch.bfloat16)
+    q = whole[:, 2:8, 1:]
+    want, lse = attend(cache, q.contiguous(), 0.1)
+    check_attention(c, 0, q, 0, 70, 3, 0.1, want, lse)
+    out = torch.full((6, 70, 131), 77.0, dtype=torch.bfloat16, device="cuda")
+    got, got_lse = attend(cache, q, 0.1, out=out.transpose(0, 1)[..., 1:129])
+    assert torch.equal(got, want) and torch.equal(got_lse, lse)
+    assert bool((out[..., 0] == 77).all()) and bool((out[..., 129:] == 77).all())
+
+
 @pytest.mark.parametrize("heads,group,dim", [(1, 1, 64), (1, 8, 128), (2, 2, 256), (8, 4, 128)])
 def test_attention_over_a_long_axis(heads, group, dim):
     """Few sequences: the axis is split over all SMs and joined."""
