@@ -1,12 +1,15 @@
 // Attention over a key/value cache in 4 bits for many query rows (a prompt's chunk), on the tensor cores' tcgen05 instructions.
 //
 // A CTA takes 256 query rows (D = 256: 128) of a sequence and kv head, in tiles of M = 128, and goes over the keys 128 at a time:
-//     S = Q K^T (128 x 128, tensor memory),  P = exp(S - m) vs (fp16, over S in tensor memory),  O += P V (tensor memory)
-// The operands are the codes, as in kv_attention.cu: fp16 subnormals c 2^-24, the values' less 8; keys' parameters are applied to S,
-// the values' to P, sum_t p_t (vo_t + 8 vs_t) is added at the end.  Four bits become 16 on their way from global to shared memory:
-// eight codes are one word and, as (0, 4), (1, 5), (2, 6), (3, 7), one 16-byte piece of a row, swizzled as the instructions want
-// it; Q's dimensions are put in the same order, and the output's taken out of it.  Keys and values have the same layout, [token][64
-// dimensions], read K-major by the first product and MN-major by the second.
+//     S = Q K^T (128 x 128, tensor memory),  P = exp(S - m) (fp16, over S in tensor memory),  O += P V (tensor memory)
+// Four bits become 16 on their way from global to shared memory.  A code alone is the fp16 subnormal c 2^-24, and one multiply-add
+// makes it  ks (c - 8)  for a key, exactly: 8 bits of scale times 3 of code.  What is left of a key, (ko + 8 ks) times the sum of the query,
+// is added to the score in fp32.  A value becomes  vs c + vo,  rounded to fp16 (2^-12, as P is).  Parameters are applied here, by a
+// thread a key, because a thread of the softmax meets every key: read from shared memory for each of them, four numbers a key took
+// 4100 cycles of a key tile's 10000.  Powers of two keep all of it in fp16's range: the largest ks of a tile below 2^-9, the values by the
+// largest so far, the rows of Q with their largest value at 2^14.  Eight codes are one word and, as (0, 4), (1, 5), (2, 6), (3, 7), one
+// 16-byte piece of a row, swizzled as the instructions want it; Q's dimensions are put in the same order, and the output's taken out
+// of it.  Keys and values have the same layout, [token][64 dimensions], read K-major by the first product and MN-major by the second.
 //
 // Warps: four for each tile of rows (a thread a row: scores, exponentials, P, O's rescaling), four that unpack (a thread a key), one
 // that issues the products.  While one tile's rows are in the softmax the other's products run.  4096 queries of 32 heads over 16384
@@ -20,6 +23,7 @@ namespace {
 
 constexpr int KEYS = 128;                 // of a key tile
 constexpr float SLACK = 8.f;              // a maximum may grow by this (in powers of two) before O is rescaled
+constexpr float LIFT = 6.f;               // P is held 2^6 larger: with SLACK below 2^14, and 2^-20 of the largest is a normal number yet
 
 template <int DIM>
 struct Prompt {
@@ -38,9 +42,11 @@ struct Prompt {
 };
 
 struct alignas(16) Params {                                            // of a key tile; read in 16-byte pieces
-  float ks[KEYS], ko[KEYS], vs[KEYS], vo[KEYS];
-  uint32_t field;                                                      // exponent field of the largest vs so far
+  float kz[KEYS];                                                      // (ko + 8 ks) times `shrink`
+  float grow, shrink;                                                  // powers of two: of the tile's scores, of kz
+  uint32_t field;                                                      // the values' power of two: exponent field, the largest so far
   uint32_t valid;                                                      // groups of 16 keys that have a page
+  int odd;                                                             // the first key whose value is a NaN
 };
 
 __device__ __forceinline__ bool elect_one() {
@@ -84,7 +90,8 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
   __shared__ __align__(16) Params s_params[STAGES];
   __shared__ __align__(8) uint64_t s_bars[2 + 4 * STAGES + 3 * TILES];
   __shared__ uint32_t s_tmem;
-  __shared__ uint32_t s_fields[4];
+  __shared__ uint32_t s_keys[2][4], s_values[2][4];
+  __shared__ int s_odd[2][4];
   __shared__ Share s_share;
   __shared__ int64_t s_sums[P::THREADS / 32];
   __shared__ int s_last;
@@ -226,46 +233,75 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     };
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) k[w] = v[w] = 0u;
-    uint32_t field = 7u;
+    uint32_t field = 20u;
     if (key_tiles > 0) fetch(0);
     auto wait = [&](uint32_t at, int phase) { return __all_sync(0xffffffffu, tc::mbar_wait(at, (uint32_t)phase & 1u, a.d_status)); };
+    // eight codes times a factor (`high`: of the codes four bits up) plus an offset, as a piece of a row
+    auto store = [&](uint32_t at, uint32_t x, __half2 low, __half2 high, __half2 offset) {
+      auto value = [&](uint32_t code, __half2 by) {
+        const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&code), by, offset);
+        return *reinterpret_cast<const uint32_t*>(&r);
+      };
+      const uint32_t y = x >> 8;
+      store16(at, make_uint4(value(low_codes(x), low), value(high_codes(x), high), value(low_codes(y), low), value(high_codes(y), high)));
+    };
     // After a wait that gave up these warps go on without waiting: they meet at barriers of their own.
     for (int i = 0; i < key_tiles; ++i) {
       const int s = i % STAGES, turn = i / STAGES;
-      ok = ok && wait(k_empty(s), turn + 1);
-      const uint32_t k_tile = smem + P::K_AT + s * P::TILE_BYTES, v_tile = smem + P::V_AT + s * P::TILE_BYTES;
+      const float ks = scale_of(kp), kz = offset_of(kp) + 8.f * ks, vs = scale_of(vp), vo = offset_of(vp);
+      // exponent fields of the tile's largest ks, and of what the values are divided by: vs below 2^-9, values below 2^6.  A NaN does
+      // not count, and a value that is one is held as zero: not all rows may see it.
+      const bool nan = !(fabsf(vs) <= 3.402823466e38f && fabsf(vo) <= 3.402823466e38f);
+      const int k_field = (int)(kp >> 7 & 255u), spread = (int)(vp >> 7 & 255u) + 10;
+      const int size = (int)max(mx::exponent_field(vo), mx::exponent_field(fmaf(15.f, vs, vo))) - 4;
+      const uint32_t k_most = __reduce_max_sync(0xffffffffu, k_field == 255 ? 0u : (uint32_t)k_field);
+      const uint32_t v_most = __reduce_max_sync(0xffffffffu, nan ? 0u : (uint32_t)max(spread, size));
+      const uint32_t votes = __ballot_sync(0xffffffffu, there), odd = __ballot_sync(0xffffffffu, nan);
+      if (lane == 0) {
+        s_keys[i & 1][w4] = k_most;
+        s_values[i & 1][w4] = v_most | (votes & 1u) << 16 | (votes >> 16 & 1u) << 17;
+        s_odd[i & 1][w4] = odd ? (tile0 + i) * KEYS + w4 * 32 + __ffs(odd) - 1 : INT_MAX;
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      uint32_t valid = 0u, key_field = 10u;
+      int first_odd = INT_MAX;
 #pragma unroll
-      for (int w = 0; w < WORDS; ++w) {
-        const uint32_t x = k[w], y = x >> 8;
-        store16(piece_at(k_tile, t, w), make_uint4(low_codes(x), high_codes(x), low_codes(y), high_codes(y)));
+      for (int x = 0; x < 4; ++x) {
+        key_field = max(key_field, s_keys[i & 1][x]);
+        field = max(field, s_values[i & 1][x] & 0xffffu);
+        valid |= (s_values[i & 1][x] >> 16) << (2 * x);
+        first_odd = min(first_odd, s_odd[i & 1][x]);
+      }
+      key_field = min(key_field, 243u);
+      field = min(field, 240u);
+      const float k_by = __uint_as_float((244u - key_field) << 23), v_by = __uint_as_float((254u - field) << 23);
+      const uint32_t k_tile = smem + P::K_AT + s * P::TILE_BYTES, v_tile = smem + P::V_AT + s * P::TILE_BYTES;
+      constexpr float LOW = 16777216.f, HIGH = 1048576.f;               // 2^24 and 2^20: of the codes
+      ok = ok && wait(k_empty(s), turn + 1);
+      {
+        const float by = ks * k_by;
+        const __half2 low = __float2half2_rn(by * LOW), high = __float2half2_rn(by * HIGH), offset = __float2half2_rn(-8.f * by);
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) store(piece_at(k_tile, t, w), k[w], low, high, offset);
       }
       fence_async();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(k_full(s));
       ok = ok && wait(v_empty(s), turn + 1);
-      // (a NaN's field does not count: not all rows may see it)
-      const uint32_t mine = vp >> 7 & 255u;
-      const uint32_t largest = __reduce_max_sync(0xffffffffu, mine == 255u ? 0u : mine), votes = __ballot_sync(0xffffffffu, there);
-      if (lane == 0) s_fields[w4] = largest | (votes & 1u) << 16 | (votes >> 16 & 1u) << 17;
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-      uint32_t valid = 0u;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        field = max(field, s_fields[x] & 255u);
-        valid |= (s_fields[x] >> 16) << (2 * x);
-      }
-      asm volatile("bar.sync 1, 128;" ::: "memory");
       Params& p = s_params[s];
-      const float vs = scale_of(vp);
-      p.ks[t] = scale_of(kp);
-      p.ko[t] = offset_of(kp);
-      p.vs[t] = vs * __uint_as_float((260u - field) << 23);            // below 2^7
-      p.vo[t] = offset_of(vp) + 8.f * vs;
-      if (t == 0) { p.field = field; p.valid = valid; }
+      p.kz[t] = kz * k_by;
+      if (t == 0) {
+        p.grow = __uint_as_float((10u + key_field) << 23);
+        p.shrink = k_by;
+        p.field = field;
+        p.valid = valid;
+        p.odd = first_odd;
+      }
+      {
+        const float by = nan ? 0.f : vs * v_by;
+        const __half2 low = __float2half2_rn(by * LOW), high = __float2half2_rn(by * HIGH), offset = __float2half2_rn(nan ? 0.f : vo * v_by);
 #pragma unroll
-      for (int w = 0; w < WORDS; ++w) {
-        const uint32_t x = v[w], y = x >> 8;
-        store16(piece_at(v_tile, t, w), make_uint4(low_centred(x), high_centred(x), low_centred(y), high_centred(y)));
+        for (int w = 0; w < WORDS; ++w) store(piece_at(v_tile, t, w), v[w], low, high, offset);
       }
       fence_async();
       __syncwarp();
@@ -280,8 +316,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_at = tmem + lanes + m * 128, o_at = tmem + lanes + P::O_COLUMN + m * DIM;
     auto wait = [&](uint32_t at, int phase) { return __all_sync(0xffffffffu, tc::mbar_wait(at, (uint32_t)phase & 1u, a.d_status)); };
-    // the row into shared memory, times a power of two that brings its largest value to 2^14 (odd dimensions 2^-4 less, as their codes
-    // lie four bits up), and with the scale's sign
+    // the row into shared memory, times a power of two that brings its largest value to 2^14, and with the scale's sign
     float by, sum_by;
     {
       const T* p = reinterpret_cast<const T*>(a.q.p) + (first + token) * a.q.token + (int64_t)head * a.q.head;
@@ -307,18 +342,17 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
           most_q = fmaxf(most_q, fmaxf(fabsf(f.x), fabsf(f.y)));
         }
       }
-      const int field = min(max((int)mx::exponent_field(most_q), 14), 244);
-      const float sign = a.scale < 0.f ? -1.f : 1.f;
-      const float up = __uint_as_float((uint32_t)(268 - field) << 23) * sign, up4 = up * 0.0625f;
-      by = fmaxf(__uint_as_float((uint32_t)(field + 10) << 23) * fabsf(a.scale) * LOG2E, 1.2e-38f);   // (not zero: it meets infinities)
-      sum_by = sum * sign * (fabsf(a.scale) * LOG2E) / by;
+      const int field = min(max((int)mx::exponent_field(most_q), 15), 244);
+      const float up = __uint_as_float((uint32_t)(268 - field) << 23) * (a.scale < 0.f ? -1.f : 1.f);
+      by = fmaxf(__uint_as_float((uint32_t)(field - 14) << 23) * fabsf(a.scale) * LOG2E, 1.2e-38f);   // (not zero: it meets infinities)
+      sum_by = sum * up;
       const uint32_t tile = smem + P::Q_AT + m * P::TILE_BYTES;
 #pragma unroll 4
       for (int w = 0; w < WORDS; ++w) {
         const mx::Vec8<T> x = load(w);
         const float2 d01 = x.pair(0), d23 = x.pair(1), d45 = x.pair(2), d67 = x.pair(3);
-        store16(piece_at(tile, r, w), make_uint4(half_pair(d01.x * up, d45.x * up), half_pair(d01.y * up4, d45.y * up4),
-                                                 half_pair(d23.x * up, d67.x * up), half_pair(d23.y * up4, d67.y * up4)));
+        store16(piece_at(tile, r, w), make_uint4(half_pair(d01.x * up, d45.x * up), half_pair(d01.y * up, d45.y * up),
+                                                 half_pair(d23.x * up, d67.x * up), half_pair(d23.y * up, d67.y * up)));
       }
       fence_async();
       __syncwarp();
@@ -328,8 +362,9 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     // what all rows of the warp that there are see
     const int least = __reduce_min_sync(0xffffffffu, there ? sees : INT_MAX);
     float top = -INFINITY;
-    float2 sum = both(0.f), off = both(0.f);
-    uint32_t field = 7u;
+    float2 sum = both(0.f);
+    uint32_t field = 20u;
+    bool odd = false;                                                   // the row sees a value that is a NaN
     for (int i = 0; i < key_tiles && ok; ++i) {
       const int s = i % STAGES, slot0 = (tile0 + i) * KEYS;
       ok = wait(v_full(s), i / STAGES) && wait(s_full(m), i);
@@ -341,15 +376,17 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
       uint32_t raw[4][32];
 #pragma unroll
       for (int c = 0; c < 4; ++c) tc::tmem_ld32(s_at + 32 * c, raw[c]);
-      float2 x[KEYS / 2];                                               // scores, without `by`
+      float2 x[KEYS / 2];                                               // scores, without `tile_by`
       float now = -INFINITY;
+      const float tile_by = by * p.grow;
+      odd |= p.odd < sees;
       tc::tmem_ld_wait();
 #pragma unroll
       for (int e = 0; e < KEYS / 4; ++e) {
-        const float4 ks = *reinterpret_cast<const float4*>(p.ks + 4 * e), ko = *reinterpret_cast<const float4*>(p.ko + 4 * e);
+        const float4 kz = *reinterpret_cast<const float4*>(p.kz + 4 * e);
         const uint32_t* v = &raw[e >> 3][(e & 7) * 4];
-        x[2 * e] = fma2(make_float2(ko.x, ko.y), both(sum_by), mul2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), make_float2(ks.x, ks.y)));
-        x[2 * e + 1] = fma2(make_float2(ko.z, ko.w), both(sum_by), mul2(make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])), make_float2(ks.z, ks.w)));
+        x[2 * e] = fma2(make_float2(kz.x, kz.y), both(sum_by), make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])));
+        x[2 * e + 1] = fma2(make_float2(kz.z, kz.w), both(sum_by), make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])));
       }
       if (masked)
 #pragma unroll
@@ -360,7 +397,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
         }
 #pragma unroll
       for (int e = 0; e < KEYS / 2; ++e) now = fmaxf(now, fmaxf(x[e].x, x[e].y));
-      now *= by;
+      now *= tile_by;
       const uint32_t wider = p.field - field;
       field = p.field;
       if (__any_sync(0xffffffffu, now > top + SLACK) || wider) {
@@ -368,7 +405,6 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
         top = fmaxf(top, now);
         const float f = old == -INFINITY ? (sum.x + sum.y == 0.f ? 0.f : 1.f) : exp2_of(old - top);
         sum = mul2(sum, both(f));
-        off = mul2(off, both(f));
         if (i > 0) {
           const float o_by = wider > 126u ? 0.f : f * __uint_as_float((127u - wider) << 23);
 #pragma unroll 1
@@ -382,30 +418,16 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
           }
         }
       }
-      const float base = top == -INFINITY ? 0.f : -top;
+      const float base = top == -INFINITY ? 0.f : LIFT - top;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         uint32_t packed[16];
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          const float4 vs = *reinterpret_cast<const float4*>(p.vs + 32 * c + 2 * e), vo = *reinterpret_cast<const float4*>(p.vo + 32 * c + 2 * e);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float2 u = j ? make_float2(vs.z, vs.w) : make_float2(vs.x, vs.y), o = j ? make_float2(vo.z, vo.w) : make_float2(vo.x, vo.y);
-            const float2 z = x[16 * c + e + j];
-            float2 q = fma2(z, both(by), both(base)), pv, po;
-            q = make_float2(exp2_of(q.x), exp2_of(q.y));
-            sum = add2(sum, q);
-            pv = mul2(q, u);
-            if (!masked) off = fma2(q, o, off);
-            else {   // (a NaN times the zero of a row that does not see it)
-              po = mul2(q, o);
-              if (z.x == -INFINITY) pv.x = po.x = 0.f;
-              if (z.y == -INFINITY) pv.y = po.y = 0.f;
-              off = add2(off, po);
-            }
-            packed[e + j] = half_pair(pv.x, pv.y);
-          }
+        for (int e = 0; e < 16; ++e) {
+          float2 q = fma2(x[16 * c + e], both(tile_by), both(base));
+          q = make_float2(exp2_of(q.x), exp2_of(q.y));
+          sum = add2(sum, q);
+          packed[e] = half_pair(q.x, q.y);
         }
         tmem_st16(s_at + 32 * c, packed);
       }
@@ -417,9 +439,8 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     if (ok && key_tiles > 0) ok = wait(pv_done(m), key_tiles - 1);
     tc::tc_fence_after();
     if (ok) {
-      const float l = sum.x + sum.y, o0 = off.x + off.y;
-      const float grow = __uint_as_float((field - 6u) << 23);
-      const float low = key_tiles > 0 ? grow * 16777216.f : 0.f, high = key_tiles > 0 ? grow * 1048576.f : 0.f;
+      const float l = sum.x + sum.y;
+      const float grow = odd ? __uint_as_float(0x7fc00000u) : __uint_as_float(field << 23);
       float* part_at = reinterpret_cast<float*>(a.workspace + TICKET_BYTES) + (int64_t)blockIdx.x * P::PART;
       const float over = l == 0.f ? 0.f : 1.f / l;
       T* out = reinterpret_cast<T*>(a.out.p) + (first + token) * a.out.token + (int64_t)head * a.out.head;
@@ -434,8 +455,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
           float d[8];
 #pragma unroll
           for (int x = 0; x < 8; ++x) {
-            const float o = key_tiles > 0 ? __uint_as_float(v[e + x]) : 0.f;
-            d[(x >> 1) + 4 * (x & 1)] = o * (x & 2 ? high : low) + o0;
+            d[(x >> 1) + 4 * (x & 1)] = (key_tiles > 0 ? __uint_as_float(v[e + x]) : 0.f) * grow;
           }
           if (splits > 1) {
             // (by column, rows side by side: the joining CTA reads them so)
@@ -453,10 +473,10 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
         }
       }
       if (splits > 1) {
-        __stcg(part_at + (int64_t)DIM * P::ROWS + m * 128 + r, top);
+        __stcg(part_at + (int64_t)DIM * P::ROWS + m * 128 + r, top - LIFT);
         __stcg(part_at + (int64_t)(DIM + 1) * P::ROWS + m * 128 + r, l);
         __threadfence();
-      } else if (there && a.lse) a.lse[(first + token) * a.q.heads + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * LN2;
+      } else if (there && a.lse) a.lse[(first + token) * a.q.heads + head] = l == 0.f ? -INFINITY : (top - LIFT + log2f(l)) * LN2;
     }
     tc::tc_fence_before();
     if (splits > 1) {   // the CTA that finishes an item last joins its parts, in order; a thread a row (only these warps have registers)

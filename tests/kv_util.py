@@ -74,7 +74,9 @@ def check_attention(c, b, q, first, n, group, scale, out, lse):
     """Rows first .. first + n of out and lse against the oracle.  p = exp(S - top) / l is off by twice the logits' error relatively
     (S and l), by 2^-20 for the exponentials, sums and joins, and by half an fp16 step, 2^-11, where it is rounded for the product:
     of a term that is at least 2^-20 of what a key with p = 1 and the largest scale of its stage has (2^6 .. 2^7, fp16's normal numbers
-    begin at 2^-14), else by 2^-25 / 2^6 of the latter; the output is then rounded once."""
+    begin at 2^-14), else by 2^-25 / 2^6 of the latter.  For many rows the values are rounded to fp16 too: by 2^-11, or 2^-25 where the
+    largest scale is above 2^-10 (2^-15 of it, 2^-17 of the largest value: a scale is at most 2/15 of that).  The output is then rounded
+    once."""
     dtype = q.dtype
     for h in range(c.heads):
         heads = slice(h * group, (h + 1) * group)
@@ -85,7 +87,7 @@ def check_attention(c, b, q, first, n, group, scale, out, lse):
         assert (np.isneginf(got) == empty).all()
         full = ~empty
         assert (np.abs(got[full] - r["lse"][full]) <= e[full] + 2.0 ** -21 * (1 + np.abs(r["lse"][full]))).all()
-        bound = (2 * e[..., None] + 2.0 ** -20 + 2.0 ** -11) * r["terms"] * 1.01 + UNIT[dtype] * np.abs(r["out"]) * 1.01 + LEAST[dtype]
-        bound += c.length(b) * 2.0 ** -31 * r["largest"]
+        bound = (2 * e[..., None] + 2.0 ** -20 + 2 * 2.0 ** -11) * r["terms"] * 1.01 + UNIT[dtype] * np.abs(r["out"]) * 1.01 + LEAST[dtype]
+        bound += (c.length(b) * 2.0 ** -31 + 2.0 ** -17) * r["largest"]
         got = f64(out[first:first + n, heads])
         assert (np.abs(got - r["out"]) <= bound).all(), float((np.abs(got - r["out"]) / bound).max())
