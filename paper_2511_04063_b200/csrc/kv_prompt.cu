@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
   constexpr int TILES = P::TILES, STAGES = P::STAGES, WORDS = DIM / 8;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(16) Params s_params[STAGES];
-  __shared__ __align__(8) uint64_t s_bars[2 + 4 * STAGES + 3 * TILES];
+  __shared__ __align__(8) uint64_t s_bars[2 + 4 * STAGES + 4 * TILES];
   __shared__ uint32_t s_tmem;
   __shared__ uint32_t s_keys[2][4], s_values[2][4];
   __shared__ int s_odd[2][4];
@@ -106,6 +106,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
   auto s_full = [&](int m) { return bar(2 + 4 * STAGES + m); };
   auto p_full = [&](int m) { return bar(2 + 4 * STAGES + TILES + m); };
   auto pv_done = [&](int m) { return bar(2 + 4 * STAGES + 2 * TILES + m); };
+  auto p_half = [&](int m) { return bar(2 + 4 * STAGES + 3 * TILES + m); };
   if (tid == 0) {
     tc::mbar_init(q_full, 4 * TILES);
     tc::mbar_init(drained, 1);
@@ -117,6 +118,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     }
     for (int m = 0; m < TILES; ++m) {
       tc::mbar_init(s_full(m), 1);
+      tc::mbar_init(p_half(m), 4);
       tc::mbar_init(p_full(m), 4);
       tc::mbar_init(pv_done(m), 1);
     }
@@ -184,15 +186,22 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
         const uint64_t v = tc::make_mnmajor_sw128_desc(smem + P::V_AT + s * P::TILE_BYTES, P::BOX);
         ok = wait(v_full(s), i / STAGES);
         for (int m = 0; m < TILES && ok; ++m) {
+          auto values = [&](int half, uint32_t done) {
+            tc::tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int k = 4 * half; k < 4 * half + 4; ++k)
+                mma_ts(tmem + P::O_COLUMN + m * DIM, tmem + m * 128 + (k >> 1) * 32 + (k & 1) * 8, v + ((k * 16 * 128) >> 4), VALUES, i > 0 || k > 0);
+              if (half) tc::umma_commit(done);
+            }
+            __syncwarp();
+          };
+          ok = wait(p_half(m), i);                                      // the first keys' P, while the others' is formed
+          if (!ok) break;
+          values(0, 0u);
           ok = wait(p_full(m), i);
           if (!ok) break;
-          tc::tc_fence_after();
-          if (elect_one()) {
-#pragma unroll
-            for (int k = 0; k < KEYS / 16; ++k)
-              mma_ts(tmem + P::O_COLUMN + m * DIM, tmem + m * 128 + (k >> 1) * 32 + (k & 1) * 8, v + ((k * 16 * 128) >> 4), VALUES, i > 0 || k > 0);
-            tc::umma_commit(pv_done(m));
-          }
+          values(1, pv_done(m));
           __syncwarp();
           if (m == TILES - 1) commit(v_empty(s));
           if (i + 1 < key_tiles) {   // the next scores go over this P: it has to have been read
@@ -430,11 +439,13 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
           packed[e] = half_pair(q.x, q.y);
         }
         tmem_st16(s_at + 32 * c, packed);
+        if (c & 1) {
+          tmem_st_wait();
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(c == 1 ? p_half(m) : p_full(m));
+        }
       }
-      tmem_st_wait();
-      tc::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(p_full(m));
     }
     if (ok && key_tiles > 0) ok = wait(pv_done(m), key_tiles - 1);
     tc::tc_fence_after();
