@@ -185,10 +185,12 @@ dq_status run_append(cudaStream_t stream, int dtype, int dim, const AppendArgs& 
 // ------------------------------------------------------------------------------------------------ eviction
 // One CTA for each (sequence, kv head) finds the `keep` slots that stay: the order is (protected, weight, lower slot first).  A
 // radix selection over the weights' order-preserving bits, 8 at a time, finds the key of the last one that stays and how many of
-// its equals do.  Slots from `keep` on that stay move into the slots below that do not, the i-th into the i-th: what is moved is
+// its equals do.  A warp takes neighbouring slots, 32 at a time, and keeps their keys in registers, so that a row is read twice, votes
+// number the equals, holes and movers of a warp and one scan each those of the warps before (rows of more than 32768 slots go round
+// in blocks of that, and read their keys again).  Slots from `keep` on that stay move into the slots below that do not, the i-th into the i-th: what is moved is
 // read from slots that nothing writes, so no order between the moves is needed, and a sequence that is over its budget by a
 // few tokens moves a few.
-constexpr int SELECT = 1024;
+constexpr int SELECT = 1024, PER_THREAD = 32, BLOCK = SELECT * PER_THREAD;
 
 __device__ __forceinline__ uint32_t order_key(float w, int position, int64_t guarded_above) {
   if ((int64_t)position > guarded_above) return 0xffffffffu;
@@ -197,42 +199,60 @@ __device__ __forceinline__ uint32_t order_key(float w, int position, int64_t gua
   return (int)u < 0 ? ~u : u | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(SELECT) evict_select_kernel(const EvictArgs a) {
-  __shared__ int s_count[256], s_sum[SELECT / 32][3], s_pick[2], s_newest[SELECT / 32];
+__global__ void __launch_bounds__(SELECT, 1) evict_select_kernel(const EvictArgs a) {
+  __shared__ int s_count[2][256], s_pick[2], s_newest[SELECT / 32];
+  __shared__ int64_t s_scan[SELECT / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t row = blockIdx.x;                              // sequence x heads + head
   const int b = (int)(row / a.cache.heads);
+  if (tid < 256) s_count[0][tid] = 0;
   mx::wait_for_previous();
+  mx::allow_next();
   const int n = a.cache.length(b), keep = min(n, a.keep);
   const float* weights = a.weights + row * a.ld_slots;
   const int* positions = a.positions + row * a.ld_slots;
   int* ws = a.workspace + row * evict_stride(a.keep);
+  const int per = min(PER_THREAD, (n + SELECT - 1) / SELECT);   // slots of a thread in each block: mine + 32 j
+  const int mine = warp * per * 32 + lane;
   int64_t guarded_above = 0;
   uint32_t last = 0u;      // the key of the last slot that stays
   int equals = n;          // how many slots with that key stay
+  uint32_t key[PER_THREAD];
+  auto load_keys = [&](int base) {
+#pragma unroll
+    for (int j = 0; j < PER_THREAD; ++j) {
+      if (j >= per) break;
+      const int i = base + mine + 32 * j;
+      key[j] = i < n ? order_key(weights[i], positions[i], guarded_above) : 0u;
+    }
+  };
   if (n > keep) {
     int newest = INT_MIN;
     for (int i = tid; i < n; i += SELECT) newest = max(newest, positions[i]);
     newest = __reduce_max_sync(0xffffffffu, newest);
     if (lane == 0) s_newest[warp] = newest;
     __syncthreads();
-    for (int w = 0; w < SELECT / 32; ++w) newest = max(newest, s_newest[w]);
+    newest = __reduce_max_sync(0xffffffffu, lane < SELECT / 32 ? s_newest[lane] : INT_MIN);
     guarded_above = (int64_t)newest - a.recent;
+    load_keys(0);
     int wanted = keep;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) s_count[tid] = 0;
-      __syncthreads();
+    for (int shift = 24, now = 0; shift >= 0; shift -= 8, now ^= 1) {
       const uint32_t known = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-      for (int i = tid; i < n; i += SELECT) {
-        const uint32_t key = order_key(weights[i], positions[i], guarded_above);
-        if ((key & known) == last) atomicAdd(&s_count[(key >> shift) & 255u], 1);
+      for (int base = 0; base < n; base += BLOCK) {
+        if (n > BLOCK) load_keys(base);
+#pragma unroll
+        for (int j = 0; j < PER_THREAD; ++j) {
+          if (j >= per) break;
+          if (base + mine + 32 * j < n && (key[j] & known) == last) atomicAdd(&s_count[now][(key[j] >> shift) & 255u], 1);
+        }
       }
+      if (tid < 256) s_count[now ^ 1][tid] = 0;
       __syncthreads();
       if (warp == 0) {   // from the largest digit down: the first at which the count reaches what is wanted
         int sum = 0;
         int c[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += c[i] = s_count[255 - (lane * 8 + i)];
+        for (int i = 0; i < 8; ++i) sum += c[i] = s_count[now][255 - (lane * 8 + i)];
         int upto = sum;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -254,39 +274,80 @@ __global__ void __launch_bounds__(SELECT) evict_select_kernel(const EvictArgs a)
   }
   float* weights_out = a.weights_out + row * a.ld_slots;
   int* positions_out = a.positions_out + row * a.ld_slots;
-  int same = 0, holes = 0, movers = 0;                          // so far
-  for (int i0 = 0; i0 < n; i0 += SELECT) {
-    const int i = i0 + tid;
-    float w = 0.f;
-    int position = 0;
-    uint32_t key = 0u;
-    if (i < n) {
-      w = weights[i];
-      position = positions[i];
-      key = order_key(w, position, guarded_above);
+  // The sum over the warps before this one of a count that is the same in all lanes of a warp; two kinds in one number, 21 bits each
+  // (a block has 2^15 slots).
+  auto scan = [&](int64_t of_mine, int64_t& all) {
+    __syncthreads();
+    if (lane == 0) s_scan[warp] = of_mine;
+    __syncthreads();
+    const int64_t of_warp = lane < SELECT / 32 ? s_scan[lane] : 0;
+    int64_t upto = of_warp;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += v;
     }
-    const uint32_t below = (1u << lane) - 1u;
-    const bool equal = i < n && n > keep && key == last;
-    uint32_t votes = __ballot_sync(0xffffffffu, equal);
-    __syncthreads();
-    if (lane == 0) s_sum[warp][0] = __popc(votes);
-    __syncthreads();
-    int before = same + __popc(votes & below);
-    for (int v = 0; v < SELECT / 32; ++v) { if (v < warp) before += s_sum[v][0]; same += s_sum[v][0]; }
-    const bool stays = i < n && (n <= keep || key > last || (equal && before < equals));
-    const bool hole = i < keep && !stays, mover = i >= keep && stays;
-    const uint32_t h_votes = __ballot_sync(0xffffffffu, hole), m_votes = __ballot_sync(0xffffffffu, mover);
-    if (lane == 0) { s_sum[warp][1] = __popc(h_votes); s_sum[warp][2] = __popc(m_votes); }
-    __syncthreads();
-    int h_before = holes + __popc(h_votes & below), m_before = movers + __popc(m_votes & below);
-    for (int v = 0; v < SELECT / 32; ++v) {
-      if (v < warp) { h_before += s_sum[v][1]; m_before += s_sum[v][2]; }
-      holes += s_sum[v][1];
-      movers += s_sum[v][2];
+    all = __shfl_sync(0xffffffffu, upto, 31);
+    return __shfl_sync(0xffffffffu, upto - of_warp, warp);
+  };
+  constexpr int64_t MASK = ((int64_t)1 << 21) - 1;
+  const uint32_t below = (1u << lane) - 1u;
+  int same = 0, holes = 0, movers = 0;                          // in the blocks so far
+  for (int base = 0; base < n; base += BLOCK) {
+    if (n > keep && n > BLOCK) load_keys(base);
+    int64_t all;
+    uint32_t stays = 0u;                                        // bit j
+    if (n > keep) {
+      int count = 0;
+#pragma unroll
+      for (int j = 0; j < PER_THREAD; ++j) {
+        if (j >= per) break;
+        count += __popc(__ballot_sync(0xffffffffu, base + mine + 32 * j < n && key[j] == last));
+      }
+      int before = same + (int)scan(count, all);
+      same += (int)all;
+#pragma unroll
+      for (int j = 0; j < PER_THREAD; ++j) {
+        if (j >= per) break;
+        const bool there = base + mine + 32 * j < n, equal = there && key[j] == last;
+        const uint32_t votes = __ballot_sync(0xffffffffu, equal);
+        if (there && (key[j] > last || (equal && before + __popc(votes & below) < equals))) stays |= 1u << j;
+        before += __popc(votes);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < PER_THREAD; ++j) {
+        if (j >= per) break;
+        if (base + mine + 32 * j < n) stays |= 1u << j;
+      }
     }
-    if (hole) ws[4 + 2 * h_before + 1] = i;
-    if (mover) ws[4 + 2 * m_before] = i;
-    if (stays && i < keep) { weights_out[i] = w; positions_out[i] = position; }
+    int64_t kinds = 0;
+#pragma unroll
+    for (int j = 0; j < PER_THREAD; ++j) {
+      if (j >= per) break;
+      const int i = base + mine + 32 * j;
+      const bool stay = stays >> j & 1u;
+      kinds += __popc(__ballot_sync(0xffffffffu, i < keep && !stay)) + ((int64_t)__popc(__ballot_sync(0xffffffffu, i >= keep && stay)) << 21);
+    }
+    const int64_t at = scan(kinds, all);
+    int hole = holes + (int)(at & MASK), mover = movers + (int)(at >> 21);
+    holes += (int)(all & MASK);
+    movers += (int)(all >> 21);
+#pragma unroll
+    for (int j = 0; j < PER_THREAD; ++j) {
+      if (j >= per) break;
+      const int i = base + mine + 32 * j;
+      const bool stay = stays >> j & 1u, is_hole = i < keep && !stay, is_mover = i >= keep && stay;
+      const uint32_t h_votes = __ballot_sync(0xffffffffu, is_hole), m_votes = __ballot_sync(0xffffffffu, is_mover);
+      if (is_hole) ws[4 + 2 * (hole + __popc(h_votes & below)) + 1] = i;
+      if (is_mover) ws[4 + 2 * (mover + __popc(m_votes & below))] = i;
+      if (stay && i < keep) {
+        weights_out[i] = weights[i];
+        positions_out[i] = positions[i];
+      }
+      hole += __popc(h_votes);
+      mover += __popc(m_votes);
+    }
   }
   if (tid == 0) ws[0] = movers;
   __syncthreads();
@@ -295,7 +356,6 @@ __global__ void __launch_bounds__(SELECT) evict_select_kernel(const EvictArgs a)
     weights_out[to] = weights[from];
     positions_out[to] = positions[from];
   }
-  mx::allow_next();
 }
 
 template <int DIM>
@@ -305,24 +365,44 @@ __global__ void __launch_bounds__(THREADS) evict_move_kernel(const EvictArgs a, 
   const int part = blockIdx.x % parts, b = (int)(row / a.cache.heads), h = (int)(row % a.cache.heads);
   const int l = threadIdx.x % LANES;
   mx::wait_for_previous();
+  mx::allow_next();
   const int* ws = a.workspace + row * evict_stride(a.keep);
   const int moves = ws[0];
-  for (int i = part * GROUPS + threadIdx.x / LANES; i < moves; i += parts * GROUPS) {
-    const int from = ws[4 + 2 * i], to = ws[4 + 2 * i + 1];
-    const int64_t from_page = a.cache.page_of(b, from), to_page = a.cache.page_of(b, to);
-    if (from_page < 0 || to_page < 0) continue;
-    const int half = l >= LANES / 2 ? HALF : 0, chunk = l % (LANES / 2);
-    const uint8_t* src = a.cache.group_at(from_page, h, from, DIM) + half;
-    uint8_t* dst = a.cache.group_at(to_page, h, to, DIM) + half;
-    const int f = from & (GROUP - 1), t = to & (GROUP - 1);
-    const uint4 codes = *reinterpret_cast<const uint4*>(src + f * (DIM / 2) + chunk * 16);
-    uint32_t p = 0u;
-    if (chunk == 0) p = *reinterpret_cast<const uint32_t*>(src + GROUP * (DIM / 2) + f * 4);
-    *reinterpret_cast<uint4*>(dst + t * (DIM / 2) + chunk * 16) = codes;
-    if (chunk == 0) *reinterpret_cast<uint32_t*>(dst + GROUP * (DIM / 2) + t * 4) = p;
+  const int half = l >= LANES / 2 ? HALF : 0, chunk = l % (LANES / 2);
+  constexpr int AT_ONCE = 4;                                   // moves whose chains of loads go side by side
+  for (int i0 = part * GROUPS + threadIdx.x / LANES; i0 < moves; i0 += AT_ONCE * parts * GROUPS) {
+    const uint8_t* src[AT_ONCE];
+    uint8_t* dst[AT_ONCE];
+    int f[AT_ONCE], t[AT_ONCE];
+#pragma unroll
+    for (int x = 0; x < AT_ONCE; ++x) {
+      const int i = i0 + x * parts * GROUPS;
+      src[x] = nullptr;
+      if (i >= moves) continue;
+      const int from = ws[4 + 2 * i], to = ws[4 + 2 * i + 1];
+      const int64_t from_page = a.cache.page_of(b, from), to_page = a.cache.page_of(b, to);
+      if (from_page < 0 || to_page < 0) continue;
+      src[x] = a.cache.group_at(from_page, h, from, DIM) + half;
+      dst[x] = a.cache.group_at(to_page, h, to, DIM) + half;
+      f[x] = from & (GROUP - 1);
+      t[x] = to & (GROUP - 1);
+    }
+    uint4 codes[AT_ONCE];
+    uint32_t p[AT_ONCE];
+#pragma unroll
+    for (int x = 0; x < AT_ONCE; ++x)
+      if (src[x]) {
+        codes[x] = *reinterpret_cast<const uint4*>(src[x] + f[x] * (DIM / 2) + chunk * 16);
+        if (chunk == 0) p[x] = *reinterpret_cast<const uint32_t*>(src[x] + GROUP * (DIM / 2) + f[x] * 4);
+      }
+#pragma unroll
+    for (int x = 0; x < AT_ONCE; ++x)
+      if (src[x]) {
+        *reinterpret_cast<uint4*>(dst[x] + t[x] * (DIM / 2) + chunk * 16) = codes[x];
+        if (chunk == 0) *reinterpret_cast<uint32_t*>(dst[x] + GROUP * (DIM / 2) + t[x] * 4) = p[x];
+      }
   }
   if (h == 0 && part == 0 && threadIdx.x == 0) a.lengths_out[b] = min(a.cache.length(b), a.keep);   // (may be the lengths themselves)
-  mx::allow_next();
 }
 
 }  // namespace

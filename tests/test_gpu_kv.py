@@ -562,6 +562,27 @@ def test_evict_long_rows_ties_and_odd_weights():
     evict_case(rng, [60, 50], 2, 64, 16, 20, 3, missing=True)
 
 
+def test_evict_rows_of_several_blocks():
+    """More slots than a CTA holds keys of (weights and positions alone: the cache has no pages)."""
+    rng = np.random.default_rng(2)
+    lengths, heads, page, keep = [70001, 32768, 32769], 2, 4096, 20000
+    table = np.full((3, 18), -1)
+    cache = on_device(kv.Cache(1, heads, 64, page, table, lengths))
+    shape = (3, heads, cache.slots)
+    weights = rng.integers(0, 5000, shape).astype(np.float32)
+    positions = np.stack([[rng.permutation(shape[2]) for _ in range(heads)] for _ in lengths]).astype(np.int32)
+    w, p = torch.from_numpy(weights).cuda(), torch.from_numpy(positions).cuda()
+    w_out, p_out, n_out = torch.zeros_like(w), torch.zeros_like(p), torch.zeros_like(cache.lengths)
+    work = torch.empty(dq.dq_kv_evict_workspace(3, heads, keep), dtype=torch.uint8, device="cuda")
+    dq.dq_kv_evict(cache, w, p, keep, 100, w_out, p_out, n_out, work)
+    assert n_out.tolist() == [keep] * 3
+    for b, n in enumerate(lengths):
+        for h in range(heads):
+            source = kv.evict(weights[b, h], positions[b, h], n, keep, 100)
+            np.testing.assert_array_equal(p_out[b, h, :keep].cpu().numpy(), positions[b, h, source])
+            np.testing.assert_array_equal(w_out[b, h, :keep].cpu().numpy(), weights[b, h, source])
+
+
 # ------------------------------------------------------------------------------------------------ together
 def test_a_decoding_loop():
     """Prompts, then tokens one by one: norm and rotation, append, attention, weights, eviction, against the oracle's cache that is
