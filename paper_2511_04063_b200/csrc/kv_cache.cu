@@ -28,38 +28,34 @@ __device__ __forceinline__ float bf16_below(float v) {
 }
 
 template <typename T>
-__device__ __forceinline__ void load16(float (&x)[16], const T* p, bool vec) {
+__device__ __forceinline__ void load16(Vec8<T>& a, Vec8<T>& b, const T* p, bool vec) {
   if (vec) {
-    Vec8<T> a, b;
     a.load(p);
     b.load(p + 8);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 u = a.pair(i), w = b.pair(i);
-      x[2 * i] = u.x; x[2 * i + 1] = u.y;
-      x[8 + 2 * i] = w.x; x[8 + 2 * i + 1] = w.y;
-    }
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = to_f32(p[i]);
+    for (int i = 0; i < 4; ++i) {
+      a.set_pair(i, make_float2(to_f32(p[2 * i]), to_f32(p[2 * i + 1])));
+      b.set_pair(i, make_float2(to_f32(p[8 + 2 * i]), to_f32(p[8 + 2 * i + 1])));
+    }
   }
 }
 template <typename T>
-__device__ __forceinline__ void store16(const float (&x)[16], T* p, bool vec) {
+__device__ __forceinline__ void store16(const float2 (&x)[8], T* p, bool vec) {
   if (vec) {
     Vec8<T> a, b;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      a.set_pair(i, make_float2(x[2 * i], x[2 * i + 1]));
-      b.set_pair(i, make_float2(x[8 + 2 * i], x[8 + 2 * i + 1]));
-    }
+    for (int i = 0; i < 4; ++i) { a.set_pair(i, x[i]); b.set_pair(i, x[4 + i]); }
     a.store(p);
     b.store(p + 8);
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] = from_f32<T>(x[i]);
+    for (int i = 0; i < 8; ++i) { p[2 * i] = from_f32<T>(x[i].x); p[2 * i + 1] = from_f32<T>(x[i].y); }
   }
 }
+
+__device__ __forceinline__ float min_nan(float a, float b) { float d; asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b)); return d; }
+__device__ __forceinline__ float max_nan(float a, float b) { float d; asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b)); return d; }
 
 // Where the tokens of a CTA lie: the first kv head's group of a token's slot (null: in no page), and whether it is a sequence's.
 struct Place { uint8_t* group; int in_group, there; };
@@ -93,17 +89,36 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const AppendArgs a, int
   const int64_t t0 = (int64_t)blockIdx.x * tile;
   const int heads = a.cache.heads, jobs = tile * 2 * heads;
   mx::wait_for_previous();
+  mx::allow_next();
   if ((int)threadIdx.x < tile) s_place[threadIdx.x] = place_of(a, t0 + threadIdx.x, DIM);
   __syncthreads();
-  for (int j0 = 0; j0 < jobs; j0 += GROUPS) {   // all lanes of a warp go round equally often
-    const int j = j0 + threadIdx.x / LANES;
-    const int i = j / (2 * heads), which = j % (2 * heads), h = which < heads ? which : which - heads;
+  struct Job { int i, which; };                                // a tile's token; a head's key, or from `heads` on its value
+  const int i_step = GROUPS / (2 * heads), which_step = GROUPS % (2 * heads);
+  auto next = [&](Job k) {
+    k.i += i_step;
+    k.which += which_step;
+    if (k.which >= 2 * heads) { k.which -= 2 * heads; ++k.i; }
+    return k;
+  };
+  Vec8<T> va, vb;                                              // the next job's values
+  auto fetch = [&](const Job& k) {
+    va.clear();
+    vb.clear();
+    if (!WRITE || k.i >= tile || !s_place[k.i].there) return;
+    const Heads& src = k.which >= heads ? a.v : a.k;
+    load16<T>(va, vb, reinterpret_cast<const T*>(src.p) + (t0 + k.i) * src.token + (k.which >= heads ? k.which - heads : k.which) * src.head + l * 16, src.vec);
+  };
+  Job job{(int)(threadIdx.x / LANES) / (2 * heads), (int)(threadIdx.x / LANES) % (2 * heads)};
+  fetch(job);
+  for (int j0 = 0; j0 < jobs; j0 += GROUPS, job = next(job)) {   // all lanes of a warp go round equally often
+    const int i = job.i, which = job.which;
     const bool value = which >= heads;
-    const Place at = j < jobs ? s_place[i] : Place{nullptr, 0, 0};
+    const int h = value ? which - heads : which;
+    const Place at = i < tile ? s_place[i] : Place{nullptr, 0, 0};
     const Heads& src = value ? a.v : a.k;
     const int64_t t = t0 + i;
     uint8_t* group = at.group ? at.group + h * a.cache.page_bytes + (value ? HALF : 0) : nullptr;
-    float x[16];
+    float2 x[8];
     if constexpr (!WRITE) {
       if (!at.there) continue;
       float scale = 0.f, offset = 0.f;
@@ -115,45 +130,60 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const AppendArgs a, int
         offset = offset_of(p);
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = __fadd_rn(offset, __fmul_rn(scale, (float)(((e < 8 ? w.x : w.y) >> (4 * (e & 7))) & 15u)));
+      for (int e = 0; e < 8; ++e) {                              // (scale times a code is exact)
+        const uint32_t c = (e < 4 ? w.x : w.y) >> (8 * (e & 3));
+        x[e] = fma2(make_float2((float)(c & 15u), (float)((c >> 4) & 15u)), both(scale), both(offset));
+      }
       store16<T>(x, reinterpret_cast<T*>(src.p) + t * src.token + h * src.head + l * 16, src.vec);
     } else {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = 0.f;
-      if (at.there) load16<T>(x, reinterpret_cast<const T*>(src.p) + t * src.token + h * src.head + l * 16, src.vec);
-      float lo = x[0], hi = x[0], most = x[0];
+      for (int e = 0; e < 4; ++e) { x[e] = va.pair(e); x[4 + e] = vb.pair(e); }
+      fetch(next(job));
+      float lo = x[0].x, hi = x[0].x;                            // NaN if any value is
 #pragma unroll
-      for (int e = 1; e < 16; ++e) {
-        lo = fminf(lo, x[e]);
-        hi = fmaxf(hi, x[e]);
-        most = mx::larger(most, x[e]);
+      for (int e = 0; e < 8; ++e) {
+        lo = min_nan(lo, min_nan(x[e].x, x[e].y));
+        hi = max_nan(hi, max_nan(x[e].x, x[e].y));
       }
 #pragma unroll
       for (int d = 1; d < LANES; d <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-        most = mx::larger(most, __shfl_xor_sync(0xffffffffu, most, d));
+        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
       }
       float offset = bf16_below(lo + 0.f);                       // (-0 becomes 0)
       float scale = 0.f - bf16_below(-((hi - offset) / 15.f));
-      const bool good = fabsf(most) <= 3.402823466e38f && scale <= 3.402823466e38f;
+      constexpr float LARGEST = 3.402823466e38f;
+      const bool good = lo >= -LARGEST && hi <= LARGEST && scale <= LARGEST;
       uint32_t w[2] = {0u, 0u};
       if (good && scale > 0.f) {
+        // A sum with 1.5 2^23 rounds to an integer, which stands in its lowest bits.  The quotient by the reciprocal is off by two
+        // roundings, 15 x 2 x 2^-24 at most: near a half, where that could decide, and where the reciprocal might be out of range, the
+        // division itself.
+        constexpr float MAGIC = 12582912.f;
+        constexpr uint32_t BITS = 0x4b400000u;
         const float inverse = 1.f / scale;
+        float2 d[8], c[8];
+        const float near = scale > 1e-36f ? 0.49999f : -1.f;
+        constexpr uint32_t ALL = BITS * 0x11111111u;             // what the eight sums' upper bits add up to
+        w[0] = w[1] = 0u - ALL;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float d = x[e] - offset;
-          // the quotient by the reciprocal is off by three roundings, 15 x 3 x 2^-24 at most: near a half, where that could
-          // decide, and where the reciprocal is out of range, the division itself
-          float q = d * inverse, c = rintf(q);
-          if (!(fabsf(fabsf(q - c) - 0.5f) > 1e-5f)) c = rintf(__fdiv_rn(d, scale));
-          w[e >> 3] |= (uint32_t)c << (4 * (e & 7));
-          x[e] = __fadd_rn(offset, __fmul_rn(scale, c));
+        for (int e = 0; e < 8; ++e) {
+          d[e] = add2(x[e], both(-offset));
+          float2 sum = fma2(d[e], both(inverse), both(MAGIC));
+          c[e] = add2(sum, both(-MAGIC));
+          const float2 rest = fma2(d[e], both(inverse), make_float2(-c[e].x, -c[e].y));
+          if (!(fmaxf(fabsf(rest.x), fabsf(rest.y)) <= near)) {   // (inputs of 16 bits often lie at a half exactly)
+            sum = make_float2(rintf(__fdiv_rn(d[e].x, scale)) + MAGIC, rintf(__fdiv_rn(d[e].y, scale)) + MAGIC);
+            c[e] = add2(sum, both(-MAGIC));
+          }
+          w[e >> 2] += __float_as_uint(sum.x) * (1u << (8 * (e & 3))) + __float_as_uint(sum.y) * (16u << (8 * (e & 3)));
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = fma2(c[e], both(scale), both(offset));
       } else {
         if (!good) scale = offset = __uint_as_float(0x7fc00000u);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = offset;
+        for (int e = 0; e < 8; ++e) x[e] = both(offset);
       }
       if (group) {
         *reinterpret_cast<uint2*>(group + at.in_group * (DIM / 2) + l * 8) = make_uint2(w[0], w[1]);
@@ -165,14 +195,13 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const AppendArgs a, int
       if (at.there && dst.p) store16<T>(x, reinterpret_cast<T*>(dst.p) + t * dst.token + h * dst.head + l * 16, dst.vec);
     }
   }
-  mx::allow_next();
 }
 
 template <bool WRITE>
 dq_status run_append(cudaStream_t stream, int dtype, int dim, const AppendArgs& a) {
-  // about two rounds of heads a CTA, so that its search of sequences and pages is worth one
-  const int groups = THREADS / (dim / 16);
-  const int tile = max(1, min(TILE, (2 * groups) / (2 * a.cache.heads)));
+  // A CTA's search of sequences and pages (a chain of five loads or so) is paid once a tile: as many tokens as leave four CTAs an SM.
+  const int64_t waves = (a.batch.tokens + TILE * 592 - 1) / (TILE * 592);
+  const int tile = (int)max((int64_t)1, min((int64_t)TILE, (a.batch.tokens + waves * 592 - 1) / (waves * 592)));
   return by_type(dtype, [&](auto t) {
     using T = decltype(t);
     return by_dim(dim, [&](auto d) {
