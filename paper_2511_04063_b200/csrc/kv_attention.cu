@@ -185,8 +185,8 @@ struct Walk {
   __device__ __forceinline__ void start(const AttentionArgs& a, const Share& share) {
     b = share.seq;
     s.describe(a, b);
-    const int64_t index = (share.lo - share.before) / s.stages;        // of the sequence's items
-    h = (int)(index / s.tiles);
+    const int64_t index = quotient(share.lo - share.before, s.stages);   // of the sequence's items
+    h = (int)quotient(index, s.tiles);
     tile = (int)(index - (int64_t)h * s.tiles);
     begin = share.before + index * s.stages;
   }
@@ -356,14 +356,14 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   mx::wait_for_previous();
   mx::allow_next();
-  find_share(&s_share, a.batch.n_seqs, LEAST_STAGES, s_sums, [&](int b) {
+  const Share share = find_share(&s_share, a.batch.n_seqs, LEAST_STAGES, s_sums, [&](int b) {
     Sequence<ROWS> s;
     s.describe(a, b);
     return s.units(a);
   });
-  const Share share = s_share;
   if (share.lo >= share.hi) return;
 
+  __syncthreads();                                                      // the barriers are ready
   Walk<ROWS> at;
   at.start(a, share);
   int slot0 = (int)(share.lo - at.begin + warp) * STAGE;                // this warp's next, within the item
@@ -791,13 +791,13 @@ __global__ void __launch_bounds__(FewWeights<DIM>::WARPS * 32, FewWeights<DIM>::
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   mx::wait_for_previous();
   mx::allow_next();
-  find_share(&s_share, a.batch.n_seqs, LEAST_STAGES, s_sums, [&](int b) {
+  const Share share = find_share(&s_share, a.batch.n_seqs, LEAST_STAGES, s_sums, [&](int b) {
     Sequence<0> s;
     s.describe(a, b);
     return s.units(a);
   });
-  const Share share = s_share;
   if (share.lo >= share.hi) return;
+  __syncthreads();                                                      // the barriers are ready
   Walk<0> at;
   at.start(a, share);
   int slot0 = (int)(share.lo - at.begin + warp) * STAGE, page = 0;
@@ -918,8 +918,7 @@ __global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_
   mx::wait_for_previous();
   mx::allow_next();
   auto share_of = [&](int keys) {
-    find_share(&s_share, a.batch.n_seqs, 1, s_sums, [&](int b) { return (int64_t)a.cache.heads * ((a.cache.length(b) + keys - 1) / keys); });
-    return s_share;
+    return find_share(&s_share, a.batch.n_seqs, 1, s_sums, [&](int b) { return (int64_t)a.cache.heads * ((a.cache.length(b) + keys - 1) / keys); });
   };
   int sets = 1;
   Share share = share_of(W::KEYS);

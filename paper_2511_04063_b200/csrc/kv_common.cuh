@@ -75,8 +75,12 @@ struct Share {
   int seq;                 // the sequence in which this CTA begins, and the units before it
   int64_t before;
 };
+// Quotients of non-negative numbers, mostly small ones (a 64-bit division is 70 instructions, a 32-bit one 20).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return (uint64_t)(a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
 // The CTA that has unit x: lo(i) = floor(i total / ctas).
-__device__ __forceinline__ int cta_of(int64_t x, int64_t total, int ctas) { return (int)(((x + 1) * ctas - 1) / total); }
+__device__ __forceinline__ int cta_of(int64_t x, int64_t total, int ctas) { return (int)quotient((x + 1) * ctas - 1, total); }
 
 // Two fp32 operations in one instruction.
 using mx::add2;
@@ -111,33 +115,47 @@ __device__ __forceinline__ uint32_t less(uint32_t w, uint32_t eight) {
 __device__ __forceinline__ uint32_t low_centred(uint32_t w) { return less(low_codes(w), 0x00080008u); }
 __device__ __forceinline__ uint32_t high_centred(uint32_t w) { return less(high_codes(w), 0x00800080u); }
 
-// Called by a whole CTA of `threads` threads.  `least`: units that are worth a CTA.
+// The share of this CTA, for all of its threads together.  `least`: units that are worth a CTA.
 template <typename F>
-__device__ void find_share(Share* out, int n_seqs, int64_t least, int64_t* warp_sums, F cost) {
-  const int tid = threadIdx.x, threads = blockDim.x, warps = threads >> 5;
+__device__ __forceinline__ Share find_share(Share* out, int n_seqs, int64_t least, int64_t* warp_sums, F cost) {
+  Share s{};
+  auto take = [&](int64_t total) {
+    s.total = total;
+    s.ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, quotient(total + least - 1, least)));
+    const int64_t i = blockIdx.x;
+    s.lo = i < s.ctas ? quotient(i * total, s.ctas) : 0;
+    s.hi = i < s.ctas ? quotient((i + 1) * total, s.ctas) : 0;
+  };
+  const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x, warps = threads >> 5;
+  auto upto = [&](int64_t sum) {                                        // the sum over the lanes up to this one
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, sum, d);
+      if (lane >= d) sum += v;
+    }
+    return sum;
+  };
+  if (n_seqs <= 32) {   // every warp for itself
+    const int64_t c = lane < n_seqs ? cost(lane) : 0, sum = upto(c);
+    take(__shfl_sync(0xffffffffu, sum, 31));
+    const uint32_t votes = __ballot_sync(0xffffffffu, c > 0 && s.lo >= sum - c && s.lo < sum);
+    s.seq = votes ? __ffs(votes) - 1 : 0;
+    s.before = __shfl_sync(0xffffffffu, sum - c, s.seq);
+    return s;
+  }
   const int64_t once = tid < n_seqs ? cost(tid) : 0;   // (kept where there are no more sequences than threads)
   int64_t base = 0;
-  Share s{};
   for (int pass = 0; pass < 2; ++pass) {
     if (pass) {
-      s.total = base;
-      s.ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, (s.total + least - 1) / least));
-      const int64_t i = blockIdx.x;
-      s.lo = i < s.ctas ? i * s.total / s.ctas : 0;
-      s.hi = i < s.ctas ? (i + 1) * s.total / s.ctas : 0;
+      take(base);
       base = 0;
     }
     for (int b0 = 0; b0 < n_seqs; b0 += threads) {
       const int b = b0 + tid;
       const int64_t c = b0 == 0 ? once : b < n_seqs ? cost(b) : 0;
-      int64_t sum = c;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int64_t v = __shfl_up_sync(0xffffffffu, sum, d);
-        if ((tid & 31) >= d) sum += v;
-      }
+      const int64_t sum = upto(c);
       __syncthreads();
-      if ((tid & 31) == 31) warp_sums[tid >> 5] = sum;
+      if (lane == 31) warp_sums[tid >> 5] = sum;
       __syncthreads();
       int64_t all = 0, mine = 0;
       for (int w = 0; w < warps; ++w) {
@@ -153,6 +171,7 @@ __device__ void find_share(Share* out, int n_seqs, int64_t least, int64_t* warp_
   }
   if (tid == 0 && s.lo >= s.hi) { s.seq = 0; s.before = 0; *out = s; }
   __syncthreads();
+  return *out;
 }
 
 inline bool pieces(const void* p, int64_t token, int64_t head, int dtype) {

@@ -127,13 +127,12 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
   mx::wait_for_previous();
   mx::allow_next();
   // an item (or a part of its keys) a CTA: the grid has at least as many
-  find_share(&s_share, a.batch.n_seqs, 1, s_sums, [&](int b) {
+  const Share share = find_share(&s_share, a.batch.n_seqs, 1, s_sums, [&](int b) {
     int64_t first;
     int n;
     a.batch.range(b, first, n);
     return (((int64_t)n * a.group + P::ROWS - 1) / P::ROWS) * a.cache.heads * splits;
   });
-  const Share share = s_share;
   if (share.lo >= share.hi) return;
   const int b = share.seq;
   int64_t first;

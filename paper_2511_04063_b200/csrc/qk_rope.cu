@@ -89,6 +89,18 @@ __global__ void __launch_bounds__(MAX_THREADS, MIN_CTAS) rope_kernel(const RopeA
   mx::allow_next();
   int j = part * groups + threadIdx.x / LANES;
   fetch(j);
+  float2 gamma[8];
+  const void* gammas_of = nullptr;                                     // whose gamma that is
+  auto fetch_gamma = [&]() {
+    const void* mine = j < q_heads ? a.q_gamma : a.k_gamma;
+    if (!mine)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) gamma[i] = both(1.f);
+    else if (a.gamma_fp32) load_gamma(gamma, reinterpret_cast<const float*>(mine), a.gamma_vec, at_a, at_b);
+    else load_gamma(gamma, reinterpret_cast<const T*>(mine), a.gamma_vec, at_a, at_b);
+    gammas_of = mine;
+  };
+  if (norm && held) fetch_gamma();
   if (half) {
     for (int i = threadIdx.x; i < half; i += blockDim.x) {
       constexpr double TURNS = 0.15915494309189533577;                  // 1 / (2 pi)
@@ -106,8 +118,6 @@ __global__ void __launch_bounds__(MAX_THREADS, MIN_CTAS) rope_kernel(const RopeA
     cosine[i] = rotated ? make_float2(s_cos[8 * l + 2 * i], s_cos[8 * l + 2 * i + 1]) : both(1.f);
     sine[i] = rotated ? make_float2(s_sin[8 * l + 2 * i], s_sin[8 * l + 2 * i + 1]) : both(0.f);
   }
-  float2 gamma[8];
-  const void* gammas_of = nullptr;                                     // whose gamma that is
   const float over = 1.f / (float)a.dim;
   const float down = hadamard ? rsqrtf((float)a.dim) : 1.f;            // (everything behind the norm is linear)
   // all lanes of a warp go round equally often: they exchange values
@@ -124,15 +134,7 @@ __global__ void __launch_bounds__(MAX_THREADS, MIN_CTAS) rope_kernel(const RopeA
 #pragma unroll
       for (int d = 1; d < LANES; d <<= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
       const float by = rsqrtf(s * over + a.eps) * down;
-      const void* mine = j < q_heads ? a.q_gamma : a.k_gamma;
-      if (held && (mine != gammas_of || first == part * groups + (int)(threadIdx.x / 32) * AT_ONCE)) {
-        if (!mine)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) gamma[i] = both(1.f);
-        else if (a.gamma_fp32) load_gamma(gamma, reinterpret_cast<const float*>(mine), a.gamma_vec, at_a, at_b);
-        else load_gamma(gamma, reinterpret_cast<const T*>(mine), a.gamma_vec, at_a, at_b);
-        gammas_of = mine;
-      }
+      if (held && (j < q_heads ? a.q_gamma : a.k_gamma) != gammas_of) fetch_gamma();
       if (held)
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = mul2(mul2(x[i], both(by)), gamma[i]);
