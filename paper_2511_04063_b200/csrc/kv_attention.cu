@@ -1050,17 +1050,28 @@ __global__ void __launch_bounds__(ManyWeights<DIM>::WARPS * 32, 1) many_weights_
   }
 }
 
-#ifndef PROMPT_ROWS
-#define PROMPT_ROWS 64
-#endif
 }  // namespace
 
 int64_t attention_workspace(int dim) {
   return TICKET_BYTES + max((int64_t)MAX_CTAS * 2 * 16 * (dim + 2), MAX_SMS * prompt_part(dim)) * 4;
 }
 
+// Which of the two: what 128 keys of every sequence take.  A CTA of prompt_kernel needs 2.6 us for them whatever part of its 256 rows
+// there is, and as its items are not of equal length about half as much again; few_kernel takes 9.5 ns for each 16 rows, balanced over
+// all SMs.  8 sequences of up to 8192 slots and 80 rows on average (8 kv heads): 169 and 121 us; 32 of 2048 (D = 64, 4 kv
+// heads): 45 and 67.  Where prompt_kernel's items are few it cuts their keys and joins the parts, which pays from 256 rows on (one
+// sequence of 16384, 8 kv heads, 128 rows: 109 and 66 us).
+static bool prompt_is_faster(const mx::Device& dev, int dim, const AttentionArgs& a) {
+  const int64_t rows = a.batch.tokens * a.group / a.batch.n_seqs, tile = dim == 256 ? 128 : 256;
+  const int64_t items = a.batch.n_seqs * a.cache.heads * ((rows + tile - 1) / tile);
+  if (rows >= 256) return true;
+  if (rows < 64 || items < dev.sms / 2) return false;
+  const int64_t sixteens = (a.batch.tokens * a.group / 16 + a.batch.n_seqs / 2) * a.cache.heads;
+  return 3900 * ((items + dev.sms - 1) / dev.sms) < sixteens * 19 / 2;
+}
+
 dq_status attention(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AttentionArgs& a) {
-  if (a.batch.tokens * a.group >= (int64_t)PROMPT_ROWS * a.batch.n_seqs) return prompt_attention(stream, dev, dtype, dim, a);
+  if (prompt_is_faster(dev, dim, a)) return prompt_attention(stream, dev, dtype, dim, a);
   auto by_rows = [&](auto t) {
     using T = decltype(t);
     const bool two = a.batch.tokens * a.group > (int64_t)8 * a.batch.n_seqs;

@@ -512,6 +512,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
 #pragma unroll 1
           for (int d = 0; d < DIM; d += 16) {
             float o[16] = {};
+#pragma unroll 4
             for (int i = 0; i < splits; ++i) {
               const float* p = parts + (int64_t)i * P::PART;
               const float pm = __ldcg(p + (int64_t)DIM * P::ROWS);
