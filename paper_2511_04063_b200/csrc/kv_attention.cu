@@ -1058,13 +1058,13 @@ int64_t attention_workspace(int dim) {
 
 // Which of the two: what 128 keys of every sequence take.  A CTA of prompt_kernel needs 2.6 us for them whatever part of its 256 rows
 // there is, and as its items are not of equal length about half as much again; few_kernel takes 9.5 ns for each 16 rows, balanced over
-// all SMs.  8 sequences of up to 8192 slots and 80 rows on average (8 kv heads): 169 and 121 us; 32 of 2048 (D = 64, 4 kv
-// heads): 45 and 67.  Where prompt_kernel's items are few it cuts their keys and joins the parts, which pays from 256 rows on (one
-// sequence of 16384, 8 kv heads, 128 rows: 109 and 66 us).
+// all SMs.  32 sequences of up to 2048 slots, 4 kv heads of 64, 80 rows on average: 44 and 68 us.  Where prompt_kernel's items are few
+// it cuts their keys and joins the parts, which pays from 128 rows on (256 for D = 256, whose items are half as large): one sequence
+// of 16384, 8 kv heads, 256 rows 72 and 106 us; 8 of up to 8192, 80 rows on average 169 and 121, 160 rows 175 and 221.
 static bool prompt_is_faster(const mx::Device& dev, int dim, const AttentionArgs& a) {
   const int64_t rows = a.batch.tokens * a.group / a.batch.n_seqs, tile = dim == 256 ? 128 : 256;
   const int64_t items = a.batch.n_seqs * a.cache.heads * ((rows + tile - 1) / tile);
-  if (rows >= 256) return true;
+  if (rows >= (dim == 256 ? 256 : 128)) return true;
   if (rows < 64 || items < dev.sms / 2) return false;
   const int64_t sixteens = (a.batch.tokens * a.group / 16 + a.batch.n_seqs / 2) * a.cache.heads;
   return 3900 * ((items + dev.sms - 1) / dev.sms) < sixteens * 19 / 2;

@@ -329,36 +329,33 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     {
       const T* p = reinterpret_cast<const T*>(a.q.p) + (first + token) * a.q.token + (int64_t)head * a.q.head;
       float most_q = 0.f, sum = 0.f;
-      auto load = [&](int w) {
-        mx::Vec8<T> x;
-        x.clear();
+      mx::Vec8<T> x[WORDS];                                             // (all of the row's loads at once)
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) {
+        x[w].clear();
         if (there) {
-          if (a.q.vec) x.load(p + w * 8);
+          if (a.q.vec) x[w].load(p + w * 8);
           else
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x.set_pair(e, make_float2(mx::to_f32(p[w * 8 + 2 * e]), mx::to_f32(p[w * 8 + 2 * e + 1])));
+            for (int e = 0; e < 4; ++e) x[w].set_pair(e, make_float2(mx::to_f32(p[w * 8 + 2 * e]), mx::to_f32(p[w * 8 + 2 * e + 1])));
         }
-        return x;
-      };
-#pragma unroll 4
-      for (int w = 0; w < WORDS; ++w) {
-        const mx::Vec8<T> x = load(w);
+      }
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float2 f = x.pair(e);
+          const float2 f = x[w].pair(e);
           sum += f.x + f.y;
           most_q = fmaxf(most_q, fmaxf(fabsf(f.x), fabsf(f.y)));
         }
-      }
       const int field = min(max((int)mx::exponent_field(most_q), 15), 244);
       const float up = __uint_as_float((uint32_t)(268 - field) << 23) * (a.scale < 0.f ? -1.f : 1.f);
       by = fmaxf(__uint_as_float((uint32_t)(field - 14) << 23) * fabsf(a.scale) * LOG2E, 1.2e-38f);   // (not zero: it meets infinities)
       sum_by = sum * up;
       const uint32_t tile = smem + P::Q_AT + m * P::TILE_BYTES;
-#pragma unroll 4
+#pragma unroll
       for (int w = 0; w < WORDS; ++w) {
-        const mx::Vec8<T> x = load(w);
-        const float2 d01 = x.pair(0), d23 = x.pair(1), d45 = x.pair(2), d67 = x.pair(3);
+        const float2 d01 = x[w].pair(0), d23 = x[w].pair(1), d45 = x[w].pair(2), d67 = x[w].pair(3);
         store16(piece_at(tile, r, w), make_uint4(half_pair(d01.x * up, d45.x * up), half_pair(d01.y * up, d45.y * up),
                                                  half_pair(d23.x * up, d67.x * up), half_pair(d23.y * up, d67.y * up)));
       }
@@ -521,7 +518,15 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
               for (int x = 0; x < 16; ++x) o[x] += __ldcg(p + (int64_t)(d + x) * P::ROWS) * f;
             }
 #pragma unroll
-            for (int x = 0; x < 16; ++x) out[d + x] = mx::from_f32<T>(o[x] * over);
+            for (int w = 0; w < 16; w += 8) {
+              mx::Vec8<T> y;
+#pragma unroll
+              for (int x = 0; x < 4; ++x) y.set_pair(x, make_float2(o[w + 2 * x] * over, o[w + 2 * x + 1] * over));
+              if (a.out.vec) y.store(out + d + w);
+              else
+#pragma unroll
+                for (int x = 0; x < 8; ++x) out[d + w + x] = mx::from_f32<T>(o[w + x] * over);
+            }
           }
         }
       }
