@@ -470,7 +470,7 @@ dq_status dq_kv_append(const dq_heads_t* K, const dq_heads_t* V, int32_t dtype, 
 dq_status dq_kv_dequantize(const dq_kv_cache_t* cache, const int32_t* d_starts, int64_t tokens, const dq_heads_t* K,
                            const dq_heads_t* V, int32_t dtype, void* cuda_stream);
 
-/* out = softmax(scale * q k^T) v over the slots that each query sees; query head j reads kv head j / (Q's heads / cache's heads).
+/* out = softmax(scale * q k^T) v over the slots that each query sees (out overlaps neither Q nor the cache); query head j reads kv head j / (Q's heads / cache's heads).
  * dtype: DQ_BF16 or DQ_FP16.  A query that sees nothing gets zeros.  d_lse (nullable, [tokens][Q's heads]): the natural logarithm of the
  * sums of exp(scale * q . k), -infinity for a query that sees nothing.  d_workspace: dq_kv_attention_workspace bytes, 16-byte
  * aligned, set to zero once before its first use (every call leaves it ready for the next); calls that overlap on the GPU need one each.

@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     a.batch.range(b, first, n);
     return (((int64_t)n * a.group + P::ROWS - 1) / P::ROWS) * a.cache.heads * splits;
   });
-  if (share.lo >= share.hi) return;
+  if (share.lo >= share.hi || share.total > gridDim.x) return;   // (more than the grid was made for: starts that decrease)
   const int b = share.seq;
   int64_t first;
   int n;
@@ -259,10 +259,12 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
       const float ks = scale_of(kp), kz = offset_of(kp) + 8.f * ks, vs = scale_of(vp), vo = offset_of(vp);
       // exponent fields of the tile's largest ks, and of what the values are divided by: vs below 2^-9, values below 2^6.  A NaN does
       // not count, and a value that is one is held as zero: not all rows may see it.
-      const bool nan = !(fabsf(vs) <= 3.402823466e38f && fabsf(vo) <= 3.402823466e38f);
-      const int k_field = (int)(kp >> 7 & 255u), spread = (int)(vp >> 7 & 255u) + 10;
+      auto nan_of = [](float v) { return !(fabsf(v) <= 3.402823466e38f); };
+      const bool nan = nan_of(vs) || nan_of(vo);
+      // (and kz within 2^91, where a tile's scales are small or zero)
+      const int k_field = nan_of(ks) || nan_of(kz) ? 0 : max((int)(kp >> 7 & 255u), (int)mx::exponent_field(kz) - 100), spread = (int)(vp >> 7 & 255u) + 10;
       const int size = (int)max(mx::exponent_field(vo), mx::exponent_field(fmaf(15.f, vs, vo))) - 4;
-      const uint32_t k_most = __reduce_max_sync(0xffffffffu, k_field == 255 ? 0u : (uint32_t)k_field);
+      const uint32_t k_most = __reduce_max_sync(0xffffffffu, (uint32_t)k_field);
       const uint32_t v_most = __reduce_max_sync(0xffffffffu, nan ? 0u : (uint32_t)max(spread, size));
       const uint32_t votes = __ballot_sync(0xffffffffu, there), odd = __ballot_sync(0xffffffffu, nan);
       if (lane == 0) {

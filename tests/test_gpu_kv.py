@@ -299,6 +299,27 @@ def test_chunks_with_missing_pages_and_values_that_are_not_numbers():
             assert bool(torch.isnan(out[50:]).all()) and bool(torch.isnan(lse[50:]).all()) == (second == 0)
 
 
+def test_chunks_over_keys_and_values_of_no_range():
+    """Keys and values whose scale is zero (all dimensions the same), of one size or many, alone in a tile of keys and among others."""
+    rng = np.random.default_rng(18)
+    for dim in (64, 128, 256):
+        c, _ = filled(rng, [400], 2, dim, 16)
+        for slot in range(400):
+            if slot < 270 or slot % 7 == 0:
+                for h in range(2):
+                    c.write(0, h, slot, 0, np.full(dim, [0.0, -3.25, 1e-3, 2.0][slot % 4] / dim ** 0.5))
+                    c.write(0, h, slot, 1, np.full(dim, [0.0, 3.25, -1e4][slot % 3]))
+        c.write(0, 1, 5, 0, np.full(dim, 1e20))                       # too large for any query that is not zero
+        cache = on_device(c)
+        q = rng.standard_normal((130, 4, dim))
+        q[:, 2:] = 0.0
+        q[129] = 1e-30
+        q = put(q, torch.bfloat16)
+        for n in (130, 2):                                            # both kernels
+            out, lse = attend(cache, q[-n:], 0.1)
+            check_attention(c, 0, q[-n:], 0, n, 2, 0.1, out, lse)
+
+
 def test_chunks_of_views():
     rng = np.random.default_rng(17)
     c, cache = filled(rng, [90], 2, 128, 16)
