@@ -491,7 +491,8 @@ def dq_kv_pages(n_pages: int, heads: int, head_dim: int, page_size: int, device=
 
 class dq_kv_cache:
     """A cache: pages (dq_kv_pages), table (int32 [n_seqs, pages of a sequence]: which page holds its tokens, -1: none) and
-    lengths (int32 [n_seqs], a call's own tokens counted).  Holds the tensors; their contents may change between calls."""
+    lengths (int32 [n_seqs], a call's own tokens counted).  Holds the tensors, whose contents may change between calls; another
+    table or other lengths are another handle."""
 
     __slots__ = ("pages", "table", "lengths", "head_dim", "page_size", "heads", "n_seqs", "slots", "_struct", "_call")
 
@@ -508,11 +509,15 @@ class dq_kv_cache:
             raise ValueError("pages: %d bytes are no page of heads of %r values" % (pages.shape[2], head_dim))
         if pages.shape[1] < 1 or table.shape[1] < 1:
             raise ValueError("a cache has at least one head, and a table at least one column")
-        self.pages, self.table, self.lengths, self.head_dim, self.page_size = pages, table, lengths, head_dim, page_size
-        self.heads, self.n_seqs, self.slots = pages.shape[1], table.shape[0], table.shape[1] * page_size
-        self._struct = dq_kv_cache_t(pages.data_ptr(), pages.shape[0], table.data_ptr(), lengths.data_ptr(), table.shape[0],
-                                     table.shape[1], pages.shape[1], head_dim, page_size)
-        self._call = (C.addressof(self._struct), pages.get_device())
+        struct = dq_kv_cache_t(pages.data_ptr(), pages.shape[0], table.data_ptr(), lengths.data_ptr(), table.shape[0],
+                               table.shape[1], pages.shape[1], head_dim, page_size)
+        for name, value in (("pages", pages), ("table", table), ("lengths", lengths), ("head_dim", head_dim), ("page_size", page_size),
+                            ("heads", pages.shape[1]), ("n_seqs", table.shape[0]), ("slots", table.shape[1] * page_size),
+                            ("_struct", struct), ("_call", (C.addressof(struct), pages.get_device()))):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        raise AttributeError("%s of a cache is fixed: make another handle" % name)
 
 
 def dq_qk_norm_rope(Q, K, positions, inv_freq, Q_out, K_out, q_gamma=None, k_gamma=None, eps: float = 1e-6, flags: int = DQ_QK_NORM,

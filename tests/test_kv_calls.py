@@ -246,3 +246,5 @@ def test_the_handle_checks_its_tensors(lib):
         dq.dq_kv_cache(pages, table, lengths, 128)               # not on a device
     with pytest.raises(ValueError, match="pages of"):
         dq.dq_kv_pages(4, 2, 96, 16)
+    with pytest.raises(AttributeError, match="fixed"):
+        dq.dq_kv_cache.__setattr__(object.__new__(dq.dq_kv_cache), "lengths", lengths)
