@@ -414,8 +414,8 @@ dq_status dq_mx_selftest_bounded_wait(int32_t a_fmt, const void* d_a_codes, cons
  * A head of a token with a NaN, an infinity or a range past fp32's gets NaN parameters and reads back as NaN.  d_pages: 128-byte
  * aligned.
  * d_table [n_seqs][table_width]: the pages of a sequence, in order; an index outside [0, n_pages) is no page: what would be
- * written there is dropped, and keys there take no part.  Pages may be shared between sequences as long as no call writes to
- * one from two.  d_lengths [n_seqs]: tokens (slots) of a sequence, those of the call included; taken as 0 where negative and as
+ * written there is dropped, and keys there take no part.  Pages may be shared between sequences as long as no call writes
+ * to one that the table names twice.  d_lengths [n_seqs]: tokens (slots) of a sequence, those of the call included; taken as 0 where negative and as
  * table_width * page_size (at most 2^30) where above.  Both are read on the device when the call runs.
  * Tokens of a call: sequence b has rows d_starts[b] .. d_starts[b + 1] - 1 of the call's tensors (d_starts [n_seqs + 1], not
  * decreasing), or tokens / n_seqs each where d_starts is NULL.  They are its last: token i of n has slot length - n + i, and
@@ -470,11 +470,13 @@ dq_status dq_kv_append(const dq_heads_t* K, const dq_heads_t* V, int32_t dtype, 
 dq_status dq_kv_dequantize(const dq_kv_cache_t* cache, const int32_t* d_starts, int64_t tokens, const dq_heads_t* K,
                            const dq_heads_t* V, int32_t dtype, void* cuda_stream);
 
-/* out = softmax(scale * q k^T) v over the slots that each query sees (out overlaps neither Q nor the cache); query head j reads kv head j / (Q's heads / cache's heads).
+/* out = softmax(scale * q k^T) v over the slots that each query sees; query head j reads kv head j / (Q's heads / cache's heads).
  * dtype: DQ_BF16 or DQ_FP16.  A query that sees nothing gets zeros.  d_lse (nullable, [tokens][Q's heads]): the natural logarithm of the
  * sums of exp(scale * q . k), -infinity for a query that sees nothing.  d_workspace: dq_kv_attention_workspace bytes, 16-byte
  * aligned, set to zero once before its first use (every call leaves it ready for the next); calls that overlap on the GPU need one each.
- * Results do not depend on the run. */
+ * out overlaps neither Q nor the cache.  Results do not depend on the run.  Products take 16-bit operands and fp32 sums; queries that
+ * are worked on together share a power of two for the keys and one for the values, so a key or value whose scale is 2^20 times below
+ * the largest in its sequence loses digits. */
 dq_status dq_kv_attention(const dq_heads_t* Q, int32_t dtype, int64_t tokens, const dq_kv_cache_t* cache, const int32_t* d_starts,
                           float scale, const dq_heads_t* out, float* d_lse, void* d_workspace, void* cuda_stream);
 

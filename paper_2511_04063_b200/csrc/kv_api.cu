@@ -82,7 +82,9 @@ int64_t dq_kv_page_bytes(int32_t page_size, int32_t head_dim) {
 int64_t dq_kv_attention_workspace(int32_t head_dim) { return cache_dim(head_dim) ? kv::attention_workspace(head_dim) : -1; }
 
 int64_t dq_kv_evict_workspace(int32_t n_seqs, int32_t heads, int32_t keep) {
-  return n_seqs < 0 || heads <= 0 || heads > 65536 || keep <= 0 ? -1 : (int64_t)n_seqs * heads * kv::evict_stride(keep) * 4;
+  if (n_seqs < 0 || heads <= 0 || heads > 65536 || keep <= 0) return -1;
+  const int64_t rows = (int64_t)n_seqs * heads, each = kv::evict_stride(keep) * 4;
+  return rows > MAX_TOKENS || rows > INT64_MAX / each ? -1 : rows * each;
 }
 
 dq_status dq_qk_norm_rope(const dq_heads_t* Q, const dq_heads_t* K, int32_t dtype, int64_t tokens, int32_t head_dim,
@@ -182,6 +184,7 @@ dq_status dq_kv_evict(const dq_kv_cache_t* cache, const float* d_weights, const 
   DQ_CHECK(cache_of(cache, a.cache));
   if (keep <= 0 || recent < 0 || recent > keep || ld_slots < (int64_t)cache->table_width * cache->page_size) return DQ_ERR_INVALID_ARG;
   if (cache->n_seqs == 0) return DQ_OK;
+  if (dq_kv_evict_workspace(cache->n_seqs, cache->heads, keep) < 0) return DQ_ERR_UNSUPPORTED;
   if (!d_weights || !d_positions || !d_weights_out || !d_positions_out || !d_lengths_out || !d_workspace) return DQ_ERR_INVALID_ARG;
   if (!aligned(d_weights, 4) || !aligned(d_positions, 4) || !aligned(d_weights_out, 4) || !aligned(d_positions_out, 4) ||
       !aligned(d_lengths_out, 4) || !aligned(d_workspace, 4))

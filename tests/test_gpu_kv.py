@@ -346,6 +346,14 @@ def test_attention_of_many_sequences():
     attention_case(11, lengths, [1] * 1200, 1, 2, 64, 16, torch.float16)
 
 
+@pytest.mark.parametrize("n_seqs", (40, 600))
+def test_chunks_of_many_sequences(n_seqs):
+    """More sequences than a warp, and than a CTA, has threads, with 128 rows and more of each on average, some without any."""
+    queries = [(0, 17, 18, 16, 33)[i % 5] for i in range(n_seqs)]
+    lengths = [n + (i % 4) * 9 if i % 7 else n // 2 for i, n in enumerate(queries)]
+    attention_case(12, lengths, queries, 1, 8, 64, 16, torch.bfloat16)
+
+
 @pytest.mark.parametrize("dtype", HALVES)
 def test_attention_with_large_logits(dtype):
     """Logits of some hundreds: one key takes nearly all; and keys far from zero."""
@@ -512,6 +520,23 @@ def test_weights_of_a_long_axis_and_of_many_sequences():
     weights_case(2, [(5 * i) % 19 for i in range(600)], [1] * 600, 1, 1, 64, 16, torch.float16)
 
 
+@pytest.mark.parametrize("n_seqs,n,group", [(40, 3, 8), (600, 3, 8), (34, 66, 8), (3, 70, 16)])
+def test_weights_of_chunks_of_many_sequences(n_seqs, n, group):
+    """By every number of CTAs that share a block of keys; sequences without queries keep their weights."""
+    queries = [0 if i % 9 == 8 else n + i % 3 for i in range(n_seqs)]
+    weights_case(3, [q + (i % 5) * 11 for i, q in enumerate(queries)], queries, 1, group, 64, 16, torch.bfloat16)
+
+
+def test_weights_without_tokens():
+    rng = np.random.default_rng(4)
+    _, cache = filled(rng, [20, 0, 33], 2, 64, 16)
+    old, out = torch.rand((3, 2, cache.slots), device="cuda"), torch.full((3, 2, cache.slots), 77.0, device="cuda")
+    dq.dq_kv_attention_weights(torch.empty((0, 4, 64), dtype=torch.bfloat16, device="cuda"), torch.empty((0, 4), device="cuda"), cache, 0.1, out,
+                               weights=old)
+    for b, length in enumerate((20, 0, 33)):
+        assert torch.equal(out[b, :, :length], old[b, :, :length]) and bool((out[b, :, length:] == 77).all())
+
+
 # ------------------------------------------------------------------------------------------------ eviction
 def evict_case(rng, lengths, heads, dim, page, keep, recent, weights=None, positions=None, in_place=False, missing=False):
     c, _ = filled(rng, lengths, heads, dim, page)
@@ -650,3 +675,56 @@ def test_a_decoding_loop():
             for h in range(heads):
                 kept = set(held[b, h, :int(cache.lengths[b])].tolist())
                 assert set(range(seen[b] - recent, seen[b])) <= kept
+
+
+@pytest.mark.parametrize("tokens", (1, 40))
+def test_the_operators_captured_together(tokens):
+    """A step of all operators replayed, as it runs by itself on the current stream and on another: the same bytes."""
+    rng = np.random.default_rng(22)
+    heads, group, dim, page, keep, n_seqs = 2, 4, 128, 16, 96, 3
+    table, n_pages = table_of(rng, [keep + 2 * tokens] * n_seqs, page)
+    x = [put(rng.standard_normal((n_seqs * tokens, (group + 2) * heads, dim)), torch.bfloat16) for _ in range(6)]
+    freq = torch.from_numpy((10000.0 ** (-np.arange(dim // 2) / (dim // 2))).astype(np.float32)).cuda()
+
+    class State:
+        def __init__(self):
+            self.cache = on_device(kv.Cache(n_pages, heads, dim, page, table, [0] * n_seqs, 0))
+            self.x = torch.empty_like(x[0])
+            self.positions = (torch.arange(tokens, dtype=torch.int32).repeat(n_seqs) - tokens).cuda()
+            self.weights = torch.zeros((n_seqs, heads, self.cache.slots), device="cuda")
+            self.held = torch.zeros((n_seqs, heads, self.cache.slots), dtype=torch.int32, device="cuda")
+            self.out = torch.empty_like(x[0][:, :group * heads])
+            self.lse = torch.empty((n_seqs * tokens, group * heads), device="cuda")
+            self.work, self.evict_work = workspace(dim), torch.empty(dq.dq_kv_evict_workspace(n_seqs, heads, keep), dtype=torch.uint8, device="cuda")
+
+        def step(self, stream=None):
+            q, k, v = self.x[:, :group * heads], self.x[:, group * heads:-heads], self.x[:, -heads:]
+            self.positions.add_(tokens)
+            self.cache.lengths.add_(tokens)
+            dq.dq_qk_norm_rope(q, k, self.positions, freq, q, k, flags=dq.DQ_QK_NORM | dq.DQ_QK_HADAMARD, stream=stream)
+            dq.dq_kv_append(k, v, self.cache, positions=self.positions, slot_positions=self.held, stream=stream)
+            dq.dq_kv_attention(q, self.cache, 0.1, self.out, self.work, lse=self.lse, stream=stream)
+            dq.dq_kv_attention_weights(q, self.lse, self.cache, 0.1, self.weights, weights=self.weights, stream=stream)
+            dq.dq_kv_evict(self.cache, self.weights, self.held, keep, 8, self.weights, self.held, self.cache.lengths, self.evict_work, stream=stream)
+
+        def all(self):
+            return [self.cache.pages, self.cache.lengths, self.weights, self.held, self.out, self.lse]
+
+    eager, other, replayed = State(), State(), State()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        replayed.step()
+    for data in x * (4 if tokens > 1 else 20):
+        eager.x.copy_(data)
+        eager.step()
+        with torch.cuda.stream(side):
+            other.x.copy_(data)
+            other.step(side)
+        replayed.x.copy_(data)
+        graph.replay()
+    torch.cuda.synchronize()
+    assert eager.cache.lengths.tolist() == [keep] * n_seqs
+    for one, two, three in zip(eager.all(), other.all(), replayed.all()):
+        assert torch.equal(one, two) and torch.equal(one, three)
+    assert dq.dq_mx_status() == dq.DQ_OK and dq.dq_mx_status(side) == dq.DQ_OK

@@ -34,6 +34,9 @@ def test_sizes_and_structs(lib):
     for bad in (dq.dq_kv_page_bytes(8, 128), dq.dq_kv_page_bytes(48, 128), dq.dq_kv_page_bytes(8192, 128), dq.dq_kv_page_bytes(16, 96),
                 dq.dq_kv_attention_workspace(32), dq.dq_kv_evict_workspace(1, 0, 4), dq.dq_kv_evict_workspace(1, 1, 0)):
         assert bad == -1
+    most = 2 ** 31 - 1
+    assert dq.dq_kv_evict_workspace(most, 2, 4) == -1 and dq.dq_kv_evict_workspace(2 ** 30, 1, most) == -1
+    assert dq.dq_kv_evict_workspace(2 ** 20, 1, most) == 2 ** 20 * (4 + 2 * most) * 4
     assert C.sizeof(dq.dq_heads_t) == 32 and C.sizeof(dq.dq_kv_cache_t) == 56
     assert dq.dq_heads_t.heads.offset == 24 and dq.dq_kv_cache_t.n_seqs.offset == 32
 
@@ -90,6 +93,7 @@ def test_attention_weights_and_eviction_refuse(lib):
     e = lambda keep=4, recent=2, ld=48, work=A, lengths=A: lib.dq_kv_evict(cache(), A, A, ld, keep, recent, A, A, lengths, work, None)  # noqa: E731
     assert e(keep=0) == BAD and e(recent=-1) == BAD and e(recent=5) == BAD and e(ld=47) == BAD and e(work=None) == BAD
     assert e(lengths=None) == BAD and e(lengths=A + 1) == BAD
+    assert lib.dq_kv_evict(cache(n_seqs=2 ** 30, heads=1), A, A, 48, 2 ** 31 - 1, 2, A, A, A, A, None) == NOT_HERE
     assert lib.dq_kv_evict(cache(n_seqs=0, table=None, lengths=None), A, A, 48, 4, 2, A, A, A, A, None) == OK
 
 
