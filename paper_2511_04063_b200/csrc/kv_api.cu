@@ -117,7 +117,7 @@ dq_status dq_qk_norm_rope(const dq_heads_t* Q, const dq_heads_t* K, int32_t dtyp
   a.positions = d_positions; a.inv_freq = d_inv_freq;
   a.q_gamma = d_q_gamma; a.k_gamma = d_k_gamma; a.gamma_fp32 = gamma_dtype == DQ_FP32;
   a.eps = eps; a.flags = flags;
-  return kv::rope((cudaStream_t)cuda_stream, dtype, a);
+  return kv::rope((cudaStream_t)cuda_stream, dev, dtype, a);
 }
 
 dq_status dq_kv_append(const dq_heads_t* K, const dq_heads_t* V, int32_t dtype, int64_t tokens, const dq_kv_cache_t* cache,

@@ -203,7 +203,7 @@ struct RopeArgs {
   int gamma_fp32, gamma_vec, flags, splits;
   float eps;
 };
-dq_status rope(cudaStream_t stream, int dtype, const RopeArgs& a);
+dq_status rope(cudaStream_t stream, const mx::Device& dev, int dtype, const RopeArgs& a);
 
 struct AppendArgs {
   Heads k, v, k_values, v_values;
