@@ -1,7 +1,7 @@
 // Attention over a key/value cache in 4 bits for many query rows (a prompt's chunk), on the tensor cores' tcgen05 instructions.
 //
 // A CTA takes 256 query rows (D = 256: 128) of a sequence and kv head, in tiles of M = 128, and goes over the keys 128 at a time:
-//     S = Q K^T (128 x 128, tensor memory),  P = exp(S - m) (fp16, over S in tensor memory),  O += P V (tensor memory)
+//     S = Q K^T (128 x 128, tensor memory),  P = exp(S - m) (fp16, tensor memory),  O += P V (tensor memory)
 // Four bits become 16 on their way from global to shared memory.  A code alone is the fp16 subnormal c 2^-24, and one multiply-add
 // makes it  ks (c - 8)  for a key, exactly: 8 bits of scale times 3 of code.  What is left of a key, (ko + 8 ks) times the sum of the query,
 // is added to the score in fp32.  A value becomes  vs c + vo,  rounded to fp16 (2^-12, as P is).  Parameters are applied here, by a
@@ -12,8 +12,14 @@
 // of it.  Keys and values have the same layout, [token][64 dimensions], read K-major by the first product and MN-major by the second.
 //
 // Warps: four for each tile of rows (a thread a row: scores, exponentials, P, O's rescaling), four that unpack (a thread a key), one
-// that issues the products.  While one tile's rows are in the softmax the other's products run.  4096 queries of 32 heads over 16384
-// slots: 570 us of products at the measured rate, 430 us of exponentials at 16 a cycle and SM.
+// that issues the products.  While one tile's rows are in the softmax the other's products run.  The two tiles share one place for S,
+// which is free again as soon as its rows have it in registers, so that a tile's next scores are there when its softmax is done (P over
+// S, and the next scores behind its product: 1110 us for the case below instead of 1061; a warp for each tile's products 1577, because
+// instructions of two sums take turns; S in halves of 64 keys with a place each 1353: 64 columns take as long as 128).
+//
+// 4096 queries of 32 heads of 128 over 16384 slots: 1061 us, 907 TFLOP/s, 54 % of the measured rate; 570 us of products at that rate
+// (562 measured with nothing between them) and 430 us of exponentials at 16 a cycle and SM.  Without exponentials 1020 us, without the
+// unpackers' stores 980, without both and all reads of scores 794: what is left is the way from product to softmax and back.
 #include "kv_common.cuh"
 #include "tc_gemm.cuh"
 
@@ -37,7 +43,7 @@ struct Prompt {
   static constexpr int TILE_BYTES = 128 * DIM * 2, BOX = 128 * 128;    // a box: 128 rows of 64 values
   static constexpr int Q_AT = 0, K_AT = TILES * TILE_BYTES, V_AT = K_AT + STAGES * TILE_BYTES, END = V_AT + STAGES * TILE_BYTES;
   static constexpr int SMEM = END + 1024;
-  static constexpr uint32_t O_COLUMN = TILES * 128;                    // of tensor memory, behind the scores
+  static constexpr uint32_t P_COLUMN = KEYS, O_COLUMN = 2 * KEYS;      // of tensor memory, behind the scores of one tile
   static constexpr int PART = ROWS * (DIM + 2);
 };
 
@@ -88,7 +94,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
   constexpr int TILES = P::TILES, STAGES = P::STAGES, WORDS = DIM / 8;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(16) Params s_params[STAGES];
-  __shared__ __align__(8) uint64_t s_bars[2 + 4 * STAGES + 4 * TILES];
+  __shared__ __align__(8) uint64_t s_bars[3 + (2 + 2 * TILES) * STAGES + 2 * TILES];
   __shared__ uint32_t s_tmem;
   __shared__ uint32_t s_keys[2][4], s_values[2][4];
   __shared__ int s_odd[2][4];
@@ -100,27 +106,28 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
   auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
   const uint32_t q_full = bar(0), drained = bar(1);
   auto k_full = [&](int s) { return bar(2 + s); };
-  auto k_empty = [&](int s) { return bar(2 + STAGES + s); };
-  auto v_full = [&](int s) { return bar(2 + 2 * STAGES + s); };
-  auto v_empty = [&](int s) { return bar(2 + 3 * STAGES + s); };
-  auto s_full = [&](int m) { return bar(2 + 4 * STAGES + m); };
-  auto p_full = [&](int m) { return bar(2 + 4 * STAGES + TILES + m); };
-  auto pv_done = [&](int m) { return bar(2 + 4 * STAGES + 2 * TILES + m); };
-  auto p_half = [&](int m) { return bar(2 + 4 * STAGES + 3 * TILES + m); };
+  auto v_full = [&](int s) { return bar(2 + STAGES + s); };
+  // of a tile of rows and a stage: the scores are there, and the keys read; the values' product is done, and P and the values read
+  auto s_full = [&](int m, int s) { return bar(2 + 2 * STAGES + m * STAGES + s); };
+  auto pv_done = [&](int m, int s) { return bar(2 + 2 * STAGES + (TILES + m) * STAGES + s); };
+  auto p_half = [&](int m) { return bar(2 + (2 + 2 * TILES) * STAGES + m); };
+  auto p_full = [&](int m) { return bar(2 + (2 + 2 * TILES) * STAGES + TILES + m); };
+  const uint32_t s_taken = bar(2 + (2 + 2 * TILES) * STAGES + 2 * TILES);   // the scores are in registers
   if (tid == 0) {
     tc::mbar_init(q_full, 4 * TILES);
     tc::mbar_init(drained, 1);
+    tc::mbar_init(s_taken, 4);
     for (int s = 0; s < STAGES; ++s) {
       tc::mbar_init(k_full(s), 4);
-      tc::mbar_init(k_empty(s), 1);
       tc::mbar_init(v_full(s), 4);
-      tc::mbar_init(v_empty(s), 1);
+      for (int m = 0; m < TILES; ++m) {
+        tc::mbar_init(s_full(m, s), 1);
+        tc::mbar_init(pv_done(m, s), 1);
+      }
     }
     for (int m = 0; m < TILES; ++m) {
-      tc::mbar_init(s_full(m), 1);
       tc::mbar_init(p_half(m), 4);
       tc::mbar_init(p_full(m), 4);
-      tc::mbar_init(pv_done(m), 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -157,63 +164,57 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     if (warp == P::ISSUE) {
       auto wait = [&](uint32_t at, int phase) { return __all_sync(0xffffffffu, tc::mbar_wait(at, (uint32_t)phase & 1u, a.d_status)); };
       constexpr uint32_t SCORES = idesc_f16(KEYS), VALUES = idesc_f16(DIM) | tc::IDESC_B_MN_MAJOR;
-      auto scores = [&](int m, int i) {
+      const int items = key_tiles * TILES;
+      auto scores = [&](int item) {                                     // of tiles (item / TILES) of keys and (item % TILES) of rows
+        const int i = item / TILES, m = item % TILES, s = i % STAGES;
+        if (m == 0) ok = wait(k_full(s), i / STAGES);
+        if (item > 0) ok = ok && wait(s_taken, item - 1);
+        if (!ok) return;
+        tc::tc_fence_after();
         const uint64_t q = tc::make_kmajor_sw128_desc(smem + P::Q_AT + m * P::TILE_BYTES);
-        const uint64_t k = tc::make_kmajor_sw128_desc(smem + P::K_AT + (i % STAGES) * P::TILE_BYTES);
+        const uint64_t k = tc::make_kmajor_sw128_desc(smem + P::K_AT + s * P::TILE_BYTES);
         if (elect_one()) {
 #pragma unroll
-          for (int s = 0; s < DIM / 16; ++s) {
-            const uint32_t step = ((s >> 2) * P::BOX + (s & 3) * 32) >> 4;
-            mma_ss(tmem + m * 128, q + step, k + step, SCORES, s > 0);
+          for (int x = 0; x < DIM / 16; ++x) {
+            const uint32_t step = ((x >> 2) * P::BOX + (x & 3) * 32) >> 4;
+            mma_ss(tmem, q + step, k + step, SCORES, x > 0);
           }
-          tc::umma_commit(s_full(m));
+          tc::umma_commit(s_full(m, s));
         }
         __syncwarp();
       };
-      auto commit = [&](uint32_t at) {
-        if (elect_one()) tc::umma_commit(at);
-        __syncwarp();
-      };
-      if (key_tiles > 0) ok = wait(q_full, 0) && wait(k_full(0), 0);
-      tc::tc_fence_after();
-      if (ok && key_tiles > 0) {
-        for (int m = 0; m < TILES; ++m) scores(m, 0);
-        commit(k_empty(0));
+      if (items > 0) {
+        ok = wait(q_full, 0);
+        for (int item = 0; item < 2 * TILES - 1 && item < items && ok; ++item) scores(item);
       }
       for (int i = 0; i < key_tiles && ok; ++i) {
-        const int s = i % STAGES, s1 = (i + 1) % STAGES;
+        const int s = i % STAGES;
         const uint64_t v = tc::make_mnmajor_sw128_desc(smem + P::V_AT + s * P::TILE_BYTES, P::BOX);
         ok = wait(v_full(s), i / STAGES);
         for (int m = 0; m < TILES && ok; ++m) {
-          auto values = [&](int half, uint32_t done) {
+          auto values = [&](int half) {
             tc::tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-              for (int k = 4 * half; k < 4 * half + 4; ++k)
-                mma_ts(tmem + P::O_COLUMN + m * DIM, tmem + m * 128 + (k >> 1) * 32 + (k & 1) * 8, v + ((k * 16 * 128) >> 4), VALUES, i > 0 || k > 0);
-              if (half) tc::umma_commit(done);
+              for (int x = 4 * half; x < 4 * half + 4; ++x)
+                mma_ts(tmem + P::O_COLUMN + m * DIM, tmem + P::P_COLUMN + m * (KEYS / 2) + x * 8, v + ((x * 16 * 128) >> 4), VALUES, i > 0 || x > 0);
+              if (half) tc::umma_commit(pv_done(m, s));
             }
             __syncwarp();
           };
           ok = wait(p_half(m), i);                                      // the first keys' P, while the others' is formed
           if (!ok) break;
-          values(0, 0u);
+          values(0);
           ok = wait(p_full(m), i);
           if (!ok) break;
-          values(1, pv_done(m));
-          __syncwarp();
-          if (m == TILES - 1) commit(v_empty(s));
-          if (i + 1 < key_tiles) {   // the next scores go over this P: it has to have been read
-            if (m == 0) ok = wait(k_full(s1), (i + 1) / STAGES);
-            ok = ok && wait(pv_done(m), i);
-            if (!ok) break;
-            tc::tc_fence_after();
-            scores(m, i + 1);
-            if (m == TILES - 1) commit(k_empty(s1));
-          }
+          values(1);
+          // (of two tiles, these rows have their next scores already, the other's have not)
+          const int next = i * TILES + m + 2 * TILES - 1;
+          if (next < items) scores(next);
         }
       }
-      commit(drained);   // nothing is in flight when tensor and shared memory are given up
+      if (elect_one()) tc::umma_commit(drained);   // nothing is in flight when tensor and shared memory are given up
+      __syncwarp();
       ok = wait(drained, 0) && ok;
     }
   } else if (warp >= P::UNPACK) {   // ---------------------------------------- codes to operands
@@ -287,7 +288,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
       const float k_by = __uint_as_float((244u - key_field) << 23), v_by = __uint_as_float((254u - field) << 23);
       const uint32_t k_tile = smem + P::K_AT + s * P::TILE_BYTES, v_tile = smem + P::V_AT + s * P::TILE_BYTES;
       constexpr float LOW = 16777216.f, HIGH = 1048576.f;               // 2^24 and 2^20: of the codes
-      ok = ok && wait(k_empty(s), turn + 1);
+      ok = ok && wait(s_full(TILES - 1, s), turn + 1);
       {
         const float by = ks * k_by;
         const __half2 low = __float2half2_rn(by * LOW), high = __float2half2_rn(by * HIGH), offset = __float2half2_rn(-8.f * by);
@@ -297,7 +298,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
       fence_async();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(k_full(s));
-      ok = ok && wait(v_empty(s), turn + 1);
+      ok = ok && wait(pv_done(TILES - 1, s), turn + 1);
       Params& p = s_params[s];
       p.kz[t] = kz * k_by;
       if (t == 0) {
@@ -324,7 +325,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     const bool there = row < rows;
     const int token = there ? a.token_of(row) : 0, head = h * a.group + (there ? row - token * a.group : 0);
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t s_at = tmem + lanes + m * 128, o_at = tmem + lanes + P::O_COLUMN + m * DIM;
+    const uint32_t s_at = tmem + lanes, p_at = tmem + lanes + P::P_COLUMN + m * (KEYS / 2), o_at = tmem + lanes + P::O_COLUMN + m * DIM;
     auto wait = [&](uint32_t at, int phase) { return __all_sync(0xffffffffu, tc::mbar_wait(at, (uint32_t)phase & 1u, a.d_status)); };
     // the row into shared memory, times a power of two that brings its largest value to 2^14, and with the scale's sign
     float by, sum_by;
@@ -374,7 +375,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     bool odd = false;                                                   // the row sees a value that is a NaN
     for (int i = 0; i < key_tiles && ok; ++i) {
       const int s = i % STAGES, slot0 = (tile0 + i) * KEYS;
-      ok = wait(v_full(s), i / STAGES) && wait(s_full(m), i);
+      ok = wait(v_full(s), i / STAGES) && wait(s_full(m, s), i / STAGES);
       if (!ok) break;
       tc::tc_fence_after();
       const Params& p = s_params[s];
@@ -384,10 +385,12 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
 #pragma unroll
       for (int c = 0; c < 4; ++c) tc::tmem_ld32(s_at + 32 * c, raw[c]);
       float2 x[KEYS / 2];                                               // scores, without `tile_by`
-      float now = -INFINITY;
       const float tile_by = by * p.grow;
       odd |= p.odd < sees;
       tc::tmem_ld_wait();
+      tc::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(s_taken);
 #pragma unroll
       for (int e = 0; e < KEYS / 4; ++e) {
         const float4 kz = *reinterpret_cast<const float4*>(p.kz + 4 * e);
@@ -402,9 +405,16 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
           if (none || slot0 + 2 * e >= sees) x[e].x = -INFINITY;
           if (none || slot0 + 2 * e + 1 >= sees) x[e].y = -INFINITY;
         }
+      // (four chains: in one, each maximum waits for the one before)
+      float most_of[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-      for (int e = 0; e < KEYS / 2; ++e) now = fmaxf(now, fmaxf(x[e].x, x[e].y));
-      now *= tile_by;
+      for (int e = 0; e < KEYS / 2; ++e) most_of[e & 3] = fmaxf(most_of[e & 3], fmaxf(x[e].x, x[e].y));
+      const float now = fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3])) * tile_by;
+      if (i > 0) {   // P and O are this thread's again
+        ok = wait(pv_done(m, (i - 1) % STAGES), (i - 1) / STAGES);
+        if (!ok) break;
+        tc::tc_fence_after();
+      }
       const uint32_t wider = p.field - field;
       field = p.field;
       if (__any_sync(0xffffffffu, now > top + SLACK) || wider) {
@@ -436,7 +446,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
           sum = add2(sum, q);
           packed[e] = half_pair(q.x, q.y);
         }
-        tmem_st16(s_at + 32 * c, packed);
+        tmem_st16(p_at + 16 * c, packed);
         if (c & 1) {
           tmem_st_wait();
           tc::tc_fence_before();
@@ -445,7 +455,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
         }
       }
     }
-    if (ok && key_tiles > 0) ok = wait(pv_done(m), key_tiles - 1);
+    if (ok && key_tiles > 0) ok = wait(pv_done(m, (key_tiles - 1) % STAGES), (key_tiles - 1) / STAGES);
     tc::tc_fence_after();
     if (ok) {
       const float l = sum.x + sum.y;
