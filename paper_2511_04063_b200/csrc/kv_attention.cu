@@ -320,7 +320,7 @@ struct Stream {
 // its own: while it works on one the other is on its way, across items too.  An item that crosses CTAs is left in the workspace in parts,
 // and the CTA that finishes last joins them, in order.
 //
-// Bound by the integer pipe that takes codes apart (48 % of its cycles) and the issue of instructions (54 %) where the cache is long:
+// Bound by the integer pipe that takes codes apart (56 % of its cycles) and the issue of instructions (54 %) where the cache is long:
 // 64 ragged sequences up to 16384 slots, 8 kv heads of 128, 171 us, 4.2 TB/s.  131072 slots of one sequence: 46.5 us, 3.1 TB/s, of which
 // 10 are start and join.  1024 slots: 10.9 us, a chain of table, codes, products, ticket and parts.
 template <int DIM, int NT>

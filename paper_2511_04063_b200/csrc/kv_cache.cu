@@ -9,7 +9,7 @@
 // Bound by HBM and instructions alike: 2 D bytes read and D / 2 + 4 written for each key and each value in 16 bits (and 2 D where the
 // values that the codes stand for are asked for).  A lane takes 16 values, D / 16 lanes a head; a CTA takes some tokens, for which it
 // finds sequence, slot and page first.  12 prompts of up to 2048 tokens, 40 heads of 128, fp16, with the values: 151 us, 4.8 TB/s, a
-// scheduler issues 58 % of the time (207 us without the next head's values on their way and the packed arithmetic).
+// scheduler issues 70 % of the time (207 us without the next head's values on their way and the packed arithmetic).
 #include "kv_common.cuh"
 
 namespace dq {

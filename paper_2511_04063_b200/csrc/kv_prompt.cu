@@ -17,7 +17,7 @@
 // S, and the next scores behind its product: 1110 us for the case below instead of 1061; a warp for each tile's products 1577, because
 // instructions of two sums take turns; S in halves of 64 keys with a place each 1353: 64 columns take as long as 128).
 //
-// 4096 queries of 32 heads of 128 over 16384 slots: 1061 us, 907 TFLOP/s, 54 % of the measured rate; 570 us of products at that rate
+// 4096 queries of 32 heads of 128 over 16384 slots: 1061 us (1083 in a long row of calls), 907 TFLOP/s, 54 % of the measured rate; 570 us of products at that rate
 // (562 measured with nothing between them) and 430 us of exponentials at 16 a cycle and SM.  Without exponentials 1020 us, without the
 // unpackers' stores 980, without both and all reads of scores 794: what is left is the way from product to softmax and back.
 #include "kv_common.cuh"

@@ -12,7 +12,7 @@
 // there up to 2^-53, and at position 10^6 a product in fp32 would be off by 0.06.
 //
 // Bound by the instructions with the Hadamard rotation (16384 x 72 heads of 128: 145 us, 4.2 TB/s; 340 instructions for 16 values a lane,
-// a scheduler issues 64 % of the time), by HBM without (16384 x 40 heads: 72 us, 4.7 TB/s); few tokens by latency (2.7 us).
+// a scheduler issues 60 % of the time), by HBM without (16384 x 40 heads: 72 us, 4.7 TB/s); few tokens by latency (2.7 us).
 #include "kv_common.cuh"
 
 namespace dq {
