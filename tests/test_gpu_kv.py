@@ -83,6 +83,15 @@ def test_rope_sizes_and_views(tokens, q_heads, k_heads, views):
         run_rope(*rope_case(tokens, q_heads, k_heads, 128, 128, dtype, flags, tokens, views), flags)
 
 
+@pytest.mark.parametrize("tokens,q_heads,k_heads,dim,rot,flags", [(4000, 7, 2, 64, 64, 5), (1500, 10, 3, 128, 128, 5), (4000, 3, 2, 256, 128, 7),
+                                                                  (1500, 6, 1, 128, 96, 5), (4000, 5, 1, 80, 64, 1)])
+def test_rope_of_many_tokens(tokens, q_heads, k_heads, dim, rot, flags):
+    """A warp or a few for each token, which go round over its heads, from queries to keys between two rounds."""
+    for views in ("fused", "unaligned"):
+        q, k, positions, freq, gamma = rope_case(tokens, q_heads, k_heads, dim, rot, torch.bfloat16, flags, tokens + dim, views)
+        run_rope(q, k, positions, freq, gamma, flags)
+
+
 def test_rope_far_positions_and_gammas():
     q, k, p, f, g = rope_case(5, 3, 1, 128, 128, torch.float32, 1, 3, far=2 ** 31 - 100, gamma_type=torch.float32)
     run_rope(q, k, p, f, g, 1)
