@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
         }
       const int field = min(max((int)mx::exponent_field(most_q), 15), 244);
       const float up = __uint_as_float((uint32_t)(268 - field) << 23) * (a.scale < 0.f ? -1.f : 1.f);
-      by = fmaxf(__uint_as_float((uint32_t)(field - 14) << 23) * fabsf(a.scale) * LOG2E, 1.2e-38f);   // (not zero: it meets infinities)
+      by = __uint_as_float((uint32_t)(field - 14) << 23) * fabsf(a.scale) * LOG2E;
       sum_by = sum * up;
       const uint32_t tile = smem + P::Q_AT + m * P::TILE_BYTES;
 #pragma unroll
@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
 #pragma unroll
       for (int c = 0; c < 4; ++c) tc::tmem_ld32(s_at + 32 * c, raw[c]);
       float2 x[KEYS / 2];                                               // scores, without `tile_by`
-      const float tile_by = by * p.grow;
+      float tile_by = by * p.grow;
       odd |= p.odd < sees;
       tc::tmem_ld_wait();
       tc::tc_fence_before();
@@ -398,13 +398,16 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
         x[2 * e] = fma2(make_float2(kz.x, kz.y), both(sum_by), make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])));
         x[2 * e + 1] = fma2(make_float2(kz.z, kz.w), both(sum_by), make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])));
       }
-      if (masked)
+      if (masked) {   // behind the factor, which may be zero: a row of zeros, keys without a range, a scale of zero
 #pragma unroll
         for (int e = 0; e < KEYS / 2; ++e) {
           const bool none = !(valid >> (e >> 3) & 1u);
+          x[e] = mul2(x[e], both(tile_by));
           if (none || slot0 + 2 * e >= sees) x[e].x = -INFINITY;
           if (none || slot0 + 2 * e + 1 >= sees) x[e].y = -INFINITY;
         }
+        tile_by = 1.f;
+      }
       // (four chains: in one, each maximum waits for the one before)
       float most_of[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll

@@ -1,0 +1,97 @@
+"""The operators around the 4-bit key/value cache where their parts meet: rows, keys and scales of zero behind a mask, against the
+float64 oracle."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_04063_b200 as dq
+from kv_util import attend, check_attention, filled, on_device, put, starts_of, table_of
+from oracle import kv_cache as kv
+
+pytestmark = pytest.mark.gpu
+
+DIMS = (64, 128, 256)
+# One sequence of so few query rows that its keys are cut between CTAs where the table is wide, and where it is not one CTA goes
+# over all of them.
+WIDE, NARROW = 2048, None
+
+
+def chunk_rows(dim):
+    """Queries of two heads, enough for the kernel of many rows."""
+    return 140 if dim == 256 else 90
+
+
+def check_all(c, cache, q, scale, queries):
+    out, lse = attend(cache, q, scale, starts_of(queries))
+    group, first = q.shape[1] // c.heads, 0
+    for b, n in enumerate(queries):
+        check_attention(c, b, q, first, n, group, scale, out, lse)
+        first += n
+
+
+@pytest.mark.parametrize("slots", (NARROW, WIDE))
+@pytest.mark.parametrize("dim", DIMS)
+def test_a_prompt_of_zeros(dim, slots):
+    """Queries, keys and values are zero, as in a pass over padding: every output is zero, a token's lse the logarithm of what it sees."""
+    n = 150
+    table, n_pages = table_of(np.random.default_rng(dim), [n], 16, width=slots and slots // 16)
+    c = kv.Cache(n_pages, 2, dim, 16, table, [n], 0xff)
+    cache = on_device(c)
+    zeros = torch.zeros((n, 4, dim), dtype=torch.bfloat16, device="cuda")
+    dq.dq_kv_append(zeros[:, :2], zeros[:, 2:], cache)
+    for queries in (n, 1):                                       # by both kernels
+        out, lse = attend(cache, zeros[:queries], 0.1)
+        sees = torch.arange(n - queries + 1, n + 1, dtype=torch.float64, device="cuda")
+        assert bool((out == 0).all())
+        assert float((lse.double() - sees.log()[:, None]).abs().max()) <= 2.0 ** -20 * (1 + np.log(n))   # (an exponential's and a logarithm's error)
+        weights = torch.full((1, 2, cache.slots), 77.0, device="cuda")
+        dq.dq_kv_attention_weights(zeros[:queries], lse, cache, 0.1, weights)
+        assert bool(torch.isfinite(weights[..., :n]).all()) and bool((weights[..., n:] == 77).all())
+        assert float((weights[..., :n].double().sum(-1) - 2 * queries).abs().max()) <= 2 * queries * 2.0 ** -16   # (lse's error, and as much again)
+
+
+@pytest.mark.parametrize("slots", (NARROW, WIDE))
+@pytest.mark.parametrize("dim", DIMS)
+def test_zero_queries_over_keys_without_a_range_behind_a_mask(dim, slots):
+    """Keys that are one number each in the tile that the causal mask cuts, in the last tile, which the length cuts, and beside pages that
+    are missing; some query rows of zeros among others that are not, and values of a row's own size."""
+    rng = np.random.default_rng(dim + 1)
+    n, length = chunk_rows(dim), 300
+    for level in (0.0, 0.4, -3.0, 100.0):
+        c, _ = filled(rng, [length], 1, dim, 16, width=slots and slots // 16)
+        c.table[0, [1, 17]] = -1                                 # a tile has a hole before the queries, another among them
+        for slot in range(length):
+            c.write(0, 0, slot, 0, np.full(dim, level))
+        q = rng.standard_normal((n, 2, dim))
+        q[::3], q[1::3, 1] = 0.0, 0.0
+        check_all(c, on_device(c), put(q, torch.bfloat16), 0.1, [n])
+
+
+@pytest.mark.parametrize("slots", (NARROW, WIDE))
+@pytest.mark.parametrize("dim", DIMS)
+def test_zero_queries_over_a_tile_without_pages(dim, slots):
+    rng = np.random.default_rng(dim + 2)
+    n, length = chunk_rows(dim), 400
+    c, _ = filled(rng, [length], 1, dim, 16, width=slots and slots // 16)
+    c.table[0, 8:16] = -1
+    q = rng.standard_normal((n, 2, dim))
+    q[::2] = 0.0
+    check_all(c, on_device(c), put(q, torch.float16), 0.1, [n])
+    c.table[0] = -1                                              # none at all
+    out, lse = attend(on_device(c), put(q, torch.float16), 0.1)
+    assert bool((out == 0).all()) and bool((lse == -torch.inf).all())
+
+
+@pytest.mark.parametrize("slots", (NARROW, WIDE))
+@pytest.mark.parametrize("dim", DIMS)
+def test_a_scale_of_zero(dim, slots):
+    """All that is seen counts alike, whatever the keys: zeros, ordinary ones, large ones."""
+    rng = np.random.default_rng(dim + 3)
+    n, length = chunk_rows(dim), 200
+    for size in (0.0, 1.0, 1e33):
+        c, _ = filled(rng, [length], 1, dim, 16, width=slots and slots // 16)
+        for slot in range(length):
+            c.write(0, 0, slot, 0, size * rng.standard_normal(dim))
+        q = put(rng.standard_normal((n, 2, dim)), torch.bfloat16)
+        check_all(c, on_device(c), q, 0.0, [n])
+        check_all(c, on_device(c), q[-1:], 0.0, [1])
