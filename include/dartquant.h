@@ -476,7 +476,8 @@ dq_status dq_kv_dequantize(const dq_kv_cache_t* cache, const int32_t* d_starts, 
  * aligned, set to zero once before its first use (every call leaves it ready for the next); calls that overlap on the GPU need one each.
  * out overlaps neither Q nor the cache.  Results do not depend on the run.  Products take 16-bit operands and fp32 sums; queries that
  * are worked on together share a power of two for the keys and one for the values, so a key or value whose scale is 2^20 times below
- * the largest in its sequence loses digits. */
+ * the largest in its sequence loses digits.  With few rows a sequence values times exponentials are added before the division, so the
+ * values' size times 2^8 times their number has to stay within fp32's range. */
 dq_status dq_kv_attention(const dq_heads_t* Q, int32_t dtype, int64_t tokens, const dq_kv_cache_t* cache, const int32_t* d_starts,
                           float scale, const dq_heads_t* out, float* d_lse, void* d_workspace, void* cuda_stream);
 

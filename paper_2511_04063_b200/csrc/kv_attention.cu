@@ -620,14 +620,14 @@ __global__ void __launch_bounds__(Few<DIM, NT>::THREADS, Few<DIM, NT>::PER_SM) f
         float* row = reinterpret_cast<float*>(stages.ring + place * F::STAGE_BYTES) + (2 * c + j) * F::PAD + g * (DIM / 8);
         // out of the codes' 2^24 and 2^20, and the scales' power of two
         const float grow = __uint_as_float((scale_field - 6u) << 23) * by, o0 = (j ? off[nt].y : off[nt].x) * by;
-        const float low = 16777216.f * grow, high = 1048576.f * grow;
+        constexpr float LOW = 16777216.f, HIGH = 1048576.f;             // (apart from grow, with which they may leave fp32's range)
 #pragma unroll
         for (int i = 0; i < VW; ++i)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             auto at_j = [&](int k) { const float2 v = o[nt][4 * i + k][e]; return j ? v.y : v.x; };
             *reinterpret_cast<float4*>(row + 8 * i + 4 * e) =
-                make_float4(at_j(0) * low + o0, at_j(1) * high + o0, at_j(2) * low + o0, at_j(3) * high + o0);
+                make_float4(at_j(0) * LOW * grow + o0, at_j(1) * HIGH * grow + o0, at_j(2) * LOW * grow + o0, at_j(3) * HIGH * grow + o0);
           }
       }
       __syncthreads();

@@ -48,8 +48,8 @@ struct Prompt {
 };
 
 struct alignas(16) Params {                                            // of a key tile; read in 16-byte pieces
-  float kz[KEYS];                                                      // (ko + 8 ks) times `shrink`
-  float grow, shrink;                                                  // powers of two: of the tile's scores, of kz
+  float kz[KEYS];                                                      // (ko + 8 ks) 2^-10 / grow
+  float grow;                                                          // power of two of the tile's scores, which are 2^-10 of it
   uint32_t field;                                                      // the values' power of two: exponent field, the largest so far
   uint32_t valid;                                                      // groups of 16 keys that have a page
   int odd;                                                             // the first key whose value is a NaN
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     };
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) k[w] = v[w] = 0u;
-    uint32_t field = 20u;
+    uint32_t field = 10u;
     if (key_tiles > 0) fetch(0);
     auto wait = [&](uint32_t at, int phase) { return __all_sync(0xffffffffu, tc::mbar_wait(at, (uint32_t)phase & 1u, a.d_status)); };
     // eight codes times a factor (`high`: of the codes four bits up) plus an offset, as a piece of a row
@@ -258,13 +258,14 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     for (int i = 0; i < key_tiles; ++i) {
       const int s = i % STAGES, turn = i / STAGES;
       const float ks = scale_of(kp), kz = offset_of(kp) + 8.f * ks, vs = scale_of(vp), vo = offset_of(vp);
-      // exponent fields of the tile's largest ks, and of what the values are divided by: vs below 2^-9, values below 2^6.  A NaN does
+      // exponent fields of the tile's largest ks, and of what the values are divided by: vs below 2, values below 2^16, both held 2^10
+      // smaller.  (That factor stands apart: with it the powers of two of the largest numbers would leave fp32's range.)  A NaN does
       // not count, and a value that is one is held as zero: not all rows may see it.
       auto nan_of = [](float v) { return !(fabsf(v) <= 3.402823466e38f); };
       const bool nan = nan_of(vs) || nan_of(vo);
       // (and kz within 2^91, where a tile's scales are small or zero)
-      const int k_field = nan_of(ks) || nan_of(kz) ? 0 : max((int)(kp >> 7 & 255u), (int)mx::exponent_field(kz) - 100), spread = (int)(vp >> 7 & 255u) + 10;
-      const int size = (int)max(mx::exponent_field(vo), mx::exponent_field(fmaf(15.f, vs, vo))) - 4;
+      const int k_field = nan_of(ks) || nan_of(kz) ? 0 : max((int)(kp >> 7 & 255u), (int)mx::exponent_field(kz) - 100), spread = (int)(vp >> 7 & 255u);
+      const int size = (int)max(mx::exponent_field(vo), mx::exponent_field(fmaf(15.f, vs, vo))) - 14;
       const uint32_t k_most = __reduce_max_sync(0xffffffffu, (uint32_t)k_field);
       const uint32_t v_most = __reduce_max_sync(0xffffffffu, nan ? 0u : (uint32_t)max(spread, size));
       const uint32_t votes = __ballot_sync(0xffffffffu, there), odd = __ballot_sync(0xffffffffu, nan);
@@ -283,15 +284,15 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
         valid |= (s_values[i & 1][x] >> 16) << (2 * x);
         first_odd = min(first_odd, s_odd[i & 1][x]);
       }
-      key_field = min(key_field, 243u);
-      field = min(field, 240u);
-      const float k_by = __uint_as_float((244u - key_field) << 23), v_by = __uint_as_float((254u - field) << 23);
+      key_field = min(key_field, 253u);
+      field = min(field, 253u);
+      const float k_by = __uint_as_float((254u - key_field) << 23), v_by = __uint_as_float((254u - field) << 23);
       const uint32_t k_tile = smem + P::K_AT + s * P::TILE_BYTES, v_tile = smem + P::V_AT + s * P::TILE_BYTES;
-      constexpr float LOW = 16777216.f, HIGH = 1048576.f;               // 2^24 and 2^20: of the codes
+      constexpr float SMALLER = 1.f / 1024.f, LOW = SMALLER * 16777216.f, HIGH = SMALLER * 1048576.f;   // (2^24 and 2^20: of the codes)
       ok = ok && wait(s_full(TILES - 1, s), turn + 1);
       {
         const float by = ks * k_by;
-        const __half2 low = __float2half2_rn(by * LOW), high = __float2half2_rn(by * HIGH), offset = __float2half2_rn(-8.f * by);
+        const __half2 low = __float2half2_rn(by * LOW), high = __float2half2_rn(by * HIGH), offset = __float2half2_rn(-8.f * SMALLER * by);
 #pragma unroll
         for (int w = 0; w < WORDS; ++w) store(piece_at(k_tile, t, w), k[w], low, high, offset);
       }
@@ -300,17 +301,16 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
       if (lane == 0) tc::mbar_arrive(k_full(s));
       ok = ok && wait(pv_done(TILES - 1, s), turn + 1);
       Params& p = s_params[s];
-      p.kz[t] = kz * k_by;
+      p.kz[t] = kz * k_by * SMALLER;
       if (t == 0) {
-        p.grow = __uint_as_float((10u + key_field) << 23);
-        p.shrink = k_by;
+        p.grow = __uint_as_float(key_field << 23);
         p.field = field;
         p.valid = valid;
         p.odd = first_odd;
       }
       {
         const float by = nan ? 0.f : vs * v_by;
-        const __half2 low = __float2half2_rn(by * LOW), high = __float2half2_rn(by * HIGH), offset = __float2half2_rn(nan ? 0.f : vo * v_by);
+        const __half2 low = __float2half2_rn(by * LOW), high = __float2half2_rn(by * HIGH), offset = __float2half2_rn(nan ? 0.f : vo * v_by * SMALLER);
 #pragma unroll
         for (int w = 0; w < WORDS; ++w) store(piece_at(v_tile, t, w), v[w], low, high, offset);
       }
@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
         }
       const int field = min(max((int)mx::exponent_field(most_q), 15), 244);
       const float up = __uint_as_float((uint32_t)(268 - field) << 23) * (a.scale < 0.f ? -1.f : 1.f);
-      by = __uint_as_float((uint32_t)(field - 14) << 23) * fabsf(a.scale) * LOG2E;
+      by = __uint_as_float((uint32_t)(field - 4) << 23) * fabsf(a.scale) * LOG2E;   // (the scores' 2^10 with it)
       sum_by = sum * up;
       const uint32_t tile = smem + P::Q_AT + m * P::TILE_BYTES;
 #pragma unroll
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
     const int least = __reduce_min_sync(0xffffffffu, there ? sees : INT_MAX);
     float top = -INFINITY;
     float2 sum = both(0.f);
-    uint32_t field = 20u;
+    uint32_t field = 10u;
     bool odd = false;                                                   // the row sees a value that is a NaN
     for (int i = 0; i < key_tiles && ok; ++i) {
       const int s = i % STAGES, slot0 = (tile0 + i) * KEYS;
@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
       const float l = sum.x + sum.y;
       const float grow = odd ? __uint_as_float(0x7fc00000u) : __uint_as_float(field << 23);
       float* part_at = reinterpret_cast<float*>(a.workspace + TICKET_BYTES) + (int64_t)blockIdx.x * P::PART;
-      const float over = l == 0.f ? 0.f : 1.f / l;
+      const float over = l == 0.f ? 0.f : 1024.f / l;                     // (the values' 2^10; a mean of them is in range, their sum may not be)
       T* out = reinterpret_cast<T*>(a.out.p) + (first + token) * a.out.token + (int64_t)head * a.out.head;
 #pragma unroll 1
       for (int c = 0; c < DIM; c += 16) {
@@ -477,7 +477,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
           float d[8];
 #pragma unroll
           for (int x = 0; x < 8; ++x) {
-            d[(x >> 1) + 4 * (x & 1)] = (key_tiles > 0 ? __uint_as_float(v[e + x]) : 0.f) * grow;
+            d[(x >> 1) + 4 * (x & 1)] = (key_tiles > 0 ? __uint_as_float(v[e + x]) * over : 0.f) * grow;
           }
           if (splits > 1) {
             // (by column, rows side by side: the joining CTA reads them so)
@@ -486,11 +486,11 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
           } else if (there) {
             mx::Vec8<T> y;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) y.set_pair(x, make_float2(d[2 * x] * over, d[2 * x + 1] * over));
+            for (int x = 0; x < 4; ++x) y.set_pair(x, make_float2(d[2 * x], d[2 * x + 1]));
             if (a.out.vec) y.store(out + c + e);
             else
 #pragma unroll
-              for (int x = 0; x < 8; ++x) out[c + e + x] = mx::from_f32<T>(d[x] * over);
+              for (int x = 0; x < 8; ++x) out[c + e + x] = mx::from_f32<T>(d[x]);
           }
         }
       }
@@ -510,13 +510,15 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
         __threadfence();
         if (tid == 0) *ticket = 0;
         if (there) {
-          const float* parts = reinterpret_cast<const float*>(a.workspace + TICKET_BYTES) + (int64_t)(blockIdx.x - part) * P::PART + m * 128 + r;
+          float* parts = reinterpret_cast<float*>(a.workspace + TICKET_BYTES) + (int64_t)(blockIdx.x - part) * P::PART + m * 128 + r;
           float all_top = -INFINITY, l = 0.f;
           for (int i = 0; i < splits; ++i) all_top = fmaxf(all_top, __ldcg(parts + (int64_t)i * P::PART + (int64_t)DIM * P::ROWS));
-          for (int i = 0; i < splits; ++i) {
-            const float* p = parts + (int64_t)i * P::PART;
+          for (int i = 0; i < splits; ++i) {                              // (a part's sum takes its maximum's place)
+            float* p = parts + (int64_t)i * P::PART;
             const float pl = __ldcg(p + (int64_t)(DIM + 1) * P::ROWS), pm = __ldcg(p + (int64_t)DIM * P::ROWS);
-            l += pl == 0.f ? 0.f : pl * (pm == -INFINITY ? 1.f : exp2_of(pm - all_top));
+            const float f = pl == 0.f ? 0.f : pl * (pm == -INFINITY ? 1.f : exp2_of(pm - all_top));
+            __stcg(p + (int64_t)DIM * P::ROWS, f);
+            l += f;
           }
           const float over = l == 0.f ? 0.f : 1.f / l;
           T* out = reinterpret_cast<T*>(a.out.p) + (first + token) * a.out.token + (int64_t)head * a.out.head;
@@ -527,8 +529,7 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
 #pragma unroll 4
             for (int i = 0; i < splits; ++i) {
               const float* p = parts + (int64_t)i * P::PART;
-              const float pm = __ldcg(p + (int64_t)DIM * P::ROWS);
-              const float f = pm == -INFINITY ? 1.f : exp2_of(pm - all_top);   // (where there is no sum O is zero)
+              const float f = __ldcg(p + (int64_t)DIM * P::ROWS) * over;   // the part's share of the mean
 #pragma unroll
               for (int x = 0; x < 16; ++x) o[x] += __ldcg(p + (int64_t)(d + x) * P::ROWS) * f;
             }
@@ -536,11 +537,11 @@ __global__ void __launch_bounds__(Prompt<DIM>::THREADS, 1) prompt_kernel(const A
             for (int w = 0; w < 16; w += 8) {
               mx::Vec8<T> y;
 #pragma unroll
-              for (int x = 0; x < 4; ++x) y.set_pair(x, make_float2(o[w + 2 * x] * over, o[w + 2 * x + 1] * over));
+              for (int x = 0; x < 4; ++x) y.set_pair(x, make_float2(o[w + 2 * x], o[w + 2 * x + 1]));
               if (a.out.vec) y.store(out + d + w);
               else
 #pragma unroll
-                for (int x = 0; x < 8; ++x) out[d + w + x] = mx::from_f32<T>(o[w + x] * over);
+                for (int x = 0; x < 8; ++x) out[d + w + x] = mx::from_f32<T>(o[w + x]);
             }
           }
         }

@@ -95,3 +95,19 @@ def test_a_scale_of_zero(dim, slots):
         q = put(rng.standard_normal((n, 2, dim)), torch.bfloat16)
         check_all(c, on_device(c), q, 0.0, [n])
         check_all(c, on_device(c), q[-1:], 0.0, [1])
+
+
+@pytest.mark.parametrize("slots", (NARROW, WIDE))
+@pytest.mark.parametrize("dim", DIMS)
+def test_large_keys_and_values(dim, slots):
+    """Keys of 1e36 with queries of 1e-36, so that the logits are ordinary ones, and values whose means are in bf16's range."""
+    rng = np.random.default_rng(dim + 4)
+    n, length = chunk_rows(dim), 300
+    c, _ = filled(rng, [length], 1, dim, 16, width=slots and slots // 16)
+    for slot in range(length):
+        c.write(0, 0, slot, 0, 1e36 * rng.standard_normal(dim))
+        c.write(0, 0, slot, 1, (1e35 if slot % 3 else 2e36) * rng.standard_normal(dim))
+    q = put(1e-36 * rng.standard_normal((n, 2, dim)), torch.bfloat16)
+    check_all(c, on_device(c), q, 0.1, [n])
+    c.lengths[:] = 40                                            # (few rows: values times exponentials are added before the division)
+    check_all(c, on_device(c), q[-2:], 0.1, [2])
