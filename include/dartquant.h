@@ -474,9 +474,11 @@ dq_status dq_kv_dequantize(const dq_kv_cache_t* cache, const int32_t* d_starts, 
  * dtype: DQ_BF16 or DQ_FP16.  A query that sees nothing gets zeros.  d_lse (nullable, [tokens][Q's heads]): the natural logarithm of the
  * sums of exp(scale * q . k), -infinity for a query that sees nothing.  d_workspace: dq_kv_attention_workspace bytes, 16-byte
  * aligned, set to zero once before its first use (every call leaves it ready for the next); calls that overlap on the GPU need one each.
- * out overlaps neither Q nor the cache.  Results do not depend on the run.  Products take 16-bit operands and fp32 sums; queries that
- * are worked on together share a power of two for the keys and one for the values, so a key or value whose scale is 2^20 times below
- * the largest in its sequence loses digits.  With few rows a sequence values times exponentials are added before the division, so the
+ * out overlaps neither Q nor the cache.  Results do not depend on the run.  Products take 16-bit operands and fp32 sums: queries times a power of
+ * two (digits below 2^-24 of a row's largest value are lost) and, with few query rows a sequence (below 64 to 256), the codes themselves and exp times a
+ * value's scale (2^-11 of it, and 2^-31 of the largest scale).  With more rows keys and values are rounded: a key's element is off by up to
+ * 2^-14 of the largest scale among the same 128 slots, seen by the query or not (by nothing where its own scale is within 2^-7 of that), a
+ * value's by 2^-11 of its terms (offset and scale * code) and 2^-14 of the largest scale up to there.  With few rows a sequence values times exponentials are added before the division, so the
  * values' size times 2^8 times their number has to stay within fp32's range. */
 dq_status dq_kv_attention(const dq_heads_t* Q, int32_t dtype, int64_t tokens, const dq_kv_cache_t* cache, const int32_t* d_starts,
                           float scale, const dq_heads_t* out, float* d_lse, void* d_workspace, void* cuda_stream);

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2511_04063_b200 as dq
-from kv_util import attend, check_attention, filled, on_device, put, starts_of, table_of
+from kv_util import UNIT, attend, check_attention, f64, filled, logit_bound, on_device, put, starts_of, table_of
 from oracle import kv_cache as kv
 
 pytestmark = pytest.mark.gpu
@@ -111,3 +111,43 @@ def test_large_keys_and_values(dim, slots):
     check_all(c, on_device(c), q, 0.1, [n])
     c.lengths[:] = 40                                            # (few rows: values times exponentials are added before the division)
     check_all(c, on_device(c), q[-2:], 0.1, [2])
+
+
+@pytest.mark.parametrize("slots", (NARROW, WIDE))
+@pytest.mark.parametrize("dim", DIMS)
+@pytest.mark.parametrize("apart", (1, 4, 8))
+def test_scales_far_apart_in_a_tile(apart, dim, slots):
+    """Keys and values next to some with scales 2^(apart + 4) times theirs or so, which a query does not see yet, or sees with a probability of zero.  An
+    element of a tile of keys is off by up to 2^-14 of the tile's largest scale, which is held at 2^-10 or more (half of fp16's least step, 2^-25,
+    twice: offset and sum), but by nothing where its scale is within 2^-7 of that (8 bits and 3, 2^-10-7-7 = 2^-24); that enters a
+    logit with the sum of the query's magnitudes.  An element of a value is off by 2^-14 of the largest scale up to there beside its
+    own roundings."""
+    rng = np.random.default_rng(dim + apart)
+    n, length, big, group, scale = chunk_rows(dim), 250, 2.0 ** apart, 2, 0.1
+    c, _ = filled(rng, [length], 1, dim, 16, width=slots and slots // 16)
+    q = rng.standard_normal((n, group, dim))
+    q[..., 0] = 4.0
+    large = [130, length - 2, length - 1]                        # the first one's logit is far below the others'
+    for slot in range(length):
+        k, v = rng.standard_normal(dim), rng.standard_normal(dim)
+        c.write(0, 0, slot, 0, k if slot not in large else big * np.r_[-4.0 * (20 + dim ** 0.5), k[1:] * 0.25])
+        c.write(0, 0, slot, 1, v if slot not in large else 32.0 * big * v)
+    q = put(q, torch.bfloat16)
+    largest = [max(c.raw(0, 0, slot, which)[1] for slot in large) for which in (0, 1)]
+    smallest = min(c.raw(0, 0, slot, 0)[1] for slot in range(length))
+    held = 0.0 if smallest >= 2.0 ** -6 * largest[0] else 2.0 ** -14 * largest[0]      # (of two scales' powers of two)
+    k_terms, v_terms = (c.exact(0, 0, length, which)[1] for which in (0, 1))
+    for rows in (q, q[-3:]):                                     # by both kernels
+        out, lse = attend(on_device(c), rows, scale)
+        r = kv.attention(c, 0, 0, f64(rows), scale)
+        for i in range(len(rows) - 2):                           # (the last two see one or both of the others)
+            seen = np.arange(length) < length - len(rows) + i + 1
+            seen[large[0]] = False
+            for g in range(group):
+                assert r["p"][i, g, large].max() < 1e-30
+                x = np.abs(f64(rows[i, g]))
+                e = logit_bound((k_terms[seen] @ x).max() * scale, dim) + held * x.sum() * scale
+                assert abs(float(lse[i, g]) - r["lse"][i, g]) <= e + 2.0 ** -21 * (1 + abs(r["lse"][i, g]))
+                bound = (np.expm1(2 * e) + 2.0 ** -20 + 2 * 2.0 ** -11) * (r["p"][i, g] @ v_terms) * 1.01
+                bound += UNIT[q.dtype] * np.abs(r["out"][i, g]) * 1.01 + 2.0 ** -14 * largest[1]
+                assert (np.abs(f64(out[i, g]) - r["out"][i, g]) <= bound).all()
