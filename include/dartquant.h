@@ -495,7 +495,9 @@ dq_status dq_kv_attention_weights(const dq_heads_t* Q, int32_t dtype, int64_t to
 /* Leaves the sequences min(length, keep) slots: in each head those whose position is above the head's largest less `recent`, then
  * those with the largest weights (a NaN last); of equals the lower slots.  Kept slots from `keep` on move, in order, into the
  * slots below that are given up, with their codes, weights and positions, so a head's slots are in no order of positions
- * afterwards, and the heads of a sequence keep different tokens.  d_lengths_out [n_seqs] receives the new lengths.  The outputs may be the
+ * afterwards, and the heads of a sequence keep different tokens.  Pages play no part in the choice; a kept slot that moves to where there is no page
+ * takes its weight and position along and loses its codes, and one without a page, whose place would be a slot with one, is given up: there
+ * the slot's token stays, with its weight and position.  d_lengths_out [n_seqs] receives the new lengths.  The outputs may be the
  * inputs (d_lengths_out the cache's lengths); entries from the new length on are left as they are.  0 <= recent <= keep, keep > 0.
  * d_workspace: dq_kv_evict_workspace bytes; calls that overlap on the GPU need one each. */
 dq_status dq_kv_evict(const dq_kv_cache_t* cache, const float* d_weights, const int32_t* d_positions, int64_t ld_slots, int32_t keep,

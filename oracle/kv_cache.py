@@ -154,8 +154,9 @@ def attention(cache, b, h, q, scale):
     return dict(out=out, lse=lse, p=p, terms=terms, logits=logits, largest=np.nanmax(v_terms, initial=0.0))
 
 
-def evict(weights, positions, length, keep, recent):
-    """One head's row: (source slot of each slot that is left)."""
+def evict(weights, positions, length, keep, recent, paged=None):
+    """One head's row: (source slot of each slot that is left).  paged: which slots have a page (None: all); one that has none is no
+    source for one that has, which stays as it is."""
     if length <= keep:
         return np.arange(length)
     newest = positions[:length].max()
@@ -166,4 +167,7 @@ def evict(weights, positions, length, keep, recent):
     holes = [i for i in range(keep) if i not in stays]
     source = np.arange(keep)
     source[holes] = [i for i in range(keep, length) if i in stays]
+    if paged is not None:
+        lost = ~np.asarray(paged, bool)[source] & np.asarray(paged, bool)[:keep]
+        source[lost] = np.arange(keep)[lost]
     return source

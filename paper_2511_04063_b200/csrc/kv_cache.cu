@@ -219,7 +219,7 @@ dq_status run_append(cudaStream_t stream, int dtype, int dim, const AppendArgs& 
 // number the equals, holes and movers of a warp and one scan each those of the warps before (rows of more than 32768 slots go round
 // in blocks of that, and read their keys again).  Slots from `keep` on that stay move into the slots below that do not, the i-th into the i-th: what is moved is
 // read from slots that nothing writes, so no order between the moves is needed, and a sequence that is over its budget by a
-// few tokens moves a few.
+// few tokens moves a few.  A slot without a page has nothing to move: where its turn is a slot with one, what is there stays.
 //
 // 32 sequences up to 16384 slots, 8 heads of 128, 4096 stay: 119 us, 57 for the choice (256 rows are 1.7 waves of CTAs; half the
 // threads a CTA were slower) and 52 for the moves (72 bytes at either end, in whole sectors 2.0 times the bytes).  One sequence over by
@@ -386,9 +386,16 @@ __global__ void __launch_bounds__(SELECT, 1) evict_select_kernel(const EvictArgs
   if (tid == 0) ws[0] = movers;
   __syncthreads();
   for (int i = tid; i < movers; i += SELECT) {
+    // (without codes to bring along, the slot's weight and position must not come to lie on another token's)
     const int from = ws[4 + 2 * i], to = ws[4 + 2 * i + 1];
-    weights_out[to] = weights[from];
-    positions_out[to] = positions[from];
+    float w = weights[from];
+    int position = positions[from];
+    if (a.cache.page_of(b, from) < 0 && a.cache.page_of(b, to) >= 0) {
+      w = weights[to];
+      position = positions[to];
+    }
+    weights_out[to] = w;
+    positions_out[to] = position;
   }
 }
 

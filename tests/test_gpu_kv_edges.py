@@ -151,3 +151,37 @@ def test_scales_far_apart_in_a_tile(apart, dim, slots):
                 bound = (np.expm1(2 * e) + 2.0 ** -20 + 2 * 2.0 ** -11) * (r["p"][i, g] @ v_terms) * 1.01
                 bound += UNIT[q.dtype] * np.abs(r["out"][i, g]) * 1.01 + 2.0 ** -14 * largest[1]
                 assert (np.abs(f64(out[i, g]) - r["out"][i, g]) <= bound).all()
+
+
+# ------------------------------------------------------------------------------------------------ eviction
+@pytest.mark.parametrize("missing", [(4,), (0,), (2, 3, 5), (1, 4, 6), (0, 1, 2, 3, 4, 5, 6)])
+@pytest.mark.parametrize("in_place", (False, True))
+def test_evict_where_the_table_names_no_page(missing, in_place):
+    """Pages are missing where slots move from, where they move to, at both ends: what has a page is the token that its position says."""
+    rng = np.random.default_rng(sum(missing))
+    length, keep, recent, heads, dim, page = 108, 40, 8, 2, 64, 16
+    c, _ = filled(rng, [length, length], heads, dim, page)
+    c.table[0, list(missing)] = [-1, len(c.pages), -9, -1, -1, -1, -1][:len(missing)]   # (the other sequence has all of its pages)
+    cache = on_device(c)
+    shape = (2, heads, cache.slots)
+    weights = rng.exponential(size=shape).astype(np.float32)
+    positions = np.stack([[rng.permutation(shape[2]) for _ in range(heads)] for _ in range(2)]).astype(np.int32)
+    w, p = torch.from_numpy(weights).cuda(), torch.from_numpy(positions).cuda()
+    w_out, p_out, n_out = (w, p, cache.lengths) if in_place else (torch.zeros_like(w), torch.zeros_like(p), torch.zeros_like(cache.lengths))
+    work = torch.empty(dq.dq_kv_evict_workspace(2, heads, keep), dtype=torch.uint8, device="cuda")
+    dq.dq_kv_evict(cache, w, p, keep, recent, w_out, p_out, n_out, work)
+    assert n_out.tolist() == [keep, keep]
+    left = kv.Cache(len(c.pages), heads, dim, page, c.table, [keep, keep])
+    left.pages = cache.pages.cpu().numpy()
+    for b in range(2):
+        paged = np.array([c.place(b, slot) is not None for slot in range(length)])
+        for h in range(heads):
+            source = kv.evict(weights[b, h], positions[b, h], length, keep, recent, paged)
+            np.testing.assert_array_equal(p_out[b, h, :keep].cpu().numpy(), positions[b, h, source])
+            np.testing.assert_array_equal(w_out[b, h, :keep].cpu().numpy(), weights[b, h, source])
+            for slot in np.flatnonzero(paged[:keep]):
+                was = int(np.flatnonzero(positions[b, h, :length] == int(p_out[b, h, slot]))[0])
+                assert paged[was]
+                for second in (0, 1):
+                    for one, two in zip(left._at(b, h, slot, second), c._at(b, h, was, second)):
+                        assert (one == two).all()
