@@ -134,7 +134,7 @@ dq_status dq_kv_append(const dq_heads_t* K, const dq_heads_t* V, int32_t dtype, 
   mx::Device dev;
   DQ_CHECK(mx::current_device(dev));
   a.positions = d_positions; a.slot_positions = d_slot_positions; a.ld_slots = ld_slots;
-  return kv::append((cudaStream_t)cuda_stream, dtype, cache->head_dim, a);
+  return kv::append((cudaStream_t)cuda_stream, dev, dtype, cache->head_dim, a);
 }
 
 dq_status dq_kv_dequantize(const dq_kv_cache_t* cache, const int32_t* d_starts, int64_t tokens, const dq_heads_t* K,
@@ -144,7 +144,7 @@ dq_status dq_kv_dequantize(const dq_kv_cache_t* cache, const int32_t* d_starts, 
   if (tokens == 0 || cache->n_seqs == 0) return DQ_OK;
   mx::Device dev;
   DQ_CHECK(mx::current_device(dev));
-  return kv::dequantize((cudaStream_t)cuda_stream, dtype, cache->head_dim, a);
+  return kv::dequantize((cudaStream_t)cuda_stream, dev, dtype, cache->head_dim, a);
 }
 
 dq_status dq_kv_attention(const dq_heads_t* Q, int32_t dtype, int64_t tokens, const dq_kv_cache_t* cache, const int32_t* d_starts,

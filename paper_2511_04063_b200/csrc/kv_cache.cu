@@ -199,10 +199,10 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const AppendArgs a, int
 }
 
 template <bool WRITE>
-dq_status run_append(cudaStream_t stream, int dtype, int dim, const AppendArgs& a) {
+dq_status run_append(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AppendArgs& a) {
   // A CTA's search of sequences and pages (a chain of five loads or so) is paid once a tile: as many tokens as leave four CTAs an SM.
-  const int64_t waves = (a.batch.tokens + TILE * 592 - 1) / (TILE * 592);
-  const int tile = (int)max((int64_t)1, min((int64_t)TILE, (a.batch.tokens + waves * 592 - 1) / (waves * 592)));
+  const int64_t at_once = 4 * (int64_t)dev.sms, waves = (a.batch.tokens + TILE * at_once - 1) / (TILE * at_once);
+  const int tile = (int)max((int64_t)1, min((int64_t)TILE, (a.batch.tokens + waves * at_once - 1) / (waves * at_once)));
   return by_type(dtype, [&](auto t) {
     using T = decltype(t);
     return by_dim(dim, [&](auto d) {
@@ -448,8 +448,12 @@ __global__ void __launch_bounds__(THREADS) evict_move_kernel(const EvictArgs a, 
 
 }  // namespace
 
-dq_status append(cudaStream_t stream, int dtype, int dim, const AppendArgs& a) { return run_append<true>(stream, dtype, dim, a); }
-dq_status dequantize(cudaStream_t stream, int dtype, int dim, const AppendArgs& a) { return run_append<false>(stream, dtype, dim, a); }
+dq_status append(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AppendArgs& a) {
+  return run_append<true>(stream, dev, dtype, dim, a);
+}
+dq_status dequantize(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AppendArgs& a) {
+  return run_append<false>(stream, dev, dtype, dim, a);
+}
 
 dq_status evict(cudaStream_t stream, const mx::Device& dev, int dim, const EvictArgs& a) {
   const int64_t rows = (int64_t)a.cache.n_seqs * a.cache.heads;

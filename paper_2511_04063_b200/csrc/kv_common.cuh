@@ -213,8 +213,8 @@ struct AppendArgs {
   int* slot_positions;
   int64_t ld_slots;
 };
-dq_status append(cudaStream_t stream, int dtype, int dim, const AppendArgs& a);
-dq_status dequantize(cudaStream_t stream, int dtype, int dim, const AppendArgs& a);   // k and v are written
+dq_status append(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AppendArgs& a);
+dq_status dequantize(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AppendArgs& a);   // k and v are written
 
 struct AttentionArgs {
   Heads q, out;
