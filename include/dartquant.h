@@ -423,7 +423,7 @@ dq_status dq_mx_selftest_bounded_wait(int32_t a_fmt, const void* d_a_codes, cons
  * Tensors of heads (dq_heads_t): [token][head][head_dim] with contiguous values and any strides, counted in values, so that
  * views of a fused projection can be given; heads that start on 16-byte boundaries are read and written fastest.
  * Calls behave as the microscaled operators' do: asynchronous, nothing allocated or kept, capturable, dependent launch; a wait
- * that gives up (dq_kv_attention's, 1 s) is reported by dq_mx_status.
+ * that gives up (of dq_kv_attention and dq_kv_attention_weights, 1 s) is reported by dq_mx_status.
  * Errors: INVALID_ARG (null, sizes, enums, heads that do not fit, a pointer that its type's alignment rules out), UNSUPPORTED
  * (head_dim, page_size, alignment of pages and workspace, limits, a type, a device that is not sm_100), CUDA. */
 typedef struct {

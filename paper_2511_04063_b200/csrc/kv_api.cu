@@ -174,6 +174,7 @@ dq_status dq_kv_attention_weights(const dq_heads_t* Q, int32_t dtype, int64_t to
   mx::Device dev;
   DQ_CHECK(mx::current_device(dev));
   a.lse = const_cast<float*>(d_lse); a.weights = d_weights; a.weights_out = d_weights_out; a.ld_slots = ld_slots;
+  a.d_status = dev.d_status;
   return kv::attention_weights((cudaStream_t)cuda_stream, dev, dtype, cache->head_dim, a);
 }
 
