@@ -1,5 +1,5 @@
-"""The operators around the 4-bit key/value cache where their parts meet: rows, keys and scales of zero behind a mask, against the
-float64 oracle."""
+"""The operators around the 4-bit key/value cache where their parts meet: rows, keys and scales of zero behind a mask, scales far apart,
+long axes that one CTA goes over, batches of decoding sequences and a chunk, missing pages in eviction.  Against the float64 oracle."""
 import numpy as np
 import pytest
 import torch
@@ -7,6 +7,7 @@ import torch
 import paper_2511_04063_b200 as dq
 from kv_util import UNIT, attend, check_attention, f64, filled, logit_bound, on_device, put, starts_of, table_of
 from oracle import kv_cache as kv
+from test_gpu_kv import attention_case, weights_case
 
 pytestmark = pytest.mark.gpu
 
@@ -151,6 +152,40 @@ def test_scales_far_apart_in_a_tile(apart, dim, slots):
                 bound = (np.expm1(2 * e) + 2.0 ** -20 + 2 * 2.0 ** -11) * (r["p"][i, g] @ v_terms) * 1.01
                 bound += UNIT[q.dtype] * np.abs(r["out"][i, g]) * 1.01 + 2.0 ** -14 * largest[1]
                 assert (np.abs(f64(out[i, g]) - r["out"][i, g]) <= bound).all()
+
+
+@pytest.mark.parametrize("dim", DIMS)
+def test_many_items_over_a_long_axis(dim):
+    """More items than SMs, so none is cut: each CTA goes over 21 to 24 tiles of keys, with maxima and the values' largest scale that go on growing.
+    One query head of each kv head's is checked, at all of its tokens."""
+    rng = np.random.default_rng(dim + 5)
+    n, length, heads, group = 300, 3000, 2, 32 if dim == 256 else 64
+    c, _ = filled(rng, [1], heads, dim, 64, width=47)
+    c.lengths[:] = length
+    c.table[0] = rng.permutation(47)
+    c.pages = np.full((47, heads, 64 * (dim + 8)), 255, np.uint8)
+    for slot in range(length):
+        for h in range(heads):
+            c.write(0, h, slot, 0, (1 + 3 * slot / length) * rng.standard_normal(dim))
+            c.write(0, h, slot, 1, 2.0 ** (slot // 500) * rng.standard_normal(dim))
+    cache = on_device(c)
+    q = put(2 * rng.standard_normal((n, heads * group, dim)), torch.bfloat16)
+    out, lse = attend(cache, q, dim ** -0.5)
+    for one in (0, group - 1):
+        heads_of = [one, group + one]
+        check_attention(c, 0, q[:, heads_of], 0, n, 1, dim ** -0.5, out[:, heads_of], lse[:, heads_of])
+
+
+@pytest.mark.parametrize("dim", DIMS)
+@pytest.mark.parametrize("decoding,chunk", [(40, 30), (5, 400)])
+def test_decoding_sequences_and_a_chunk(decoding, chunk, dim):
+    """Sequences of one query and one of many in a call: by the kernels for few rows and for many."""
+    lengths = [(37 * i) % 150 + 1 for i in range(decoding)]
+    at = decoding // 2
+    queries = [1] * at + [chunk] + [1] * (decoding - at)
+    lengths = lengths[:at] + [chunk + 70] + lengths[at:]
+    attention_case(dim, lengths, queries, 1, 4, dim, 32, torch.bfloat16)
+    weights_case(dim, lengths, queries, 1, 4, dim, 32, torch.float16)
 
 
 # ------------------------------------------------------------------------------------------------ eviction
