@@ -320,13 +320,14 @@ struct Stream {
 // its own: while it works on one the other is on its way, across items too.  An item that crosses CTAs is left in the workspace in parts,
 // and the CTA that finishes last joins them, in order.
 //
-// Bound by the integer pipe that takes codes apart (56 % of its cycles) and the issue of instructions (54 %) where the cache is long:
-// 64 ragged sequences up to 16384 slots, 8 kv heads of 128, 171 us, 4.2 TB/s.  131072 slots of one sequence: 46.5 us, 3.1 TB/s, of which
-// 10 are start and join.  1024 slots: 10.9 us, a chain of table, codes, products, ticket and parts.
+// Where the cache is long no unit is full (integer pipe 56 % of its cycles, issue 54 %, HBM 65 % of the copy rate): with 16 or 12 warps an SM
+// the chain inside a stage, from codes over product, maxima and exponentials to the second product, is what is waited for.  64 ragged
+// sequences up to 16384 slots, 8 kv heads of 128, 168 us, 4.25 TB/s.  131072 slots of one sequence: 46 us, 3.1 TB/s, of which 10 are start and
+// join.  1024 slots: 10.9 us, a chain of table, codes, products, ticket and parts.
 template <int DIM, int NT>
 struct Few {
   static constexpr int ROWS = 8 * NT;
-  // two CTAs an SM: while one joins its warps the other works (64 ragged sequences up to 16384 slots: 171 us; one CTA of twice the
+  // two CTAs an SM: while one joins its warps the other works (64 ragged sequences up to 16384 slots: 171 us when this was chosen; one CTA of twice the
   // warps 190; more warps of fewer registers, 20 or 18 an SM, 185 and 200)
   static constexpr int WARPS = DIM * NT > 128 ? 6 : 8, PER_SM = 2;
   static constexpr int PLACES = 2;
@@ -773,8 +774,9 @@ __device__ __forceinline__ float over_columns(float2 got) {
   return w + __shfl_xor_sync(0xffffffffu, w, 2);
 }
 
-// Few rows: bound by HBM.  The keys come as in few_kernel; the first two tiles of rows lie in shared memory, of this item and the next.
-// 16 sequences up to 8192 slots, 8 kv heads of 128: 23 us on the GPU, 2.3 TB/s; the bytes take 8, start, queries and first copies the rest.
+// Few rows: the keys come as in few_kernel; the first two tiles of rows lie in shared memory, of this item and the next.  There is nothing to
+// join, as a weight is its key's.  16 sequences up to 8192 slots, 8 kv heads of 128: 23 us on the GPU, 2.3 TB/s; the bytes take 8, and which part of
+// the rest is start, lookup of pages, queries or the first copies has not been measured.
 template <int DIM>
 struct FewWeights {
   static constexpr int WARPS = DIM == 256 ? 8 : 10, PER_SM = 2, PLACES = DIM == 256 ? 2 : 4, TILES = 2;
@@ -889,7 +891,7 @@ __global__ void __launch_bounds__(FewWeights<DIM>::WARPS * 32, FewWeights<DIM>::
   stages.end();
 }
 
-// Many rows: bound by the exponentials (16 a cycle and SM) and the instructions of the product.  A warp holds 32 keys as fragments (D =
+// Many rows: exponentials (16 a cycle and SM) are a quarter of the time, no unit is full (issue 35 %, tensor cores 22 %).  A warp holds 32 keys as fragments (D =
 // 256: 16) and goes over the rows, 128 at a time from shared memory.  Bringing rows in costs a warp several times what a tile of them
 // does afterwards, so the warps of a CTA hold different keys; the CTAs of a cluster hold the same and take blocks of 128 rows in turn.
 // Where that leaves too few units for all SMs, `sets` warps of a CTA share keys too, and take a block's tiles in turn.  2 x 777 queries
@@ -1062,7 +1064,9 @@ int64_t attention_workspace(int dim) {
   return TICKET_BYTES + max((int64_t)MAX_CTAS * 2 * 16 * (dim + 2), MAX_SMS * prompt_part(dim)) * 4;
 }
 
-// Which of the two: what 128 keys of every sequence take.  A CTA of prompt_kernel needs 2.5 us for them whatever part of its 256 rows
+// Which of the two, for all sequences of a call, by their rows on average (the host does not know `starts`; a batch of decoding sequences and
+// one long chunk is right either way, but the chunk, or the others, may take several times what the other kernel would): what 128 keys of
+// every sequence take.  A CTA of prompt_kernel needs 2.5 us for them whatever part of its 256 rows
 // there is, and as its items are not of equal length about half as much again; few_kernel takes 9.5 ns for each 16 rows, balanced over
 // all SMs.  32 sequences of up to 2048 slots, 4 kv heads of 64, 80 rows on average: 44 and 68 us.  Where prompt_kernel's items are few
 // it cuts their keys and joins the parts, which pays from 128 rows on (256 for D = 256, whose items are half as large): one sequence
@@ -1089,7 +1093,7 @@ dq_status attention(cudaStream_t stream, const mx::Device& dev, int dtype, int d
 }
 
 dq_status attention_weights(cudaStream_t stream, const mx::Device& dev, int dtype, int dim, const AttentionArgs& a) {
-  // up to two tiles of rows a sequence: the keys' way from HBM is what takes time
+  // up to two tiles of rows a sequence, on average: the keys' way from HBM is what takes time
   const bool few = a.batch.tokens * a.group <= (int64_t)16 * a.cache.n_seqs;
   const int64_t slots = (int64_t)a.cache.width << a.cache.shift, rows = (int64_t)a.cache.n_seqs * a.cache.heads;
   auto run = [&](auto t) {

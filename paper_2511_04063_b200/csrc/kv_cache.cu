@@ -8,7 +8,7 @@
 //
 // Bound by HBM and instructions alike: 2 D bytes read and D / 2 + 4 written for each key and each value in 16 bits (and 2 D where the
 // values that the codes stand for are asked for).  A lane takes 16 values, D / 16 lanes a head; a CTA takes some tokens, for which it
-// finds sequence, slot and page first.  12 prompts of up to 2048 tokens, 40 heads of 128, fp16, with the values: 151 us, 4.8 TB/s, a
+// finds sequence, slot and page first.  12 prompts of up to 2048 tokens, 40 heads of 128, fp16, with the values: 148 to 153 us, 4.8 TB/s, a
 // scheduler issues 70 % of the time (207 us without the next head's values on their way and the packed arithmetic).
 #include "kv_common.cuh"
 
@@ -221,7 +221,7 @@ dq_status run_append(cudaStream_t stream, const mx::Device& dev, int dtype, int 
 // read from slots that nothing writes, so no order between the moves is needed, and a sequence that is over its budget by a
 // few tokens moves a few.  A slot without a page has nothing to move: where its turn is a slot with one, what is there stays.
 //
-// 32 sequences up to 16384 slots, 8 heads of 128, 4096 stay: 119 us, 57 for the choice (256 rows are 1.7 waves of CTAs; half the
+// 32 sequences up to 16384 slots, 8 heads of 128, 4096 stay: 119 to 121 us, 57 for the choice (256 rows are 1.7 waves of CTAs; half the
 // threads a CTA were slower) and 52 for the moves (72 bytes at either end, in whole sectors 2.0 times the bytes).  One sequence over by
 // eight: 9.9 us on the GPU, two launches and the choice's chain of counts.
 constexpr int SELECT = 1024, PER_THREAD = 32, BLOCK = SELECT * PER_THREAD;

@@ -18,12 +18,14 @@
 // Warps: four for each tile of rows (a thread a row: scores, exponentials, P, O's rescaling), four that unpack (a thread a key), one
 // that issues the products.  While one tile's rows are in the softmax the other's products run.  The two tiles share one place for S,
 // which is free again as soon as its rows have it in registers, so that a tile's next scores are there when its softmax is done (P over
-// S, and the next scores behind its product: 1110 us for the case below instead of 1061; a warp for each tile's products 1577, because
+// S, and the next scores behind its product: 1110 us for the case below when this took 1061; a warp for each tile's products 1577, because
 // instructions of two sums take turns; S in halves of 64 keys with a place each 1353: 64 columns take as long as 128).
 //
-// 4096 queries of 32 heads of 128 over 16384 slots: 1061 us (1083 in a long row of calls), 907 TFLOP/s, 54 % of the measured rate; 570 us of products at that rate
-// (562 measured with nothing between them) and 430 us of exponentials at 16 a cycle and SM.  Without exponentials 1020 us, without the
-// unpackers' stores 980, without both and all reads of scores 794: what is left is the way from product to softmax and back.
+// 4096 queries of 32 heads of 128 over 16384 slots: 1077 to 1122 us in a long row of calls (1061 in a short one, cool), 51 to 53 % of the
+// measured rate; 570 us of products at that rate (562 measured with nothing between them) and 430 us of exponentials at 16 a cycle and SM.  Left
+// out of a copy that took 1061: exponentials 1020 us, the unpackers' stores 980, both and all reads of scores 794.  The rest is the way from product to
+// softmax and back, and the last round of CTAs: 512 items of 97 to 128 key tiles, the longest first, end on 148 SMs after 441 tiles, where an
+// even share is 389.
 #include "kv_common.cuh"
 #include "tc_gemm.cuh"
 

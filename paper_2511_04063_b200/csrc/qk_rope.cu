@@ -6,13 +6,14 @@
 // rot / 2 + 8 l for pairs of halves, 16 l for neighbours.  With the Hadamard rotation, a butterfly over the bits of the index, they are
 // eight pairs of neighbours D / 8 apart (through shared memory where the rotated pairs do not allow it): four bits are a lane's own,
 // then the lanes exchange their values once, through shared memory, take 16 neighbours each, and the other bits are their own.  (An
-// exchange of all values for each of those bits: 187 us for 16384 tokens of 72 heads of 128 instead of 170.)
+// exchange of all values for each of those bits took 187 us for 16384 tokens of 72 heads of 128 when this took 170, before a warp took a token.)
 //
 // A warp takes all heads of a token where there are many, so that its angles are formed once, in 64 bits: position x inv_freq is exact
 // there up to 2^-53, and at position 10^6 a product in fp32 would be off by 0.06.
 //
-// Bound by the instructions with the Hadamard rotation (16384 x 72 heads of 128: 145 us, 4.2 TB/s; 340 instructions for 16 values a lane,
-// a scheduler issues 60 % of the time), by HBM without (16384 x 40 heads: 72 us, 4.7 TB/s); few tokens by latency (2.7 us).
+// With the Hadamard rotation 16384 x 72 heads of 128 take 145 us, 4.15 TB/s: 340 instructions for 16 values a lane are about as long as the
+// bytes, and neither is full (a scheduler issues 60 % of the time, with 34 % of an SM's warps and one head's loads ahead): latency.  Without it
+// 16384 x 40 heads take 72 us, 4.7 TB/s.  Few tokens: latency (2.7 us).
 #include "kv_common.cuh"
 
 namespace dq {
