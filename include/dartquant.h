@@ -478,8 +478,9 @@ dq_status dq_kv_dequantize(const dq_kv_cache_t* cache, const int32_t* d_starts, 
  * two (digits below 2^-24 of a row's largest value are lost) and, with few query rows a sequence (below 64 to 256), the codes themselves and exp times a
  * value's scale (2^-11 of it, and 2^-31 of the largest scale).  With more rows keys and values are rounded: a key's element is off by up to
  * 2^-14 of the largest scale among the same 128 slots, seen by the query or not (by nothing where its own scale is within 2^-7 of that), a
- * value's by 2^-11 of its terms (offset and scale * code) and 2^-14 of the largest scale or 2^-28 of the largest value up to there.  With few rows a sequence values times exponentials are added before the division, so the
- * values' size times 2^8 times their number has to stay within fp32's range.  Queries of 2^118 and more count as infinite. */
+ * value's by 2^-11 of its terms (offset and scale * code) and 2^-14 of the largest scale or 2^-28 of the largest value up to there.  With few
+ * rows values times exponentials are added before the division, so the values' size times 2^8 times their number has to stay within fp32's
+ * range.  Queries of 2^118 and more count as infinite. */
 dq_status dq_kv_attention(const dq_heads_t* Q, int32_t dtype, int64_t tokens, const dq_kv_cache_t* cache, const int32_t* d_starts,
                           float scale, const dq_heads_t* out, float* d_lse, void* d_workspace, void* cuda_stream);
 

@@ -7,8 +7,9 @@
 // is added to the score in fp32.  A value becomes  vs c + vo,  rounded to fp16 (2^-11, as P is).  The factor of a code is 2^24 times a
 // scale, so the largest scale of a tile is held between 2^-10 and 2^-9, seen by a row or not, and fp16's least step is 2^-14 of it: keys are exact
 // where their scales are within 2^-7 of the tile's largest, and an element of a smaller one is off by up to 2^-14 of the largest (two
-// roundings), as an element of a value is of the largest so far (or 2^-28 of the largest value, where that is far above its scale).  Codes shifted to the upper bits of the mantissa, each by itself, would leave
-// 2^-20; they took 1110 us instead of 1079 for the case below, and 429 instead of 414 for D = 256.  Parameters are applied here, by a
+// roundings), as an element of a value is of the largest so far (or 2^-28 of the largest value, where that is far above its scale).  Codes
+// shifted to the upper bits of the mantissa, each by itself, would leave 2^-20; they took 1110 us instead of 1079 for the case below, and
+// 429 instead of 414 for D = 256.  Parameters are applied here, by a
 // thread a key, because a thread of the softmax meets every key: read from shared memory for each of them, four numbers a key took
 // 4100 cycles of a key tile's 10000.  Powers of two keep all of it in fp16's range: the largest ks of a tile below 2^-9, the values by the
 // largest so far, the rows of Q with their largest value at 2^14.  Eight codes are one word and, as (0, 4), (1, 5), (2, 6), (3, 7), one
